@@ -150,7 +150,8 @@ enum {
     MMEE_ENOFEASIBLE = -3,  /* every candidate is masked; out->cost.valid = 0                 */
     MMEE_EDEVICE = -4,      /* HIP error or no device                                         */
     MMEE_EOVERFLOW = -5,    /* mmee_pareto: more front points than `capacity`                 */
-    MMEE_ETOOBIG = -6       /* mmee_search_noalloc: the problem exceeds its fixed scratch     */
+    MMEE_ETOOBIG = -6,      /* mmee_search_noalloc: the problem exceeds its fixed scratch     */
+    MMEE_EWORKSPACE = -7    /* mmee_attn_*, mmee_tree_attn_*, mmee_ffn_*: no workspace, or one smaller than asked for */
 };
 
 /* Number of candidates of (workload, hw): #tilings (integer factorisations, Sec. VI-A)
@@ -278,6 +279,87 @@ int mmee_offline_rows(uint32_t group, uint32_t which, uint32_t *rows_out, uint32
  * walked fronts are launched with (default: two per compute unit).  It changes how the work is split
  * and in which order partial results meet, never a result.  Problems that share their shape's part
  * and fronts over the surviving rows take one block per 64 tilings and do not look at it. */
+
+/* ---- running the chains -------------------------------------------------------------------------
+ * The two chained matrix products whose mappings the calls above search, run on this GPU: attention of queries over
+ * keys of another length (I != L) with its gradient, the same over a paged cache with a tree of drafted tokens, and a gated
+ * feed-forward block with its gradient.
+ *
+ * Conventions of these calls.  Every tensor pointer is a DEVICE pointer (current device); strides are in elements, the last
+ * dimension is contiguous.  Pointers are 16-byte aligned and strides of 16-bit tensors multiples of 8, strides of inputs may be 0 (a
+ * broadcast input: its gradient comes out unreduced); the stride of a dimension of extent 1 is not looked at.  The calls allocate nothing, enqueue kernels
+ * on the library's stream (mmee_set_stream) and return without waiting; the caller keeps the buffers alive and orders other streams' work against
+ * that stream.  They may be captured into a HIP graph.  `workspace` is device memory that the call uses while its kernels run; the
+ * *_workspace calls say how much it needs (0: none) and look at no pointer.  What lies in the workspace before does not matter.
+ * The same call on the same inputs gives the same bits.  Inputs and outputs are 16 bits, sums 32 bits. */
+enum { MMEE_F16 = 0, MMEE_BF16 = 1 };   /* dtype */
+
+/* Cross attention.  q [batch][q_len][heads][head_dim], k and v [batch][kv_len][kv_heads][head_dim], o as q; strides of the
+ * first three dimensions.  heads is a multiple of kv_heads: query head a reads key/value head a / (heads / kv_heads).
+ *   o = softmax(scale q k^T) v     over the keys l < kv_lens[batch] (when given; clamped to 0 .. kv_len) whose key_mask byte is
+ *   not 0 (when given).  Keys that do not count are not read into any result, whatever they hold.  A row without keys gives zeros,
+ *   and lse -inf.  head_dim: a multiple of 8 up to 128.  scale > 0. */
+typedef struct mmee_attn {
+    uint32_t dtype;
+    uint32_t batch, heads, kv_heads, head_dim;
+    uint32_t q_len, kv_len;
+    float scale;
+    const void *q, *k, *v;
+    void *o;
+    int64_t q_stride[3], k_stride[3], v_stride[3], o_stride[3];     /* batch, token, head         */
+    float *lse;                     /* [batch][heads][q_len] contiguous: log sum exp of the scaled scores; may be null for forward */
+    const int32_t *kv_lens;         /* [batch] or null                                            */
+    const uint8_t *key_mask;        /* [batch][kv_len] or null                                    */
+    int64_t mask_stride;            /* bytes from one batch to the next, 0: one mask for all      */
+    void *workspace;
+    uint64_t workspace_bytes;
+    uint64_t reserved;              /* must be 0                                                  */
+} mmee_attn;
+
+/* Gradients of mmee_attn: d_o as o; dq as q, dk and dv as k and v. */
+typedef struct mmee_attn_grads {
+    const void *d_o;
+    void *dq, *dk, *dv;
+    int64_t do_stride[3], dq_stride[3], dk_stride[3], dv_stride[3];
+} mmee_attn_grads;
+
+/* backward != 0: enough for the forward and the backward call. */
+int mmee_attn_workspace(const mmee_attn *a, int backward, uint64_t *bytes);
+int mmee_attn_forward(const mmee_attn *a);
+/* Reads o and lse as the forward call left them. */
+int mmee_attn_backward(const mmee_attn *a, const mmee_attn_grads *g);
+
+/* Attention of a tree of drafted tokens over a paged cache: nodes rows per sequence, q and o [batch][nodes][heads][head_dim].
+ * Keys and values lie in pages [n_pages][page_tokens][kv_heads][head_dim] (page_tokens a power of two, at most 65536);
+ * position p of sequence b is token p % page_tokens of page page_table[b][p / page_tokens], pages_per_seq entries a sequence.
+ * cache_lens[b] positions hold the sequence so far, node j's key and value are at position cache_lens[b] + j.  Row i sees
+ * the positions of the sequence so far and node j where bit j % 64 of ancestors[b][i][j / 64] is set (its own bit too, if it
+ * sees itself), j < node_counts[b].  ancestors is [batch][nodes][(nodes + 63) / 64] contiguous.  Rows i >= node_counts[b] give zeros, and lse -inf.
+ * Lengths and counts are clamped to what there is room for; positions in a page outside 0 .. n_pages-1 are not read and count as masked, like those
+ * past the last node.  The values of a node that some row sees must be finite also for the rows that do not see it.
+ * nodes at most 1024. */
+typedef struct mmee_tree_attn {
+    uint32_t dtype;
+    uint32_t batch, heads, kv_heads, head_dim;
+    uint32_t nodes;
+    uint32_t page_tokens, pages_per_seq, n_pages;
+    float scale;
+    const void *q, *k_pages, *v_pages;
+    void *o;
+    int64_t q_stride[3], k_stride[3], v_stride[3], o_stride[3];     /* batch or page, token, head */
+    const int32_t *page_table;
+    int64_t table_stride;           /* entries from one sequence to the next                      */
+    const int32_t *cache_lens;      /* [batch]                                                    */
+    const int32_t *node_counts;     /* [batch], or null: nodes everywhere                         */
+    const uint64_t *ancestors;
+    float *lse;                     /* [batch][heads][nodes] or null                              */
+    void *workspace;
+    uint64_t workspace_bytes;
+    uint64_t reserved;              /* must be 0                                                  */
+} mmee_tree_attn;
+
+int mmee_tree_attn_workspace(const mmee_tree_attn *a, uint64_t *bytes);
+int mmee_tree_attn_forward(const mmee_tree_attn *a);
 
 /* Use this HIP stream (a hipStream_t passed as void*) for all later launches; NULL = default. */
 int mmee_set_stream(void *hip_stream);

@@ -16,7 +16,8 @@ LIB_PATH = os.environ.get("MMEE_LIB") or os.path.join(_HERE, "libmmee.so")
 
 OBJ_ENERGY, OBJ_LATENCY, OBJ_LATENCY_THEN_ENERGY, OBJ_EDP = 0, 1, 2, 3
 SEARCH_PRUNED, SEARCH_EXHAUSTIVE, SEARCH_ORDERED_SUM = 0, 1, 2
-OK, EINVAL, ERANGE, ENOFEASIBLE, EDEVICE, EOVERFLOW, ETOOBIG = 0, -1, -2, -3, -4, -5, -6
+OK, EINVAL, ERANGE, ENOFEASIBLE, EDEVICE, EOVERFLOW, ETOOBIG, EWORKSPACE = 0, -1, -2, -3, -4, -5, -6, -7
+F16, BF16 = 0, 1
 
 
 class MmeeError(RuntimeError):
@@ -68,6 +69,44 @@ class RowStats(C.Structure):
                 ("rows_kept", C.c_uint32 * 4)]
 
 
+class _Call(C.Structure):
+    """Arguments of a call on device buffers, marshalled once for repeated calls; holds on to the tensors it was made from."""
+
+    def use_workspace(self, tensor):
+        """Give the call a contiguous device buffer as its workspace."""
+        self.workspace, self.workspace_bytes = tensor.data_ptr(), tensor.numel() * tensor.element_size()
+        self._workspace = tensor
+        return self
+
+
+_Strides = C.c_int64 * 3
+
+
+class Attn(_Call):
+    _fields_ = [("dtype", C.c_uint32), ("batch", C.c_uint32), ("heads", C.c_uint32), ("kv_heads", C.c_uint32),
+                ("head_dim", C.c_uint32), ("q_len", C.c_uint32), ("kv_len", C.c_uint32), ("scale", C.c_float),
+                ("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("o", C.c_void_p),
+                ("q_stride", _Strides), ("k_stride", _Strides), ("v_stride", _Strides), ("o_stride", _Strides),
+                ("lse", C.c_void_p), ("kv_lens", C.c_void_p), ("key_mask", C.c_void_p), ("mask_stride", C.c_int64),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64), ("reserved", C.c_uint64)]
+
+
+class AttnGrads(_Call):
+    _fields_ = [("d_o", C.c_void_p), ("dq", C.c_void_p), ("dk", C.c_void_p), ("dv", C.c_void_p),
+                ("do_stride", _Strides), ("dq_stride", _Strides), ("dk_stride", _Strides), ("dv_stride", _Strides)]
+
+
+class TreeAttn(_Call):
+    _fields_ = [("dtype", C.c_uint32), ("batch", C.c_uint32), ("heads", C.c_uint32), ("kv_heads", C.c_uint32),
+                ("head_dim", C.c_uint32), ("nodes", C.c_uint32), ("page_tokens", C.c_uint32), ("pages_per_seq", C.c_uint32),
+                ("n_pages", C.c_uint32), ("scale", C.c_float),
+                ("q", C.c_void_p), ("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("o", C.c_void_p),
+                ("q_stride", _Strides), ("k_stride", _Strides), ("v_stride", _Strides), ("o_stride", _Strides),
+                ("page_table", C.c_void_p), ("table_stride", C.c_int64), ("cache_lens", C.c_void_p), ("node_counts", C.c_void_p),
+                ("ancestors", C.c_void_p), ("lse", C.c_void_p),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64), ("reserved", C.c_uint64)]
+
+
 COST_DTYPE = np.dtype([("bs_words", "<u8"), ("da_words", "<u8"), ("br_words", "<u8"),
                        ("mac_total", "<u8"), ("comp_cycles", "<u8"),
                        ("energy_pj", "<f8"), ("latency_cycles", "<f8"),
@@ -105,6 +144,11 @@ def _load() -> C.CDLL:
     L.mmee_search_noalloc.argtypes = [P(Workload), P(Hw), C.c_int, C.c_uint32, C.c_void_p]
     L.mmee_offline_stats.argtypes = [P(RowStats)]
     L.mmee_offline_rows.argtypes = [C.c_uint32, C.c_uint32, P(C.c_uint32), C.c_uint32, P(C.c_uint32)]
+    L.mmee_attn_workspace.argtypes = [P(Attn), C.c_int, P(C.c_uint64)]
+    L.mmee_attn_forward.argtypes = [P(Attn)]
+    L.mmee_attn_backward.argtypes = [P(Attn), P(AttnGrads)]
+    L.mmee_tree_attn_workspace.argtypes = [P(TreeAttn), P(C.c_uint64)]
+    L.mmee_tree_attn_forward.argtypes = [P(TreeAttn)]
     L.mmee_set_stream.argtypes = [C.c_void_p]
     L.mmee_shutdown.argtypes = []
     L.mmee_shutdown.restype = None
@@ -114,7 +158,8 @@ def _load() -> C.CDLL:
                  "mmee_search_multi", "mmee_search_many", "mmee_search_noalloc", "mmee_offline_stats", "mmee_offline_rows", "mmee_set_stream",
                  "mmee_chain_space_size", "mmee_chain_decode", "mmee_chain_eval_batch",
                  "mmee_chain_search_multi", "mmee_chain_search_many", "mmee_pareto", "mmee_chain_pareto",
-                 "mmee_front_bs_da", "mmee_chain_front_bs_da"):
+                 "mmee_front_bs_da", "mmee_chain_front_bs_da",
+                 "mmee_attn_workspace", "mmee_attn_forward", "mmee_attn_backward", "mmee_tree_attn_workspace", "mmee_tree_attn_forward"):
         getattr(L, name).restype = C.c_int
     return L
 
@@ -329,6 +374,146 @@ def mmee_offline_rows(group: int, which: int = 1):
     n = C.c_uint32()
     _check(_lib.mmee_offline_rows(group, which, out, 15000, C.byref(n)), "mmee_offline_rows")
     return list(out[:n.value])
+
+
+# ---- running the chains: tensors of any library that have data_ptr(), shape, stride(), dtype, element_size() and numel() ----
+
+_FLOATS = {"torch.float16": F16, "torch.bfloat16": BF16}
+
+
+def _invalid(where: str, why: str):
+    e = MmeeError(EINVAL, where)
+    e.args = (f"{e.args[0]}: {why}",)
+    return e
+
+
+def _float_type(where, tensors):
+    """The common dtype of 16-bit device tensors whose last dimension is contiguous."""
+    kinds = {str(t.dtype) for t in tensors.values()}
+    if len(kinds) != 1 or not kinds <= set(_FLOATS):
+        raise _invalid(where, f"float16 or bfloat16 throughout is wanted, got {', '.join(sorted(kinds))}")
+    for name, t in tensors.items():
+        _on_device(where, name, t)
+        if t.shape[-1] > 1 and t.stride()[-1] != 1:
+            raise _invalid(where, f"{name}: the last dimension has to be contiguous")
+    return _FLOATS[kinds.pop()]
+
+
+def _on_device(where, name, t):
+    if not t.is_cuda:
+        raise _invalid(where, f"{name} is not on the GPU")
+
+
+def _shaped(where, name, t, *shape):
+    if tuple(t.shape) != shape:
+        raise _invalid(where, f"{name} has shape {tuple(t.shape)}, {shape} is wanted")
+
+
+def _whole(where, name, t, shape, kinds, contiguous=True):
+    """A device pointer to whole numbers or 32-bit floats of that shape, or None."""
+    if t is None:
+        return None
+    _shaped(where, name, t, *shape)
+    _on_device(where, name, t)
+    if str(t.dtype) not in kinds:
+        raise _invalid(where, f"{name} is {t.dtype}, {' or '.join(kinds)} is wanted")
+    if contiguous and not t.is_contiguous():
+        raise _invalid(where, f"{name} has to be contiguous")
+    return t.data_ptr()
+
+
+def _three(t):
+    return _Strides(*t.stride()[:3])
+
+
+def attn(q, k, v, o, lse=None, scale: float | None = None, kv_lens=None, key_mask=None) -> Attn:
+    """Arguments of mmee_attn_forward and mmee_attn_backward.  q, o [batch, q_len, heads, head_dim]; k, v [batch, kv_len, kv_heads,
+    head_dim], any strides but of the last dimension; lse float32 [batch, heads, q_len] (wanted for the backward call); kv_lens int32 [batch]; key_mask
+    uint8 or bool [batch, kv_len], 0: the key does not count.  scale: 1 / sqrt(head_dim) unless given."""
+    where = "attn"
+    dtype = _float_type(where, {"q": q, "k": k, "v": v, "o": o})
+    if len(q.shape) != 4 or len(k.shape) != 4:
+        raise _invalid(where, "q and k have four dimensions")
+    B, Lq, H, d = q.shape
+    Lk, Hkv = k.shape[1:3]
+    _shaped(where, "k", k, B, Lk, Hkv, d)
+    _shaped(where, "v", v, B, Lk, Hkv, d)
+    _shaped(where, "o", o, B, Lq, H, d)
+    mask = _whole(where, "key_mask", key_mask, (B, Lk), ("torch.uint8", "torch.bool"), contiguous=False)
+    if mask and Lk > 1 and key_mask.stride()[1] != 1:
+        raise _invalid(where, "key_mask: the last dimension has to be contiguous")
+    a = Attn(dtype, B, H, Hkv, d, Lq, Lk, d ** -0.5 if scale is None else scale, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
+             _three(q), _three(k), _three(v), _three(o), _whole(where, "lse", lse, (B, H, Lq), ("torch.float32",)),
+             _whole(where, "kv_lens", kv_lens, (B,), ("torch.int32",)), mask, key_mask.stride()[0] if mask else 0)
+    a._tensors = (q, k, v, o, lse, kv_lens, key_mask)
+    return a
+
+
+def attn_grads(do, dq, dk, dv) -> AttnGrads:
+    """Output gradient and gradients of mmee_attn_backward, shaped as o, q, k and v."""
+    _float_type("attn_grads", {"do": do, "dq": dq, "dk": dk, "dv": dv})
+    _shaped("attn_grads", "dq", dq, *do.shape)
+    _shaped("attn_grads", "dv", dv, *dk.shape)
+    g = AttnGrads(do.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), _three(do), _three(dq), _three(dk), _three(dv))
+    g._tensors = (do, dq, dk, dv)
+    return g
+
+
+def mmee_attn_workspace(a: Attn, backward: bool = False) -> int:
+    out = C.c_uint64()
+    _check(_lib.mmee_attn_workspace(C.byref(a), int(backward), C.byref(out)), "mmee_attn_workspace")
+    return out.value
+
+
+def mmee_attn_forward(a: Attn) -> None:
+    _check(_lib.mmee_attn_forward(C.byref(a)), "mmee_attn_forward")
+
+
+def mmee_attn_backward(a: Attn, g: AttnGrads) -> None:
+    do, dq, dk, dv = g._tensors
+    q, k = a._tensors[:2]
+    for name, t, like in (("do", do, q), ("dk", dk, k)):
+        _shaped("mmee_attn_backward", name, t, *like.shape)
+        if t.dtype != like.dtype:
+            raise _invalid("mmee_attn_backward", f"{name} is {t.dtype}, {like.dtype} is wanted")
+    _check(_lib.mmee_attn_backward(C.byref(a), C.byref(g)), "mmee_attn_backward")
+
+
+def tree_attn(q, k_pages, v_pages, page_table, cache_lens, ancestors, o, node_counts=None, lse=None, scale: float | None = None) -> TreeAttn:
+    """Arguments of mmee_tree_attn_forward.  q, o [batch, nodes, heads, head_dim]; k_pages, v_pages [n_pages, page_tokens, kv_heads, head_dim];
+    page_table int32 [batch, pages_per_seq]; cache_lens, node_counts int32 [batch]; ancestors int64 (bit patterns) [batch, nodes,
+    ceil(nodes / 64)]; lse float32 [batch, heads, nodes]."""
+    where = "tree_attn"
+    dtype = _float_type(where, {"q": q, "k_pages": k_pages, "v_pages": v_pages, "o": o})
+    if len(q.shape) != 4 or len(k_pages.shape) != 4 or len(page_table.shape) != 2:
+        raise _invalid(where, "q and k_pages have four dimensions, page_table two")
+    B, n, H, d = q.shape
+    P, page, Hkv = k_pages.shape[:3]
+    _shaped(where, "k_pages", k_pages, P, page, Hkv, d)
+    _shaped(where, "v_pages", v_pages, P, page, Hkv, d)
+    _shaped(where, "o", o, B, n, H, d)
+    width = page_table.shape[1]
+    table = _whole(where, "page_table", page_table, (B, width), ("torch.int32",), contiguous=False)
+    if width > 1 and page_table.stride()[1] != 1:
+        raise _invalid(where, "page_table: the last dimension has to be contiguous")
+    t = TreeAttn(dtype, B, H, Hkv, d, n, page, width, P, d ** -0.5 if scale is None else scale,
+                 q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), o.data_ptr(), _three(q), _three(k_pages), _three(v_pages), _three(o),
+                 table, page_table.stride()[0], _whole(where, "cache_lens", cache_lens, (B,), ("torch.int32",)),
+                 _whole(where, "node_counts", node_counts, (B,), ("torch.int32",)),
+                 _whole(where, "ancestors", ancestors, (B, n, (n + 63) // 64), ("torch.int64", "torch.uint64")),
+                 _whole(where, "lse", lse, (B, H, n), ("torch.float32",)))
+    t._tensors = (q, k_pages, v_pages, page_table, cache_lens, ancestors, o, node_counts, lse)
+    return t
+
+
+def mmee_tree_attn_workspace(t: TreeAttn) -> int:
+    out = C.c_uint64()
+    _check(_lib.mmee_tree_attn_workspace(C.byref(t), C.byref(out)), "mmee_tree_attn_workspace")
+    return out.value
+
+
+def mmee_tree_attn_forward(t: TreeAttn) -> None:
+    _check(_lib.mmee_tree_attn_forward(C.byref(t)), "mmee_tree_attn_forward")
 
 
 def mmee_set_stream(stream_ptr: int | None):

@@ -1,0 +1,661 @@
+// Attention of rows of queries over keys of another length: forward, over plain tensors or over a paged cache with a tree of
+// drafted tokens, and backward.
+//
+//   S = scale Q K^T, masked entries -inf;  P = softmax(S);  O = P V;  lse = log sum exp S
+//   D = rowsum(dO * O);  dV = P^T dO;  dS = P (dO V^T - D);  dQ = scale dS K;  dK = scale dS^T Q
+//
+// The query heads that share a key/value head are rows of one problem: row r = token * group + head in group, so one tile of keys
+// serves them all, and dK, dV sum over them without another pass.  Scores are formed transposed (keys along the matrix
+// instruction's m, rows along n): a lane holds one row's scores, the softmax needs one exchange between two lanes, and the
+// probabilities are the next product's operand as they stand.  Products take 16-bit operands and accumulate in 32 bits; maximum, sum,
+// accumulators, lse, D and partial results are 32 bits; probabilities and dS are rounded to the operands' type, as the matrix
+// instructions need them.
+#pragma once
+
+#include "launch.h"
+#include "mfma.h"
+
+namespace mmee {
+
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+
+struct Strides {                // in elements
+    int64_t batch, token, head;
+};
+
+struct AttnArgs {
+    const uint16_t *q, *k, *v;
+    Strides qs, ks, vs, os;     // of pages: batch is the page's stride
+    uint16_t *o;
+    float *lse;                 // [batch][heads][q_len] or null
+    uint32_t batch, heads, kv_heads, group, q_len, rows, kv_len, head_dim;
+    uint64_t group_inverse;     // ceil(2^40 / group)
+    float scale, scale_log2;
+    const int32_t *kv_lens;
+    const uint8_t *key_mask;
+    int64_t mask_stride;
+    // paged cache and tree
+    const int32_t *page_table, *cache_lens, *node_counts;
+    const uint64_t *ancestors;
+    int64_t table_stride;
+    uint32_t page_shift, n_pages, words;
+    // keys in pieces
+    uint32_t row_tiles, splits;
+    float *part_o, *part_lse;   // [split][batch][kv_head][row][DP], [..][row]; lse in powers of two
+    // backward
+    const uint16_t *d_o, *o_in;
+    const float *lse_in;
+    Strides dos, dqs, dks, dvs;
+    uint16_t *dq, *dk, *dv;
+    float *delta;               // [batch][kv_head][row]
+};
+
+enum { MODE_PLAIN = 0, MODE_MASK = 1, MODE_TREE = 2 };
+
+__device__ __forceinline__ uint32_t token_of(const AttnArgs &a, uint32_t row) { return (uint32_t)((row * a.group_inverse) >> 40); }
+
+// Place of a row in a tensor of query heads.
+__device__ __forceinline__ int64_t row_at(const AttnArgs &a, const Strides &s, uint32_t b, uint32_t kvh, uint32_t row)
+{
+    const uint32_t token = token_of(a, row), head = kvh * a.group + (row - token * a.group);
+    return b * s.batch + token * s.token + head * s.head;
+}
+
+__device__ __forceinline__ int64_t lse_at(const AttnArgs &a, uint32_t b, uint32_t kvh, uint32_t row)
+{
+    const uint32_t token = token_of(a, row), head = kvh * a.group + (row - token * a.group);
+    return ((int64_t)b * a.heads + head) * a.q_len + token;
+}
+
+__device__ __forceinline__ u32x4 zeros() { return u32x4{0, 0, 0, 0}; }
+
+// Eight values of a row, as a B operand along the head's dimension: chunk 2 t + h of lane 32 h + i.
+template <class T, int DP>
+__device__ __forceinline__ void row_operands(typename T::V8 (&out)[DP / 16], const uint16_t *row, bool valid, uint32_t head_dim)
+{
+    const int h = (threadIdx.x >> 5) & 1;
+#pragma unroll
+    for (int t = 0; t < DP / 16; ++t) {
+        const int at = 16 * t + 8 * h;
+        out[t] = as_operand<T>(valid && at < (int)head_dim ? *reinterpret_cast<const u32x4 *>(row + at) : zeros());
+    }
+}
+
+// Where the keys of a block's piece lie, and which of them count.
+template <int MODE>
+struct Keys {
+    const AttnArgs &a;
+    uint32_t b, kvh;
+    uint32_t end;               // keys 0 .. end-1 exist
+    uint32_t held, nodes;       // tree: keys in the cache before the tree, nodes
+
+    __device__ __forceinline__ Keys(const AttnArgs &args, uint32_t b_, uint32_t kvh_) : a(args), b(b_), kvh(kvh_), held(0), nodes(0)
+    {
+        if (MODE == MODE_TREE) {
+            const int64_t room = (int64_t)a.kv_len;
+            const int64_t len = a.cache_lens[b], n = a.node_counts ? a.node_counts[b] : (int32_t)a.q_len;
+            held = (uint32_t)(len < 0 ? 0 : len > room ? room : len);
+            nodes = (uint32_t)(n < 0 ? 0 : n > (int64_t)a.q_len ? (int64_t)a.q_len : n);
+            end = held + nodes > a.kv_len ? a.kv_len : held + nodes;
+            if (!nodes) end = 0;                        // no row looks at anything
+        } else {
+            end = a.kv_len;
+            if (a.kv_lens) {
+                const int32_t len = a.kv_lens[b];
+                end = len < 0 ? 0 : (uint32_t)len < end ? (uint32_t)len : end;
+            }
+        }
+    }
+
+    // What decides whether key `at` counts: its page, or -1; its mask byte.
+    __device__ __forceinline__ int info(uint32_t at) const
+    {
+        if (MODE == MODE_PLAIN) return 0;
+        if (at >= end) return -1;
+        if (MODE == MODE_MASK) return a.key_mask[b * a.mask_stride + at] ? 0 : -1;
+        const int32_t page = a.page_table[b * a.table_stride + (at >> a.page_shift)];
+        return (uint32_t)page < a.n_pages ? page : -1;
+    }
+};
+
+// One thread's share of a tile of TN keys by GT threads: loads in flight in registers, then to shared memory.
+template <int DP, int TN, int GT, int MODE>
+struct Stage {
+    static constexpr int CH = DP / 8, LOADS = TN * CH / GT, ROWS = GT / CH;     // rows that one load of all threads covers
+    static_assert(LOADS * GT == TN * CH && ROWS * CH == GT, "a tile is dealt out evenly");
+    u32x4 k[LOADS], v[LOADS];
+
+    // info: of key first + (lane mod TN), as Keys::info gives it
+    __device__ __forceinline__ void load(const Keys<MODE> &keys, int thread, uint32_t first, int info)
+    {
+        const AttnArgs &a = keys.a;
+        const int c = thread % CH, row0 = thread / CH;
+        const bool column = c * 8 < (int)a.head_dim;
+        if (MODE == MODE_TREE) {
+            const uint16_t *kb = a.k + keys.kvh * a.ks.head + c * 8, *vb = a.v + keys.kvh * a.vs.head + c * 8;
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                const int row = row0 + i * ROWS, page = __shfl(info, row);
+                const uint32_t inside = (first + row) & ((1u << a.page_shift) - 1);
+                const bool valid = column && page >= 0;
+                k[i] = valid ? *reinterpret_cast<const u32x4 *>(kb + page * a.ks.batch + inside * a.ks.token) : zeros();
+                v[i] = valid ? *reinterpret_cast<const u32x4 *>(vb + page * a.vs.batch + inside * a.vs.token) : zeros();
+            }
+            return;
+        }
+        const uint16_t *kb = a.k + keys.b * a.ks.batch + keys.kvh * a.ks.head + first * a.ks.token;
+        const uint16_t *vb = a.v + keys.b * a.vs.batch + keys.kvh * a.vs.head + first * a.vs.token;
+        const uint32_t kt = (uint32_t)a.ks.token, vt = (uint32_t)a.vs.token;    // a tile spans less than 2^31 elements
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int row = row0 + i * ROWS;
+            bool valid = column && first + row < keys.end;
+            if (MODE == MODE_MASK) {
+                const int counts = __shfl(info, row);           // (by all lanes, whatever their column)
+                valid = valid && counts >= 0;
+            }
+            k[i] = valid ? *reinterpret_cast<const u32x4 *>(kb + (row * kt + c * 8)) : zeros();
+            v[i] = valid ? *reinterpret_cast<const u32x4 *>(vb + (row * vt + c * 8)) : zeros();
+        }
+    }
+
+    __device__ __forceinline__ void store(u32x4 *ks, u32x4 *vs, int thread) const
+    {
+        const int c = thread % CH, row0 = thread / CH;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int at = chunk_at<CH>(row0 + i * ROWS, c);
+            ks[at] = k[i];
+            vs[at] = v[i];
+        }
+    }
+};
+
+// S^T of 32 keys (rows `first` .. of a tile) and the wave's 32 rows.
+template <class T, int DP>
+__device__ __forceinline__ f32x16 keys_by_rows(const u32x4 *tile, int first, const typename T::V8 (&rows)[DP / 16])
+{
+    constexpr int CH = DP / 8;
+    const int lane = threadIdx.x & 63, i = lane & 31, h = lane >> 5;
+    f32x16 s = {};
+#pragma unroll
+    for (int t = 0; t < DP / 16; ++t) s = T::mma(as_operand<T>(tile[first * CH + chunk_at<CH>(i, 2 * t + h)]), rows[t], s);
+    return s;
+}
+
+// acc[dt] += (columns 32 dt .. of the tile's rows first .. first+15)^T times an operand that holds these rows in the order of a
+// 32x32 result: rows 4 h + {0..3}, 8 + 4 h + {0..3} in lane 32 h + i.
+template <class T, int DP>
+__device__ __forceinline__ void columns_times(f32x16 (&acc)[DP / 32], const u32x4 *tile, int first, typename T::V8 p)
+{
+    constexpr int CH = DP / 8;
+    const int lane = threadIdx.x & 63, i = lane & 15, g = (lane >> 4) & 1, h = lane >> 5;
+    const char *base = reinterpret_cast<const char *>(tile + first * CH) + 8 * (i & 1);
+#pragma unroll
+    for (int dt = 0; dt < DP / 32; ++dt) {
+        const int c = 4 * dt + 2 * g + ((i >> 1) & 1), row = 4 * h + (i >> 2);
+        const s16x4 lo = read_transposed(base + 16 * chunk_at<CH>(row, c)), hi = read_transposed(base + 16 * chunk_at<CH>(row + 8, c));
+        acc[dt] = T::mma(join<T>(lo, hi), p, acc[dt]);
+    }
+}
+
+template <class T>
+__device__ __forceinline__ typename T::V8 rounded(const f32x16 &x, int part)
+{
+    f32x8 y;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) y[j] = x[8 * part + j];
+    return __builtin_convertvector(y, typename T::V8);
+}
+
+// Stores a lane's column of a transposed result: values 32 dt + 8 u + 4 h + {0..3} of one row.
+template <class T, int DP>
+__device__ __forceinline__ void store_row(uint16_t *row, const f32x16 (&acc)[DP / 32], float times, uint32_t head_dim)
+{
+    const int h = (threadIdx.x >> 5) & 1;
+#pragma unroll
+    for (int dt = 0; dt < DP / 32; ++dt)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int d = 32 * dt + 8 * u + 4 * h;
+            const f32x4 x = {acc[dt][4 * u] * times, acc[dt][4 * u + 1] * times, acc[dt][4 * u + 2] * times, acc[dt][4 * u + 3] * times};
+            if (d < (int)head_dim) *reinterpret_cast<typename T::V4 *>(row + d) = __builtin_convertvector(x, typename T::V4);
+        }
+}
+
+template <int DP>
+__device__ __forceinline__ void store_part(float *row, const f32x16 (&acc)[DP / 32], float times)
+{
+    const int h = (threadIdx.x >> 5) & 1;
+#pragma unroll
+    for (int dt = 0; dt < DP / 32; ++dt)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const f32x4 x = {acc[dt][4 * u] * times, acc[dt][4 * u + 1] * times, acc[dt][4 * u + 2] * times, acc[dt][4 * u + 3] * times};
+            *reinterpret_cast<f32x4 *>(row + 32 * dt + 8 * u + 4 * h) = x;
+        }
+}
+
+// Which keys of a tile a lane's row sees, one bit each.
+template <int MODE, int TN>
+__device__ __forceinline__ uint64_t seen(const Keys<MODE> &keys, uint32_t first, uint64_t counted, uint32_t token, bool &all)
+{
+    const uint64_t whole = TN == 64 ? ~0ull : (1ull << TN) - 1;
+    if (MODE == MODE_PLAIN) {
+        const uint32_t left = keys.end > first ? keys.end - first : 0;
+        counted = left >= TN ? whole : (1ull << left) - 1;
+    }
+    all = counted == whole;
+    if (MODE != MODE_TREE) return counted;
+    const AttnArgs &a = keys.a;
+    if (first + TN > keys.held || token >= keys.nodes) {        // (rows beyond the nodes see nothing)
+        uint64_t bits = 0;
+        if (token < keys.nodes) {
+            const uint64_t *words = a.ancestors + ((int64_t)keys.b * a.q_len + token) * a.words;
+            const int64_t j = (int64_t)first - keys.held;       // > -64
+            if (j < 0) {
+                bits = j <= -64 ? ~0ull : words[0] << -j | ((1ull << -j) - 1);
+            } else if ((uint32_t)(j >> 6) < a.words) {
+                const uint32_t w = (uint32_t)(j >> 6), by = (uint32_t)(j & 63);
+                bits = words[w] >> by;
+                if (by && w + 1 < a.words) bits |= words[w + 1] << (64 - by);
+            }
+        }
+        counted &= bits;
+    }
+    all = __all(counted == whole);
+    return counted;
+}
+
+// Forward.  WR waves share a tile of keys, 32 rows each; WK such groups take every WK-th tile of the block's piece and are joined
+// at the end.  WR = 4 for many rows: a tile serves 128 rows.  WK = 4 for 32 rows or fewer (single tokens): nothing is shared
+// between waves and no barrier is met while keys stream in.
+template <class T, int DP, int WR, int WK, int MODE>
+__global__ __launch_bounds__(64 * WR * WK, 2) void k_attn_forward(const AttnArgs a)
+{
+    constexpr int TN = WR == 1 ? 32 : 64, MT = TN / 32, CH = DP / 8, GT = 64 * WR, NB = WR == 4 ? 2 : 1;
+    static_assert(NB == 1 || WK == 1, "two buffers for one group");
+    __shared__ u32x4 tiles[NB * WK][2][TN * CH];
+    __shared__ float marks[2][WK][32 * WR];
+    const int thread = threadIdx.x % GT, wave = threadIdx.x >> 6, wr = wave % WR, wk = wave / WR, lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
+
+    uint32_t at = by_die(blockIdx.x, gridDim.x);
+    const uint32_t rt = at % a.row_tiles;
+    at /= a.row_tiles;
+    const uint32_t split = at % a.splits;
+    at /= a.splits;
+    const uint32_t kvh = at % a.kv_heads, b = at / a.kv_heads;
+
+    const Keys<MODE> keys(a, b, kvh);
+    // pieces of whole steps (TN keys for every group)
+    constexpr uint32_t STEP = TN * WK;
+    const uint32_t steps = (keys.end + STEP - 1) / STEP, per = (steps + a.splits - 1) / a.splits;
+    const uint32_t step0 = split * per < steps ? split * per : steps, count = step0 + per < steps ? per : steps - step0;
+
+    const uint32_t row = (rt * WR + wr) * 32 + n;
+    const bool live = row < a.rows;
+    const uint32_t token = token_of(a, live ? row : 0);
+    typename T::V8 q[DP / 16];
+    row_operands<T, DP>(q, a.q + (live ? row_at(a, a.qs, b, kvh, row) : 0), live, a.head_dim);
+
+    f32x16 o[DP / 32] = {};
+    float top = -INFINITY, total = 0.0f;                // maximum (scaled, in powers of two); this lane's share of the sum
+
+    Stage<DP, TN, GT, MODE> stage;
+    auto first_of = [&](uint32_t s) { return ((step0 + s) * WK + wk) * TN; };
+    auto info_of = [&](uint32_t s) { return keys.info(first_of(s) + lane % TN); };
+    int info = 0, next_info = 0;
+    if (count) {
+        info = info_of(0);
+        stage.load(keys, thread, first_of(0), info);
+        next_info = info_of(1);
+    }
+    for (uint32_t s = 0; s < count; ++s) {
+        u32x4 *kt = tiles[NB == 2 ? s & 1 : wk][0], *vt = tiles[NB == 2 ? s & 1 : wk][1];
+        if (NB == 1 && s) {
+            if (WR > 1) __syncthreads(); else wave_sync();
+        }
+        stage.store(kt, vt, thread);
+        const uint64_t counted = MODE == MODE_PLAIN ? 0 : __ballot(info >= 0) & (TN == 64 ? ~0ull : (1ull << TN) - 1);
+        const uint32_t first = first_of(s);
+        if (WR > 1) __syncthreads(); else wave_sync();
+        if (s + 1 < count) {
+            info = next_info;
+            stage.load(keys, thread, first_of(s + 1), info);
+            next_info = info_of(s + 2);
+        }
+
+        f32x16 x[MT];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) x[mt] = keys_by_rows<T, DP>(kt, 32 * mt, q);
+        bool all;
+        const uint64_t bits = seen<MODE, TN>(keys, first, counted, token, all);
+        if (!all) {
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                const uint32_t mine = (uint32_t)(bits >> (32 * mt)) >> (4 * h);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) x[mt][r] = mine >> (8 * (r / 4) + r % 4) & 1 ? x[mt][r] : -INFINITY;
+            }
+        }
+        float m = x[0][0];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) m = __builtin_elementwise_maximum(m, x[mt][r]);
+        m = max_of_halves(m) * a.scale_log2;
+        // The sum may be taken against any mark near the maximum.  A mark that is kept until a row outgrows it by 2^8 spares
+        // scaling 16 DP / 32 accumulators a tile; 32-bit sums hold 2^8 times as much, and so do probabilities in 16 bits.
+        if (__any(!(m <= top + 8.0f))) {
+            const float mark = __builtin_elementwise_maximum(top, m);
+            const float keep = top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top - mark);
+            top = mark;
+            total *= keep;
+#pragma unroll
+            for (int dt = 0; dt < DP / 32; ++dt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[dt][r] *= keep;
+        }
+        const float off = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) x[mt][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[mt][r], a.scale_log2, -off));
+            float sum = 0.0f;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sum += x[mt][r];
+            total += sum;
+#pragma unroll
+            for (int part = 0; part < 2; ++part) columns_times<T, DP>(o, vt, 32 * mt + 16 * part, rounded<T>(x[mt], part));
+        }
+    }
+    total = sum_of_halves(total);
+
+    const int64_t bh = (int64_t)b * a.kv_heads + kvh, part_row = ((int64_t)split * a.batch * a.kv_heads + bh) * a.rows;
+    if (WK == 1) {
+        if (!live) return;
+        const float times = total != 0.0f ? 1.0f / total : 0.0f, sum2 = total != 0.0f ? top + __log2f(total) : -INFINITY;
+        if (a.splits == 1) {
+            store_row<T, DP>(a.o + row_at(a, a.os, b, kvh, row), o, times, a.head_dim);
+            if (a.lse && h == 0) a.lse[lse_at(a, b, kvh, row)] = sum2 * LN2;
+        } else {
+            store_part<DP>(a.part_o + (part_row + row) * DP, o, times);
+            if (h == 0) a.part_lse[part_row + row] = sum2;
+        }
+        return;
+    }
+    // Join the groups: accumulators through the tiles' memory, chunks of four values spread over the banks.
+    constexpr int C4 = DP / 4, ALL = 64 * WR * WK, PER_ROW = ALL / (32 * WR);
+    static_assert(sizeof(tiles) >= sizeof(float) * WK * 32 * WR * DP, "accumulators fit");
+    __syncthreads();
+    f32x4 *acc = reinterpret_cast<f32x4 *>(&tiles[0][0][0]);
+    const int mine = wr * 32 + n;
+#pragma unroll
+    for (int dt = 0; dt < DP / 32; ++dt)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const f32x4 x = {o[dt][4 * u], o[dt][4 * u + 1], o[dt][4 * u + 2], o[dt][4 * u + 3]};
+            acc[(wk * 32 * WR + mine) * C4 + ((8 * dt + 2 * u + h) ^ (n & (C4 - 1)))] = x;
+        }
+    if (h == 0) {
+        marks[0][wk][mine] = top;
+        marks[1][wk][mine] = total;
+    }
+    __syncthreads();
+    const int r = threadIdx.x / PER_ROW, sub = threadIdx.x % PER_ROW;
+    const uint32_t out_row = rt * WR * 32 + r;
+    if (out_row >= a.rows) return;
+    float high = -INFINITY, sum = 0.0f, weight[WK];
+#pragma unroll
+    for (int g = 0; g < WK; ++g) high = __builtin_elementwise_maximum(high, marks[0][g][r]);
+#pragma unroll
+    for (int g = 0; g < WK; ++g) {
+        weight[g] = marks[0][g][r] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(marks[0][g][r] - high);
+        sum += weight[g] * marks[1][g][r];
+    }
+    const float times = sum != 0.0f ? 1.0f / sum : 0.0f, sum2 = sum != 0.0f ? high + __log2f(sum) : -INFINITY;
+    uint16_t *to = a.o + (a.splits == 1 ? row_at(a, a.os, b, kvh, out_row) : 0);
+    float *part = a.part_o + (part_row + out_row) * DP;
+#pragma unroll
+    for (int c = sub; c < C4; c += PER_ROW) {
+        f32x4 x = {0, 0, 0, 0};
+#pragma unroll
+        for (int g = 0; g < WK; ++g) x += acc[(g * 32 * WR + r) * C4 + (c ^ (r & 31 & (C4 - 1)))] * weight[g];
+        x *= times;
+        if (a.splits == 1) {
+            if (4 * c < (int)a.head_dim) *reinterpret_cast<typename T::V4 *>(to + 4 * c) = __builtin_convertvector(x, typename T::V4);
+        } else {
+            *reinterpret_cast<f32x4 *>(part + 4 * c) = x;
+        }
+    }
+    if (sub == 0) {
+        if (a.splits > 1) a.part_lse[part_row + out_row] = sum2;
+        else if (a.lse) a.lse[lse_at(a, b, kvh, out_row)] = sum2 * LN2;
+    }
+}
+
+// Joins the pieces' results: O = sum_s 2^(lse_s - max) O_s / sum_s 2^(lse_s - max), pieces in ascending order.  DP / 4 threads a row.
+template <class T, int DP>
+__global__ __launch_bounds__(256) void k_attn_join(const AttnArgs a)
+{
+    constexpr int C4 = DP / 4, ROWS = 256 / C4;
+    const int64_t all = (int64_t)a.batch * a.kv_heads * a.rows, at = (int64_t)blockIdx.x * ROWS + threadIdx.x / C4;
+    const int c = threadIdx.x % C4;
+    if (at >= all) return;
+    float high = -INFINITY, sum = 0.0f;
+    for (uint32_t s = 0; s < a.splits; ++s) high = __builtin_elementwise_maximum(high, a.part_lse[s * all + at]);
+    const float off = high == -INFINITY ? 0.0f : high;
+    f32x4 x = {0, 0, 0, 0};
+#pragma unroll 4
+    for (uint32_t s = 0; s < a.splits; ++s) {
+        const float w = __builtin_amdgcn_exp2f(a.part_lse[s * all + at] - off);
+        sum += w;
+        x += *reinterpret_cast<const f32x4 *>(a.part_o + (s * all + at) * DP + 4 * c) * w;
+    }
+    const uint32_t row = (uint32_t)(at % a.rows), kvh = (uint32_t)(at / a.rows % a.kv_heads), b = (uint32_t)(at / a.rows / a.kv_heads);
+    x *= sum != 0.0f ? 1.0f / sum : 0.0f;
+    if (4 * c < (int)a.head_dim) *reinterpret_cast<typename T::V4 *>(a.o + row_at(a, a.os, b, kvh, row) + 4 * c) = __builtin_convertvector(x, typename T::V4);
+    if (a.lse && c == 0) a.lse[lse_at(a, b, kvh, row)] = sum != 0.0f ? (high + __log2f(sum)) * LN2 : -INFINITY;
+}
+
+// dQ, and D on the way.  As the forward pass with four waves on a tile: per tile three products, S^T = K Q^T, dP^T = V dO^T and
+// dQ^T += K^T dS^T.  Split over the keys, the pieces leave their dQ in 32 bits and k_sum_parts adds them in order.
+template <class T, int DP, int MODE>
+__global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a)
+{
+    constexpr int TN = 64, CH = DP / 8;
+    __shared__ u32x4 tiles[2][2][TN * CH];
+    const int thread = threadIdx.x, wave = thread >> 6, lane = thread & 63, n = lane & 31, h = lane >> 5;
+    uint32_t at = by_die(blockIdx.x, gridDim.x);
+    const uint32_t rt = at % a.row_tiles;
+    at /= a.row_tiles;
+    const uint32_t split = at % a.splits;
+    at /= a.splits;
+    const uint32_t kvh = at % a.kv_heads, b = at / a.kv_heads;
+    const Keys<MODE> keys(a, b, kvh);
+    const uint32_t steps = (keys.end + TN - 1) / TN, per = (steps + a.splits - 1) / a.splits;
+    const uint32_t step0 = split * per < steps ? split * per : steps, count = step0 + per < steps ? per : steps - step0;
+
+    const uint32_t row = (rt * 4 + wave) * 32 + n;
+    const bool live = row < a.rows;
+    const int64_t bh = (int64_t)b * a.kv_heads + kvh;
+    typename T::V8 q[DP / 16], d_o[DP / 16];
+    row_operands<T, DP>(q, a.q + (live ? row_at(a, a.qs, b, kvh, row) : 0), live, a.head_dim);
+    row_operands<T, DP>(d_o, a.d_o + (live ? row_at(a, a.dos, b, kvh, row) : 0), live, a.head_dim);
+    float lse2 = INFINITY, delta = 0.0f;                // rows that see nothing: probabilities 0
+    if (live) {
+        const float l = a.lse_in[lse_at(a, b, kvh, row)];
+        lse2 = l == -INFINITY ? INFINITY : l * LOG2E;
+    }
+    {
+        typename T::V8 o[DP / 16];
+        row_operands<T, DP>(o, a.o_in + (live ? row_at(a, a.os, b, kvh, row) : 0), live, a.head_dim);
+#pragma unroll
+        for (int t = 0; t < DP / 16; ++t)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) delta += (float)o[t][j] * (float)d_o[t][j];
+        delta = sum_of_halves(delta);
+        if (live && h == 0 && split == 0) a.delta[bh * a.rows + row] = delta;
+    }
+
+    f32x16 dq[DP / 32] = {};
+    Stage<DP, TN, 256, MODE> stage;
+    auto first_of = [&](uint32_t s) { return (step0 + s) * TN; };
+    auto info_of = [&](uint32_t s) { return keys.info(first_of(s) + lane); };
+    int info = 0, next_info = 0;
+    if (count) {
+        info = info_of(0);
+        stage.load(keys, thread, first_of(0), info);
+        next_info = info_of(1);
+    }
+    for (uint32_t s = 0; s < count; ++s) {
+        u32x4 *kt = tiles[s & 1][0], *vt = tiles[s & 1][1];
+        stage.store(kt, vt, thread);
+        const uint64_t counted = MODE == MODE_PLAIN ? 0 : __ballot(info >= 0);
+        const uint32_t first = first_of(s);
+        __syncthreads();
+        if (s + 1 < count) {
+            info = next_info;
+            stage.load(keys, thread, first_of(s + 1), info);
+            next_info = info_of(s + 2);
+        }
+        bool all;
+        const uint64_t bits = seen<MODE, TN>(keys, first, counted, 0, all);
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt) {
+            f32x16 x = keys_by_rows<T, DP>(kt, 32 * mt, q);
+            const f32x16 dp = keys_by_rows<T, DP>(vt, 32 * mt, d_o);
+            if (!all) {
+                const uint32_t mine = (uint32_t)(bits >> (32 * mt)) >> (4 * h);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) x[r] = mine >> (8 * (r / 4) + r % 4) & 1 ? x[r] : -INFINITY;
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) x[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], a.scale_log2, -lse2)) * (dp[r] - delta);
+#pragma unroll
+            for (int part = 0; part < 2; ++part) columns_times<T, DP>(dq, kt, 32 * mt + 16 * part, rounded<T>(x, part));
+        }
+    }
+    if (!live) return;
+    if (a.splits == 1) store_row<T, DP>(a.dq + row_at(a, a.dqs, b, kvh, row), dq, a.scale, a.head_dim);
+    else store_part<DP>(a.part_o + (((int64_t)split * a.batch * a.kv_heads + bh) * a.rows + row) * DP, dq, a.scale);
+}
+
+// dK and dV of 128 keys, 32 a wave, over the rows of a piece.  Per 32 rows: S = Q K^T, dP = dO V^T (rows along m, a lane holds one
+// key), dV^T += dO^T P, dK^T += Q^T dS; the rows' Q and dO are read from shared memory both along and across.
+template <class T, int DP, int MODE>
+__global__ __launch_bounds__(256, 2) void k_attn_dkv(const AttnArgs a)
+{
+    constexpr int TR = 32, CH = DP / 8, LOADS = TR * CH / 256 ? TR * CH / 256 : 1, ROWS = 256 / CH;
+    __shared__ u32x4 tiles[2][2][TR * CH];
+    __shared__ f32x4 stats[2][2][TR / 4];               // lse in powers of two, D
+    const int thread = threadIdx.x, wave = thread >> 6, lane = thread & 63, n = lane & 31, h = lane >> 5;
+    const uint32_t key_tiles = (a.kv_len + 127) / 128;
+    uint32_t at = by_die(blockIdx.x, gridDim.x);
+    const uint32_t kt = at % key_tiles;
+    at /= key_tiles;
+    const uint32_t split = at % a.splits;
+    at /= a.splits;
+    const uint32_t kvh = at % a.kv_heads, b = at / a.kv_heads;
+    const Keys<MODE> keys(a, b, kvh);
+    const uint32_t key = kt * 128 + wave * 32 + n;
+    const bool inside = key < a.kv_len, valid = key < keys.end && keys.info(key) >= 0;
+    const bool whole = __all(valid);
+    const uint32_t steps = kt * 128 < keys.end ? (a.rows + TR - 1) / TR : 0, per = (steps + a.splits - 1) / a.splits;
+    const uint32_t step0 = split * per < steps ? split * per : steps, count = step0 + per < steps ? per : steps - step0;
+
+    typename T::V8 k[DP / 16], v[DP / 16];
+    row_operands<T, DP>(k, a.k + (valid ? b * a.ks.batch + key * a.ks.token + kvh * a.ks.head : 0), valid, a.head_dim);
+    row_operands<T, DP>(v, a.v + (valid ? b * a.vs.batch + key * a.vs.token + kvh * a.vs.head : 0), valid, a.head_dim);
+    const int64_t bh = (int64_t)b * a.kv_heads + kvh;
+
+    u32x4 rq[LOADS], ro[LOADS];
+    float stat = 0.0f;
+    const int c = thread % CH, row0 = thread / CH;
+    auto load = [&](uint32_t s) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const uint32_t in_tile = row0 + i * ROWS, row = (step0 + s) * TR + in_tile;
+            const bool ok = in_tile < TR && row < a.rows && c * 8 < (int)a.head_dim;
+            rq[i] = ok ? *reinterpret_cast<const u32x4 *>(a.q + row_at(a, a.qs, b, kvh, row) + c * 8) : zeros();
+            ro[i] = ok ? *reinterpret_cast<const u32x4 *>(a.d_o + row_at(a, a.dos, b, kvh, row) + c * 8) : zeros();
+        }
+        if (thread < 2 * TR) {
+            const uint32_t row = (step0 + s) * TR + thread % TR;
+            stat = thread < TR ? INFINITY : 0.0f;       // rows that are not there, or see nothing: probabilities 0
+            if (row < a.rows) {
+                stat = thread < TR ? a.lse_in[lse_at(a, b, kvh, row)] : a.delta[bh * a.rows + row];
+                if (thread < TR) stat = stat == -INFINITY ? INFINITY : stat * LOG2E;
+            }
+        }
+    };
+    f32x16 dk[DP / 32] = {}, dv[DP / 32] = {};
+    if (count) load(0);
+    for (uint32_t s = 0; s < count; ++s) {
+        u32x4 *qt = tiles[s & 1][0], *ot = tiles[s & 1][1];
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int in_tile = row0 + i * ROWS;
+            if (TR * CH >= 256 || in_tile < TR) {
+                qt[chunk_at<CH>(in_tile, c)] = rq[i];
+                ot[chunk_at<CH>(in_tile, c)] = ro[i];
+            }
+        }
+        if (thread < 2 * TR) reinterpret_cast<float *>(stats[s & 1])[thread] = stat;
+        __syncthreads();
+        if (s + 1 < count) load(s + 1);
+        f32x16 x = keys_by_rows<T, DP>(qt, 0, k);
+        const f32x16 dp = keys_by_rows<T, DP>(ot, 0, v);
+        f32x16 ds;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const f32x4 lse2 = stats[s & 1][0][2 * u + h], delta = stats[s & 1][1][2 * u + h];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int r = 4 * u + j;
+                float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], a.scale_log2, -lse2[j]));
+                if (!whole) p = valid ? p : 0.0f;
+                x[r] = p;
+                ds[r] = p * (dp[r] - delta[j]);
+            }
+        }
+#pragma unroll
+        for (int part = 0; part < 2; ++part) {
+            columns_times<T, DP>(dv, ot, 16 * part, rounded<T>(x, part));
+            columns_times<T, DP>(dk, qt, 16 * part, rounded<T>(ds, part));
+        }
+    }
+    if (!inside) return;
+    if (a.splits == 1) {
+        store_row<T, DP>(a.dk + b * a.dks.batch + key * a.dks.token + kvh * a.dks.head, dk, a.scale, a.head_dim);
+        store_row<T, DP>(a.dv + b * a.dvs.batch + key * a.dvs.token + kvh * a.dvs.head, dv, 1.0f, a.head_dim);
+    } else {
+        float *part = a.part_o + ((((int64_t)split * a.batch * a.kv_heads + bh) * a.kv_len + key) * 2) * DP;
+        store_part<DP>(part, dk, a.scale);
+        store_part<DP>(part + DP, dv, 1.0f);
+    }
+}
+
+// Sums of pieces in ascending order, rounded once: which = 0: dQ rows; 1: dK and dV of a key beside each other.
+template <class T, int DP, int WHICH>
+__global__ __launch_bounds__(256) void k_attn_sum(const AttnArgs a)
+{
+    constexpr int C4 = DP / 4 * (WHICH + 1), LINES = 256 / C4;
+    const uint32_t lines = WHICH ? a.kv_len : a.rows;
+    const int64_t all = (int64_t)a.batch * a.kv_heads * lines, at = (int64_t)blockIdx.x * LINES + threadIdx.x / C4;
+    const int c = threadIdx.x % C4;
+    if (at >= all) return;
+    f32x4 x = {0, 0, 0, 0};
+#pragma unroll 4
+    for (uint32_t s = 0; s < a.splits; ++s) x += *reinterpret_cast<const f32x4 *>(a.part_o + ((s * all + at) * C4 + c) * 4);
+    const uint32_t line = (uint32_t)(at % lines), kvh = (uint32_t)(at / lines % a.kv_heads), b = (uint32_t)(at / lines / a.kv_heads);
+    const int d = 4 * c % DP;
+    if (d >= (int)a.head_dim) return;
+    uint16_t *to;
+    if (!WHICH) to = a.dq + row_at(a, a.dqs, b, kvh, line);
+    else if (4 * c < DP) to = a.dk + b * a.dks.batch + line * a.dks.token + kvh * a.dks.head;
+    else to = a.dv + b * a.dvs.batch + line * a.dvs.token + kvh * a.dvs.head;
+    *reinterpret_cast<typename T::V4 *>(to + d) = __builtin_convertvector(x, typename T::V4);
+}
+
+}  // namespace mmee

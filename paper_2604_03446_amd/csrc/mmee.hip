@@ -19,6 +19,7 @@
 #include "fronts.h"
 #include "dense.h"
 #include "pinned.h"
+#include "launch.h"
 
 // ---- fixed scratch of the entry point that allocates nothing (mmee_search_noalloc) ------------
 // One array per GPU, held from the moment the library is loaded until the process ends.  In host
@@ -1557,6 +1558,23 @@ int noalloc_setup(int dev, NoAllocDevice *&out)
 }
 
 }  // namespace
+Launching::Launching() : held(g_lock), stream(S.stream), rc(MMEE_OK)
+{
+    int n = 0;
+    if (hipGetDeviceCount(&n) == hipSuccess && n > 0) return;
+    (void)hipGetLastError();
+    std::snprintf(g_last_error, sizeof(g_last_error), "no HIP device");
+    rc = MMEE_EDEVICE;
+}
+
+int launched(const char *what)
+{
+    const hipError_t e = hipGetLastError();
+    if (e == hipSuccess) return MMEE_OK;
+    std::snprintf(g_last_error, sizeof(g_last_error), "%s: %s", what, hipGetErrorString(e));
+    return MMEE_EDEVICE;
+}
+
 }  // namespace mmee
 
 using namespace mmee;
@@ -2216,6 +2234,7 @@ const char *mmee_strerror(int code)
     case MMEE_ERANGE: return "candidate index out of range";
     case MMEE_ENOFEASIBLE: return "no feasible candidate";
     case MMEE_EDEVICE: return g_last_error[0] ? g_last_error : "HIP device error";
+    case MMEE_EWORKSPACE: return "no workspace, or one smaller than the workspace call asks for";
     case MMEE_EOVERFLOW: return "the Pareto front has more points than the caller made room for";
     case MMEE_ETOOBIG: return g_last_error[0] ? g_last_error : "the problem exceeds the fixed scratch of mmee_search_noalloc";
     default: return "unknown error";

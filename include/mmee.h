@@ -361,6 +361,37 @@ typedef struct mmee_tree_attn {
 int mmee_tree_attn_workspace(const mmee_tree_attn *a, uint64_t *bytes);
 int mmee_tree_attn_forward(const mmee_tree_attn *a);
 
+/* Gated feed-forward block of `rows` tokens:
+ *   g = x w_gate^T, u = x w_up^T, hidden = act(g) u, y = hidden w_down^T
+ * x [rows][in_dim], w_gate and w_up [hidden_dim][in_dim] (one row stride for both), w_down [out_dim][hidden_dim], y [rows][out_dim]; row strides
+ * of at least a row.  hidden [rows][hidden_dim] is contiguous; so are gate and up, which keep g and u for the backward call, or null.
+ * Widths: multiples of 8 up to 2^22. */
+enum { MMEE_ACT_SILU = 0, MMEE_ACT_GELU = 1, MMEE_ACT_GELU_TANH = 2, MMEE_ACT_RELU = 3, MMEE_ACT_SIGMOID = 4 };
+
+typedef struct mmee_ffn {
+    uint32_t dtype, act;
+    uint32_t rows, in_dim, hidden_dim, out_dim;
+    const void *x, *w_gate, *w_up, *w_down;
+    void *y, *hidden, *gate, *up;
+    int64_t x_stride, gate_stride, up_stride, down_stride, y_stride;
+    void *workspace;
+    uint64_t workspace_bytes;
+    uint64_t reserved;              /* must be 0                                                  */
+} mmee_ffn;
+
+/* dy as y, dx as x; dw_gate, dw_up and dw_down as the weights, contiguous. */
+typedef struct mmee_ffn_grads {
+    const void *dy;
+    void *dx, *dw_gate, *dw_up, *dw_down;
+    int64_t dy_stride, dx_stride;
+} mmee_ffn_grads;
+
+/* backward != 0: enough for the forward and the backward call. */
+int mmee_ffn_workspace(const mmee_ffn *f, int backward, uint64_t *bytes);
+int mmee_ffn_forward(const mmee_ffn *f);
+/* Reads hidden, gate and up as the forward call left them. */
+int mmee_ffn_backward(const mmee_ffn *f, const mmee_ffn_grads *g);
+
 /* Use this HIP stream (a hipStream_t passed as void*) for all later launches; NULL = default. */
 int mmee_set_stream(void *hip_stream);
 

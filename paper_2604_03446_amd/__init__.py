@@ -18,6 +18,7 @@ OBJ_ENERGY, OBJ_LATENCY, OBJ_LATENCY_THEN_ENERGY, OBJ_EDP = 0, 1, 2, 3
 SEARCH_PRUNED, SEARCH_EXHAUSTIVE, SEARCH_ORDERED_SUM = 0, 1, 2
 OK, EINVAL, ERANGE, ENOFEASIBLE, EDEVICE, EOVERFLOW, ETOOBIG, EWORKSPACE = 0, -1, -2, -3, -4, -5, -6, -7
 F16, BF16 = 0, 1
+ACTS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3, "sigmoid": 4}
 
 
 class MmeeError(RuntimeError):
@@ -107,6 +108,19 @@ class TreeAttn(_Call):
                 ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64), ("reserved", C.c_uint64)]
 
 
+class Ffn(_Call):
+    _fields_ = [("dtype", C.c_uint32), ("act", C.c_uint32), ("rows", C.c_uint32), ("in_dim", C.c_uint32), ("hidden_dim", C.c_uint32),
+                ("out_dim", C.c_uint32), ("x", C.c_void_p), ("w_gate", C.c_void_p), ("w_up", C.c_void_p), ("w_down", C.c_void_p),
+                ("y", C.c_void_p), ("hidden", C.c_void_p), ("gate", C.c_void_p), ("up", C.c_void_p),
+                ("x_stride", C.c_int64), ("gate_stride", C.c_int64), ("up_stride", C.c_int64), ("down_stride", C.c_int64),
+                ("y_stride", C.c_int64), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64), ("reserved", C.c_uint64)]
+
+
+class FfnGrads(_Call):
+    _fields_ = [("dy", C.c_void_p), ("dx", C.c_void_p), ("dw_gate", C.c_void_p), ("dw_up", C.c_void_p), ("dw_down", C.c_void_p),
+                ("dy_stride", C.c_int64), ("dx_stride", C.c_int64)]
+
+
 COST_DTYPE = np.dtype([("bs_words", "<u8"), ("da_words", "<u8"), ("br_words", "<u8"),
                        ("mac_total", "<u8"), ("comp_cycles", "<u8"),
                        ("energy_pj", "<f8"), ("latency_cycles", "<f8"),
@@ -149,6 +163,9 @@ def _load() -> C.CDLL:
     L.mmee_attn_backward.argtypes = [P(Attn), P(AttnGrads)]
     L.mmee_tree_attn_workspace.argtypes = [P(TreeAttn), P(C.c_uint64)]
     L.mmee_tree_attn_forward.argtypes = [P(TreeAttn)]
+    L.mmee_ffn_workspace.argtypes = [P(Ffn), C.c_int, P(C.c_uint64)]
+    L.mmee_ffn_forward.argtypes = [P(Ffn)]
+    L.mmee_ffn_backward.argtypes = [P(Ffn), P(FfnGrads)]
     L.mmee_set_stream.argtypes = [C.c_void_p]
     L.mmee_shutdown.argtypes = []
     L.mmee_shutdown.restype = None
@@ -159,7 +176,8 @@ def _load() -> C.CDLL:
                  "mmee_chain_space_size", "mmee_chain_decode", "mmee_chain_eval_batch",
                  "mmee_chain_search_multi", "mmee_chain_search_many", "mmee_pareto", "mmee_chain_pareto",
                  "mmee_front_bs_da", "mmee_chain_front_bs_da",
-                 "mmee_attn_workspace", "mmee_attn_forward", "mmee_attn_backward", "mmee_tree_attn_workspace", "mmee_tree_attn_forward"):
+                 "mmee_attn_workspace", "mmee_attn_forward", "mmee_attn_backward", "mmee_tree_attn_workspace", "mmee_tree_attn_forward",
+                 "mmee_ffn_workspace", "mmee_ffn_forward", "mmee_ffn_backward"):
         getattr(L, name).restype = C.c_int
     return L
 
@@ -514,6 +532,64 @@ def mmee_tree_attn_workspace(t: TreeAttn) -> int:
 
 def mmee_tree_attn_forward(t: TreeAttn) -> None:
     _check(_lib.mmee_tree_attn_forward(C.byref(t)), "mmee_tree_attn_forward")
+
+
+def ffn(x, w_gate, w_up, w_down, y, hidden, act: str = "silu", gate=None, up=None) -> Ffn:
+    """Arguments of mmee_ffn_forward and mmee_ffn_backward.  x [rows, in_dim], w_gate and w_up [hidden_dim, in_dim], w_down [out_dim,
+    hidden_dim], y [rows, out_dim]; hidden, and gate and up (wanted for the backward call), [rows, hidden_dim] contiguous."""
+    where = "ffn"
+    kept = {name: t for name, t in (("hidden", hidden), ("gate", gate), ("up", up)) if t is not None}
+    dtype = _float_type(where, {"x": x, "w_gate": w_gate, "w_up": w_up, "w_down": w_down, "y": y, **kept})
+    if act not in ACTS:
+        raise _invalid(where, f"act is one of {', '.join(ACTS)}")
+    if len(x.shape) != 2 or len(w_gate.shape) != 2 or len(w_down.shape) != 2:
+        raise _invalid(where, "x and the weights have two dimensions")
+    (M, K), F, J = x.shape, w_gate.shape[0], w_down.shape[0]
+    _shaped(where, "w_gate", w_gate, F, K)
+    _shaped(where, "w_up", w_up, F, K)
+    _shaped(where, "w_down", w_down, J, F)
+    _shaped(where, "y", y, M, J)
+    for name, t in kept.items():
+        _shaped(where, name, t, M, F)
+        if not t.is_contiguous():
+            raise _invalid(where, f"{name} has to be contiguous")
+    f = Ffn(dtype, ACTS[act], M, K, F, J, x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), y.data_ptr(), hidden.data_ptr(),
+            None if gate is None else gate.data_ptr(), None if up is None else up.data_ptr(),
+            x.stride()[0], w_gate.stride()[0], w_up.stride()[0], w_down.stride()[0], y.stride()[0])
+    f._tensors = (x, w_gate, w_up, w_down, y, hidden, gate, up)
+    return f
+
+
+def ffn_grads(dy, dx, dw_gate, dw_up, dw_down) -> FfnGrads:
+    """Output gradient and gradients of mmee_ffn_backward, shaped as y, x and the weights; the weights' gradients contiguous."""
+    where = "ffn_grads"
+    _float_type(where, {"dy": dy, "dx": dx, "dw_gate": dw_gate, "dw_up": dw_up, "dw_down": dw_down})
+    for name, t in (("dw_gate", dw_gate), ("dw_up", dw_up), ("dw_down", dw_down)):
+        if not t.is_contiguous():
+            raise _invalid(where, f"{name} has to be contiguous")
+    g = FfnGrads(dy.data_ptr(), dx.data_ptr(), dw_gate.data_ptr(), dw_up.data_ptr(), dw_down.data_ptr(), dy.stride()[0], dx.stride()[0])
+    g._tensors = (dy, dx, dw_gate, dw_up, dw_down)
+    return g
+
+
+def mmee_ffn_workspace(f: Ffn, backward: bool = False) -> int:
+    out = C.c_uint64()
+    _check(_lib.mmee_ffn_workspace(C.byref(f), int(backward), C.byref(out)), "mmee_ffn_workspace")
+    return out.value
+
+
+def mmee_ffn_forward(f: Ffn) -> None:
+    _check(_lib.mmee_ffn_forward(C.byref(f)), "mmee_ffn_forward")
+
+
+def mmee_ffn_backward(f: Ffn, g: FfnGrads) -> None:
+    x, w_gate, w_up, w_down, y = f._tensors[:5]
+    for (name, t), like in zip((("dy", g._tensors[0]), ("dx", g._tensors[1]), ("dw_gate", g._tensors[2]), ("dw_up", g._tensors[3]), ("dw_down", g._tensors[4])),
+                               (y, x, w_gate, w_up, w_down)):
+        _shaped("mmee_ffn_backward", name, t, *like.shape)
+        if t.dtype != like.dtype:
+            raise _invalid("mmee_ffn_backward", f"{name} is {t.dtype}, {like.dtype} is wanted")
+    _check(_lib.mmee_ffn_backward(C.byref(f), C.byref(g)), "mmee_ffn_backward")
 
 
 def mmee_set_stream(stream_ptr: int | None):

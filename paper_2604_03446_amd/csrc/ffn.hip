@@ -1,0 +1,283 @@
+// Host side of the gated feed-forward block: argument checks, the choice of variant and pieces, launches.
+#include <algorithm>
+#include <type_traits>
+
+#include "ffn.h"
+
+namespace mmee {
+namespace {
+
+constexpr uint32_t MOST_WIDTH = 1u << 22;       // columns and row strides: a tile's offsets fit 32 bits
+constexpr uint32_t FEW_TOKENS = 64;
+
+uint64_t up256(uint64_t x) { return (x + 255) & ~(uint64_t)255; }
+
+bool bad_rows(int64_t ld, uint64_t width, uint64_t rows) { return rows > 1 && (ld < (int64_t)width || ld % 8 || ld > (int64_t)MOST_WIDTH); }
+
+bool misaligned(std::initializer_list<const void *> list)
+{
+    for (const void *p : list)
+        if ((uintptr_t)p & 15) return true;
+    return false;
+}
+
+// A product and how it is run.
+struct Job {
+    ProductArgs p = {};
+    bool big = false;                           // tiles of 256 x 256, else 128 x 128
+    uint32_t blocks = 0;
+    uint64_t parts_bytes() const { return p.splits > 1 ? up256(4ull * p.problems * p.splits * p.m * p.n) : 0; }
+};
+
+// Tiles and pieces of a product.  `width`: columns that a tile of 256 covers (128 of each operand when two share a tile).
+bool plan(Job &j, uint32_t m, uint32_t n, uint32_t k, uint32_t segments, uint32_t problems, bool gated, bool may_split)
+{
+    ProductArgs &p = j.p;
+    p.m = m;
+    p.n = n;
+    p.k = k;
+    p.segments = segments;
+    p.problems = problems;
+    p.splits = 1;
+    const auto tiles = [&](uint32_t tm, uint32_t tn) { return (uint64_t)((m + tm - 1) / tm) * ((n + tn - 1) / tn) * problems; };
+    j.big = tiles(256, gated ? 128 : 256) >= 192;
+    const uint32_t tm = j.big ? 256 : 128, tn = (j.big ? 256 : 128) / (gated ? 2 : 1);
+    p.tiles_m = (m + tm - 1) / tm;
+    p.tiles_n = (n + tn - 1) / tn;
+    uint64_t blocks = tiles(tm, tn);
+    if (may_split && blocks && blocks < 192) {
+        const uint64_t steps = (uint64_t)((k + BK - 1) / BK) * segments;
+        p.splits = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>({512 / blocks, steps / 8, 16}));
+    }
+    blocks *= p.splits;
+    j.blocks = (uint32_t)blocks;
+    return blocks <= 0x7fffffff;
+}
+
+bool plan_tokens(Job &j, uint32_t m, uint32_t n, uint32_t k, uint32_t rows, bool may_split)
+{
+    ProductArgs &p = j.p;
+    p.m = m;
+    p.n = n;
+    p.k = k;
+    p.segments = p.problems = p.splits = 1;
+    uint64_t blocks = (n + rows - 1) / rows;
+    if (may_split && blocks < 192) {
+        const uint64_t steps = (k + 31) / 32;
+        p.splits = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>({512 / blocks, steps / 32, 16}));
+    }
+    j.blocks = (uint32_t)(blocks * p.splits);
+    return true;
+}
+
+struct FfnPlan {
+    bool tokens = false;                        // few tokens: weights are streamed
+    Job hidden, down, d_hidden, dx, dw_gated, dw_down;
+    uint64_t forward_bytes = 0, backward_bytes = 0, d_hidden_bytes = 0;
+};
+
+uint32_t token_rows(const mmee_ffn *x, bool gated)
+{
+    // rows of the weights for a block: 16, or 32 where that leaves two blocks for each compute unit
+    const uint32_t n = gated ? x->hidden_dim : x->out_dim;
+    return n / 32 >= 256 ? 32 : 16;
+}
+
+int plan_ffn(const mmee_ffn *x, bool pointers, FfnPlan &f)
+{
+    if (!x || x->reserved) return MMEE_EINVAL;
+    if ((x->dtype != MMEE_F16 && x->dtype != MMEE_BF16) || x->act >= N_ACTS) return MMEE_EINVAL;
+    for (const uint32_t width : {x->in_dim, x->hidden_dim, x->out_dim})
+        if (!width || width % 8 || width > MOST_WIDTH) return MMEE_EINVAL;
+    if (x->rows > 1u << 28) return MMEE_EINVAL;
+    if (bad_rows(x->x_stride, x->in_dim, x->rows) || bad_rows(x->gate_stride, x->in_dim, x->hidden_dim) || bad_rows(x->up_stride, x->in_dim, x->hidden_dim) ||
+        bad_rows(x->down_stride, x->hidden_dim, x->out_dim) || bad_rows(x->y_stride, x->out_dim, x->rows))
+        return MMEE_EINVAL;
+    if (x->gate_stride != x->up_stride && x->hidden_dim > 1) return MMEE_EINVAL;
+    if (pointers) {
+        if (!x->w_gate || !x->w_up || !x->w_down || (x->rows && (!x->x || !x->y || !x->hidden))) return MMEE_EINVAL;
+        if (misaligned({x->x, x->w_gate, x->w_up, x->w_down, x->y, x->hidden, x->gate, x->up, x->workspace})) return MMEE_EINVAL;
+    }
+    const uint32_t M = x->rows, K = x->in_dim, F = x->hidden_dim, J = x->out_dim;
+    f.tokens = M <= FEW_TOKENS;
+    bool fits = true;
+    if (f.tokens) fits = plan_tokens(f.hidden, M, F, K, token_rows(x, true), false) && plan_tokens(f.down, M, J, F, token_rows(x, false), true);
+    else fits = plan(f.hidden, M, F, K, 1, 1, true, false) && plan(f.down, M, J, F, 1, 1, false, true);
+    fits = fits && plan(f.d_hidden, M, F, J, 1, 1, false, false) && plan(f.dx, M, K, F, 2, 1, false, true) && plan(f.dw_gated, F, K, M, 1, 2, false, true) &&
+           plan(f.dw_down, J, F, M, 1, 1, false, true);
+    if (!fits) return MMEE_EINVAL;
+    f.forward_bytes = f.down.parts_bytes();
+    f.d_hidden_bytes = up256(2ull * M * F);
+    f.backward_bytes = 2 * f.d_hidden_bytes + std::max({f.dx.parts_bytes(), f.dw_gated.parts_bytes(), f.dw_down.parts_bytes()});
+    return MMEE_OK;
+}
+
+template <class T, bool A_ACROSS, bool B_ACROSS, int EPI>
+void product(const Job &j, hipStream_t stream)
+{
+    if (!j.blocks) return;
+    if (j.big) hipLaunchKernelGGL((k_product<T, 256, 256, 2, 4, A_ACROSS, B_ACROSS, EPI>), dim3(j.blocks), dim3(512), 0, stream, j.p);
+    else hipLaunchKernelGGL((k_product<T, 128, 128, 2, 2, A_ACROSS, B_ACROSS, EPI>), dim3(j.blocks), dim3(256), 0, stream, j.p);
+}
+
+template <class T>
+void sum_parts(const Job &j, hipStream_t stream)
+{
+    if (j.blocks && j.p.splits > 1)
+        hipLaunchKernelGGL((k_sum_parts<T>), dim3((uint32_t)(((uint64_t)j.p.problems * j.p.m * (j.p.n / 4) + 255) / 256)), dim3(256), 0, stream, j.p);
+}
+
+template <class T, bool GATED>
+void tokens(const Job &j, uint32_t rows, hipStream_t stream)
+{
+    auto with_rows = [&](auto mt) {
+        if (rows == 16) hipLaunchKernelGGL((k_tokens<T, mt.value, 1, GATED>), dim3(j.blocks), dim3(512), 0, stream, j.p);
+        else hipLaunchKernelGGL((k_tokens<T, mt.value, 2, GATED>), dim3(j.blocks), dim3(512), 0, stream, j.p);
+    };
+    if (j.p.m <= 16) with_rows(std::integral_constant<int, 1>());
+    else if (j.p.m <= 32) with_rows(std::integral_constant<int, 2>());
+    else if (j.p.m <= 48) with_rows(std::integral_constant<int, 3>());
+    else with_rows(std::integral_constant<int, 4>());
+}
+
+template <class T>
+void forward_as(const mmee_ffn *x, const FfnPlan &f, hipStream_t stream)
+{
+    if (f.tokens) {
+        tokens<T, true>(f.hidden, token_rows(x, true), stream);
+        tokens<T, false>(f.down, token_rows(x, false), stream);
+    } else {
+        product<T, false, false, EPI_GATED>(f.hidden, stream);
+        product<T, false, false, EPI_STORE>(f.down, stream);
+    }
+    sum_parts<T>(f.down, stream);
+}
+
+template <class T>
+void backward_as(const FfnPlan &f, hipStream_t stream)
+{
+    product<T, false, true, EPI_DGATED>(f.d_hidden, stream);
+    product<T, false, true, EPI_STORE>(f.dx, stream);
+    sum_parts<T>(f.dx, stream);
+    product<T, true, true, EPI_STORE>(f.dw_gated, stream);
+    sum_parts<T>(f.dw_gated, stream);
+    product<T, true, true, EPI_STORE>(f.dw_down, stream);
+    sum_parts<T>(f.dw_down, stream);
+}
+
+int64_t stride_of(int64_t given, uint64_t rows) { return rows > 1 ? given : 0; }
+
+}  // namespace
+}  // namespace mmee
+
+using namespace mmee;
+
+extern "C" {
+
+int mmee_ffn_workspace(const mmee_ffn *x, int backward, uint64_t *bytes)
+{
+    if (!bytes) return MMEE_EINVAL;
+    FfnPlan f;
+    const int rc = plan_ffn(x, false, f);
+    if (rc) return rc;
+    *bytes = backward ? std::max(f.forward_bytes, f.backward_bytes) : f.forward_bytes;
+    return MMEE_OK;
+}
+
+int mmee_ffn_forward(const mmee_ffn *x)
+{
+    FfnPlan f;
+    const int rc = plan_ffn(x, true, f);
+    if (rc) return rc;
+    if (f.forward_bytes && (!x->workspace || x->workspace_bytes < f.forward_bytes)) return MMEE_EWORKSPACE;
+    if (!x->rows) return MMEE_OK;
+    ProductArgs &h = f.hidden.p, &d = f.down.p;
+    h.a[0] = (const uint16_t *)x->x;
+    h.lda = stride_of(x->x_stride, x->rows);
+    h.b[0] = (const uint16_t *)x->w_gate;
+    h.b[1] = (const uint16_t *)x->w_up;
+    h.ldb = x->gate_stride;
+    h.c[0] = (uint16_t *)x->hidden;
+    h.ldc = h.ld_hidden = x->hidden_dim;
+    h.gate = (uint16_t *)x->gate;
+    h.up = (uint16_t *)x->up;
+    h.act = (int)x->act;
+    d.a[0] = (const uint16_t *)x->hidden;
+    d.lda = x->hidden_dim;
+    d.b[0] = (const uint16_t *)x->w_down;
+    d.ldb = x->down_stride;
+    d.c[0] = (uint16_t *)x->y;
+    d.ldc = stride_of(x->y_stride, x->rows);
+    d.parts = (float *)x->workspace;
+    Launching l;
+    if (l.rc) return l.rc;
+    if (x->dtype == MMEE_F16) forward_as<F16>(x, f, l.stream);
+    else forward_as<BF16>(x, f, l.stream);
+    return launched("gated feed-forward block, forward");
+}
+
+int mmee_ffn_backward(const mmee_ffn *x, const mmee_ffn_grads *g)
+{
+    FfnPlan f;
+    const int rc = plan_ffn(x, true, f);
+    if (rc) return rc;
+    if (!g || !g->dw_gate || !g->dw_up || !g->dw_down || (x->rows && (!x->gate || !x->up || !g->dy || !g->dx))) return MMEE_EINVAL;
+    if (misaligned({g->dy, g->dx, g->dw_gate, g->dw_up, g->dw_down})) return MMEE_EINVAL;
+    if (bad_rows(g->dy_stride, x->out_dim, x->rows) || bad_rows(g->dx_stride, x->in_dim, x->rows)) return MMEE_EINVAL;
+    if (f.backward_bytes && (!x->workspace || x->workspace_bytes < f.backward_bytes)) return MMEE_EWORKSPACE;
+    const int64_t F = x->hidden_dim, K = x->in_dim;
+    uint16_t *dg = (uint16_t *)x->workspace, *du = dg + f.d_hidden_bytes / 2;
+    float *parts = (float *)(du + f.d_hidden_bytes / 2);
+    const int64_t x_stride = stride_of(x->x_stride, x->rows), dy_stride = stride_of(g->dy_stride, x->rows);
+
+    ProductArgs &h = f.d_hidden.p;
+    h.a[0] = (const uint16_t *)g->dy;
+    h.lda = dy_stride;
+    h.b[0] = (const uint16_t *)x->w_down;
+    h.ldb = x->down_stride;
+    h.c[0] = dg;
+    h.c[1] = du;
+    h.ldc = h.ld_hidden = F;
+    h.gate_in = (const uint16_t *)x->gate;
+    h.up_in = (const uint16_t *)x->up;
+    h.act = (int)x->act;
+
+    ProductArgs &dx = f.dx.p;
+    dx.a[0] = dg;
+    dx.a[1] = du;
+    dx.lda = F;
+    dx.b[0] = (const uint16_t *)x->w_gate;
+    dx.b[1] = (const uint16_t *)x->w_up;
+    dx.ldb = x->gate_stride;
+    dx.c[0] = (uint16_t *)g->dx;
+    dx.ldc = stride_of(g->dx_stride, x->rows);
+    dx.parts = parts;
+
+    ProductArgs &dw = f.dw_gated.p;
+    dw.a[0] = dg;
+    dw.a[1] = du;
+    dw.lda = F;
+    dw.b[0] = (const uint16_t *)x->x;
+    dw.ldb = x_stride;
+    dw.c[0] = (uint16_t *)g->dw_gate;
+    dw.c[1] = (uint16_t *)g->dw_up;
+    dw.ldc = K;
+    dw.parts = parts;
+
+    ProductArgs &dd = f.dw_down.p;
+    dd.a[0] = (const uint16_t *)g->dy;
+    dd.lda = dy_stride;
+    dd.b[0] = (const uint16_t *)x->hidden;
+    dd.ldb = F;
+    dd.c[0] = (uint16_t *)g->dw_down;
+    dd.ldc = F;
+    dd.parts = parts;
+
+    Launching l;
+    if (l.rc) return l.rc;
+    if (x->dtype == MMEE_F16) backward_as<F16>(f, l.stream);
+    else backward_as<BF16>(f, l.stream);
+    return launched("gated feed-forward block, backward");
+}
+
+}  // extern "C"

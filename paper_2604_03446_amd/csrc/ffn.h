@@ -9,6 +9,8 @@
 // du because the next product takes them as operands.
 #pragma once
 
+#include <type_traits>
+
 #include "launch.h"
 #include "mfma.h"
 
@@ -16,41 +18,48 @@ namespace mmee {
 
 enum { ACT_SILU = 0, ACT_GELU = 1, ACT_GELU_TANH = 2, ACT_RELU = 3, ACT_SIGMOID = 4, N_ACTS = 5 };
 
-__device__ __forceinline__ float sigmoid_of(float x) { return 1.0f / (1.0f + __builtin_amdgcn_exp2f(-1.4426950408889634f * x)); }
+__device__ __forceinline__ float sigmoid_of(float x) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.4426950408889634f * x)); }
 
-// Activation and its derivative, in 32 bits.
-__device__ __forceinline__ void activate(int kind, float g, float &value, float &slope)
+// An activation and its derivative, in 32 bits.
+template <int KIND>
+__device__ __forceinline__ void activate(float g, float &value, float &slope)
 {
-    switch (kind) {
-    case ACT_SILU: {
+    if (KIND == ACT_SILU) {
         const float e = sigmoid_of(g);
         value = g * e;
         slope = e * (1.0f + g * (1.0f - e));
-        return;
-    }
-    case ACT_GELU: {
-        const float e = 0.5f * (1.0f + erff(0.7071067811865476f * g));
+    } else if (KIND == ACT_GELU) {
+        // erfc(z) = t (a1 + t (a2 + ..)) exp(-z^2), t = 1 / (1 + 0.3275911 z), z >= 0, to 1.5e-7 (Abramowitz and Stegun, 7.1.26); erff
+        // in its place made the epilogue of a tile of 256 x 128 results 10 us longer.
+        const float t = __builtin_amdgcn_rcpf(1.0f + 0.23164189f * __builtin_fabsf(g)), bell = __builtin_amdgcn_exp2f(-0.7213475204444817f * g * g);
+        const float half = 0.5f * t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f)))) * bell;
+        const float e = g < 0.0f ? half : 1.0f - half;
         value = g * e;
-        slope = e + g * 0.3989422804014327f * __builtin_amdgcn_exp2f(-0.7213475204444817f * g * g);
-        return;
-    }
-    case ACT_GELU_TANH: {
-        // (1 + tanh z) / 2 = sigmoid(2 z)
-        const float z2 = 1.5957691216057308f * (g + 0.044715f * g * g * g), e = sigmoid_of(z2);
+        slope = e + g * 0.3989422804014327f * bell;
+    } else if (KIND == ACT_GELU_TANH) {                 // (1 + tanh z) / 2 = sigmoid(2 z)
+        const float e = sigmoid_of(1.5957691216057308f * (g + 0.044715f * g * g * g));
         value = g * e;
         slope = e + g * e * (1.0f - e) * 1.5957691216057308f * (1.0f + 0.134145f * g * g);
-        return;
-    }
-    case ACT_RELU:
+    } else if (KIND == ACT_RELU) {
         value = __builtin_elementwise_maximum(g, 0.0f);
         slope = g > 0.0f ? 1.0f : 0.0f;
-        return;
-    default: {
+    } else {
         const float e = sigmoid_of(g);
         value = e;
         slope = e * (1.0f - e);
-        return;
     }
+}
+
+// f(std::integral_constant) for the activation of a call.
+template <class F>
+__device__ __forceinline__ void with_activation(int kind, F f)
+{
+    switch (kind) {
+    case ACT_SILU: f(std::integral_constant<int, ACT_SILU>()); break;
+    case ACT_GELU: f(std::integral_constant<int, ACT_GELU>()); break;
+    case ACT_GELU_TANH: f(std::integral_constant<int, ACT_GELU_TANH>()); break;
+    case ACT_RELU: f(std::integral_constant<int, ACT_RELU>()); break;
+    default: f(std::integral_constant<int, ACT_SIGMOID>()); break;
     }
 }
 
@@ -78,17 +87,21 @@ struct ProductArgs {
 
 constexpr int BK = 64;
 
-// One thread's share of an operand's tile of ROWS x 64, by THREADS threads: registers in flight, then shared memory.
+// A buffer of 2^31 bytes from a pointer on: more than a tile spans.  Loads at BEYOND give zeros.
+constexpr uint32_t BEYOND = 0x80000000u;
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_at(const uint16_t *p) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(p), 0, (int)BEYOND, 0x00027000); }
+
+// One thread's share of an operand's tile of ROWS x 64, by THREADS threads: registers in flight, then shared memory.  What does not
+// exist is asked for beyond the buffer's end and comes back as zeros, without a branch in the products' loop.
 template <int ROWS, int THREADS, bool ACROSS>
 struct OperandStage {
     static constexpr int CH = ACROSS ? ROWS / 8 : BK / 8, LINES = ACROSS ? BK : ROWS, LOADS = LINES * CH / THREADS, PER = THREADS / CH;
     static_assert(LOADS * THREADS == LINES * CH && PER * CH == THREADS, "a tile is dealt out evenly");
     u32x4 r[LOADS];
-    uint32_t offset[LOADS];             // elements from the tile's first column (along) or line (across) on
+    uint32_t offset[LOADS];             // bytes from the tile's first row (along) or the operand (across) on, at the step's k
     int chunk, line0;
 
-    // `rows` rows from the tile's first on exist (more than none).  Rows past them repeat the last one: their results are not stored.
-    // `halves`: the tile's second half begins at row `second` of the operand instead (gate and up columns of one tile).
+    // `rows` rows of the operand exist, more than `first`, the tile's first.  Rows past them repeat the last one: their results are not stored.
     __device__ __forceinline__ void aim(int thread, uint32_t first, uint32_t rows, int64_t ld)
     {
         chunk = thread % CH;
@@ -98,23 +111,19 @@ struct OperandStage {
             const uint32_t line = line0 + i * PER;
             if (ACROSS) {
                 const uint32_t col = first + 8 * chunk;
-                offset[i] = line * (uint32_t)ld + (col < rows ? col : rows - 8);
+                offset[i] = 2 * (line * (uint32_t)ld + (col < rows ? col : rows - 8));
             } else {
                 const uint32_t row = first + line;
-                offset[i] = (row < rows ? line : rows - 1 - first) * (uint32_t)ld + 8 * chunk;
+                offset[i] = 2 * ((row < rows ? line : rows - 1 - first) * (uint32_t)ld + 8 * chunk);
             }
         }
     }
 
-    // k values k0 .. k0+63 of which `left` exist; at: the tile's first row (along) or the operand (across), at k0.
-    __device__ __forceinline__ void load_one(int i, const uint16_t *at, uint32_t left)
+    // k values from the step's first on, of which `left` exist; at: the tile's first row (along) or the operand (across), at that k.
+    __device__ __forceinline__ void load_one(int i, __amdgpu_buffer_rsrc_t at, uint32_t left)
     {
-        if (left >= BK) {
-            r[i] = *reinterpret_cast<const u32x4 *>(at + offset[i]);
-        } else {
-            const bool there = (ACROSS ? (uint32_t)(line0 + i * PER) : (uint32_t)(8 * chunk)) < left;
-            r[i] = there ? *reinterpret_cast<const u32x4 *>(at + offset[i]) : u32x4{0, 0, 0, 0};
-        }
+        const bool there = (ACROSS ? (uint32_t)(line0 + i * PER) : (uint32_t)(8 * chunk)) < left;
+        r[i] = __builtin_amdgcn_raw_buffer_load_b128(at, there ? offset[i] : BEYOND, 0, 0);
     }
 
     __device__ __forceinline__ void store_one(int i, u32x4 *tile) const { tile[chunk_at<CH>(line0 + i * PER, chunk)] = r[i]; }
@@ -136,9 +145,11 @@ __device__ __forceinline__ typename T::V8 operand(const u32x4 *tile, int first, 
 }
 
 // A tile of TM x TN by WM x WN waves, in steps of 64 along k.  Two buffers in shared memory: while a step's products run, the next
-// step's tile is stored and the one after it is on its way in registers.
+// step's tile is stored and the one after it is on its way in registers.  A quarter of a step ahead of their use operands are
+// read into registers; the step's one barrier lies ahead of its last quarter, so that the next step's first operands are there
+// when it begins.
 template <class T, int TM, int TN, int WM, int WN, bool A_ACROSS, bool B_ACROSS, int EPI>
-__global__ __launch_bounds__(64 * WM * WN, 2) void k_product(const ProductArgs p)
+__global__ __launch_bounds__(64 * WM * WN, TM == 256 ? 1 : 2) void k_product(const ProductArgs p)
 {
     constexpr int THREADS = 64 * WM * WN, MS = TM / WM / 32, NS = TN / WN / 32;        // 32 x 32 blocks of a wave
     constexpr bool GATED = EPI == EPI_GATED;
@@ -167,112 +178,173 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_product(const ProductArgs p
     const uint32_t steps1 = (p.k + BK - 1) / BK, steps = steps1 * p.segments, each = (steps + p.splits - 1) / p.splits;
     const uint32_t step0 = split * each < steps ? split * each : steps, count = step0 + each < steps ? each : steps - step0;
 
-    auto load_a = [&](int i, uint32_t s) {
-        const uint32_t seg = s >= steps1, k0 = (s - seg * steps1) * BK;
-        const uint16_t *from = p.a[p.problems > 1 ? problem : seg];
-        sa.load_one(i, from + (A_ACROSS ? k0 * p.lda : m0 * p.lda + k0), p.k - k0);
-    };
-    auto load_b = [&](int half, int i, uint32_t s) {
-        const uint32_t seg = s >= steps1, k0 = (s - seg * steps1) * BK;
-        const uint16_t *from = p.b[GATED ? half : p.segments > 1 ? seg : 0];
-        sb[half].load_one(i, from + (B_ACROSS ? k0 * p.ldb : n0 * p.ldb + k0), p.k - k0);
-    };
     constexpr int LA = decltype(sa)::LOADS, LB = OperandStage<BN, THREADS, B_ACROSS>::LOADS, HALVES = GATED ? 2 : 1, ALL = LA + HALVES * LB;
-    static_assert(ALL % 4 == 0, "a quarter of the loads with each quarter of a step");
-    auto load = [&](int i, uint32_t s) {
-        if (i < LA) load_a(i, s);
-        else load_b((i - LA) / LB, (i - LA) % LB, s);
+    // Loads first .. last-1 of a step; steps past the piece's last load nothing.
+    auto load = [&](int first, int last, uint32_t s) {
+        const uint32_t step = step0 + s, seg = step >= steps1, k0 = (step - seg * steps1) * BK, left = s < count ? p.k - k0 : 0;
+        const auto at_a = buffer_at((p.problems > 1 ? problem : seg) ? p.a[1] + (A_ACROSS ? k0 * p.lda : m0 * p.lda + k0) : p.a[0] + (A_ACROSS ? k0 * p.lda : m0 * p.lda + k0));
+        const int64_t b_at = B_ACROSS ? k0 * p.ldb : n0 * p.ldb + k0;
+        const auto at_b = buffer_at((!GATED && p.segments > 1 && seg ? p.b[1] : p.b[0]) + b_at), at_b2 = buffer_at(p.b[1] + b_at);
+#pragma unroll
+        for (int i = first; i < last; ++i) {
+            if (i < LA) sa.load_one(i, at_a, left);
+            else if (i < LA + LB) sb[0].load_one(i - LA, at_b, left);
+            else sb[HALVES - 1].load_one(i - LA - LB, at_b2, left);
+        }
     };
-    auto store = [&](int i, u32x4 *buf) {
-        if (i < LA) sa.store_one(i, buf);
-        else sb[(i - LA) / LB].store_one((i - LA) % LB, buf + (TM + (i - LA) / LB * BN) * BK / 8);
+    auto store = [&](int first, int last, u32x4 *buf) {
+#pragma unroll
+        for (int i = first; i < last; ++i) {
+            if (i < LA) sa.store_one(i, buf);
+            else sb[(i - LA) / LB].store_one((i - LA) % LB, buf + (TM + (i - LA) / LB * BN) * BK / 8);
+        }
+    };
+    typename T::V8 a[2][MS], b[2][NS];
+    auto read = [&](int to, const u32x4 *tile, int t) {
+#pragma unroll
+        for (int ms = 0; ms < MS; ++ms) a[to][ms] = operand<T, TM, A_ACROSS>(tile, (wm * MS + ms) * 32, t);
+#pragma unroll
+        for (int ns = 0; ns < NS; ++ns) {
+            const int half = GATED ? ns / (NS / 2) : 0, block = GATED ? wn * (NS / 2) + ns % (NS / 2) : wn * NS + ns;
+            b[to][ns] = operand<T, BN, B_ACROSS>(tile + (TM + half * BN) * BK / 8, block * 32, t);
+        }
     };
 
     f32x16 acc[MS][NS] = {};
-    if (count) {
-#pragma unroll
-        for (int i = 0; i < ALL; ++i) load(i, step0);
-#pragma unroll
-        for (int i = 0; i < ALL; ++i) store(i, tiles[0]);
-        if (count > 1) {
-#pragma unroll
-            for (int i = 0; i < ALL; ++i) load(i, step0 + 1);
-        }
-    }
+    load(0, ALL, 0);
+    store(0, ALL, tiles[0]);
+    load(0, ALL, 1);
     __syncthreads();
+    read(0, tiles[0], 0);
     for (uint32_t s = 0; s < count; ++s) {
-        const u32x4 *ta = tiles[s & 1], *tb = ta + TM * BK / 8;
+        const u32x4 *now = tiles[s & 1];
         u32x4 *next = tiles[(s + 1) & 1];
 #pragma unroll
-        for (int t = 0; t < BK / 16; ++t) {
-            typename T::V8 a[MS], b[NS];
-#pragma unroll
-            for (int ms = 0; ms < MS; ++ms) a[ms] = operand<T, TM, A_ACROSS>(ta, (wm * MS + ms) * 32, t);
-#pragma unroll
-            for (int ns = 0; ns < NS; ++ns) {
-                const int half = GATED ? ns / (NS / 2) : 0, block = GATED ? wn * (NS / 2) + ns % (NS / 2) : wn * NS + ns;
-                b[ns] = operand<T, BN, B_ACROSS>(tb + half * BN * BK / 8, block * 32, t);
-            }
-            if (s + 1 < count) {
-#pragma unroll
-                for (int i = t * ALL / 4; i < (t + 1) * ALL / 4; ++i) store(i, next);
-            }
-            if (s + 2 < count) {
-#pragma unroll
-                for (int i = t * ALL / 4; i < (t + 1) * ALL / 4; ++i) load(i, step0 + s + 2);
+        for (int t = 0; t < 4; ++t) {
+            if (t == 3) __syncthreads();                // the next tile is complete, and this one's operands are all in registers
+            read((t + 1) & 1, t < 3 ? now : next, (t + 1) & 3);
+            if (t < 3) {
+                store(t * ALL / 3, (t + 1) * ALL / 3, next);
+                load(t * ALL / 3, (t + 1) * ALL / 3, s + 2);
             }
 #pragma unroll
             for (int ms = 0; ms < MS; ++ms)
 #pragma unroll
-                for (int ns = 0; ns < NS; ++ns) acc[ms][ns] = T::mma(b[ns], a[ms], acc[ms][ns]);       // C^T: a lane holds one row of C
-        }
-        __syncthreads();
-    }
-
+                for (int ns = 0; ns < NS; ++ns) acc[ms][ns] = T::mma(b[t & 1][ns], a[t & 1][ms], acc[ms][ns]);       // C^T: a lane holds one row of C
+            // The order of a quarter: a product after every operand read, then after every store and load.
+            constexpr int READS = MS * (A_ACROSS ? 2 : 1) + NS * (B_ACROSS ? 2 : 1), PRODUCTS = MS * NS;
 #pragma unroll
-    for (int ms = 0; ms < MS; ++ms) {
-        const uint32_t row = m0 + (wm * MS + ms) * 32 + i32;
-        if (row >= p.m) continue;
-        constexpr int OUT = GATED ? NS / 2 : NS;
-#pragma unroll
-        for (int ns = 0; ns < OUT; ++ns)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const uint32_t col = n0 + (wn * OUT + ns) * 32 + 8 * q + 4 * h;
-                if (col >= p.n) continue;
-                f32x4 x;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) x[j] = acc[ms][ns][4 * q + j];
-                typedef typename T::V4 V4;
-                if (EPI == EPI_STORE) {
-                    if (p.splits > 1) *reinterpret_cast<f32x4 *>(p.parts + ((uint64_t)(problem * p.splits + split) * p.m + row) * p.n + col) = x;
-                    else *reinterpret_cast<V4 *>(p.c[problem] + row * p.ldc + col) = __builtin_convertvector(x, V4);
-                } else if (GATED) {
-                    f32x4 u, y;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        u[j] = acc[ms][GATED ? ns + NS / 2 : ns][4 * q + j];
-                        float value, slope;
-                        activate(p.act, x[j], value, slope);
-                        y[j] = value * u[j];
-                    }
-                    *reinterpret_cast<V4 *>(p.c[0] + row * p.ldc + col) = __builtin_convertvector(y, V4);
-                    if (p.gate) *reinterpret_cast<V4 *>(p.gate + row * p.ld_hidden + col) = __builtin_convertvector(x, V4);
-                    if (p.up) *reinterpret_cast<V4 *>(p.up + row * p.ld_hidden + col) = __builtin_convertvector(u, V4);
-                } else {
-                    const V4 g = *reinterpret_cast<const V4 *>(p.gate_in + row * p.ld_hidden + col), u = *reinterpret_cast<const V4 *>(p.up_in + row * p.ld_hidden + col);
-                    f32x4 dg, du;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        float value, slope;
-                        activate(p.act, (float)g[j], value, slope);
-                        dg[j] = x[j] * (float)u[j] * slope;
-                        du[j] = x[j] * value;
-                    }
-                    *reinterpret_cast<V4 *>(p.c[0] + row * p.ldc + col) = __builtin_convertvector(dg, V4);
-                    *reinterpret_cast<V4 *>(p.c[1] + row * p.ldc + col) = __builtin_convertvector(du, V4);
-                }
+            for (int i = 0; i < PRODUCTS / 2; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x100, (READS + PRODUCTS / 2 - 1) / (PRODUCTS / 2), 0);
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
             }
+#pragma unroll
+            for (int i = 0; i < PRODUCTS / 2; ++i) {
+                if (t < 3) {
+                    __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+                }
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+    __syncthreads();
+
+    // Results go through the wave's share of the tiles' memory, 32 rows at a time, so that lanes next to each other hold eight
+    // columns each of one row: whole lines are read and written.  What the epilogue reads is asked for 32 rows ahead.
+    constexpr int COLS = 32 * NS, C4 = COLS / 4, OUT = GATED ? COLS / 2 : COLS, PER_ROW = OUT / 8, ROWS = 64 / PER_ROW, PASSES = 32 / ROWS;
+    constexpr bool DGATED = EPI == EPI_DGATED;
+    static_assert(sizeof(tiles) >= sizeof(float) * WM * WN * 32 * COLS, "32 rows of every wave fit");
+    typedef typename T::V8 V8;
+    f32x4 *mine = reinterpret_cast<f32x4 *>(&tiles[0][0]) + wave * 32 * C4;
+    const int c8 = lane % PER_ROW, r0 = lane / PER_ROW;
+    const uint32_t col = n0 + wn * OUT + 8 * c8, rows0 = m0 + wm * MS * 32 + r0;
+    const bool column = col < p.n;
+    V8 kept[2][DGATED ? PASSES : 1];                    // g and u
+    auto ask = [&](int ms) {
+        if (!DGATED) return;
+#pragma unroll
+        for (int pass = 0; pass < PASSES; ++pass) {
+            const uint32_t row = rows0 + ms * 32 + pass * ROWS;
+            const uint64_t at = (uint64_t)(row < p.m ? row : p.m - 1) * p.ld_hidden + (column ? col : 0);
+            kept[0][DGATED ? pass : 0] = *reinterpret_cast<const V8 *>(p.gate_in + at);
+            kept[1][DGATED ? pass : 0] = *reinterpret_cast<const V8 *>(p.up_in + at);
+        }
+    };
+    auto take = [&](int in, int c) {
+        const f32x4 lo = mine[in * C4 + (c ^ (in & (C4 - 1)))], hi = mine[in * C4 + ((c + 1) ^ (in & (C4 - 1)))];
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    ask(0);
+#pragma unroll 1
+    for (int ms = 0; ms < MS; ++ms) {
+        wave_sync();
+#pragma unroll
+        for (int which = 0; which < MS; ++which)
+            if (which == ms) {
+#pragma unroll
+                for (int ns = 0; ns < NS; ++ns)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const f32x16 &from = acc[which][ns];
+                        mine[i32 * C4 + ((8 * ns + 2 * q + h) ^ (i32 & (C4 - 1)))] = f32x4{from[4 * q], from[4 * q + 1], from[4 * q + 2], from[4 * q + 3]};
+                    }
+            }
+        wave_sync();
+        V8 g[DGATED ? PASSES : 1], u[DGATED ? PASSES : 1];
+        if (DGATED) {
+#pragma unroll
+            for (int pass = 0; pass < PASSES; ++pass) {
+                g[DGATED ? pass : 0] = kept[0][DGATED ? pass : 0];
+                u[DGATED ? pass : 0] = kept[1][DGATED ? pass : 0];
+            }
+            ask(ms + 1 < MS ? ms + 1 : ms);
+        }
+        const uint32_t row0 = rows0 + ms * 32;
+        if (EPI == EPI_STORE) {
+#pragma unroll
+            for (int pass = 0; pass < PASSES; ++pass) {
+                const uint32_t row = row0 + pass * ROWS;
+                const f32x8 x = take(pass * ROWS + r0, 2 * c8);
+                if (row >= p.m || !column) continue;
+                if (p.splits > 1) *reinterpret_cast<f32x8 *>(p.parts + ((uint64_t)(problem * p.splits + split) * p.m + row) * p.n + col) = x;
+                else *reinterpret_cast<V8 *>(p.c[problem] + row * p.ldc + col) = __builtin_convertvector(x, V8);
+            }
+        } else {
+            with_activation(p.act, [&](auto kind) {
+#pragma unroll
+                for (int pass = 0; pass < PASSES; ++pass) {
+                    const uint32_t row = row0 + pass * ROWS;
+                    const f32x8 x = take(pass * ROWS + r0, 2 * c8);
+                    f32x8 value, slope;
+                    if (GATED) {
+                        const f32x8 up = take(pass * ROWS + r0, 2 * c8 + C4 / 2);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            float y, unused;
+                            activate<kind.value>(x[j], y, unused);
+                            value[j] = y * up[j];
+                        }
+                        if (row >= p.m || !column) continue;
+                        *reinterpret_cast<V8 *>(p.c[0] + row * p.ldc + col) = __builtin_convertvector(value, V8);
+                        if (p.gate) *reinterpret_cast<V8 *>(p.gate + row * p.ld_hidden + col) = __builtin_convertvector(x, V8);
+                        if (p.up) *reinterpret_cast<V8 *>(p.up + row * p.ld_hidden + col) = __builtin_convertvector(up, V8);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            float y, dy;
+                            activate<kind.value>((float)g[DGATED ? pass : 0][j], y, dy);
+                            value[j] = x[j] * y;
+                            slope[j] = x[j] * (float)u[DGATED ? pass : 0][j] * dy;
+                        }
+                        if (row >= p.m || !column) continue;
+                        *reinterpret_cast<V8 *>(p.c[0] + row * p.ldc + col) = __builtin_convertvector(slope, V8);
+                        *reinterpret_cast<V8 *>(p.c[1] + row * p.ldc + col) = __builtin_convertvector(value, V8);
+                    }
+                }
+            });
+        }
     }
 }
 
@@ -368,12 +440,14 @@ __global__ __launch_bounds__(512, 2) void k_tokens(const ProductArgs p)
         typedef typename T::V4 V4;
         if (GATED) {
             const f32x4 g = y;
+            with_activation(p.act, [&](auto kind) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                float value, slope;
-                activate(p.act, g[j], value, slope);
-                y[j] = value * u[j];
-            }
+                for (int j = 0; j < 4; ++j) {
+                    float value, unused;
+                    activate<kind.value>(g[j], value, unused);
+                    y[j] = value * u[j];
+                }
+            });
             if (p.gate) *reinterpret_cast<V4 *>(p.gate + token * p.ld_hidden + col) = __builtin_convertvector(g, V4);
             if (p.up) *reinterpret_cast<V4 *>(p.up + token * p.ld_hidden + col) = __builtin_convertvector(u, V4);
             *reinterpret_cast<V4 *>(p.c[0] + token * p.ldc + col) = __builtin_convertvector(y, V4);

@@ -29,7 +29,20 @@ struct Job {
     uint64_t parts_bytes() const { return p.splits > 1 ? up256(4ull * p.problems * p.splits * p.m * p.n) : 0; }
 };
 
-// Tiles and pieces of a product.  `width`: columns that a tile of 256 covers (128 of each operand when two share a tile).
+// What a product is estimated to take, in us.  Measured (eight shapes of 128 to 8192 tokens, 768 to 12288 wide, all six products of a
+// step, both tiles, one to eight pieces): a step of 64 takes 0.53 us with one tile of 128 x 128 on a compute unit, 1.1 us with two; 1.85 us
+// with a tile of 256 x 256 on every one, 1.35 us while half of them have none.  A tile's first loads and its results add 4 us (128) or 7 us (256), 2 and
+// 11 us more where results come in two or three tensors.  Pieces are written and read once more in 32 bits.
+double estimate(bool big, uint64_t tiles, uint64_t steps, uint64_t splits, uint64_t results, bool many_results)
+{
+    const uint64_t blocks = tiles * splits, slots = big ? 256 : 512, whole = blocks / slots, rest = blocks % slots;
+    const double full = big ? 1.85 : 1.1, half = big ? 1.35 : 0.53, each = (double)((steps + splits - 1) / splits);
+    const double last = !rest ? 0.0 : rest <= slots / 2 ? half : full;
+    const double ends = (whole + (rest ? 1 : 0)) * (big ? (many_results ? 18.0 : 7.0) : (many_results ? 6.0 : 4.0));
+    return each * (whole * full + last) + ends + (splits > 1 ? 3.5 + results * splits * (4.0 / 6e6 + 4.0 / 8e6) : 0.0);
+}
+
+// Tiles and pieces of a product: those that are estimated to take least.
 bool plan(Job &j, uint32_t m, uint32_t n, uint32_t k, uint32_t segments, uint32_t problems, bool gated, bool may_split)
 {
     ProductArgs &p = j.p;
@@ -38,18 +51,22 @@ bool plan(Job &j, uint32_t m, uint32_t n, uint32_t k, uint32_t segments, uint32_
     p.k = k;
     p.segments = segments;
     p.problems = problems;
-    p.splits = 1;
-    const auto tiles = [&](uint32_t tm, uint32_t tn) { return (uint64_t)((m + tm - 1) / tm) * ((n + tn - 1) / tn) * problems; };
-    j.big = tiles(256, gated ? 128 : 256) >= 192;
-    const uint32_t tm = j.big ? 256 : 128, tn = (j.big ? 256 : 128) / (gated ? 2 : 1);
+    const uint64_t steps = (uint64_t)((k + BK - 1) / BK) * segments;
+    const auto tiles = [&](uint32_t side) { return (uint64_t)((m + side - 1) / side) * ((n + side / (gated ? 2 : 1) - 1) / (side / (gated ? 2 : 1))) * problems; };
+    double least = 0;
+    for (const bool big : {true, false})
+        for (uint64_t splits = 1; splits == 1 || (may_split && splits <= 16 && splits * 4 <= steps); ++splits) {
+            const double t = estimate(big, tiles(big ? 256 : 128), steps, splits, (uint64_t)m * n * problems, !may_split);
+            if (least == 0 || t < least) {
+                least = t;
+                j.big = big;
+                p.splits = (uint32_t)splits;
+            }
+        }
+    const uint32_t tm = j.big ? 256 : 128, tn = tm / (gated ? 2 : 1);
     p.tiles_m = (m + tm - 1) / tm;
     p.tiles_n = (n + tn - 1) / tn;
-    uint64_t blocks = tiles(tm, tn);
-    if (may_split && blocks && blocks < 192) {
-        const uint64_t steps = (uint64_t)((k + BK - 1) / BK) * segments;
-        p.splits = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>({512 / blocks, steps / 8, 16}));
-    }
-    blocks *= p.splits;
+    const uint64_t blocks = tiles(tm) * p.splits;
     j.blocks = (uint32_t)blocks;
     return blocks <= 0x7fffffff;
 }
@@ -116,7 +133,7 @@ template <class T, bool A_ACROSS, bool B_ACROSS, int EPI>
 void product(const Job &j, hipStream_t stream)
 {
     if (!j.blocks) return;
-    if (j.big) hipLaunchKernelGGL((k_product<T, 256, 256, 2, 4, A_ACROSS, B_ACROSS, EPI>), dim3(j.blocks), dim3(512), 0, stream, j.p);
+    if (j.big) hipLaunchKernelGGL((k_product<T, 256, 256, 2, 2, A_ACROSS, B_ACROSS, EPI>), dim3(j.blocks), dim3(256), 0, stream, j.p);
     else hipLaunchKernelGGL((k_product<T, 128, 128, 2, 2, A_ACROSS, B_ACROSS, EPI>), dim3(j.blocks), dim3(256), 0, stream, j.p);
 }
 

@@ -97,7 +97,7 @@ struct Keys {
             held = (uint32_t)(len < 0 ? 0 : len > room ? room : len);
             nodes = (uint32_t)(n < 0 ? 0 : n > (int64_t)a.q_len ? (int64_t)a.q_len : n);
             end = held + nodes > a.kv_len ? a.kv_len : held + nodes;
-            if (!nodes) end = 0;                        // no row looks at anything
+            if (!nodes || !a.n_pages) end = 0;          // no row looks at anything
         } else {
             end = a.kv_len;
             if (a.kv_lens) {
@@ -118,44 +118,44 @@ struct Keys {
     }
 };
 
-// One thread's share of a tile of TN keys by GT threads: loads in flight in registers, then to shared memory.
+// One thread's share of a tile of TN keys by GT threads: loads in flight in registers, then to shared memory.  Keys past the last one and
+// columns past the head's repeat existing ones (probabilities, and the rows' operands, are 0 there), so that nothing branches; masked keys
+// and those of pages that are not there become zeros on the way, since they may hold anything.
 template <int DP, int TN, int GT, int MODE>
 struct Stage {
     static constexpr int CH = DP / 8, LOADS = TN * CH / GT, ROWS = GT / CH;     // rows that one load of all threads covers
     static_assert(LOADS * GT == TN * CH && ROWS * CH == GT, "a tile is dealt out evenly");
     u32x4 k[LOADS], v[LOADS];
+    bool counts[MODE == MODE_PLAIN ? 1 : LOADS];
 
-    // info: of key first + (lane mod TN), as Keys::info gives it
+    // info: of key first + (lane mod TN), as Keys::info gives it.  There is a key at least.
     __device__ __forceinline__ void load(const Keys<MODE> &keys, int thread, uint32_t first, int info)
     {
         const AttnArgs &a = keys.a;
-        const int c = thread % CH, row0 = thread / CH;
-        const bool column = c * 8 < (int)a.head_dim;
+        const int row0 = thread / CH, c = 8 * (thread % CH) < (int)a.head_dim ? thread % CH : 0;
         if (MODE == MODE_TREE) {
             const uint16_t *kb = a.k + keys.kvh * a.ks.head + c * 8, *vb = a.v + keys.kvh * a.vs.head + c * 8;
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) {
                 const int row = row0 + i * ROWS, page = __shfl(info, row);
                 const uint32_t inside = (first + row) & ((1u << a.page_shift) - 1);
-                const bool valid = column && page >= 0;
-                k[i] = valid ? *reinterpret_cast<const u32x4 *>(kb + page * a.ks.batch + inside * a.ks.token) : zeros();
-                v[i] = valid ? *reinterpret_cast<const u32x4 *>(vb + page * a.vs.batch + inside * a.vs.token) : zeros();
+                counts[MODE == MODE_PLAIN ? 0 : i] = page >= 0;
+                const int64_t from = page >= 0 ? page : 0;
+                k[i] = *reinterpret_cast<const u32x4 *>(kb + from * a.ks.batch + inside * a.ks.token);
+                v[i] = *reinterpret_cast<const u32x4 *>(vb + from * a.vs.batch + inside * a.vs.token);
             }
             return;
         }
-        const uint16_t *kb = a.k + keys.b * a.ks.batch + keys.kvh * a.ks.head + first * a.ks.token;
-        const uint16_t *vb = a.v + keys.b * a.vs.batch + keys.kvh * a.vs.head + first * a.vs.token;
+        const uint32_t base = first < keys.end ? first : keys.end - 1, last = keys.end - 1 - base;
+        const uint16_t *kb = a.k + keys.b * a.ks.batch + keys.kvh * a.ks.head + base * a.ks.token;
+        const uint16_t *vb = a.v + keys.b * a.vs.batch + keys.kvh * a.vs.head + base * a.vs.token;
         const uint32_t kt = (uint32_t)a.ks.token, vt = (uint32_t)a.vs.token;    // a tile spans less than 2^31 elements
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int row = row0 + i * ROWS;
-            bool valid = column && first + row < keys.end;
-            if (MODE == MODE_MASK) {
-                const int counts = __shfl(info, row);           // (by all lanes, whatever their column)
-                valid = valid && counts >= 0;
-            }
-            k[i] = valid ? *reinterpret_cast<const u32x4 *>(kb + (row * kt + c * 8)) : zeros();
-            v[i] = valid ? *reinterpret_cast<const u32x4 *>(vb + (row * vt + c * 8)) : zeros();
+            const uint32_t row = row0 + i * ROWS, at = row < last ? row : last;
+            if (MODE == MODE_MASK) counts[MODE == MODE_PLAIN ? 0 : i] = __shfl(info, row) >= 0;
+            k[i] = *reinterpret_cast<const u32x4 *>(kb + (at * kt + c * 8));
+            v[i] = *reinterpret_cast<const u32x4 *>(vb + (at * vt + c * 8));
         }
     }
 
@@ -165,8 +165,9 @@ struct Stage {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int at = chunk_at<CH>(row0 + i * ROWS, c);
-            ks[at] = k[i];
-            vs[at] = v[i];
+            const bool as_is = MODE == MODE_PLAIN || counts[MODE == MODE_PLAIN ? 0 : i];
+            ks[at] = as_is ? k[i] : zeros();
+            vs[at] = as_is ? v[i] : zeros();
         }
     }
 };
@@ -183,10 +184,10 @@ __device__ __forceinline__ f32x16 keys_by_rows(const u32x4 *tile, int first, con
     return s;
 }
 
-// acc[dt] += (columns 32 dt .. of the tile's rows first .. first+15)^T times an operand that holds these rows in the order of a
+// acc[u][dt] += (columns 32 dt .. of the tile's rows first .. first+15)^T times operands that hold these rows in the order of a
 // 32x32 result: rows 4 h + {0..3}, 8 + 4 h + {0..3} in lane 32 h + i.
-template <class T, int DP>
-__device__ __forceinline__ void columns_times(f32x16 (&acc)[DP / 32], const u32x4 *tile, int first, typename T::V8 p)
+template <class T, int DP, int N>
+__device__ __forceinline__ void columns_times(f32x16 (&acc)[N][DP / 32], const u32x4 *tile, int first, const typename T::V8 (&p)[N])
 {
     constexpr int CH = DP / 8;
     const int lane = threadIdx.x & 63, i = lane & 15, g = (lane >> 4) & 1, h = lane >> 5;
@@ -195,7 +196,8 @@ __device__ __forceinline__ void columns_times(f32x16 (&acc)[DP / 32], const u32x
     for (int dt = 0; dt < DP / 32; ++dt) {
         const int c = 4 * dt + 2 * g + ((i >> 1) & 1), row = 4 * h + (i >> 2);
         const s16x4 lo = read_transposed(base + 16 * chunk_at<CH>(row, c)), hi = read_transposed(base + 16 * chunk_at<CH>(row + 8, c));
-        acc[dt] = T::mma(join<T>(lo, hi), p, acc[dt]);
+#pragma unroll
+        for (int u = 0; u < N; ++u) acc[u][dt] = T::mma(join<T>(lo, hi), p[u], acc[u][dt]);
     }
 }
 
@@ -298,7 +300,8 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void k_attn_forward(const AttnArgs
     typename T::V8 q[DP / 16];
     row_operands<T, DP>(q, a.q + (live ? row_at(a, a.qs, b, kvh, row) : 0), live, a.head_dim);
 
-    f32x16 o[DP / 32] = {};
+    f32x16 sums[1][DP / 32] = {};
+    f32x16(&o)[DP / 32] = sums[0];
     float top = -INFINITY, total = 0.0f;                // maximum (scaled, in powers of two); this lane's share of the sum
 
     Stage<DP, TN, GT, MODE> stage;
@@ -366,7 +369,10 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void k_attn_forward(const AttnArgs
             for (int r = 0; r < 16; ++r) sum += x[mt][r];
             total += sum;
 #pragma unroll
-            for (int part = 0; part < 2; ++part) columns_times<T, DP>(o, vt, 32 * mt + 16 * part, rounded<T>(x[mt], part));
+            for (int part = 0; part < 2; ++part) {
+                const typename T::V8 p[1] = {rounded<T>(x[mt], part)};
+                columns_times<T, DP, 1>(sums, vt, 32 * mt + 16 * part, p);
+            }
         }
     }
     total = sum_of_halves(total);
@@ -498,7 +504,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a)
         if (live && h == 0 && split == 0) a.delta[bh * a.rows + row] = delta;
     }
 
-    f32x16 dq[DP / 32] = {};
+    f32x16 dq[1][DP / 32] = {};
     Stage<DP, TN, 256, MODE> stage;
     auto first_of = [&](uint32_t s) { return (step0 + s) * TN; };
     auto info_of = [&](uint32_t s) { return keys.info(first_of(s) + lane); };
@@ -533,24 +539,29 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a)
 #pragma unroll
             for (int r = 0; r < 16; ++r) x[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], a.scale_log2, -lse2)) * (dp[r] - delta);
 #pragma unroll
-            for (int part = 0; part < 2; ++part) columns_times<T, DP>(dq, kt, 32 * mt + 16 * part, rounded<T>(x, part));
+            for (int part = 0; part < 2; ++part) {
+                const typename T::V8 ds[1] = {rounded<T>(x, part)};
+                columns_times<T, DP, 1>(dq, kt, 32 * mt + 16 * part, ds);
+            }
         }
     }
     if (!live) return;
-    if (a.splits == 1) store_row<T, DP>(a.dq + row_at(a, a.dqs, b, kvh, row), dq, a.scale, a.head_dim);
-    else store_part<DP>(a.part_o + (((int64_t)split * a.batch * a.kv_heads + bh) * a.rows + row) * DP, dq, a.scale);
+    if (a.splits == 1) store_row<T, DP>(a.dq + row_at(a, a.dqs, b, kvh, row), dq[0], a.scale, a.head_dim);
+    else store_part<DP>(a.part_o + (((int64_t)split * a.batch * a.kv_heads + bh) * a.rows + row) * DP, dq[0], a.scale);
 }
 
-// dK and dV of 128 keys, 32 a wave, over the rows of a piece.  Per 32 rows: S = Q K^T, dP = dO V^T (rows along m, a lane holds one
+// dK and dV of 128 KT keys, 32 KT a wave, over the rows of a piece.  Per 32 rows: S = Q K^T, dP = dO V^T (rows along m, a lane holds one
 // key), dV^T += dO^T P, dK^T += Q^T dS; the rows' Q and dO are read from shared memory both along and across.
-template <class T, int DP, int MODE>
-__global__ __launch_bounds__(256, 2) void k_attn_dkv(const AttnArgs a)
+template <class T, int DP, int KT, int MODE>
+__global__ __launch_bounds__(256, KT == 1 ? 2 : 1) void k_attn_dkv(const AttnArgs a)
 {
     constexpr int TR = 32, CH = DP / 8, LOADS = TR * CH / 256 ? TR * CH / 256 : 1, ROWS = 256 / CH;
     __shared__ u32x4 tiles[2][2][TR * CH];
     __shared__ f32x4 stats[2][2][TR / 4];               // lse in powers of two, D
+    constexpr bool AWAY = DP == 128;                    // V's operands in shared memory: with them 256 registers do not suffice
+    __shared__ u32x4 away[AWAY ? KT : 1][AWAY ? 4 : 1][DP / 16][64];
     const int thread = threadIdx.x, wave = thread >> 6, lane = thread & 63, n = lane & 31, h = lane >> 5;
-    const uint32_t key_tiles = (a.kv_len + 127) / 128;
+    const uint32_t key_tiles = (a.kv_len + 128 * KT - 1) / (128 * KT);
     uint32_t at = by_die(blockIdx.x, gridDim.x);
     const uint32_t kt = at % key_tiles;
     at /= key_tiles;
@@ -558,81 +569,112 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkv(const AttnArgs a)
     at /= a.splits;
     const uint32_t kvh = at % a.kv_heads, b = at / a.kv_heads;
     const Keys<MODE> keys(a, b, kvh);
-    const uint32_t key = kt * 128 + wave * 32 + n;
-    const bool inside = key < a.kv_len, valid = key < keys.end && keys.info(key) >= 0;
-    const bool whole = __all(valid);
-    const uint32_t steps = kt * 128 < keys.end ? (a.rows + TR - 1) / TR : 0, per = (steps + a.splits - 1) / a.splits;
+    const uint32_t key0 = (kt * 4 + wave) * 32 * KT + n;
+    const uint32_t steps = kt * 128 * KT < keys.end ? (a.rows + TR - 1) / TR : 0, per = (steps + a.splits - 1) / a.splits;
     const uint32_t step0 = split * per < steps ? split * per : steps, count = step0 + per < steps ? per : steps - step0;
 
-    typename T::V8 k[DP / 16], v[DP / 16];
-    row_operands<T, DP>(k, a.k + (valid ? b * a.ks.batch + key * a.ks.token + kvh * a.ks.head : 0), valid, a.head_dim);
-    row_operands<T, DP>(v, a.v + (valid ? b * a.vs.batch + key * a.vs.token + kvh * a.vs.head : 0), valid, a.head_dim);
+    typename T::V8 k[KT][DP / 16], v[KT][DP / 16];
+    bool valid[KT], whole = true;
+#pragma unroll
+    for (int u = 0; u < KT; ++u) {
+        const uint32_t key = key0 + 32 * u;
+        valid[u] = key < keys.end && keys.info(key) >= 0;
+        whole = whole && __all(valid[u]);
+        row_operands<T, DP>(k[u], a.k + (valid[u] ? b * a.ks.batch + key * a.ks.token + kvh * a.ks.head : 0), valid[u], a.head_dim);
+        row_operands<T, DP>(v[u], a.v + (valid[u] ? b * a.vs.batch + key * a.vs.token + kvh * a.vs.head : 0), valid[u], a.head_dim);
+    }
+    if (AWAY) {                                         // a lane reads what it has written itself
+#pragma unroll
+        for (int u = 0; u < KT; ++u)
+#pragma unroll
+            for (int t = 0; t < DP / 16; ++t) away[AWAY ? u : 0][AWAY ? wave : 0][t][lane] = __builtin_bit_cast(u32x4, v[u][t]);
+    }
     const int64_t bh = (int64_t)b * a.kv_heads + kvh;
 
+    // Rows past the last one and columns past the head's repeat existing ones: probabilities are 0 there, K and V are.
     u32x4 rq[LOADS], ro[LOADS];
     float stat = 0.0f;
-    const int c = thread % CH, row0 = thread / CH;
+    const int row0 = thread / CH % TR, c = 8 * (thread % CH) < (int)a.head_dim ? thread % CH : 0;
     auto load = [&](uint32_t s) {
+        const uint32_t first = (step0 + s) * TR;
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const uint32_t in_tile = row0 + i * ROWS, row = (step0 + s) * TR + in_tile;
-            const bool ok = in_tile < TR && row < a.rows && c * 8 < (int)a.head_dim;
-            rq[i] = ok ? *reinterpret_cast<const u32x4 *>(a.q + row_at(a, a.qs, b, kvh, row) + c * 8) : zeros();
-            ro[i] = ok ? *reinterpret_cast<const u32x4 *>(a.d_o + row_at(a, a.dos, b, kvh, row) + c * 8) : zeros();
+            const uint32_t row = first + row0 + i * ROWS, token = token_of(a, row < a.rows ? row : a.rows - 1), head = kvh * a.group + ((row < a.rows ? row : a.rows - 1) - token * a.group);
+            rq[i] = *reinterpret_cast<const u32x4 *>(a.q + (b * a.qs.batch + token * a.qs.token + head * a.qs.head + c * 8));
+            ro[i] = *reinterpret_cast<const u32x4 *>(a.d_o + (b * a.dos.batch + token * a.dos.token + head * a.dos.head + c * 8));
         }
-        if (thread < 2 * TR) {
-            const uint32_t row = (step0 + s) * TR + thread % TR;
-            stat = thread < TR ? INFINITY : 0.0f;       // rows that are not there, or see nothing: probabilities 0
-            if (row < a.rows) {
-                stat = thread < TR ? a.lse_in[lse_at(a, b, kvh, row)] : a.delta[bh * a.rows + row];
-                if (thread < TR) stat = stat == -INFINITY ? INFINITY : stat * LOG2E;
-            }
+        const uint32_t row = first + thread % TR;
+        const bool there = row < a.rows;
+        if (thread < TR) {
+            const float l = a.lse_in[lse_at(a, b, kvh, there ? row : a.rows - 1)];
+            stat = there && l != -INFINITY ? l * LOG2E : INFINITY;      // rows that are not there, or see nothing: probabilities 0
+        } else if (thread < 2 * TR) {
+            stat = a.delta[bh * a.rows + (there ? row : a.rows - 1)];
         }
     };
-    f32x16 dk[DP / 32] = {}, dv[DP / 32] = {};
+    f32x16 dk[KT][DP / 32] = {}, dv[KT][DP / 32] = {};
     if (count) load(0);
     for (uint32_t s = 0; s < count; ++s) {
         u32x4 *qt = tiles[s & 1][0], *ot = tiles[s & 1][1];
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            const int in_tile = row0 + i * ROWS;
-            if (TR * CH >= 256 || in_tile < TR) {
-                qt[chunk_at<CH>(in_tile, c)] = rq[i];
-                ot[chunk_at<CH>(in_tile, c)] = ro[i];
-            }
+        for (int i = 0; i < LOADS; ++i) {               // (with 32 values a head two threads store the same)
+            qt[chunk_at<CH>(row0 + i * ROWS, thread % CH)] = rq[i];
+            ot[chunk_at<CH>(row0 + i * ROWS, thread % CH)] = ro[i];
         }
         if (thread < 2 * TR) reinterpret_cast<float *>(stats[s & 1])[thread] = stat;
         __syncthreads();
         if (s + 1 < count) load(s + 1);
-        f32x16 x = keys_by_rows<T, DP>(qt, 0, k);
-        const f32x16 dp = keys_by_rows<T, DP>(ot, 0, v);
-        f32x16 ds;
+        f32x16 x[KT] = {}, dp[KT] = {};
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const f32x4 lse2 = stats[s & 1][0][2 * u + h], delta = stats[s & 1][1][2 * u + h];
+        for (int t = 0; t < DP / 16; ++t) {
+            const auto q = as_operand<T>(qt[chunk_at<CH>(n, 2 * t + h)]);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int r = 4 * u + j;
-                float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], a.scale_log2, -lse2[j]));
-                if (!whole) p = valid ? p : 0.0f;
-                x[r] = p;
-                ds[r] = p * (dp[r] - delta[j]);
-            }
+            for (int u = 0; u < KT; ++u) x[u] = T::mma(q, k[u][t], x[u]);
+        }
+#pragma unroll
+        for (int t = 0; t < DP / 16; ++t) {
+            const auto d = as_operand<T>(ot[chunk_at<CH>(n, 2 * t + h)]);
+#pragma unroll
+            for (int u = 0; u < KT; ++u) dp[u] = T::mma(d, AWAY ? as_operand<T>(away[AWAY ? u : 0][AWAY ? wave : 0][t][lane]) : v[u][t], dp[u]);
+        }
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const f32x4 lse2 = stats[s & 1][0][2 * g + h], delta = stats[s & 1][1][2 * g + h];
+#pragma unroll
+            for (int u = 0; u < KT; ++u)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int r = 4 * g + j;
+                    float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[u][r], a.scale_log2, -lse2[j]));
+                    if (!whole) p = valid[u] ? p : 0.0f;
+                    x[u][r] = p;
+                    dp[u][r] = p * (dp[u][r] - delta[j]);
+                }
         }
 #pragma unroll
         for (int part = 0; part < 2; ++part) {
-            columns_times<T, DP>(dv, ot, 16 * part, rounded<T>(x, part));
-            columns_times<T, DP>(dk, qt, 16 * part, rounded<T>(ds, part));
+            typename T::V8 p[KT], ds[KT];
+#pragma unroll
+            for (int u = 0; u < KT; ++u) {
+                p[u] = rounded<T>(x[u], part);
+                ds[u] = rounded<T>(dp[u], part);
+            }
+            columns_times<T, DP, KT>(dv, ot, 16 * part, p);
+            columns_times<T, DP, KT>(dk, qt, 16 * part, ds);
         }
     }
-    if (!inside) return;
-    if (a.splits == 1) {
-        store_row<T, DP>(a.dk + b * a.dks.batch + key * a.dks.token + kvh * a.dks.head, dk, a.scale, a.head_dim);
-        store_row<T, DP>(a.dv + b * a.dvs.batch + key * a.dvs.token + kvh * a.dvs.head, dv, 1.0f, a.head_dim);
-    } else {
-        float *part = a.part_o + ((((int64_t)split * a.batch * a.kv_heads + bh) * a.kv_len + key) * 2) * DP;
-        store_part<DP>(part, dk, a.scale);
-        store_part<DP>(part + DP, dv, 1.0f);
+#pragma unroll
+    for (int u = 0; u < KT; ++u) {
+        const uint32_t key = key0 + 32 * u;
+        if (key >= a.kv_len) continue;
+        if (a.splits == 1) {
+            store_row<T, DP>(a.dk + b * a.dks.batch + key * a.dks.token + kvh * a.dks.head, dk[u], a.scale, a.head_dim);
+            store_row<T, DP>(a.dv + b * a.dvs.batch + key * a.dvs.token + kvh * a.dvs.head, dv[u], 1.0f, a.head_dim);
+        } else {
+            float *part = a.part_o + ((((int64_t)split * a.batch * a.kv_heads + bh) * a.kv_len + key) * 2) * DP;
+            store_part<DP>(part, dk[u], a.scale);
+            store_part<DP>(part + DP, dv[u], 1.0f);
+        }
     }
 }
 

@@ -7,6 +7,10 @@
 namespace mmee {
 namespace {
 
+#ifndef KB
+#define KB 1
+#endif
+constexpr int KEY_BLOCKS = KB;
 constexpr uint64_t MOST_ROWS = 1u << 28;        // rows of one key/value head, keys: token_of() and key numbers stay exact
 constexpr int64_t MOST_TOKEN_STRIDE = 1 << 24;  // a tile's offsets fit 32 bits
 
@@ -105,7 +109,7 @@ int plan_attn(const mmee_attn *x, bool pointers, AttnPlan &p)
             return MMEE_EINVAL;
     }
     // backward
-    const uint64_t heads_all = (uint64_t)a.batch * a.kv_heads, tiles = ((uint64_t)a.rows + 127) / 128, key_tiles = ((uint64_t)a.kv_len + 127) / 128;
+    const uint64_t heads_all = (uint64_t)a.batch * a.kv_heads, tiles = ((uint64_t)a.rows + 127) / 128, key_tiles = ((uint64_t)a.kv_len + 128 * KEY_BLOCKS - 1) / (128 * KEY_BLOCKS);
     p.dq_splits = pieces(tiles * heads_all, ((uint64_t)a.kv_len + 63) / 64, 4);
     p.dkv_splits = pieces(key_tiles * heads_all, ((uint64_t)a.rows + 31) / 32, 8);
     p.dq_blocks = tiles * heads_all * p.dq_splits;
@@ -178,7 +182,7 @@ void backward_as(const AttnPlan &p, hipStream_t stream)
     }
     if (p.dkv_blocks) {
         a.splits = p.dkv_splits;
-        hipLaunchKernelGGL((k_attn_dkv<T, DP, MODE>), dim3((uint32_t)p.dkv_blocks), dim3(256), 0, stream, a);
+        hipLaunchKernelGGL((k_attn_dkv<T, DP, KEY_BLOCKS, MODE>), dim3((uint32_t)p.dkv_blocks), dim3(256), 0, stream, a);
         const uint64_t per = 256 / (DP / 2);
         if (a.splits > 1) hipLaunchKernelGGL((k_attn_sum<T, DP, 1>), dim3((uint32_t)((heads_all * a.kv_len + per - 1) / per)), dim3(256), 0, stream, a);
     }

@@ -12,6 +12,8 @@
 // instructions need them.
 #pragma once
 
+#include <type_traits>
+
 #include "launch.h"
 #include "mfma.h"
 
@@ -98,6 +100,8 @@ struct Keys {
             nodes = (uint32_t)(n < 0 ? 0 : n > (int64_t)a.q_len ? (int64_t)a.q_len : n);
             end = held + nodes > a.kv_len ? a.kv_len : held + nodes;
             if (!nodes || !a.n_pages) end = 0;          // no row looks at anything
+            held = __builtin_amdgcn_readfirstlane(held);
+            nodes = __builtin_amdgcn_readfirstlane(nodes);
         } else {
             end = a.kv_len;
             if (a.kv_lens) {
@@ -105,6 +109,7 @@ struct Keys {
                 end = len < 0 ? 0 : (uint32_t)len < end ? (uint32_t)len : end;
             }
         }
+        end = __builtin_amdgcn_readfirstlane(end);      // the same in all lanes: loops and branches on it are scalar
     }
 
     // What decides whether key `at` counts: its page, or -1; its mask byte.
@@ -118,57 +123,48 @@ struct Keys {
     }
 };
 
-// One thread's share of a tile of TN keys by GT threads: loads in flight in registers, then to shared memory.  Keys past the last one and
-// columns past the head's repeat existing ones (probabilities, and the rows' operands, are 0 there), so that nothing branches; masked keys
-// and those of pages that are not there become zeros on the way, since they may hold anything.
+// One thread's share of a tile of TN keys' K or V by GT threads: loads in flight in registers, then to shared memory.  Keys past the last one
+// and columns past the head's repeat existing ones (probabilities, and the rows' operands, are 0 there), so that nothing branches; masked
+// keys and those of pages that are not there become zeros on the way, since they may hold anything.
 template <int DP, int TN, int GT, int MODE>
 struct Stage {
     static constexpr int CH = DP / 8, LOADS = TN * CH / GT, ROWS = GT / CH;     // rows that one load of all threads covers
     static_assert(LOADS * GT == TN * CH && ROWS * CH == GT, "a tile is dealt out evenly");
-    u32x4 k[LOADS], v[LOADS];
+    u32x4 r[LOADS];
     bool counts[MODE == MODE_PLAIN ? 1 : LOADS];
 
     // info: of key first + (lane mod TN), as Keys::info gives it.  There is a key at least.
-    __device__ __forceinline__ void load(const Keys<MODE> &keys, int thread, uint32_t first, int info)
+    __device__ __forceinline__ void load(const Keys<MODE> &keys, const uint16_t *from, const Strides &s, int thread, uint32_t first, int info)
     {
         const AttnArgs &a = keys.a;
         const int row0 = thread / CH, c = 8 * (thread % CH) < (int)a.head_dim ? thread % CH : 0;
         if (MODE == MODE_TREE) {
-            const uint16_t *kb = a.k + keys.kvh * a.ks.head + c * 8, *vb = a.v + keys.kvh * a.vs.head + c * 8;
+            const uint16_t *base = from + keys.kvh * s.head + c * 8;
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) {
                 const int row = row0 + i * ROWS, page = __shfl(info, row);
                 const uint32_t inside = (first + row) & ((1u << a.page_shift) - 1);
                 counts[MODE == MODE_PLAIN ? 0 : i] = page >= 0;
-                const int64_t from = page >= 0 ? page : 0;
-                k[i] = *reinterpret_cast<const u32x4 *>(kb + from * a.ks.batch + inside * a.ks.token);
-                v[i] = *reinterpret_cast<const u32x4 *>(vb + from * a.vs.batch + inside * a.vs.token);
+                r[i] = *reinterpret_cast<const u32x4 *>(base + (int64_t)(page >= 0 ? page : 0) * s.batch + inside * s.token);
             }
             return;
         }
-        const uint32_t base = first < keys.end ? first : keys.end - 1, last = keys.end - 1 - base;
-        const uint16_t *kb = a.k + keys.b * a.ks.batch + keys.kvh * a.ks.head + base * a.ks.token;
-        const uint16_t *vb = a.v + keys.b * a.vs.batch + keys.kvh * a.vs.head + base * a.vs.token;
-        const uint32_t kt = (uint32_t)a.ks.token, vt = (uint32_t)a.vs.token;    // a tile spans less than 2^31 elements
+        const uint32_t begin = first < keys.end ? first : keys.end - 1, last = keys.end - 1 - begin;
+        const uint16_t *base = from + keys.b * s.batch + keys.kvh * s.head + begin * s.token;
+        const uint32_t step = (uint32_t)s.token;        // a tile spans less than 2^31 elements
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const uint32_t row = row0 + i * ROWS, at = row < last ? row : last;
             if (MODE == MODE_MASK) counts[MODE == MODE_PLAIN ? 0 : i] = __shfl(info, row) >= 0;
-            k[i] = *reinterpret_cast<const u32x4 *>(kb + (at * kt + c * 8));
-            v[i] = *reinterpret_cast<const u32x4 *>(vb + (at * vt + c * 8));
+            r[i] = *reinterpret_cast<const u32x4 *>(base + (at * step + c * 8));
         }
     }
 
-    __device__ __forceinline__ void store(u32x4 *ks, u32x4 *vs, int thread) const
+    __device__ __forceinline__ void store(u32x4 *tile, int thread) const
     {
         const int c = thread % CH, row0 = thread / CH;
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            const int at = chunk_at<CH>(row0 + i * ROWS, c);
-            const bool as_is = MODE == MODE_PLAIN || counts[MODE == MODE_PLAIN ? 0 : i];
-            ks[at] = as_is ? k[i] : zeros();
-            vs[at] = as_is ? v[i] : zeros();
-        }
+        for (int i = 0; i < LOADS; ++i) tile[chunk_at<CH>(row0 + i * ROWS, c)] = MODE == MODE_PLAIN || counts[MODE == MODE_PLAIN ? 0 : i] ? r[i] : zeros();
     }
 };
 
@@ -242,7 +238,7 @@ __device__ __forceinline__ void store_part(float *row, const f32x16 (&acc)[DP / 
 template <int MODE, int TN>
 __device__ __forceinline__ uint64_t seen(const Keys<MODE> &keys, uint32_t first, uint64_t counted, uint32_t token, bool &all)
 {
-    const uint64_t whole = TN == 64 ? ~0ull : (1ull << TN) - 1;
+    const uint64_t whole = ~0ull >> (64 - TN);
     if (MODE == MODE_PLAIN) {
         const uint32_t left = keys.end > first ? keys.end - first : 0;
         counted = left >= TN ? whole : (1ull << left) - 1;
@@ -277,7 +273,7 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void k_attn_forward(const AttnArgs
 {
     constexpr int TN = WR == 1 ? 32 : 64, MT = TN / 32, CH = DP / 8, GT = 64 * WR, NB = WR == 4 ? 2 : 1;
     static_assert(NB == 1 || WK == 1, "two buffers for one group");
-    __shared__ u32x4 tiles[NB * WK][2][TN * CH];
+    __shared__ u32x4 tiles[2][NB * WK][TN * CH];        // K, V
     __shared__ float marks[2][WK][32 * WR];
     const int thread = threadIdx.x % GT, wave = threadIdx.x >> 6, wr = wave % WR, wk = wave / WR, lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
 
@@ -304,53 +300,47 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void k_attn_forward(const AttnArgs
     f32x16(&o)[DP / 32] = sums[0];
     float top = -INFINITY, total = 0.0f;                // maximum (scaled, in powers of two); this lane's share of the sum
 
-    Stage<DP, TN, GT, MODE> stage;
+    // Tile s + 1's scores are formed beside tile s's exponentials, and its maximum beside tile s's product with V, so that matrix
+    // and vector instructions of one wave overlap: K runs a tile ahead of V.
+    Stage<DP, TN, GT, MODE> sk, sv;
+    u32x4(*kt)[TN * CH] = &tiles[0][wk * NB], (*vt)[TN * CH] = &tiles[1][wk * NB];
     auto first_of = [&](uint32_t s) { return ((step0 + s) * WK + wk) * TN; };
     auto info_of = [&](uint32_t s) { return keys.info(first_of(s) + lane % TN); };
-    int info = 0, next_info = 0;
-    if (count) {
-        info = info_of(0);
-        stage.load(keys, thread, first_of(0), info);
-        next_info = info_of(1);
-    }
-    for (uint32_t s = 0; s < count; ++s) {
-        u32x4 *kt = tiles[NB == 2 ? s & 1 : wk][0], *vt = tiles[NB == 2 ? s & 1 : wk][1];
-        if (NB == 1 && s) {
-            if (WR > 1) __syncthreads(); else wave_sync();
-        }
-        stage.store(kt, vt, thread);
-        const uint64_t counted = MODE == MODE_PLAIN ? 0 : __ballot(info >= 0) & (TN == 64 ? ~0ull : (1ull << TN) - 1);
-        const uint32_t first = first_of(s);
-        if (WR > 1) __syncthreads(); else wave_sync();
-        if (s + 1 < count) {
-            info = next_info;
-            stage.load(keys, thread, first_of(s + 1), info);
-            next_info = info_of(s + 2);
-        }
+    auto sync = [&] { if (WR > 1) __syncthreads(); else wave_sync(); };
+    constexpr uint64_t WHOLE = ~0ull >> (64 - TN);
+    f32x16 x[MT], ahead[MT];
+    float most = -INFINITY;                             // of x, scaled
+    int info[3] = {};                                   // of the tile whose scores come next and the two behind it
 
-        f32x16 x[MT];
+    auto scores = [&](f32x16 (&to)[MT], uint32_t s) {
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) x[mt] = keys_by_rows<T, DP>(kt, 32 * mt, q);
+        for (int mt = 0; mt < MT; ++mt) to[mt] = keys_by_rows<T, DP>(kt[NB == 2 ? s & 1 : 0], 32 * mt, q);
+    };
+    auto mask = [&](f32x16 (&to)[MT], uint32_t s) {
         bool all;
-        const uint64_t bits = seen<MODE, TN>(keys, first, counted, token, all);
-        if (!all) {
+        const uint64_t counted = MODE == MODE_PLAIN ? 0 : __ballot(info[0] >= 0) & WHOLE, bits = seen<MODE, TN>(keys, first_of(s), counted, token, all);
+        if (all) return;
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-                const uint32_t mine = (uint32_t)(bits >> (32 * mt)) >> (4 * h);
+        for (int mt = 0; mt < MT; ++mt) {
+            const uint32_t mine = (uint32_t)(bits >> (32 * mt)) >> (4 * h);
 #pragma unroll
-                for (int r = 0; r < 16; ++r) x[mt][r] = mine >> (8 * (r / 4) + r % 4) & 1 ? x[mt][r] : -INFINITY;
-            }
+            for (int r = 0; r < 16; ++r) to[mt][r] = mine >> (8 * (r / 4) + r % 4) & 1 ? to[mt][r] : -INFINITY;
         }
-        float m = x[0][0];
+    };
+    auto maximum = [&](const f32x16 (&of)[MT]) {
+        float m = of[0][0];
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) m = __builtin_elementwise_maximum(m, x[mt][r]);
-        m = max_of_halves(m) * a.scale_log2;
-        // The sum may be taken against any mark near the maximum.  A mark that is kept until a row outgrows it by 2^8 spares
-        // scaling 16 DP / 32 accumulators a tile; 32-bit sums hold 2^8 times as much, and so do probabilities in 16 bits.
-        if (__any(!(m <= top + 8.0f))) {
-            const float mark = __builtin_elementwise_maximum(top, m);
+            for (int r = 0; r < 16; ++r) m = __builtin_elementwise_maximum(m, of[mt][r]);
+        return m;
+    };
+    // The sum may be taken against any mark near the maximum.  A mark that is kept until a row outgrows it by 2^8 spares scaling
+    // 16 DP / 32 accumulators a tile; 32-bit sums hold 2^8 times as much, and so do probabilities in 16 bits.
+    auto raise = [&] {
+        most = max_of_halves(most) * a.scale_log2;
+        if (__any(!(most <= top + 8.0f))) {
+            const float mark = __builtin_elementwise_maximum(top, most);
             const float keep = top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top - mark);
             top = mark;
             total *= keep;
@@ -359,21 +349,100 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void k_attn_forward(const AttnArgs
 #pragma unroll
                 for (int r = 0; r < 16; ++r) o[dt][r] *= keep;
         }
+    };
+
+    if (count) {
+        info[0] = info_of(0);
+        sk.load(keys, a.k, a.ks, thread, first_of(0), info[0]);
+        sv.load(keys, a.v, a.vs, thread, first_of(0), info[0]);
+        info[1] = info_of(1);
+        sk.store(kt[0], thread);
+        sv.store(vt[0], thread);
+        sync();
+        sk.load(keys, a.k, a.ks, thread, first_of(1), info[1]);
+        sv.load(keys, a.v, a.vs, thread, first_of(1), info[1]);
+        info[2] = info_of(2);
+        scores(x, 0);
+        mask(x, 0);
+        most = maximum(x);
+        raise();
+        if (NB == 1) sync();
+        sk.store(kt[NB - 1], thread);
+        sync();
+        sk.load(keys, a.k, a.ks, thread, first_of(2), info[2]);
+        info[0] = info[1];
+        info[1] = info[2];
+        info[2] = info_of(3);
+    }
+    // Tile s from its scores `now`; unless it is the last, the next one's scores into `next`.
+    auto step = [&](uint32_t s, f32x16 (&now)[MT], f32x16 (&next)[MT], auto more) {
         const float off = top == -INFINITY ? 0.0f : top;
+        typename T::V8 p[MT][2][1];
+        if (more) scores(next, s + 1);
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) x[mt][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[mt][r], a.scale_log2, -off));
+            for (int r = 0; r < 16; ++r) now[mt][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(now[mt][r], a.scale_log2, -off));
             float sum = 0.0f;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) sum += x[mt][r];
+            for (int r = 0; r < 16; ++r) sum += now[mt][r];
             total += sum;
-#pragma unroll
-            for (int part = 0; part < 2; ++part) {
-                const typename T::V8 p[1] = {rounded<T>(x[mt], part)};
-                columns_times<T, DP, 1>(sums, vt, 32 * mt + 16 * part, p);
-            }
+            p[mt][0][0] = rounded<T>(now[mt], 0);
+            p[mt][1][0] = rounded<T>(now[mt], 1);
         }
+        if (more) {
+            // a product after every operand read and a share of the exponentials' work, in one block of straight-line code
+            asm volatile("" ::"v"(total));
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int part = 0; part < 2; ++part) asm volatile("" ::"v"(p[mt][part][0]));
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+#pragma unroll
+            for (int i = 0; i < MT * DP / 16; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x002, (MT * 56 + MT * DP / 16 - 1) / (MT * DP / 16), 0);
+            }
+            mask(next, s + 1);
+        }
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int part = 0; part < 2; ++part) columns_times<T, DP, 1>(sums, vt[NB == 2 ? s & 1 : 0], 32 * mt + 16 * part, p[mt][part]);
+        if (!more) return;
+        most = maximum(next);
+        __builtin_amdgcn_sched_group_barrier(0x100, 4, 1);
+#pragma unroll
+        for (int i = 0; i < MT * DP / 16; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
+            __builtin_amdgcn_sched_group_barrier(0x002, 2, 1);
+        }
+        raise();
+        if (NB == 1) sync();
+        sk.store(kt[NB == 2 ? s & 1 : 0], thread);
+        sv.store(vt[NB == 2 ? (s + 1) & 1 : 0], thread);
+        sync();
+        sk.load(keys, a.k, a.ks, thread, first_of(s + 3), info[2]);
+        sv.load(keys, a.v, a.vs, thread, first_of(s + 2), info[1]);
+        info[0] = info[1];
+        info[1] = info[2];
+        info[2] = info_of(s + 4);
+    };
+    if (count) {
+        uint32_t s = 0;
+        for (; s + 2 < count; s += 2) {
+            step(s, x, ahead, std::true_type());
+            step(s + 1, ahead, x, std::true_type());
+        }
+        if (s + 1 < count) {
+            step(s, x, ahead, std::true_type());
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) x[mt] = ahead[mt];
+            ++s;
+        }
+        step(s, x, ahead, std::false_type());
     }
     total = sum_of_halves(total);
 
@@ -505,24 +574,27 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a)
     }
 
     f32x16 dq[1][DP / 32] = {};
-    Stage<DP, TN, 256, MODE> stage;
+    Stage<DP, TN, 256, MODE> sk, sv;
     auto first_of = [&](uint32_t s) { return (step0 + s) * TN; };
     auto info_of = [&](uint32_t s) { return keys.info(first_of(s) + lane); };
     int info = 0, next_info = 0;
     if (count) {
         info = info_of(0);
-        stage.load(keys, thread, first_of(0), info);
+        sk.load(keys, a.k, a.ks, thread, first_of(0), info);
+        sv.load(keys, a.v, a.vs, thread, first_of(0), info);
         next_info = info_of(1);
     }
     for (uint32_t s = 0; s < count; ++s) {
         u32x4 *kt = tiles[s & 1][0], *vt = tiles[s & 1][1];
-        stage.store(kt, vt, thread);
+        sk.store(kt, thread);
+        sv.store(vt, thread);
         const uint64_t counted = MODE == MODE_PLAIN ? 0 : __ballot(info >= 0);
         const uint32_t first = first_of(s);
         __syncthreads();
         if (s + 1 < count) {
             info = next_info;
-            stage.load(keys, thread, first_of(s + 1), info);
+            sk.load(keys, a.k, a.ks, thread, first_of(s + 1), info);
+            sv.load(keys, a.v, a.vs, thread, first_of(s + 1), info);
             next_info = info_of(s + 2);
         }
         bool all;

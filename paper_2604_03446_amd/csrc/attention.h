@@ -271,10 +271,11 @@ __device__ __forceinline__ uint64_t seen(const Keys<MODE> &keys, uint32_t first,
 template <class T, int DP, int WR, int WK, int MODE>
 __global__ __launch_bounds__(64 * WR * WK, 2) void k_attn_forward(const AttnArgs a)
 {
-    constexpr int TN = WR == 1 ? 32 : 64, MT = TN / 32, CH = DP / 8, GT = 64 * WR, NB = WR == 4 ? 2 : 1;
+    constexpr int TN = WR == 4 ? 64 : 32, MT = TN / 32, CH = DP / 8, GT = 64 * WR, NB = WR == 4 ? 2 : 1, TILES = 2 * NB * WK * TN * CH;
     static_assert(NB == 1 || WK == 1, "two buffers for one group");
-    __shared__ u32x4 tiles[2][NB * WK][TN * CH];        // K, V
-    __shared__ float marks[2][WK][32 * WR];
+    constexpr int JOIN = WK > 1 ? WK * 32 * WR * DP / 4 : 0;
+    __shared__ u32x4 memory[TILES > JOIN ? TILES : JOIN];
+    __shared__ float marks[2][WK][WK > 1 ? 32 * WR : 1];
     const int thread = threadIdx.x % GT, wave = threadIdx.x >> 6, wr = wave % WR, wk = wave / WR, lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
 
     uint32_t at = by_die(blockIdx.x, gridDim.x);
@@ -300,21 +301,21 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void k_attn_forward(const AttnArgs
     f32x16(&o)[DP / 32] = sums[0];
     float top = -INFINITY, total = 0.0f;                // maximum (scaled, in powers of two); this lane's share of the sum
 
-    // Tile s + 1's scores are formed beside tile s's exponentials, and its maximum beside tile s's product with V, so that matrix
-    // and vector instructions of one wave overlap: K runs a tile ahead of V.
     Stage<DP, TN, GT, MODE> sk, sv;
-    u32x4(*kt)[TN * CH] = &tiles[0][wk * NB], (*vt)[TN * CH] = &tiles[1][wk * NB];
+    u32x4 *const mine = memory + wk * 2 * NB * TN * CH;
+    auto k_tile = [&](uint32_t s) { return mine + (NB == 2 ? s & 1 : 0) * TN * CH; };
+    auto v_tile = [&](uint32_t s) { return mine + (NB + (NB == 2 ? s & 1 : 0)) * TN * CH; };
     auto first_of = [&](uint32_t s) { return ((step0 + s) * WK + wk) * TN; };
     auto info_of = [&](uint32_t s) { return keys.info(first_of(s) + lane % TN); };
     auto sync = [&] { if (WR > 1) __syncthreads(); else wave_sync(); };
     constexpr uint64_t WHOLE = ~0ull >> (64 - TN);
-    f32x16 x[MT], ahead[MT];
-    float most = -INFINITY;                             // of x, scaled
+    f32x16 x[MT];
+    float most = -INFINITY;                             // maximum of the scores that are next, scaled
     int info[3] = {};                                   // of the tile whose scores come next and the two behind it
 
     auto scores = [&](f32x16 (&to)[MT], uint32_t s) {
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) to[mt] = keys_by_rows<T, DP>(kt[NB == 2 ? s & 1 : 0], 32 * mt, q);
+        for (int mt = 0; mt < MT; ++mt) to[mt] = keys_by_rows<T, DP>(k_tile(s), 32 * mt, q);
     };
     auto mask = [&](f32x16 (&to)[MT], uint32_t s) {
         bool all;
@@ -351,34 +352,8 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void k_attn_forward(const AttnArgs
         }
     };
 
-    if (count) {
-        info[0] = info_of(0);
-        sk.load(keys, a.k, a.ks, thread, first_of(0), info[0]);
-        sv.load(keys, a.v, a.vs, thread, first_of(0), info[0]);
-        info[1] = info_of(1);
-        sk.store(kt[0], thread);
-        sv.store(vt[0], thread);
-        sync();
-        sk.load(keys, a.k, a.ks, thread, first_of(1), info[1]);
-        sv.load(keys, a.v, a.vs, thread, first_of(1), info[1]);
-        info[2] = info_of(2);
-        scores(x, 0);
-        mask(x, 0);
-        most = maximum(x);
-        raise();
-        if (NB == 1) sync();
-        sk.store(kt[NB - 1], thread);
-        sync();
-        sk.load(keys, a.k, a.ks, thread, first_of(2), info[2]);
-        info[0] = info[1];
-        info[1] = info[2];
-        info[2] = info_of(3);
-    }
-    // Tile s from its scores `now`; unless it is the last, the next one's scores into `next`.
-    auto step = [&](uint32_t s, f32x16 (&now)[MT], f32x16 (&next)[MT], auto more) {
+    auto exponentials = [&](f32x16 (&now)[MT], typename T::V8 (&p)[MT][2][1]) {
         const float off = top == -INFINITY ? 0.0f : top;
-        typename T::V8 p[MT][2][1];
-        if (more) scores(next, s + 1);
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
@@ -390,47 +365,109 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void k_attn_forward(const AttnArgs
             p[mt][0][0] = rounded<T>(now[mt], 0);
             p[mt][1][0] = rounded<T>(now[mt], 1);
         }
-        if (more) {
-            // a product after every operand read and a share of the exponentials' work, in one block of straight-line code
-            asm volatile("" ::"v"(total));
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                for (int part = 0; part < 2; ++part) asm volatile("" ::"v"(p[mt][part][0]));
-            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-#pragma unroll
-            for (int i = 0; i < MT * DP / 16; ++i) {
-                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x002, (MT * 56 + MT * DP / 16 - 1) / (MT * DP / 16), 0);
-            }
-            mask(next, s + 1);
-        }
+    };
+    auto values = [&](uint32_t s, const typename T::V8 (&p)[MT][2][1]) {
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-            for (int part = 0; part < 2; ++part) columns_times<T, DP, 1>(sums, vt[NB == 2 ? s & 1 : 0], 32 * mt + 16 * part, p[mt][part]);
-        if (!more) return;
-        most = maximum(next);
-        __builtin_amdgcn_sched_group_barrier(0x100, 4, 1);
-#pragma unroll
-        for (int i = 0; i < MT * DP / 16; ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
-            __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
-            __builtin_amdgcn_sched_group_barrier(0x002, 2, 1);
+            for (int part = 0; part < 2; ++part) columns_times<T, DP, 1>(sums, v_tile(s), 32 * mt + 16 * part, p[mt][part]);
+    };
+
+    if (WR < 4) {
+        // Few rows: bound by memory and by latencies, tile after tile, the next one on its way.
+        if (count) {
+            info[0] = info_of(0);
+            sk.load(keys, a.k, a.ks, thread, first_of(0), info[0]);
+            sv.load(keys, a.v, a.vs, thread, first_of(0), info[0]);
+            info[1] = info_of(1);
         }
-        raise();
-        if (NB == 1) sync();
-        sk.store(kt[NB == 2 ? s & 1 : 0], thread);
-        sv.store(vt[NB == 2 ? (s + 1) & 1 : 0], thread);
+#pragma unroll 1
+        for (uint32_t s = 0; s < count; ++s) {
+            if (s) sync();
+            sk.store(k_tile(s), thread);
+            sv.store(v_tile(s), thread);
+            sync();
+            if (s + 1 < count) {
+                sk.load(keys, a.k, a.ks, thread, first_of(s + 1), info[1]);
+                sv.load(keys, a.v, a.vs, thread, first_of(s + 1), info[1]);
+            }
+            typename T::V8 p[MT][2][1];
+            scores(x, s);
+            mask(x, s);
+            most = maximum(x);
+            raise();
+            exponentials(x, p);
+            values(s, p);
+            info[0] = info[1];
+            info[1] = info_of(s + 2);
+        }
+    } else if (count) {
+        // Many rows: tile s + 1's scores are formed beside tile s's exponentials, and its maximum beside tile s's product with V, so
+        // that matrix and vector instructions of one wave overlap: K runs a tile ahead of V.
+        f32x16 ahead[MT];
+        info[0] = info_of(0);
+        sk.load(keys, a.k, a.ks, thread, first_of(0), info[0]);
+        sv.load(keys, a.v, a.vs, thread, first_of(0), info[0]);
+        info[1] = info_of(1);
+        sk.store(k_tile(0), thread);
+        sv.store(v_tile(0), thread);
         sync();
-        sk.load(keys, a.k, a.ks, thread, first_of(s + 3), info[2]);
-        sv.load(keys, a.v, a.vs, thread, first_of(s + 2), info[1]);
+        sk.load(keys, a.k, a.ks, thread, first_of(1), info[1]);
+        sv.load(keys, a.v, a.vs, thread, first_of(1), info[1]);
+        info[2] = info_of(2);
+        scores(x, 0);
+        mask(x, 0);
+        most = maximum(x);
+        raise();
+        sk.store(k_tile(1), thread);
+        sync();
+        sk.load(keys, a.k, a.ks, thread, first_of(2), info[2]);
         info[0] = info[1];
         info[1] = info[2];
-        info[2] = info_of(s + 4);
-    };
-    if (count) {
+        info[2] = info_of(3);
+
+        // Tile s from its scores `now`; unless it is the last, the next one's scores into `next`.
+        auto step = [&](uint32_t s, f32x16 (&now)[MT], f32x16 (&next)[MT], auto more) {
+            typename T::V8 p[MT][2][1];
+            constexpr int PRODUCTS = MT * DP / 16;
+            if (more) scores(next, s + 1);
+            exponentials(now, p);
+            if (more) {
+                // in one block of straight-line code: a product after every operand read and a share of the exponentials' work
+                asm volatile("" ::"v"(total));
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                    for (int part = 0; part < 2; ++part) asm volatile("" ::"v"(p[mt][part][0]));
+                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+#pragma unroll
+                for (int i = 0; i < PRODUCTS; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x002, (MT * 56 + PRODUCTS - 1) / PRODUCTS, 0);
+                }
+                mask(next, s + 1);
+            }
+            values(s, p);
+            if (!more) return;
+            most = maximum(next);
+            __builtin_amdgcn_sched_group_barrier(0x100, 4, 1);
+#pragma unroll
+            for (int i = 0; i < PRODUCTS; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
+                __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
+                __builtin_amdgcn_sched_group_barrier(0x002, 2, 1);
+            }
+            raise();
+            sk.store(k_tile(s), thread);
+            sv.store(v_tile(s + 1), thread);
+            sync();
+            sk.load(keys, a.k, a.ks, thread, first_of(s + 3), info[2]);
+            sv.load(keys, a.v, a.vs, thread, first_of(s + 2), info[1]);
+            info[0] = info[1];
+            info[1] = info[2];
+            info[2] = info_of(s + 4);
+        };
         uint32_t s = 0;
         for (; s + 2 < count; s += 2) {
             step(s, x, ahead, std::true_type());
@@ -461,20 +498,19 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void k_attn_forward(const AttnArgs
     }
     // Join the groups: accumulators through the tiles' memory, chunks of four values spread over the banks.
     constexpr int C4 = DP / 4, ALL = 64 * WR * WK, PER_ROW = ALL / (32 * WR);
-    static_assert(sizeof(tiles) >= sizeof(float) * WK * 32 * WR * DP, "accumulators fit");
     __syncthreads();
-    f32x4 *acc = reinterpret_cast<f32x4 *>(&tiles[0][0][0]);
-    const int mine = wr * 32 + n;
+    f32x4 *acc = reinterpret_cast<f32x4 *>(memory);
+    const int my_row = wr * 32 + n;
 #pragma unroll
     for (int dt = 0; dt < DP / 32; ++dt)
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             const f32x4 x = {o[dt][4 * u], o[dt][4 * u + 1], o[dt][4 * u + 2], o[dt][4 * u + 3]};
-            acc[(wk * 32 * WR + mine) * C4 + ((8 * dt + 2 * u + h) ^ (n & (C4 - 1)))] = x;
+            acc[(wk * 32 * WR + my_row) * C4 + ((8 * dt + 2 * u + h) ^ (n & (C4 - 1)))] = x;
         }
     if (h == 0) {
-        marks[0][wk][mine] = top;
-        marks[1][wk][mine] = total;
+        marks[0][wk][WK > 1 ? my_row : 0] = top;
+        marks[1][wk][WK > 1 ? my_row : 0] = total;
     }
     __syncthreads();
     const int r = threadIdx.x / PER_ROW, sub = threadIdx.x % PER_ROW;

@@ -75,7 +75,7 @@ int common(AttnPlan &p, uint32_t dtype, uint32_t batch, uint32_t heads, uint32_t
     // 32 rows to a wave.  Up to 32 rows the four waves of a block take tiles of keys of their own, up to 64 two do.
     p.row_waves = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
     a.row_tiles = (uint32_t)((rows + 32 * p.row_waves - 1) / (32 * p.row_waves));
-    const uint64_t heads_all = (uint64_t)batch * kv_heads, step = p.row_waves == 2 ? 128 : p.row_waves == 1 ? 128 : 64;
+    const uint64_t heads_all = (uint64_t)batch * kv_heads, step = p.row_waves == 1 ? 128 : 64;
     a.splits = pieces(a.row_tiles * heads_all, (kv_len + step - 1) / step, p.row_waves == 4 ? 4 : 2);
     const uint64_t blocks = a.row_tiles * heads_all * a.splits;
     if (blocks > 0x7fffffff) return MMEE_EINVAL;

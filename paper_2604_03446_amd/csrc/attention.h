@@ -42,8 +42,11 @@ struct AttnArgs {
     int64_t table_stride;
     uint32_t page_shift, n_pages, words;
     // keys in pieces
-    uint32_t row_tiles, splits;
-    float *part_o, *part_lse;   // [split][batch][kv_head][row][DP], [..][row]; lse in powers of two
+    uint32_t row_tiles, splits;         // splits: pieces of every sequence
+    uint32_t slots, step_keys, least;   // forward: room for pieces of all sequences, keys of a step, steps of a piece at least
+    bool balanced;                      // forward: pieces by the sequences' lengths, not `splits` of each
+    uint32_t *cut;              // forward, balanced: every sequence's pieces and first slot, for the join
+    float *part_o, *part_lse;   // forward [slot][kv_head][row][DP], [..][row], lse in powers of two; backward [split][batch][kv_head][row or key]..
     // backward
     const uint16_t *d_o, *o_in;
     const float *lse_in;
@@ -91,25 +94,28 @@ struct Keys {
     uint32_t end;               // keys 0 .. end-1 exist
     uint32_t held, nodes;       // tree: keys in the cache before the tree, nodes
 
-    __device__ __forceinline__ Keys(const AttnArgs &args, uint32_t b_, uint32_t kvh_) : a(args), b(b_), kvh(kvh_), held(0), nodes(0)
+    // Keys of sequence b; of a tree also those before it and the nodes.
+    static __device__ __forceinline__ uint32_t length(const AttnArgs &a, uint32_t b, uint32_t &held, uint32_t &nodes)
     {
         if (MODE == MODE_TREE) {
             const int64_t room = (int64_t)a.kv_len;
             const int64_t len = a.cache_lens[b], n = a.node_counts ? a.node_counts[b] : (int32_t)a.q_len;
             held = (uint32_t)(len < 0 ? 0 : len > room ? room : len);
             nodes = (uint32_t)(n < 0 ? 0 : n > (int64_t)a.q_len ? (int64_t)a.q_len : n);
-            end = held + nodes > a.kv_len ? a.kv_len : held + nodes;
-            if (!nodes || !a.n_pages) end = 0;          // no row looks at anything
-            held = __builtin_amdgcn_readfirstlane(held);
-            nodes = __builtin_amdgcn_readfirstlane(nodes);
-        } else {
-            end = a.kv_len;
-            if (a.kv_lens) {
-                const int32_t len = a.kv_lens[b];
-                end = len < 0 ? 0 : (uint32_t)len < end ? (uint32_t)len : end;
-            }
+            if (!nodes || !a.n_pages) return 0;         // no row looks at anything
+            return held + nodes > a.kv_len ? a.kv_len : held + nodes;
         }
+        if (!a.kv_lens) return a.kv_len;
+        const int32_t len = a.kv_lens[b];
+        return len < 0 ? 0 : (uint32_t)len < a.kv_len ? (uint32_t)len : a.kv_len;
+    }
+
+    __device__ __forceinline__ Keys(const AttnArgs &args, uint32_t b_, uint32_t kvh_) : a(args), b(b_), kvh(kvh_), held(0), nodes(0)
+    {
+        end = length(a, b, held, nodes);
         end = __builtin_amdgcn_readfirstlane(end);      // the same in all lanes: loops and branches on it are scalar
+        held = __builtin_amdgcn_readfirstlane(held);
+        nodes = __builtin_amdgcn_readfirstlane(nodes);
     }
 
     // What decides whether key `at` counts: its page, or -1; its mask byte.
@@ -122,6 +128,37 @@ struct Keys {
         return (uint32_t)page < a.n_pages ? page : -1;
     }
 };
+
+// How many pieces the forward pass cuts each of up to 64 sequences into: lane b has sequence b's number and its first slot.  Pieces have
+// as nearly as possible the same number of steps, the least P for which all of them fit the slots: blocks of one round then end
+// together whatever the lengths.  64 values of P between total / slots and three times that are tried at once.
+template <int MODE>
+__device__ __forceinline__ void balance(const AttnArgs &a, uint32_t &pieces, uint32_t &first_slot)
+{
+    const uint32_t lane = threadIdx.x & 63;
+    uint32_t held, nodes;
+    const uint32_t steps = lane < a.batch ? (Keys<MODE>::length(a, lane, held, nodes) + a.step_keys - 1) / a.step_keys : 0;
+    uint32_t total = steps;
+#pragma unroll
+    for (int d = 32; d; d >>= 1) total += __shfl_xor(total, d);
+    const uint32_t low = (total + a.slots - 1) / a.slots, least = low > a.least ? low : a.least;
+    const uint32_t p = least + (uint32_t)(((uint64_t)least * lane + 31) / 32);
+    uint32_t wanted = 0;
+    for (uint32_t b = 0; b < a.batch; ++b) {
+        const uint32_t of = __builtin_amdgcn_readlane(steps, b);
+        wanted += of ? (of + p - 1) / p : 1;
+    }
+    const uint64_t fits = __ballot(wanted <= a.slots);
+    const uint32_t size = fits ? __builtin_amdgcn_readlane(p, __builtin_ctzll(fits)) : 0;
+    pieces = lane < a.batch ? (size && steps ? (steps + size - 1) / size : 1) : 0;
+    uint32_t sum = pieces;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t below = __shfl_up(sum, d);
+        sum += lane >= (uint32_t)d ? below : 0;
+    }
+    first_slot = sum - pieces;
+}
 
 // One thread's share of a tile of TN keys' K or V by GT threads: loads in flight in registers, then to shared memory.  Keys past the last one
 // and columns past the head's repeat existing ones (probabilities, and the rows' operands, are 0 there), so that nothing branches; masked
@@ -139,24 +176,36 @@ struct Stage {
         const AttnArgs &a = keys.a;
         const int row0 = thread / CH, c = 8 * (thread % CH) < (int)a.head_dim ? thread % CH : 0;
         if (MODE == MODE_TREE) {
+            // a lane works out where its key lies; the threads that load the key ask it
+            const uint32_t key = first + (threadIdx.x & 63) % TN, inside = key & ((1u << a.page_shift) - 1);
+            const int64_t place = info >= 0 ? info * s.batch + inside * s.token : -1;
             const uint16_t *base = from + keys.kvh * s.head + c * 8;
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) {
-                const int row = row0 + i * ROWS, page = __shfl(info, row);
-                const uint32_t inside = (first + row) & ((1u << a.page_shift) - 1);
-                counts[MODE == MODE_PLAIN ? 0 : i] = page >= 0;
-                r[i] = *reinterpret_cast<const u32x4 *>(base + (int64_t)(page >= 0 ? page : 0) * s.batch + inside * s.token);
+                const int row = row0 + i * ROWS, high = __shfl((int)(place >> 32), row);
+                const uint32_t low = __shfl((uint32_t)place, row);
+                counts[MODE == MODE_PLAIN ? 0 : i] = high >= 0;
+                r[i] = *reinterpret_cast<const u32x4 *>(base + (high >= 0 ? (int64_t)high << 32 | low : 0));
             }
             return;
         }
         const uint32_t begin = first < keys.end ? first : keys.end - 1, last = keys.end - 1 - begin;
         const uint16_t *base = from + keys.b * s.batch + keys.kvh * s.head + begin * s.token;
         const uint32_t step = (uint32_t)s.token;        // a tile spans less than 2^31 elements
+        if (MODE == MODE_MASK) {
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            const uint32_t row = row0 + i * ROWS, at = row < last ? row : last;
-            if (MODE == MODE_MASK) counts[MODE == MODE_PLAIN ? 0 : i] = __shfl(info, row) >= 0;
-            r[i] = *reinterpret_cast<const u32x4 *>(base + (at * step + c * 8));
+            for (int i = 0; i < LOADS; ++i) counts[MODE == MODE_PLAIN ? 0 : i] = __shfl(info, row0 + i * ROWS) >= 0;
+        }
+        if (last >= TN - 1) {                           // all of them exist: one offset, bases in scalar registers
+            const uint32_t at = row0 * step + c * 8;
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) r[i] = *reinterpret_cast<const u32x4 *>(base + (uint64_t)i * ROWS * step + at);
+        } else {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                const uint32_t row = row0 + i * ROWS, at = row < last ? row : last;
+                r[i] = *reinterpret_cast<const u32x4 *>(base + (at * step + c * 8));
+            }
         }
     }
 
@@ -266,7 +315,7 @@ __device__ __forceinline__ uint64_t seen(const Keys<MODE> &keys, uint32_t first,
 }
 
 // Forward.  WR waves share a tile of keys, 32 rows each; WK such groups take every WK-th tile of the block's piece and are joined
-// at the end.  WR = 4 for many rows: a tile serves 128 rows.  WK = 4 for 32 rows or fewer (single tokens): nothing is shared
+// at the end.  WR = 4 for many rows: a tile serves 128 rows.  WK = 4 or 8 for 32 rows or fewer (single tokens): nothing is shared
 // between waves and no barrier is met while keys stream in.
 template <class T, int DP, int WR, int WK, int MODE>
 __global__ __launch_bounds__(64 * WR * WK, 2) void k_attn_forward(const AttnArgs a)
@@ -281,14 +330,25 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void k_attn_forward(const AttnArgs
     uint32_t at = by_die(blockIdx.x, gridDim.x);
     const uint32_t rt = at % a.row_tiles;
     at /= a.row_tiles;
-    const uint32_t split = at % a.splits;
-    at /= a.splits;
-    const uint32_t kvh = at % a.kv_heads, b = at / a.kv_heads;
-
+    const uint32_t kvh = at % a.kv_heads, slot = at / a.kv_heads;
+    uint32_t b = slot / a.splits, split = slot % a.splits, pieces = a.splits;
+    if (a.balanced) {
+        uint32_t n, first;
+        balance<MODE>(a, n, first);
+        if (blockIdx.x == 0 && threadIdx.x < a.batch) {
+            a.cut[2 * threadIdx.x] = n;
+            a.cut[2 * threadIdx.x + 1] = first;
+        }
+        const uint64_t owner = __ballot(slot >= first && slot < first + n);
+        if (!owner) return;                             // by the whole block
+        b = __builtin_ctzll(owner);
+        pieces = __builtin_amdgcn_readlane(n, b);
+        split = slot - __builtin_amdgcn_readlane(first, b);
+    }
     const Keys<MODE> keys(a, b, kvh);
     // pieces of whole steps (TN keys for every group)
     constexpr uint32_t STEP = TN * WK;
-    const uint32_t steps = (keys.end + STEP - 1) / STEP, per = (steps + a.splits - 1) / a.splits;
+    const uint32_t steps = (keys.end + STEP - 1) / STEP, per = (steps + pieces - 1) / pieces;
     const uint32_t step0 = split * per < steps ? split * per : steps, count = step0 + per < steps ? per : steps - step0;
 
     const uint32_t row = (rt * WR + wr) * 32 + n;
@@ -483,11 +543,11 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void k_attn_forward(const AttnArgs
     }
     total = sum_of_halves(total);
 
-    const int64_t bh = (int64_t)b * a.kv_heads + kvh, part_row = ((int64_t)split * a.batch * a.kv_heads + bh) * a.rows;
+    const int64_t part_row = ((int64_t)slot * a.kv_heads + kvh) * a.rows;
     if (WK == 1) {
         if (!live) return;
         const float times = total != 0.0f ? 1.0f / total : 0.0f, sum2 = total != 0.0f ? top + __log2f(total) : -INFINITY;
-        if (a.splits == 1) {
+        if (pieces == 1) {
             store_row<T, DP>(a.o + row_at(a, a.os, b, kvh, row), o, times, a.head_dim);
             if (a.lse && h == 0) a.lse[lse_at(a, b, kvh, row)] = sum2 * LN2;
         } else {
@@ -525,7 +585,7 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void k_attn_forward(const AttnArgs
         sum += weight[g] * marks[1][g][r];
     }
     const float times = sum != 0.0f ? 1.0f / sum : 0.0f, sum2 = sum != 0.0f ? high + __log2f(sum) : -INFINITY;
-    uint16_t *to = a.o + (a.splits == 1 ? row_at(a, a.os, b, kvh, out_row) : 0);
+    uint16_t *to = a.o + (pieces == 1 ? row_at(a, a.os, b, kvh, out_row) : 0);
     float *part = a.part_o + (part_row + out_row) * DP;
 #pragma unroll
     for (int c = sub; c < C4; c += PER_ROW) {
@@ -533,14 +593,14 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void k_attn_forward(const AttnArgs
 #pragma unroll
         for (int g = 0; g < WK; ++g) x += acc[(g * 32 * WR + r) * C4 + (c ^ (r & 31 & (C4 - 1)))] * weight[g];
         x *= times;
-        if (a.splits == 1) {
+        if (pieces == 1) {
             if (4 * c < (int)a.head_dim) *reinterpret_cast<typename T::V4 *>(to + 4 * c) = __builtin_convertvector(x, typename T::V4);
         } else {
             *reinterpret_cast<f32x4 *>(part + 4 * c) = x;
         }
     }
     if (sub == 0) {
-        if (a.splits > 1) a.part_lse[part_row + out_row] = sum2;
+        if (pieces > 1) a.part_lse[part_row + out_row] = sum2;
         else if (a.lse) a.lse[lse_at(a, b, kvh, out_row)] = sum2 * LN2;
     }
 }
@@ -553,17 +613,22 @@ __global__ __launch_bounds__(256) void k_attn_join(const AttnArgs a)
     const int64_t all = (int64_t)a.batch * a.kv_heads * a.rows, at = (int64_t)blockIdx.x * ROWS + threadIdx.x / C4;
     const int c = threadIdx.x % C4;
     if (at >= all) return;
+    const uint32_t row = (uint32_t)(at % a.rows), kvh = (uint32_t)(at / a.rows % a.kv_heads), b = (uint32_t)(at / a.rows / a.kv_heads);
+    const uint32_t pieces = a.balanced ? a.cut[2 * b] : a.splits, slot = a.balanced ? a.cut[2 * b + 1] : b * a.splits;
+    if (pieces == 1) return;
+    const float *lse = a.part_lse + ((int64_t)slot * a.kv_heads + kvh) * a.rows + row;
+    const float *part = a.part_o + (((int64_t)slot * a.kv_heads + kvh) * a.rows + row) * DP + 4 * c;
+    const int64_t next = (int64_t)a.kv_heads * a.rows;
     float high = -INFINITY, sum = 0.0f;
-    for (uint32_t s = 0; s < a.splits; ++s) high = __builtin_elementwise_maximum(high, a.part_lse[s * all + at]);
+    for (uint32_t s = 0; s < pieces; ++s) high = __builtin_elementwise_maximum(high, lse[s * next]);
     const float off = high == -INFINITY ? 0.0f : high;
     f32x4 x = {0, 0, 0, 0};
 #pragma unroll 4
-    for (uint32_t s = 0; s < a.splits; ++s) {
-        const float w = __builtin_amdgcn_exp2f(a.part_lse[s * all + at] - off);
+    for (uint32_t s = 0; s < pieces; ++s) {
+        const float w = __builtin_amdgcn_exp2f(lse[s * next] - off);
         sum += w;
-        x += *reinterpret_cast<const f32x4 *>(a.part_o + (s * all + at) * DP + 4 * c) * w;
+        x += *reinterpret_cast<const f32x4 *>(part + s * next * DP) * w;
     }
-    const uint32_t row = (uint32_t)(at % a.rows), kvh = (uint32_t)(at / a.rows % a.kv_heads), b = (uint32_t)(at / a.rows / a.kv_heads);
     x *= sum != 0.0f ? 1.0f / sum : 0.0f;
     if (4 * c < (int)a.head_dim) *reinterpret_cast<typename T::V4 *>(a.o + row_at(a, a.os, b, kvh, row) + 4 * c) = __builtin_convertvector(x, typename T::V4);
     if (a.lse && c == 0) a.lse[lse_at(a, b, kvh, row)] = sum != 0.0f ? (high + __log2f(sum)) * LN2 : -INFINITY;

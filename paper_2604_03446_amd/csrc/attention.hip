@@ -38,7 +38,8 @@ struct AttnPlan {
     uint32_t blocks = 0;                        // of the forward pass
     uint32_t dq_splits = 1, dkv_splits = 1;
     uint64_t dq_blocks = 0, dkv_blocks = 0;
-    uint64_t forward_bytes = 0, backward_bytes = 0;
+    bool joins = false;                         // the forward pass leaves pieces
+    uint64_t part_bytes = 0, lse_bytes = 0, forward_bytes = 0, backward_bytes = 0;
 };
 
 // Pieces of the keys (or rows) such that about two blocks run on every compute unit, none of them shorter than `least` steps.
@@ -51,7 +52,7 @@ uint32_t pieces(uint64_t blocks, uint64_t steps, uint64_t least)
 
 uint64_t up256(uint64_t x) { return (x + 255) & ~(uint64_t)255; }
 
-int common(AttnPlan &p, uint32_t dtype, uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t head_dim, uint32_t q_len, uint64_t kv_len, float scale)
+int common(AttnPlan &p, uint32_t dtype, uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t head_dim, uint32_t q_len, uint64_t kv_len, float scale, bool ragged)
 {
     if (dtype != MMEE_F16 && dtype != MMEE_BF16) return MMEE_EINVAL;
     if (!batch || !heads || !kv_heads || heads % kv_heads || !head_dim || head_dim % 8 || head_dim > 128) return MMEE_EINVAL;
@@ -75,19 +76,36 @@ int common(AttnPlan &p, uint32_t dtype, uint32_t batch, uint32_t heads, uint32_t
     // 32 rows to a wave.  Up to 32 rows the four waves of a block take tiles of keys of their own, up to 64 two do.
     p.row_waves = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
     a.row_tiles = (uint32_t)((rows + 32 * p.row_waves - 1) / (32 * p.row_waves));
-    const uint64_t heads_all = (uint64_t)batch * kv_heads, step = p.row_waves == 1 ? 128 : 64;
-    a.splits = pieces(a.row_tiles * heads_all, (kv_len + step - 1) / step, p.row_waves == 4 ? 4 : 2);
-    const uint64_t blocks = a.row_tiles * heads_all * a.splits;
+    // Blocks of four waves run two to a compute unit, of eight waves alone.  Eight waves halve the number of steps, which counts while
+    // there are fewer blocks than units; pieces cost a second launch that joins them: none shorter than 512 keys.
+    const uint64_t each = (uint64_t)a.row_tiles * kv_heads;
+    a.step_keys = p.row_waves > 1 ? 64 : each * batch * std::max<uint64_t>(1, kv_len / 512) <= 256 ? 256 : 128;
+    a.least = 512 / a.step_keys;
+    const uint64_t steps = (kv_len + a.step_keys - 1) / a.step_keys;
+    a.splits = 1;
+    a.slots = batch;
+    if (each && each * batch < 512 && steps > a.least) {         // pieces for one round of blocks (two, three and four rounds were 15 to 40 % slower)
+        a.slots = (uint32_t)std::min<uint64_t>(std::max<uint64_t>(512 / each, batch), batch * (steps / a.least));
+        a.balanced = ragged && batch > 1 && batch <= 64 && a.slots > batch;
+        if (!a.balanced) {
+            a.splits = a.slots / batch;
+            a.slots = a.splits * batch;
+        }
+    }
+    const uint64_t blocks = each * a.slots;
     if (blocks > 0x7fffffff) return MMEE_EINVAL;
     p.blocks = (uint32_t)blocks;
-    p.forward_bytes = a.splits > 1 ? up256(4 * a.splits * heads_all * rows * p.dp) + up256(4 * a.splits * heads_all * rows) : 0;
+    p.joins = a.slots > batch;
+    p.part_bytes = up256(4ull * a.slots * kv_heads * rows * p.dp);
+    p.lse_bytes = up256(4ull * a.slots * kv_heads * rows);
+    p.forward_bytes = p.joins ? p.part_bytes + p.lse_bytes + (a.balanced ? up256(8 * batch) : 0) : 0;
     return MMEE_OK;
 }
 
 int plan_attn(const mmee_attn *x, bool pointers, AttnPlan &p)
 {
     if (!x || x->reserved) return MMEE_EINVAL;
-    const int rc = common(p, x->dtype, x->batch, x->heads, x->kv_heads, x->head_dim, x->q_len, x->kv_len, x->scale);
+    const int rc = common(p, x->dtype, x->batch, x->heads, x->kv_heads, x->head_dim, x->q_len, x->kv_len, x->scale, x->kv_lens != nullptr);
     if (rc) return rc;
     AttnArgs &a = p.a;
     if (!take_strides(x->q_stride, x->batch, x->q_len, x->heads, false, a.qs) || !take_strides(x->k_stride, x->batch, x->kv_len, x->kv_heads, false, a.ks) ||
@@ -124,7 +142,7 @@ int plan_attn(const mmee_attn *x, bool pointers, AttnPlan &p)
 int plan_tree(const mmee_tree_attn *x, bool pointers, AttnPlan &p)
 {
     if (!x || x->reserved || !x->page_tokens || (x->page_tokens & (x->page_tokens - 1)) || x->page_tokens > 1u << 16 || x->nodes > 1024) return MMEE_EINVAL;
-    const int rc = common(p, x->dtype, x->batch, x->heads, x->kv_heads, x->head_dim, x->nodes, (uint64_t)x->pages_per_seq * x->page_tokens, x->scale);
+    const int rc = common(p, x->dtype, x->batch, x->heads, x->kv_heads, x->head_dim, x->nodes, (uint64_t)x->pages_per_seq * x->page_tokens, x->scale, true);
     if (rc) return rc;
     AttnArgs &a = p.a;
     p.mode = MODE_TREE;
@@ -161,8 +179,9 @@ void forward_as(const AttnPlan &p, hipStream_t stream)
 {
     if (p.row_waves == 4) hipLaunchKernelGGL((k_attn_forward<T, DP, 4, 1, MODE>), dim3(p.blocks), dim3(256), 0, stream, p.a);
     else if (p.row_waves == 2) hipLaunchKernelGGL((k_attn_forward<T, DP, 2, 2, MODE>), dim3(p.blocks), dim3(256), 0, stream, p.a);
-    else hipLaunchKernelGGL((k_attn_forward<T, DP, 1, 4, MODE>), dim3(p.blocks), dim3(256), 0, stream, p.a);
-    if (p.a.splits > 1) {
+    else if (p.a.step_keys == 128) hipLaunchKernelGGL((k_attn_forward<T, DP, 1, 4, MODE>), dim3(p.blocks), dim3(256), 0, stream, p.a);
+    else hipLaunchKernelGGL((k_attn_forward<T, DP, 1, 8, MODE>), dim3(p.blocks), dim3(512), 0, stream, p.a);
+    if (p.joins) {
         const uint64_t lines = (uint64_t)p.a.batch * p.a.kv_heads * p.a.rows, per = 256 / (DP / 4);
         hipLaunchKernelGGL((k_attn_join<T, DP>), dim3((uint32_t)((lines + per - 1) / per)), dim3(256), 0, stream, p.a);
     }
@@ -211,7 +230,8 @@ int forward(AttnPlan &p, void *workspace, uint64_t workspace_bytes)
     if (p.forward_bytes && (!workspace || workspace_bytes < p.forward_bytes)) return MMEE_EWORKSPACE;
     if (!p.blocks) return MMEE_OK;
     p.a.part_o = (float *)workspace;
-    p.a.part_lse = p.a.part_o + up256(4ull * p.a.splits * p.a.batch * p.a.kv_heads * p.a.rows * p.dp) / 4;
+    p.a.part_lse = p.a.part_o + p.part_bytes / 4;
+    p.a.cut = (uint32_t *)(p.a.part_lse + p.lse_bytes / 4);
     Launching l;
     if (l.rc) return l.rc;
     dispatch(p, [&](auto type, auto dp, auto mode) { forward_as<decltype(type), dp.value, mode.value>(p, l.stream); });

@@ -31,7 +31,8 @@ struct AttnArgs {
     uint16_t *o;
     float *lse;                 // [batch][heads][q_len] or null
     uint32_t batch, heads, kv_heads, group, q_len, rows, kv_len, head_dim;
-    uint64_t group_inverse;     // ceil(2^40 / group)
+    uint64_t group_inverse;     // ceil(2^group_shift / group)
+    uint32_t group_shift;
     float scale, scale_log2;
     const int32_t *kv_lens;
     const uint8_t *key_mask;
@@ -57,7 +58,7 @@ struct AttnArgs {
 
 enum { MODE_PLAIN = 0, MODE_MASK = 1, MODE_TREE = 2 };
 
-__device__ __forceinline__ uint32_t token_of(const AttnArgs &a, uint32_t row) { return (uint32_t)((row * a.group_inverse) >> 40); }
+__device__ __forceinline__ uint32_t token_of(const AttnArgs &a, uint32_t row) { return (uint32_t)((row * a.group_inverse) >> a.group_shift); }
 
 // Place of a row in a tensor of query heads.
 __device__ __forceinline__ int64_t row_at(const AttnArgs &a, const Strides &s, uint32_t b, uint32_t kvh, uint32_t row)
@@ -723,18 +724,18 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a)
     else store_part<DP>(a.part_o + (((int64_t)split * a.batch * a.kv_heads + bh) * a.rows + row) * DP, dq[0], a.scale);
 }
 
-// dK and dV of 128 KT keys, 32 KT a wave, over the rows of a piece.  Per 32 rows: S = Q K^T, dP = dO V^T (rows along m, a lane holds one
+// dK and dV of 128 keys, 32 a wave, over the rows of a piece.  Per 32 rows: S = Q K^T, dP = dO V^T (rows along m, a lane holds one
 // key), dV^T += dO^T P, dK^T += Q^T dS; the rows' Q and dO are read from shared memory both along and across.
-template <class T, int DP, int KT, int MODE>
-__global__ __launch_bounds__(256, KT == 1 ? 2 : 1) void k_attn_dkv(const AttnArgs a)
+template <class T, int DP, int MODE>
+__global__ __launch_bounds__(256, 2) void k_attn_dkv(const AttnArgs a)
 {
     constexpr int TR = 32, CH = DP / 8, LOADS = TR * CH / 256 ? TR * CH / 256 : 1, ROWS = 256 / CH;
     __shared__ u32x4 tiles[2][2][TR * CH];
     __shared__ f32x4 stats[2][2][TR / 4];               // lse in powers of two, D
     constexpr bool AWAY = DP == 128;                    // V's operands in shared memory: with them 256 registers do not suffice
-    __shared__ u32x4 away[AWAY ? KT : 1][AWAY ? 4 : 1][DP / 16][64];
+    __shared__ u32x4 away[AWAY ? 4 : 1][DP / 16][64];
     const int thread = threadIdx.x, wave = thread >> 6, lane = thread & 63, n = lane & 31, h = lane >> 5;
-    const uint32_t key_tiles = (a.kv_len + 128 * KT - 1) / (128 * KT);
+    const uint32_t key_tiles = (a.kv_len + 127) / 128;
     uint32_t at = by_die(blockIdx.x, gridDim.x);
     const uint32_t kt = at % key_tiles;
     at /= key_tiles;
@@ -742,25 +743,17 @@ __global__ __launch_bounds__(256, KT == 1 ? 2 : 1) void k_attn_dkv(const AttnArg
     at /= a.splits;
     const uint32_t kvh = at % a.kv_heads, b = at / a.kv_heads;
     const Keys<MODE> keys(a, b, kvh);
-    const uint32_t key0 = (kt * 4 + wave) * 32 * KT + n;
-    const uint32_t steps = kt * 128 * KT < keys.end ? (a.rows + TR - 1) / TR : 0, per = (steps + a.splits - 1) / a.splits;
+    const uint32_t key = (kt * 4 + wave) * 32 + n;
+    const uint32_t steps = kt * 128 < keys.end ? (a.rows + TR - 1) / TR : 0, per = (steps + a.splits - 1) / a.splits;
     const uint32_t step0 = split * per < steps ? split * per : steps, count = step0 + per < steps ? per : steps - step0;
 
-    typename T::V8 k[KT][DP / 16], v[KT][DP / 16];
-    bool valid[KT], whole = true;
-#pragma unroll
-    for (int u = 0; u < KT; ++u) {
-        const uint32_t key = key0 + 32 * u;
-        valid[u] = key < keys.end && keys.info(key) >= 0;
-        whole = whole && __all(valid[u]);
-        row_operands<T, DP>(k[u], a.k + (valid[u] ? b * a.ks.batch + key * a.ks.token + kvh * a.ks.head : 0), valid[u], a.head_dim);
-        row_operands<T, DP>(v[u], a.v + (valid[u] ? b * a.vs.batch + key * a.vs.token + kvh * a.vs.head : 0), valid[u], a.head_dim);
-    }
+    const bool valid = key < keys.end && keys.info(key) >= 0, whole = __all(valid);
+    typename T::V8 k[DP / 16], v[DP / 16];
+    row_operands<T, DP>(k, a.k + (valid ? b * a.ks.batch + key * a.ks.token + kvh * a.ks.head : 0), valid, a.head_dim);
+    row_operands<T, DP>(v, a.v + (valid ? b * a.vs.batch + key * a.vs.token + kvh * a.vs.head : 0), valid, a.head_dim);
     if (AWAY) {                                         // a lane reads what it has written itself
 #pragma unroll
-        for (int u = 0; u < KT; ++u)
-#pragma unroll
-            for (int t = 0; t < DP / 16; ++t) away[AWAY ? u : 0][AWAY ? wave : 0][t][lane] = __builtin_bit_cast(u32x4, v[u][t]);
+        for (int t = 0; t < DP / 16; ++t) away[AWAY ? wave : 0][t][lane] = __builtin_bit_cast(u32x4, v[t]);
     }
     const int64_t bh = (int64_t)b * a.kv_heads + kvh;
 
@@ -785,7 +778,7 @@ __global__ __launch_bounds__(256, KT == 1 ? 2 : 1) void k_attn_dkv(const AttnArg
             stat = a.delta[bh * a.rows + (there ? row : a.rows - 1)];
         }
     };
-    f32x16 dk[KT][DP / 32] = {}, dv[KT][DP / 32] = {};
+    f32x16 dk[1][DP / 32] = {}, dv[1][DP / 32] = {};
     if (count) load(0);
     for (uint32_t s = 0; s < count; ++s) {
         u32x4 *qt = tiles[s & 1][0], *ot = tiles[s & 1][1];
@@ -797,57 +790,39 @@ __global__ __launch_bounds__(256, KT == 1 ? 2 : 1) void k_attn_dkv(const AttnArg
         if (thread < 2 * TR) reinterpret_cast<float *>(stats[s & 1])[thread] = stat;
         __syncthreads();
         if (s + 1 < count) load(s + 1);
-        f32x16 x[KT] = {}, dp[KT] = {};
+        f32x16 x = {}, dp = {};
 #pragma unroll
-        for (int t = 0; t < DP / 16; ++t) {
-            const auto q = as_operand<T>(qt[chunk_at<CH>(n, 2 * t + h)]);
+        for (int t = 0; t < DP / 16; ++t) x = T::mma(as_operand<T>(qt[chunk_at<CH>(n, 2 * t + h)]), k[t], x);
 #pragma unroll
-            for (int u = 0; u < KT; ++u) x[u] = T::mma(q, k[u][t], x[u]);
-        }
-#pragma unroll
-        for (int t = 0; t < DP / 16; ++t) {
-            const auto d = as_operand<T>(ot[chunk_at<CH>(n, 2 * t + h)]);
-#pragma unroll
-            for (int u = 0; u < KT; ++u) dp[u] = T::mma(d, AWAY ? as_operand<T>(away[AWAY ? u : 0][AWAY ? wave : 0][t][lane]) : v[u][t], dp[u]);
-        }
+        for (int t = 0; t < DP / 16; ++t)
+            dp = T::mma(as_operand<T>(ot[chunk_at<CH>(n, 2 * t + h)]), AWAY ? as_operand<T>(away[AWAY ? wave : 0][t][lane]) : v[t], dp);
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             const f32x4 lse2 = stats[s & 1][0][2 * g + h], delta = stats[s & 1][1][2 * g + h];
 #pragma unroll
-            for (int u = 0; u < KT; ++u)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int r = 4 * g + j;
-                    float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[u][r], a.scale_log2, -lse2[j]));
-                    if (!whole) p = valid[u] ? p : 0.0f;
-                    x[u][r] = p;
-                    dp[u][r] = p * (dp[u][r] - delta[j]);
-                }
+            for (int j = 0; j < 4; ++j) {
+                const int r = 4 * g + j;
+                float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], a.scale_log2, -lse2[j]));
+                if (!whole) p = valid ? p : 0.0f;
+                x[r] = p;
+                dp[r] = p * (dp[r] - delta[j]);
+            }
         }
 #pragma unroll
         for (int part = 0; part < 2; ++part) {
-            typename T::V8 p[KT], ds[KT];
-#pragma unroll
-            for (int u = 0; u < KT; ++u) {
-                p[u] = rounded<T>(x[u], part);
-                ds[u] = rounded<T>(dp[u], part);
-            }
-            columns_times<T, DP, KT>(dv, ot, 16 * part, p);
-            columns_times<T, DP, KT>(dk, qt, 16 * part, ds);
+            const typename T::V8 p[1] = {rounded<T>(x, part)}, ds[1] = {rounded<T>(dp, part)};
+            columns_times<T, DP, 1>(dv, ot, 16 * part, p);
+            columns_times<T, DP, 1>(dk, qt, 16 * part, ds);
         }
     }
-#pragma unroll
-    for (int u = 0; u < KT; ++u) {
-        const uint32_t key = key0 + 32 * u;
-        if (key >= a.kv_len) continue;
-        if (a.splits == 1) {
-            store_row<T, DP>(a.dk + b * a.dks.batch + key * a.dks.token + kvh * a.dks.head, dk[u], a.scale, a.head_dim);
-            store_row<T, DP>(a.dv + b * a.dvs.batch + key * a.dvs.token + kvh * a.dvs.head, dv[u], 1.0f, a.head_dim);
-        } else {
-            float *part = a.part_o + ((((int64_t)split * a.batch * a.kv_heads + bh) * a.kv_len + key) * 2) * DP;
-            store_part<DP>(part, dk[u], a.scale);
-            store_part<DP>(part + DP, dv[u], 1.0f);
-        }
+    if (key >= a.kv_len) return;
+    if (a.splits == 1) {
+        store_row<T, DP>(a.dk + b * a.dks.batch + key * a.dks.token + kvh * a.dks.head, dk[0], a.scale, a.head_dim);
+        store_row<T, DP>(a.dv + b * a.dvs.batch + key * a.dvs.token + kvh * a.dvs.head, dv[0], 1.0f, a.head_dim);
+    } else {
+        float *part = a.part_o + ((((int64_t)split * a.batch * a.kv_heads + bh) * a.kv_len + key) * 2) * DP;
+        store_part<DP>(part, dk[0], a.scale);
+        store_part<DP>(part + DP, dv[0], 1.0f);
     }
 }
 

@@ -7,10 +7,6 @@
 namespace mmee {
 namespace {
 
-#ifndef KB
-#define KB 1
-#endif
-constexpr int KEY_BLOCKS = KB;
 constexpr uint64_t MOST_ROWS = 1u << 28;        // rows of one key/value head, keys: token_of() and key numbers stay exact
 constexpr int64_t MOST_TOKEN_STRIDE = 1 << 24;  // a tile's offsets fit 32 bits
 
@@ -66,7 +62,10 @@ int common(AttnPlan &p, uint32_t dtype, uint32_t batch, uint32_t heads, uint32_t
     a.heads = heads;
     a.kv_heads = kv_heads;
     a.group = (uint32_t)group;
-    a.group_inverse = (((uint64_t)1 << 40) + group - 1) / group;
+    // r / group = r * ceil(2^shift / group) >> shift for every r < 2^32, with 2^shift >= 2^32 group; the product stays below 2^64 for r < 2^28
+    a.group_shift = 32;
+    while ((uint64_t)1 << (a.group_shift - 32) < group) ++a.group_shift;
+    a.group_inverse = (((uint64_t)1 << a.group_shift) + group - 1) / group;
     a.q_len = q_len;
     a.rows = (uint32_t)rows;
     a.kv_len = (uint32_t)kv_len;
@@ -127,7 +126,7 @@ int plan_attn(const mmee_attn *x, bool pointers, AttnPlan &p)
             return MMEE_EINVAL;
     }
     // backward
-    const uint64_t heads_all = (uint64_t)a.batch * a.kv_heads, tiles = ((uint64_t)a.rows + 127) / 128, key_tiles = ((uint64_t)a.kv_len + 128 * KEY_BLOCKS - 1) / (128 * KEY_BLOCKS);
+    const uint64_t heads_all = (uint64_t)a.batch * a.kv_heads, tiles = ((uint64_t)a.rows + 127) / 128, key_tiles = ((uint64_t)a.kv_len + 127) / 128;
     p.dq_splits = pieces(tiles * heads_all, ((uint64_t)a.kv_len + 63) / 64, 4);
     p.dkv_splits = pieces(key_tiles * heads_all, ((uint64_t)a.rows + 31) / 32, 8);
     p.dq_blocks = tiles * heads_all * p.dq_splits;
@@ -201,7 +200,7 @@ void backward_as(const AttnPlan &p, hipStream_t stream)
     }
     if (p.dkv_blocks) {
         a.splits = p.dkv_splits;
-        hipLaunchKernelGGL((k_attn_dkv<T, DP, KEY_BLOCKS, MODE>), dim3((uint32_t)p.dkv_blocks), dim3(256), 0, stream, a);
+        hipLaunchKernelGGL((k_attn_dkv<T, DP, MODE>), dim3((uint32_t)p.dkv_blocks), dim3(256), 0, stream, a);
         const uint64_t per = 256 / (DP / 2);
         if (a.splits > 1) hipLaunchKernelGGL((k_attn_sum<T, DP, 1>), dim3((uint32_t)((heads_all * a.kv_len + per - 1) / per)), dim3(256), 0, stream, a);
     }

@@ -362,6 +362,31 @@ __global__ __launch_bounds__(256) void k_sum_parts(const ProductArgs p)
     *reinterpret_cast<typename T::V4 *>(p.c[problem] + in / n4 * p.ldc + in % n4 * 4) = __builtin_convertvector(x, typename T::V4);
 }
 
+// Four columns of a token's results; of a gated product from g and u.
+template <class T, bool GATED>
+__device__ __forceinline__ void store_tokens(const ProductArgs &p, uint32_t token, uint32_t col, uint32_t split, f32x4 y, f32x4 u)
+{
+    typedef typename T::V4 V4;
+    if (GATED) {
+        const f32x4 g = y;
+        with_activation(p.act, [&](auto kind) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float value, unused;
+                activate<kind.value>(g[j], value, unused);
+                y[j] = value * u[j];
+            }
+        });
+        if (p.gate) *reinterpret_cast<V4 *>(p.gate + token * p.ld_hidden + col) = __builtin_convertvector(g, V4);
+        if (p.up) *reinterpret_cast<V4 *>(p.up + token * p.ld_hidden + col) = __builtin_convertvector(u, V4);
+        *reinterpret_cast<V4 *>(p.c[0] + token * p.ldc + col) = __builtin_convertvector(y, V4);
+    } else if (p.splits > 1) {
+        *reinterpret_cast<f32x4 *>(p.parts + ((uint64_t)split * p.m + token) * p.n + col) = y;
+    } else {
+        *reinterpret_cast<V4 *>(p.c[0] + token * p.ldc + col) = __builtin_convertvector(y, V4);
+    }
+}
+
 // A few tokens: C[token][n] = sum_k x[token][k] W[n][k] for up to 16 MT tokens, with the weights streamed once from memory straight
 // into operands.  A block owns 16 NT rows of the weights (GATED: as many of the gate's and of the up projection's each); its eight waves
 // take every eighth step of 32 along k, so that together they read 512 neighbouring bytes of a row, and are summed through
@@ -437,25 +462,113 @@ __global__ __launch_bounds__(512, 2) void k_tokens(const ProductArgs p)
         }
         const uint32_t token = 16 * m + i, col = n0 + 16 * r + 4 * kg;
         if (token >= p.m || col >= p.n) continue;
-        typedef typename T::V4 V4;
-        if (GATED) {
-            const f32x4 g = y;
-            with_activation(p.act, [&](auto kind) {
+        store_tokens<T, GATED>(p, token, col, split, y, u);
+    }
+}
+
+// As k_tokens, for more than 16 tokens, whose operands would be read as often as the weights': WR waves with 16 NT rows each share a
+// chunk of 64 values of k of all tokens in shared memory, 8 / WR such groups take every (8 / WR)-th chunk.  Weights are asked for two chunks ahead,
+// straight into operands; the tokens' next chunk is on its way meanwhile.
+template <class T, int MT, int NT, int WR, bool GATED>
+__global__ __launch_bounds__(512, 2) void k_tokens_shared(const ProductArgs p)
+{
+    constexpr int WAVES = 8, WK = WAVES / WR, R = GATED ? 2 * NT : NT, CH = BK / 8, TOKENS = 16 * MT, GT = 64 * WR;
+    constexpr int LOADS = (TOKENS * CH + GT - 1) / GT, CHUNKS = WK * 2 * TOKENS * CH, SUMS = WK > 1 ? WAVES * R * MT * 64 : 0;
+    __shared__ u32x4 memory[CHUNKS > SUMS ? CHUNKS : SUMS];
+    const int wave = threadIdx.x >> 6, wr = wave % WR, wk = wave / WR, lane = threadIdx.x & 63, i = lane & 15, kg = lane >> 4, thread = threadIdx.x % GT;
+    uint32_t at = by_die(blockIdx.x, gridDim.x);
+    const uint32_t split = at % p.splits, n0 = at / p.splits * 16 * NT * WR + wr * 16 * NT;
+    const uint32_t chunks = (p.k + BK - 1) / BK, each = (chunks + p.splits - 1) / p.splits;
+    const uint32_t chunk0 = split * each < chunks ? split * each : chunks, mine = chunk0 + each < chunks ? each : chunks - chunk0, count = (mine + WK - 1) / WK;
+
+    // what does not exist is asked for beyond the buffer's end
+    uint32_t w[R], x[LOADS];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    float value, unused;
-                    activate<kind.value>(g[j], value, unused);
-                    y[j] = value * u[j];
-                }
-            });
-            if (p.gate) *reinterpret_cast<V4 *>(p.gate + token * p.ld_hidden + col) = __builtin_convertvector(g, V4);
-            if (p.up) *reinterpret_cast<V4 *>(p.up + token * p.ld_hidden + col) = __builtin_convertvector(u, V4);
-            *reinterpret_cast<V4 *>(p.c[0] + token * p.ldc + col) = __builtin_convertvector(y, V4);
-        } else if (p.splits > 1) {
-            *reinterpret_cast<f32x4 *>(p.parts + ((uint64_t)split * p.m + token) * p.n + col) = y;
-        } else {
-            *reinterpret_cast<V4 *>(p.c[0] + token * p.ldc + col) = __builtin_convertvector(y, V4);
+    for (int r = 0; r < R; ++r) {
+        const uint32_t row = 16 * (r % NT) + i;
+        w[r] = 2 * ((n0 + row < p.n ? row : 0) * (uint32_t)p.ldb + 8 * kg);
+    }
+#pragma unroll
+    for (int l = 0; l < LOADS; ++l) {
+        const uint32_t token = (thread + l * GT) / CH;
+        x[l] = token < p.m ? 2 * (token * (uint32_t)p.lda + 8 * (thread % CH)) : BEYOND;
+    }
+    u32x4 wait[2][R][2], next[LOADS];
+    auto ask_weights = [&](u32x4 (&to)[R][2], uint32_t s) {
+        const uint32_t k0 = s < count && wk + s * WK < mine ? (chunk0 + wk + s * WK) * BK : p.k, left = p.k - k0;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const auto from = buffer_at(p.b[r / NT] + (int64_t)(n0 < p.n ? n0 : 0) * p.ldb + k0);
+#pragma unroll
+            for (int t = 0; t < 2; ++t) to[r][t] = __builtin_amdgcn_raw_buffer_load_b128(from, (uint32_t)(32 * t + 8 * kg) < left ? w[r] + 64 * t : BEYOND, 0, 0);
         }
+    };
+    auto ask_tokens = [&](uint32_t s) {
+        const uint32_t k0 = s < count && wk + s * WK < mine ? (chunk0 + wk + s * WK) * BK : p.k, left = p.k - k0;
+        const auto from = buffer_at(p.a[0] + k0);
+#pragma unroll
+        for (int l = 0; l < LOADS; ++l) next[l] = __builtin_amdgcn_raw_buffer_load_b128(from, (uint32_t)(8 * (thread % CH)) < left ? x[l] : BEYOND, 0, 0);
+    };
+    auto put_tokens = [&](uint32_t s) {
+        u32x4 *tile = memory + (wk * 2 + (s & 1)) * TOKENS * CH;
+#pragma unroll
+        for (int l = 0; l < LOADS; ++l) {
+            const int token = (thread + l * GT) / CH;
+            if (TOKENS * CH % GT == 0 || token < TOKENS) tile[chunk_at<CH>(token, thread % CH)] = next[l];
+        }
+    };
+    f32x4 acc[R][MT] = {};
+    auto step = [&](uint32_t s, u32x4 (&now)[R][2]) {
+        const u32x4 *tile = memory + (wk * 2 + (s & 1)) * TOKENS * CH;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                const auto tokens = as_operand<T>(tile[chunk_at<CH>(16 * m + i, 4 * t + kg)]);
+#pragma unroll
+                for (int r = 0; r < R; ++r) acc[r][m] = T::mma(as_operand<T>(now[r][t]), tokens, acc[r][m]);
+            }
+        put_tokens(s + 1);
+        ask_weights(now, s + 2);
+        ask_tokens(s + 2);
+        __syncthreads();
+    };
+    ask_tokens(0);
+    ask_weights(wait[0], 0);
+    ask_weights(wait[1], 1);
+    put_tokens(0);
+    ask_tokens(1);
+    __syncthreads();
+    for (uint32_t s = 0; s < count; s += 2) {           // (one step past an odd count works on zeros)
+        step(s, wait[0]);
+        step(s + 1, wait[1]);
+    }
+
+    f32x4 *sums = reinterpret_cast<f32x4 *>(memory);
+    if (WK > 1) {
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int m = 0; m < MT; ++m) sums[(wave * R * MT + r * MT + m) * 64 + lane] = acc[r][m];
+        __syncthreads();
+    }
+    // block (r, m) of 16 x 16 results of row group wr: lane holds token 16 m + i, columns 16 r + 4 kg + {0..3}; the groups' waves share them
+#pragma unroll
+    for (int job = 0; job < NT * MT; ++job) {
+        if (job % WK != wk) continue;
+        const int r = job / MT, m = job % MT;
+        f32x4 y = acc[r][m], u = acc[GATED ? NT + r : r][m];
+        if (WK > 1) {
+            y = u = f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int v = 0; v < WK; ++v) {
+                y += sums[((v * WR + wr) * R * MT + r * MT + m) * 64 + lane];
+                if (GATED) u += sums[((v * WR + wr) * R * MT + ((GATED ? NT : 0) + r) * MT + m) * 64 + lane];
+            }
+        }
+        const uint32_t token = 16 * m + i, col = n0 + 16 * r + 4 * kg;
+        if (token >= p.m || col >= p.n) continue;
+        store_tokens<T, GATED>(p, token, col, split, y, u);
     }
 }
 

@@ -25,6 +25,8 @@ bool misaligned(std::initializer_list<const void *> list)
 struct Job {
     ProductArgs p = {};
     bool big = false;                           // tiles of 256 x 256, else 128 x 128
+    bool shared = false;                        // few tokens: through shared memory
+    uint32_t columns = 0;                       // few tokens: of a block
     uint32_t blocks = 0;
     uint64_t parts_bytes() const { return p.splits > 1 ? up256(4ull * p.problems * p.splits * p.m * p.n) : 0; }
 };
@@ -71,18 +73,28 @@ bool plan(Job &j, uint32_t m, uint32_t n, uint32_t k, uint32_t segments, uint32_
     return blocks <= 0x7fffffff;
 }
 
-bool plan_tokens(Job &j, uint32_t m, uint32_t n, uint32_t k, uint32_t rows, bool may_split)
+// Few tokens.  Up to 8 read their operands with the weights; more of them share them (k_tokens_shared: 37 tokens, 4096 -> 12288 -> 4096: 108 -> 75
+// us; 16 tokens 79 -> 70), but for gated products too narrow for a block of 32 columns on most compute units, where eight waves on 16 columns are
+// sooner done (3072 columns, 37 tokens: 6.6 against 8.8 us).  A block takes 64 columns where that leaves 192 blocks, pieces of the sum counted.
+bool plan_tokens(Job &j, uint32_t m, uint32_t n, uint32_t k, bool gated)
 {
     ProductArgs &p = j.p;
     p.m = m;
     p.n = n;
     p.k = k;
     p.segments = p.problems = p.splits = 1;
-    uint64_t blocks = (n + rows - 1) / rows;
-    if (may_split && blocks < 192) {
-        const uint64_t steps = (k + 31) / 32;
-        p.splits = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>({512 / blocks, steps / 32, 16}));
+    const uint64_t steps = (k + 31) / 32;
+    j.shared = m > 8 && (!gated || n >= 32 * 192);
+    uint64_t most = 1;
+    if (j.shared) {
+        most = gated ? 1 : std::max<uint64_t>(1, std::min<uint64_t>(steps / 16, 16));
+        j.columns = n / 64 * most >= 192 ? 64 : 32;
+    } else {
+        most = gated ? 1 : std::max<uint64_t>(1, std::min<uint64_t>(steps / 32, 16));
+        j.columns = n / 32 >= 256 ? 32 : 16;
     }
+    const uint64_t blocks = (n + j.columns - 1) / j.columns;
+    if (blocks < 192) p.splits = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>((j.shared ? 256 : 512) / blocks, most));
     j.blocks = (uint32_t)(blocks * p.splits);
     return true;
 }
@@ -92,13 +104,6 @@ struct FfnPlan {
     Job hidden, down, d_hidden, dx, dw_gated, dw_down;
     uint64_t forward_bytes = 0, backward_bytes = 0, d_hidden_bytes = 0;
 };
-
-uint32_t token_rows(const mmee_ffn *x, bool gated)
-{
-    // rows of the weights for a block: 16, or 32 where that leaves two blocks for each compute unit
-    const uint32_t n = gated ? x->hidden_dim : x->out_dim;
-    return n / 32 >= 256 ? 32 : 16;
-}
 
 int plan_ffn(const mmee_ffn *x, bool pointers, FfnPlan &f)
 {
@@ -118,7 +123,7 @@ int plan_ffn(const mmee_ffn *x, bool pointers, FfnPlan &f)
     const uint32_t M = x->rows, K = x->in_dim, F = x->hidden_dim, J = x->out_dim;
     f.tokens = M <= FEW_TOKENS;
     bool fits = true;
-    if (f.tokens) fits = plan_tokens(f.hidden, M, F, K, token_rows(x, true), false) && plan_tokens(f.down, M, J, F, token_rows(x, false), true);
+    if (f.tokens) fits = plan_tokens(f.hidden, M, F, K, true) && plan_tokens(f.down, M, J, F, false);
     else fits = plan(f.hidden, M, F, K, 1, 1, true, false) && plan(f.down, M, J, F, 1, 1, false, true);
     fits = fits && plan(f.d_hidden, M, F, J, 1, 1, false, false) && plan(f.dx, M, K, F, 2, 1, false, true) && plan(f.dw_gated, F, K, M, 1, 2, false, true) &&
            plan(f.dw_down, J, F, M, 1, 1, false, true);
@@ -145,24 +150,28 @@ void sum_parts(const Job &j, hipStream_t stream)
 }
 
 template <class T, bool GATED>
-void tokens(const Job &j, uint32_t rows, hipStream_t stream)
+void tokens(const Job &j, hipStream_t stream)
 {
-    auto with_rows = [&](auto mt) {
-        if (rows == 16) hipLaunchKernelGGL((k_tokens<T, mt.value, 1, GATED>), dim3(j.blocks), dim3(512), 0, stream, j.p);
-        else hipLaunchKernelGGL((k_tokens<T, mt.value, 2, GATED>), dim3(j.blocks), dim3(512), 0, stream, j.p);
+    auto with = [&](auto mt) {
+        constexpr int MT = mt.value;
+        if (j.shared && j.columns == 64) hipLaunchKernelGGL((k_tokens_shared<T, MT, 2, 2, GATED>), dim3(j.blocks), dim3(512), 0, stream, j.p);
+        else if (j.shared) hipLaunchKernelGGL((k_tokens_shared<T, MT, 1, 2, GATED>), dim3(j.blocks), dim3(512), 0, stream, j.p);
+        else if (GATED && j.columns == 16) hipLaunchKernelGGL((k_tokens<T, GATED ? MT : 1, 1, GATED>), dim3(j.blocks), dim3(512), 0, stream, j.p);
+        else if (j.columns == 16) hipLaunchKernelGGL((k_tokens<T, 1, 1, GATED>), dim3(j.blocks), dim3(512), 0, stream, j.p);
+        else hipLaunchKernelGGL((k_tokens<T, 1, 2, GATED>), dim3(j.blocks), dim3(512), 0, stream, j.p);          // (up to 8 tokens)
     };
-    if (j.p.m <= 16) with_rows(std::integral_constant<int, 1>());
-    else if (j.p.m <= 32) with_rows(std::integral_constant<int, 2>());
-    else if (j.p.m <= 48) with_rows(std::integral_constant<int, 3>());
-    else with_rows(std::integral_constant<int, 4>());
+    if (j.p.m <= 16) with(std::integral_constant<int, 1>());
+    else if (j.p.m <= 32) with(std::integral_constant<int, 2>());
+    else if (j.p.m <= 48) with(std::integral_constant<int, 3>());
+    else with(std::integral_constant<int, 4>());
 }
 
 template <class T>
-void forward_as(const mmee_ffn *x, const FfnPlan &f, hipStream_t stream)
+void forward_as(const FfnPlan &f, hipStream_t stream)
 {
     if (f.tokens) {
-        tokens<T, true>(f.hidden, token_rows(x, true), stream);
-        tokens<T, false>(f.down, token_rows(x, false), stream);
+        tokens<T, true>(f.hidden, stream);
+        tokens<T, false>(f.down, stream);
     } else {
         product<T, false, false, EPI_GATED>(f.hidden, stream);
         product<T, false, false, EPI_STORE>(f.down, stream);
@@ -228,8 +237,8 @@ int mmee_ffn_forward(const mmee_ffn *x)
     d.parts = (float *)x->workspace;
     Launching l;
     if (l.rc) return l.rc;
-    if (x->dtype == MMEE_F16) forward_as<F16>(x, f, l.stream);
-    else forward_as<BF16>(x, f, l.stream);
+    if (x->dtype == MMEE_F16) forward_as<F16>(f, l.stream);
+    else forward_as<BF16>(f, l.stream);
     return launched("gated feed-forward block, forward");
 }
 

@@ -119,14 +119,14 @@ struct Keys {
         nodes = __builtin_amdgcn_readfirstlane(nodes);
     }
 
-    // What decides whether key `at` counts: its page, or -1; its mask byte.
+    // What decides whether key `at` counts: its page, or -1; its mask byte.  Not asked where there are no keys.
     __device__ __forceinline__ int info(uint32_t at) const
     {
         if (MODE == MODE_PLAIN) return 0;
-        if (at >= end) return -1;
-        if (MODE == MODE_MASK) return a.key_mask[b * a.mask_stride + at] ? 0 : -1;
-        const int32_t page = a.page_table[b * a.table_stride + (at >> a.page_shift)];
-        return (uint32_t)page < a.n_pages ? page : -1;
+        const uint32_t key = at < end ? at : end - 1;   // (there is one at least)
+        if (MODE == MODE_MASK) return a.key_mask[b * a.mask_stride + key] && at < end ? 0 : -1;
+        const int32_t page = a.page_table[b * a.table_stride + (key >> a.page_shift)];
+        return (uint32_t)page < a.n_pages && at < end ? page : -1;
     }
 };
 
@@ -169,7 +169,9 @@ struct Stage {
     static constexpr int CH = DP / 8, LOADS = TN * CH / GT, ROWS = GT / CH;     // rows that one load of all threads covers
     static_assert(LOADS * GT == TN * CH && ROWS * CH == GT, "a tile is dealt out evenly");
     u32x4 r[LOADS];
-    bool counts[MODE == MODE_PLAIN ? 1 : LOADS];
+    bool there[MODE == MODE_TREE ? LOADS : 1];
+    uint64_t which;                     // MODE_MASK: the tile's keys that count, one bit each
+    float bias;                         // MODE_MASK: 0 or -inf, for key first + (lane mod TN)
 
     // info: of key first + (lane mod TN), as Keys::info gives it.  There is a key at least.
     __device__ __forceinline__ void load(const Keys<MODE> &keys, const uint16_t *from, const Strides &s, int thread, uint32_t first, int info)
@@ -185,7 +187,7 @@ struct Stage {
             for (int i = 0; i < LOADS; ++i) {
                 const int row = row0 + i * ROWS, high = __shfl((int)(place >> 32), row);
                 const uint32_t low = __shfl((uint32_t)place, row);
-                counts[MODE == MODE_PLAIN ? 0 : i] = high >= 0;
+                there[MODE == MODE_TREE ? i : 0] = high >= 0;
                 r[i] = *reinterpret_cast<const u32x4 *>(base + (high >= 0 ? (int64_t)high << 32 | low : 0));
             }
             return;
@@ -194,8 +196,8 @@ struct Stage {
         const uint16_t *base = from + keys.b * s.batch + keys.kvh * s.head + begin * s.token;
         const uint32_t step = (uint32_t)s.token;        // a tile spans less than 2^31 elements
         if (MODE == MODE_MASK) {
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) counts[MODE == MODE_PLAIN ? 0 : i] = __shfl(info, row0 + i * ROWS) >= 0;
+            which = __ballot(info >= 0);
+            bias = info >= 0 ? 0.0f : -INFINITY;
         }
         if (last >= TN - 1) {                           // all of them exist: one offset, bases in scalar registers
             const uint32_t at = row0 * step + c * 8;
@@ -214,17 +216,21 @@ struct Stage {
     {
         const int c = thread % CH, row0 = thread / CH;
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) tile[chunk_at<CH>(row0 + i * ROWS, c)] = MODE == MODE_PLAIN || counts[MODE == MODE_PLAIN ? 0 : i] ? r[i] : zeros();
+        for (int i = 0; i < LOADS; ++i) {
+            bool counts = true;
+            if (MODE == MODE_TREE) counts = there[MODE == MODE_TREE ? i : 0];
+            if (MODE == MODE_MASK) counts = ROWS <= 32 ? (uint32_t)(which >> (i * ROWS % 64)) >> row0 & 1 : which >> row0 & 1;
+            tile[chunk_at<CH>(row0 + i * ROWS, c)] = counts ? r[i] : zeros();
+        }
     }
 };
 
-// S^T of 32 keys (rows `first` .. of a tile) and the wave's 32 rows.
+// S^T of 32 keys (rows `first` .. of a tile) and the wave's 32 rows, on top of s.
 template <class T, int DP>
-__device__ __forceinline__ f32x16 keys_by_rows(const u32x4 *tile, int first, const typename T::V8 (&rows)[DP / 16])
+__device__ __forceinline__ f32x16 keys_by_rows(const u32x4 *tile, int first, const typename T::V8 (&rows)[DP / 16], f32x16 s = {})
 {
     constexpr int CH = DP / 8;
     const int lane = threadIdx.x & 63, i = lane & 31, h = lane >> 5;
-    f32x16 s = {};
 #pragma unroll
     for (int t = 0; t < DP / 16; ++t) s = T::mma(as_operand<T>(tile[first * CH + chunk_at<CH>(i, 2 * t + h)]), rows[t], s);
     return s;
@@ -284,35 +290,58 @@ __device__ __forceinline__ void store_part(float *row, const f32x16 (&acc)[DP / 
         }
 }
 
-// Which keys of a tile a lane's row sees, one bit each.
-template <int MODE, int TN>
-__device__ __forceinline__ uint64_t seen(const Keys<MODE> &keys, uint32_t first, uint64_t counted, uint32_t token, bool &all)
+// Scores of 32 keys whose bits say that the key does not count become -inf.  The same keys for all rows: the lanes' masks are formed in
+// scalar registers.
+__device__ __forceinline__ void mask_keys(f32x16 &x, uint32_t bits)
 {
-    const uint64_t whole = ~0ull >> (64 - TN);
-    if (MODE == MODE_PLAIN) {
-        const uint32_t left = keys.end > first ? keys.end - first : 0;
-        counted = left >= TN ? whole : (1ull << left) - 1;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        const int key = 8 * (r / 4) + r % 4;            // in the lower half of the lanes; 4 more in the upper one
+        const uint32_t low = -(int)(bits >> key & 1), high = -(int)(bits >> (key + 4) & 1);
+        x[r] = __builtin_amdgcn_inverse_ballot_w64((uint64_t)high << 32 | low) ? x[r] : -INFINITY;
     }
-    all = counted == whole;
-    if (MODE != MODE_TREE) return counted;
+}
+
+// What the products of 32 masked keys start from: 0, or -inf for keys that do not count (whose K is zeros).  It costs four reads and no
+// vector instruction; selecting afterwards took 25 % longer at 64 values a head.
+__device__ __forceinline__ f32x16 biases(const float *of)
+{
+    const int h = (threadIdx.x >> 5) & 1;
+    f32x16 x;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        const f32x4 four = *reinterpret_cast<const f32x4 *>(of + 8 * g + 4 * h);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[4 * g + j] = four[j];
+    }
+    return x;
+}
+
+// Keys of a tile that exist and count, one bit each.
+template <int MODE, int TN>
+__device__ __forceinline__ uint64_t counted(const Keys<MODE> &keys, uint32_t first, int info)
+{
+    constexpr uint64_t WHOLE = ~0ull >> (64 - TN);
+    if (MODE != MODE_PLAIN) return __ballot(info >= 0) & WHOLE;
+    const uint32_t left = keys.end > first ? keys.end - first : 0;
+    return left >= TN ? WHOLE : (1ull << left) - 1;
+}
+
+// Those of them that a lane's row of a tree sees.
+template <int TN>
+__device__ __forceinline__ uint64_t seen(const Keys<MODE_TREE> &keys, uint32_t first, uint64_t bits, uint32_t token)
+{
     const AttnArgs &a = keys.a;
-    if (first + TN > keys.held || token >= keys.nodes) {        // (rows beyond the nodes see nothing)
-        uint64_t bits = 0;
-        if (token < keys.nodes) {
-            const uint64_t *words = a.ancestors + ((int64_t)keys.b * a.q_len + token) * a.words;
-            const int64_t j = (int64_t)first - keys.held;       // > -64
-            if (j < 0) {
-                bits = j <= -64 ? ~0ull : words[0] << -j | ((1ull << -j) - 1);
-            } else if ((uint32_t)(j >> 6) < a.words) {
-                const uint32_t w = (uint32_t)(j >> 6), by = (uint32_t)(j & 63);
-                bits = words[w] >> by;
-                if (by && w + 1 < a.words) bits |= words[w + 1] << (64 - by);
-            }
-        }
-        counted &= bits;
-    }
-    all = __all(counted == whole);
-    return counted;
+    if (token >= keys.nodes) return 0;
+    if (first + TN <= keys.held) return bits;
+    const uint64_t *words = a.ancestors + ((int64_t)keys.b * a.q_len + token) * a.words;
+    const int64_t j = (int64_t)first - keys.held;       // > -64
+    if (j < 0) return bits & (words[0] << -j | ((1ull << -j) - 1));
+    const uint32_t w = (uint32_t)(j >> 6), by = (uint32_t)(j & 63);
+    if (w >= a.words) return 0;
+    uint64_t own = words[w] >> by;
+    if (by && w + 1 < a.words) own |= words[w + 1] << (64 - by);
+    return bits & own;
 }
 
 // Forward.  WR waves share a tile of keys, 32 rows each; WK such groups take every WK-th tile of the block's piece and are joined
@@ -326,6 +355,7 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void k_attn_forward(const AttnArgs
     constexpr int JOIN = WK > 1 ? WK * 32 * WR * DP / 4 : 0;
     __shared__ u32x4 memory[TILES > JOIN ? TILES : JOIN];
     __shared__ float marks[2][WK][WK > 1 ? 32 * WR : 1];
+    __shared__ __align__(16) float bias[WK][NB][MODE == MODE_MASK ? TN : 4];
     const int thread = threadIdx.x % GT, wave = threadIdx.x >> 6, wr = wave % WR, wk = wave / WR, lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
 
     uint32_t at = by_die(blockIdx.x, gridDim.x);
@@ -376,18 +406,29 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void k_attn_forward(const AttnArgs
 
     auto scores = [&](f32x16 (&to)[MT], uint32_t s) {
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) to[mt] = keys_by_rows<T, DP>(k_tile(s), 32 * mt, q);
+        for (int mt = 0; mt < MT; ++mt)
+            to[mt] = keys_by_rows<T, DP>(k_tile(s), 32 * mt, q, MODE == MODE_MASK ? biases(bias[wk][NB == 2 ? s & 1 : 0] + (MODE == MODE_MASK ? 32 * mt : 0)) : f32x16{});
     };
     auto mask = [&](f32x16 (&to)[MT], uint32_t s) {
-        bool all;
-        const uint64_t counted = MODE == MODE_PLAIN ? 0 : __ballot(info[0] >= 0) & WHOLE, bits = seen<MODE, TN>(keys, first_of(s), counted, token, all);
-        if (all) return;
+        if (MODE == MODE_MASK) return;
+        const uint64_t bits = counted<MODE, TN>(keys, first_of(s), info[0]);
+        if constexpr (MODE != MODE_TREE) {
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            const uint32_t mine = (uint32_t)(bits >> (32 * mt)) >> (4 * h);
+            for (int mt = 0; mt < MT; ++mt) mask_keys(to[mt], (uint32_t)(bits >> (32 * mt)));
+        } else {
+            const uint64_t own = seen<TN>(keys, first_of(s), bits, token);
+            if (__all(own == WHOLE)) return;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) to[mt][r] = mine >> (8 * (r / 4) + r % 4) & 1 ? to[mt][r] : -INFINITY;
+            for (int mt = 0; mt < MT; ++mt) {
+                const uint32_t which = (uint32_t)(own >> (32 * mt)) >> (4 * h);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) to[mt][r] = which >> (8 * (r / 4) + r % 4) & 1 ? to[mt][r] : -INFINITY;
+            }
         }
+    };
+    auto put_keys = [&](uint32_t s) {
+        sk.store(k_tile(s), thread);
+        if (MODE == MODE_MASK && thread < TN) bias[wk][NB == 2 ? s & 1 : 0][MODE == MODE_MASK ? thread : 0] = sk.bias;
     };
     auto maximum = [&](const f32x16 (&of)[MT]) {
         float m = of[0][0];
@@ -445,7 +486,7 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void k_attn_forward(const AttnArgs
 #pragma unroll 1
         for (uint32_t s = 0; s < count; ++s) {
             if (s) sync();
-            sk.store(k_tile(s), thread);
+            put_keys(s);
             sv.store(v_tile(s), thread);
             sync();
             if (s + 1 < count) {
@@ -470,7 +511,7 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void k_attn_forward(const AttnArgs
         sk.load(keys, a.k, a.ks, thread, first_of(0), info[0]);
         sv.load(keys, a.v, a.vs, thread, first_of(0), info[0]);
         info[1] = info_of(1);
-        sk.store(k_tile(0), thread);
+        put_keys(0);
         sv.store(v_tile(0), thread);
         sync();
         sk.load(keys, a.k, a.ks, thread, first_of(1), info[1]);
@@ -480,7 +521,7 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void k_attn_forward(const AttnArgs
         mask(x, 0);
         most = maximum(x);
         raise();
-        sk.store(k_tile(1), thread);
+        put_keys(1);
         sync();
         sk.load(keys, a.k, a.ks, thread, first_of(2), info[2]);
         info[0] = info[1];
@@ -488,7 +529,7 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void k_attn_forward(const AttnArgs
         info[2] = info_of(3);
 
         // Tile s from its scores `now`; unless it is the last, the next one's scores into `next`.
-        auto step = [&](uint32_t s, f32x16 (&now)[MT], f32x16 (&next)[MT], auto more) {
+        auto step = [&](uint32_t s, f32x16 (&now)[MT], f32x16 (&next)[MT], auto more, auto masked) {
             typename T::V8 p[MT][2][1];
             constexpr int PRODUCTS = MT * DP / 16;
             if (more) scores(next, s + 1);
@@ -507,7 +548,7 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void k_attn_forward(const AttnArgs
                     __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
                     __builtin_amdgcn_sched_group_barrier(0x002, (MT * 56 + PRODUCTS - 1) / PRODUCTS, 0);
                 }
-                mask(next, s + 1);
+                if (masked) mask(next, s + 1);
             }
             values(s, p);
             if (!more) return;
@@ -520,7 +561,7 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void k_attn_forward(const AttnArgs
                 __builtin_amdgcn_sched_group_barrier(0x002, 2, 1);
             }
             raise();
-            sk.store(k_tile(s), thread);
+            put_keys(s);
             sv.store(v_tile(s + 1), thread);
             sync();
             sk.load(keys, a.k, a.ks, thread, first_of(s + 3), info[2]);
@@ -529,18 +570,20 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void k_attn_forward(const AttnArgs
             info[1] = info[2];
             info[2] = info_of(s + 4);
         };
+        // Without lengths in the way every tile but the last is whole.
+        constexpr std::bool_constant<MODE != MODE_PLAIN> inner;
         uint32_t s = 0;
-        for (; s + 2 < count; s += 2) {
-            step(s, x, ahead, std::true_type());
-            step(s + 1, ahead, x, std::true_type());
+        for (; s + 3 < count; s += 2) {
+            step(s, x, ahead, std::true_type(), inner);
+            step(s + 1, ahead, x, std::true_type(), inner);
         }
-        if (s + 1 < count) {
-            step(s, x, ahead, std::true_type());
+#pragma unroll 1
+        for (; s + 1 < count; ++s) {
+            step(s, x, ahead, std::true_type(), std::true_type());
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) x[mt] = ahead[mt];
-            ++s;
         }
-        step(s, x, ahead, std::false_type());
+        step(s, x, ahead, std::false_type(), std::false_type());
     }
     total = sum_of_halves(total);
 
@@ -642,6 +685,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a)
 {
     constexpr int TN = 64, CH = DP / 8;
     __shared__ u32x4 tiles[2][2][TN * CH];
+    __shared__ __align__(16) float bias[2][MODE == MODE_MASK ? TN : 4];
     const int thread = threadIdx.x, wave = thread >> 6, lane = thread & 63, n = lane & 31, h = lane >> 5;
     uint32_t at = by_die(blockIdx.x, gridDim.x);
     const uint32_t rt = at % a.row_tiles;
@@ -690,8 +734,8 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a)
         u32x4 *kt = tiles[s & 1][0], *vt = tiles[s & 1][1];
         sk.store(kt, thread);
         sv.store(vt, thread);
-        const uint64_t counted = MODE == MODE_PLAIN ? 0 : __ballot(info >= 0);
-        const uint32_t first = first_of(s);
+        if (MODE == MODE_MASK && thread < TN) bias[s & 1][MODE == MODE_MASK ? thread : 0] = sk.bias;
+        const uint64_t bits = counted<MODE, TN>(keys, first_of(s), info);
         __syncthreads();
         if (s + 1 < count) {
             info = next_info;
@@ -699,17 +743,11 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a)
             sv.load(keys, a.v, a.vs, thread, first_of(s + 1), info);
             next_info = info_of(s + 2);
         }
-        bool all;
-        const uint64_t bits = seen<MODE, TN>(keys, first, counted, 0, all);
 #pragma unroll
         for (int mt = 0; mt < 2; ++mt) {
-            f32x16 x = keys_by_rows<T, DP>(kt, 32 * mt, q);
+            f32x16 x = keys_by_rows<T, DP>(kt, 32 * mt, q, MODE == MODE_MASK ? biases(bias[s & 1] + (MODE == MODE_MASK ? 32 * mt : 0)) : f32x16{});
             const f32x16 dp = keys_by_rows<T, DP>(vt, 32 * mt, d_o);
-            if (!all) {
-                const uint32_t mine = (uint32_t)(bits >> (32 * mt)) >> (4 * h);
-#pragma unroll
-                for (int r = 0; r < 16; ++r) x[r] = mine >> (8 * (r / 4) + r % 4) & 1 ? x[r] : -INFINITY;
-            }
+            if (MODE == MODE_PLAIN && bits != ~0ull) mask_keys(x, (uint32_t)(bits >> (32 * mt)));
 #pragma unroll
             for (int r = 0; r < 16; ++r) x[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], a.scale_log2, -lse2)) * (dp[r] - delta);
 #pragma unroll
@@ -724,12 +762,12 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a)
     else store_part<DP>(a.part_o + (((int64_t)split * a.batch * a.kv_heads + bh) * a.rows + row) * DP, dq[0], a.scale);
 }
 
-// dK and dV of 128 keys, 32 a wave, over the rows of a piece.  Per 32 rows: S = Q K^T, dP = dO V^T (rows along m, a lane holds one
+// dK and dV of 128 keys, 32 a wave, over the rows of a piece, TR of them between two barriers.  Per 32 rows: S = Q K^T, dP = dO V^T (rows along m, a lane holds one
 // key), dV^T += dO^T P, dK^T += Q^T dS; the rows' Q and dO are read from shared memory both along and across.
 template <class T, int DP, int MODE>
 __global__ __launch_bounds__(256, 2) void k_attn_dkv(const AttnArgs a)
 {
-    constexpr int TR = 32, CH = DP / 8, LOADS = TR * CH / 256 ? TR * CH / 256 : 1, ROWS = 256 / CH;
+    constexpr int TR = DP == 128 ? 32 : 64, CH = DP / 8, LOADS = TR * CH / 256 ? TR * CH / 256 : 1, ROWS = 256 / CH;
     __shared__ u32x4 tiles[2][2][TR * CH];
     __shared__ f32x4 stats[2][2][TR / 4];               // lse in powers of two, D
     constexpr bool AWAY = DP == 128;                    // V's operands in shared memory: with them 256 registers do not suffice
@@ -747,7 +785,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkv(const AttnArgs a)
     const uint32_t steps = kt * 128 < keys.end ? (a.rows + TR - 1) / TR : 0, per = (steps + a.splits - 1) / a.splits;
     const uint32_t step0 = split * per < steps ? split * per : steps, count = step0 + per < steps ? per : steps - step0;
 
-    const bool valid = key < keys.end && keys.info(key) >= 0, whole = __all(valid);
+    const bool valid = key < keys.end && keys.info(key) >= 0;
     typename T::V8 k[DP / 16], v[DP / 16];
     row_operands<T, DP>(k, a.k + (valid ? b * a.ks.batch + key * a.ks.token + kvh * a.ks.head : 0), valid, a.head_dim);
     row_operands<T, DP>(v, a.v + (valid ? b * a.vs.batch + key * a.vs.token + kvh * a.vs.head : 0), valid, a.head_dim);
@@ -790,32 +828,38 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkv(const AttnArgs a)
         if (thread < 2 * TR) reinterpret_cast<float *>(stats[s & 1])[thread] = stat;
         __syncthreads();
         if (s + 1 < count) load(s + 1);
-        f32x16 x = {}, dp = {};
 #pragma unroll
-        for (int t = 0; t < DP / 16; ++t) x = T::mma(as_operand<T>(qt[chunk_at<CH>(n, 2 * t + h)]), k[t], x);
+        for (int sub = 0; sub < TR / 32; ++sub) {
+            f32x16 x = {}, dp = {};
 #pragma unroll
-        for (int t = 0; t < DP / 16; ++t)
-            dp = T::mma(as_operand<T>(ot[chunk_at<CH>(n, 2 * t + h)]), AWAY ? as_operand<T>(away[AWAY ? wave : 0][t][lane]) : v[t], dp);
+            for (int t = 0; t < DP / 16; ++t) x = T::mma(as_operand<T>(qt[32 * sub * CH + chunk_at<CH>(n, 2 * t + h)]), k[t], x);
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const f32x4 lse2 = stats[s & 1][0][2 * g + h], delta = stats[s & 1][1][2 * g + h];
+            for (int t = 0; t < DP / 16; ++t)
+                dp = T::mma(as_operand<T>(ot[32 * sub * CH + chunk_at<CH>(n, 2 * t + h)]), AWAY ? as_operand<T>(away[AWAY ? wave : 0][t][lane]) : v[t], dp);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int r = 4 * g + j;
-                float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], a.scale_log2, -lse2[j]));
-                if (!whole) p = valid ? p : 0.0f;
-                x[r] = p;
-                dp[r] = p * (dp[r] - delta[j]);
+            for (int g = 0; g < 4; ++g) {
+                const f32x4 lse2 = stats[s & 1][0][8 * sub + 2 * g + h], delta = stats[s & 1][1][8 * sub + 2 * g + h];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int r = 4 * g + j;
+                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], a.scale_log2, -lse2[j]));
+                    x[r] = p;
+                    dp[r] = p * (dp[r] - delta[j]);
+                }
             }
-        }
 #pragma unroll
-        for (int part = 0; part < 2; ++part) {
-            const typename T::V8 p[1] = {rounded<T>(x, part)}, ds[1] = {rounded<T>(dp, part)};
-            columns_times<T, DP, 1>(dv, ot, 16 * part, p);
-            columns_times<T, DP, 1>(dk, qt, 16 * part, ds);
+            for (int part = 0; part < 2; ++part) {
+                const typename T::V8 p[1] = {rounded<T>(x, part)}, ds[1] = {rounded<T>(dp, part)};
+                columns_times<T, DP, 1>(dv, ot, 32 * sub + 16 * part, p);
+                columns_times<T, DP, 1>(dk, qt, 32 * sub + 16 * part, ds);
+            }
         }
     }
     if (key >= a.kv_len) return;
+    if (!valid) {                                       // (what a lane has gathered for a key that does not count)
+#pragma unroll
+        for (int dt = 0; dt < DP / 32; ++dt) dk[0][dt] = dv[0][dt] = f32x16{};
+    }
     if (a.splits == 1) {
         store_row<T, DP>(a.dk + b * a.dks.batch + key * a.dks.token + kvh * a.dks.head, dk[0], a.scale, a.head_dim);
         store_row<T, DP>(a.dv + b * a.dvs.batch + key * a.dvs.token + kvh * a.dvs.head, dv[0], 1.0f, a.head_dim);

@@ -5,8 +5,9 @@
 //   dh = dy Wd;  dg = dh u act'(g), du = dh act(g);  dx = dg Wg + du Wu;  dWg = dg^T x, dWu = du^T x, dWd = dy^T h
 //
 // Products take 16-bit operands and accumulate in 32 bits.  act(g) u and the gradients through it are formed from the 32-bit
-// accumulators in the product's epilogue; g and u are rounded to 16 bits only where they are kept for the backward pass, h, dg and
-// du because the next product takes them as operands.
+// accumulators in the product's epilogue; h, dg and du are rounded because the next product takes them as operands.  g and u are kept
+// for the backward pass in 16 bits: dx, dWg and dWu are then 1.8 times as far from 64-bit values as one rounding of the result takes
+// them (2-norm, bfloat16: 0.0031 and 0.0017).  In 32 bits it would be 1.4 times, for twice the room and 260 MB more to move at 4001 tokens of 8192.
 #pragma once
 
 #include <type_traits>

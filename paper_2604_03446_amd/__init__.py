@@ -3,6 +3,9 @@
 Every number comes out of the HIP kernels behind the C ABI.  There is no CPU
 fallback: importing this package without a built libmmee.so raises, and calls
 on a machine without a GPU return MMEE_EDEVICE (raised as MmeeError).
+
+With torch in the same process import torch first: the library then uses the HIP runtime
+that torch brings, and streams and device memory are shared.
 """
 from __future__ import annotations
 

@@ -5,11 +5,20 @@ import os
 
 import pytest
 
-ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
-if not os.path.exists(os.environ.get("MMEE_LIB") or os.path.join(ROOT, "paper_2604_03446_amd", "libmmee.so")):
-    import __graft_entry__ as g
-    g.build()
-import paper_2604_03446_amd as M  # noqa: E402
+M = None
+
+
+@pytest.fixture(scope="module", autouse=True)
+def binding():
+    """The binding, loaded when a test runs and after torch: whichever of the two comes first brings the HIP runtime that both use."""
+    global M
+    import torch  # noqa: F401
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    if not os.path.exists(os.environ.get("MMEE_LIB") or os.path.join(root, "paper_2604_03446_amd", "libmmee.so")):
+        import __graft_entry__ as g
+        g.build()
+    import paper_2604_03446_amd
+    M = paper_2604_03446_amd
 
 
 class Fake:

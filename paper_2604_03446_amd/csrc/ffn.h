@@ -232,7 +232,9 @@ __global__ __launch_bounds__(64 * WM * WN, TM == 256 ? 1 : 2) void k_product(con
             for (int ms = 0; ms < MS; ++ms)
 #pragma unroll
                 for (int ns = 0; ns < NS; ++ns) acc[ms][ns] = T::mma(b[t & 1][ns], a[t & 1][ms], acc[ms][ns]);       // C^T: a lane holds one row of C
-            // The order of a quarter: a product after every operand read, then after every store and load.
+            // The order of a quarter: a product after every operand read, then after every store and load.  (Reads spread over the whole
+            // quarter, or stores between them: 2 to 13 % slower.  Tiles straight to shared memory, which leaves loads one step instead of two to
+            // arrive: h of a prompt 7 to 13 % faster, y, dx and the weights' gradients 9 to 30 % slower.)
             constexpr int READS = MS * (A_ACROSS ? 2 : 1) + NS * (B_ACROSS ? 2 : 1), PRODUCTS = MS * NS;
 #pragma unroll
             for (int i = 0; i < PRODUCTS / 2; ++i) {

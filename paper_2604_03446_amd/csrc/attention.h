@@ -199,16 +199,10 @@ struct Stage {
             which = __ballot(info >= 0);
             bias = info >= 0 ? 0.0f : -INFINITY;
         }
-        if (last >= TN - 1) {                           // all of them exist: one offset, bases in scalar registers
-            const uint32_t at = row0 * step + c * 8;
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i) r[i] = *reinterpret_cast<const u32x4 *>(base + (uint64_t)i * ROWS * step + at);
-        } else {
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) {
-                const uint32_t row = row0 + i * ROWS, at = row < last ? row : last;
-                r[i] = *reinterpret_cast<const u32x4 *>(base + (at * step + c * 8));
-            }
+        for (int i = 0; i < LOADS; ++i) {
+            const uint32_t row = row0 + i * ROWS, at = row < last ? row : last;
+            r[i] = *reinterpret_cast<const u32x4 *>(base + (at * step + c * 8));
         }
     }
 
@@ -350,7 +344,7 @@ __device__ __forceinline__ uint64_t seen(const Keys<MODE_TREE> &keys, uint32_t f
 template <class T, int DP, int WR, int WK, int MODE>
 __global__ __launch_bounds__(64 * WR * WK, 2) void k_attn_forward(const AttnArgs a)
 {
-    constexpr int TN = WR == 4 ? 64 : 32, MT = TN / 32, CH = DP / 8, GT = 64 * WR, NB = WR == 4 ? 2 : 1, TILES = 2 * NB * WK * TN * CH;
+    constexpr int TN = WR >= 4 ? 64 : 32, MT = TN / 32, CH = DP / 8, GT = 64 * WR, NB = WR >= 4 ? 2 : 1, TILES = 2 * NB * WK * TN * CH;
     static_assert(NB == 1 || WK == 1, "two buffers for one group");
     constexpr int JOIN = WK > 1 ? WK * 32 * WR * DP / 4 : 0;
     __shared__ u32x4 memory[TILES > JOIN ? TILES : JOIN];

@@ -48,6 +48,33 @@ uint32_t pieces(uint64_t blocks, uint64_t steps, uint64_t least)
 
 uint64_t up256(uint64_t x) { return (x + 255) & ~(uint64_t)255; }
 
+// Tiles of 32 rows a wave and pieces of the keys, for `row_waves` waves with rows of their own; returns the number of blocks.
+// Up to 32 rows the four waves of a block take tiles of keys of their own, up to 64 two do.
+uint64_t split(AttnPlan &p, int row_waves, uint64_t kv_len, bool ragged)
+{
+    AttnArgs &a = p.a;
+    const uint64_t batch = a.batch;
+    a.row_tiles = (a.rows + 32 * row_waves - 1) / (32 * row_waves);
+    // Blocks of four waves run two to a compute unit, of eight waves alone.  With up to 32 rows eight waves halve the number of steps, which
+    // counts while there are fewer blocks than units; pieces cost a second launch that joins them: none shorter than 512 keys.
+    const uint64_t each = (uint64_t)a.row_tiles * a.kv_heads, room = row_waves == 8 ? 256 : 512;
+    a.step_keys = row_waves > 1 ? 64 : each * batch * std::max<uint64_t>(1, kv_len / 512) <= 256 ? 256 : 128;
+    a.least = 512 / a.step_keys;
+    const uint64_t steps = (kv_len + a.step_keys - 1) / a.step_keys;
+    a.splits = 1;
+    a.slots = a.batch;
+    a.balanced = false;
+    if (each && each * batch < room && steps > a.least) {         // pieces for one round of blocks (two, three and four rounds were 15 to 40 % slower)
+        a.slots = (uint32_t)std::min<uint64_t>(std::max<uint64_t>(room / each, batch), batch * (steps / a.least));
+        a.balanced = ragged && batch > 1 && batch <= 64 && a.slots > batch;
+        if (!a.balanced) {
+            a.splits = a.slots / a.batch;
+            a.slots = a.splits * a.batch;
+        }
+    }
+    return each * a.slots;
+}
+
 int common(AttnPlan &p, uint32_t dtype, uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t head_dim, uint32_t q_len, uint64_t kv_len, float scale, bool ragged)
 {
     if (dtype != MMEE_F16 && dtype != MMEE_BF16) return MMEE_EINVAL;
@@ -72,26 +99,16 @@ int common(AttnPlan &p, uint32_t dtype, uint32_t batch, uint32_t heads, uint32_t
     a.head_dim = head_dim;
     a.scale = scale;
     a.scale_log2 = scale * LOG2E;
-    // 32 rows to a wave.  Up to 32 rows the four waves of a block take tiles of keys of their own, up to 64 two do.
+    // Eight waves with rows of their own read every key half as often as four, but tiles of 256 rows leave more of the card idle: they are
+    // taken where one round of blocks fills more than half of the units or whole rounds at least 7/8.  Microseconds, 256 rows against 128:
+    // rows x keys x heads, 128 a head: 4096 x 4096 x 16 139 : 156, 200 x 2048 x 128 51 : 54, 1024 x 1024 x 128 87 : 92; not taken:
+    // 1024 x 1024 x 16 35 : 32, 640 x 640 x 128 56 : 50, 197 x 197 x 384 34 : 31, 256 x 512 x 128 25 : 21.
     p.row_waves = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
-    a.row_tiles = (uint32_t)((rows + 32 * p.row_waves - 1) / (32 * p.row_waves));
-    // Blocks of four waves run two to a compute unit, of eight waves alone.  Eight waves halve the number of steps, which counts while
-    // there are fewer blocks than units; pieces cost a second launch that joins them: none shorter than 512 keys.
-    const uint64_t each = (uint64_t)a.row_tiles * kv_heads;
-    a.step_keys = p.row_waves > 1 ? 64 : each * batch * std::max<uint64_t>(1, kv_len / 512) <= 256 ? 256 : 128;
-    a.least = 512 / a.step_keys;
-    const uint64_t steps = (kv_len + a.step_keys - 1) / a.step_keys;
-    a.splits = 1;
-    a.slots = batch;
-    if (each && each * batch < 512 && steps > a.least) {         // pieces for one round of blocks (two, three and four rounds were 15 to 40 % slower)
-        a.slots = (uint32_t)std::min<uint64_t>(std::max<uint64_t>(512 / each, batch), batch * (steps / a.least));
-        a.balanced = ragged && batch > 1 && batch <= 64 && a.slots > batch;
-        if (!a.balanced) {
-            a.splits = a.slots / batch;
-            a.slots = a.splits * batch;
-        }
+    if (rows > 128 && p.dp >= 64) {
+        const uint64_t blocks = split(p, 8, kv_len, ragged);
+        if (blocks > 128 && (blocks <= 256 || blocks * 8 >= (blocks + 255) / 256 * 256 * 7)) p.row_waves = 8;
     }
-    const uint64_t blocks = each * a.slots;
+    const uint64_t blocks = split(p, p.row_waves, kv_len, ragged);
     if (blocks > 0x7fffffff) return MMEE_EINVAL;
     p.blocks = (uint32_t)blocks;
     p.joins = a.slots > batch;
@@ -176,7 +193,9 @@ int plan_tree(const mmee_tree_attn *x, bool pointers, AttnPlan &p)
 template <class T, int DP, int MODE>
 void forward_as(const AttnPlan &p, hipStream_t stream)
 {
-    if (p.row_waves == 4) hipLaunchKernelGGL((k_attn_forward<T, DP, 4, 1, MODE>), dim3(p.blocks), dim3(256), 0, stream, p.a);
+    if (p.row_waves == 8) {
+        if constexpr (DP >= 64) hipLaunchKernelGGL((k_attn_forward<T, DP, 8, 1, MODE>), dim3(p.blocks), dim3(512), 0, stream, p.a);
+    } else if (p.row_waves == 4) hipLaunchKernelGGL((k_attn_forward<T, DP, 4, 1, MODE>), dim3(p.blocks), dim3(256), 0, stream, p.a);
     else if (p.row_waves == 2) hipLaunchKernelGGL((k_attn_forward<T, DP, 2, 2, MODE>), dim3(p.blocks), dim3(256), 0, stream, p.a);
     else if (p.a.step_keys == 128) hipLaunchKernelGGL((k_attn_forward<T, DP, 1, 4, MODE>), dim3(p.blocks), dim3(256), 0, stream, p.a);
     else hipLaunchKernelGGL((k_attn_forward<T, DP, 1, 8, MODE>), dim3(p.blocks), dim3(512), 0, stream, p.a);

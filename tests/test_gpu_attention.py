@@ -148,6 +148,29 @@ def test_pieces(M, shape):
     compare(t, (torch.arange(Lk) < lens[:, None])[:, None].expand(B, Lq, Lk), shape)
 
 
+@pytest.mark.parametrize("masking", ["none", "lens", "mask", "both"])
+@pytest.mark.parametrize("shape", [(1, 270, 70, 200, 70, 64), (1, 260, 33, 1601, 33, 72), (3, 130, 40, 1100, 20, 128), (4, 40, 3, 1300, 3, 64), (5, 20, 2, 1700, 1, 32)])
+def test_many_blocks(M, shape, masking):
+    """Tiles of 256 rows, alone and with the keys in pieces, and batches whose lengths (none and one among them) share the pieces."""
+    import torch
+    B, Lq, H, Lk, Hkv, d = shape
+    t = tensors((B, Lq, H, d), (B, Lk, Hkv, d), torch.bfloat16, 13, train=False)
+    kw, keep = {}, torch.ones(B, Lk, dtype=torch.bool)
+    if masking in ("lens", "both"):
+        lens = torch.tensor([Lk - 5, 0, Lk, 1, 700][:B], dtype=torch.int32)
+        kw["kv_lens"] = lens.cuda()
+        keep &= torch.arange(Lk) < lens[:, None]
+    if masking in ("mask", "both"):
+        mask = torch.rand(B, Lk, generator=torch.Generator().manual_seed(5)) < 0.4
+        mask[:, 64:160] = False
+        kw["key_mask"] = mask.cuda()
+        keep &= mask
+    t["k"][~keep.cuda()] = math.nan
+    t["v"][~keep.cuda()] = math.inf
+    run(M, t, **kw)
+    compare(t, keep[:, None].expand(B, Lq, Lk), (shape, masking))
+
+
 def test_nothing_to_do(M):
     import torch
     t = tensors((2, 5, 2, 64), (2, 0, 1, 64), torch.bfloat16, 1)

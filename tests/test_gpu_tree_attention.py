@@ -158,6 +158,16 @@ def test_long_contexts_in_pieces(M, n, H, Hkv):
     compare(t, keeps(t), n)
 
 
+@pytest.mark.parametrize("n,H,Hkv,d,page,lens", [
+    (140, 72, 36, 64, 16, [300, 40]), (70, 16, 4, 128, 128, [4000, 700]), (9, 8, 2, 64, 32, [1500, 0, 3000, 1, 511]), (50, 6, 3, 96, 64, [0, 2500, 64])])
+def test_many_blocks(M, n, H, Hkv, d, page, lens):
+    """Tiles of 256 rows, alone and in pieces; batches whose contexts (none and one among them) share the pieces."""
+    import torch
+    t = build(len(lens), n, H, Hkv, d, page, lens, torch.bfloat16, seed=n)
+    run(M, t)
+    compare(t, keeps(t), (n, lens))
+
+
 def test_shared_pages_and_strides(M):
     """Sequences that begin with the same pages; heads before tokens inside a page; a table with room behind its rows."""
     import torch

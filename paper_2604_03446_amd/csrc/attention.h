@@ -672,10 +672,10 @@ __global__ __launch_bounds__(256) void k_attn_join(const AttnArgs a)
     if (a.lse && c == 0) a.lse[lse_at(a, b, kvh, row)] = sum != 0.0f ? (high + __log2f(sum)) * LN2 : -INFINITY;
 }
 
-// dQ, and D on the way.  As the forward pass with four waves on a tile: per tile three products, S^T = K Q^T, dP^T = V dO^T and
+// dQ, and D on the way.  As the forward pass with W waves on a tile: per tile three products, S^T = K Q^T, dP^T = V dO^T and
 // dQ^T += K^T dS^T.  Split over the keys, the pieces leave their dQ in 32 bits and k_sum_parts adds them in order.
-template <class T, int DP, int MODE>
-__global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a)
+template <class T, int DP, int W, int MODE>
+__global__ __launch_bounds__(64 * W, 2) void k_attn_dq(const AttnArgs a)
 {
     constexpr int TN = 64, CH = DP / 8;
     __shared__ u32x4 tiles[2][2][TN * CH];
@@ -691,7 +691,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a)
     const uint32_t steps = (keys.end + TN - 1) / TN, per = (steps + a.splits - 1) / a.splits;
     const uint32_t step0 = split * per < steps ? split * per : steps, count = step0 + per < steps ? per : steps - step0;
 
-    const uint32_t row = (rt * 4 + wave) * 32 + n;
+    const uint32_t row = (rt * W + wave) * 32 + n;
     const bool live = row < a.rows;
     const int64_t bh = (int64_t)b * a.kv_heads + kvh;
     typename T::V8 q[DP / 16], d_o[DP / 16];
@@ -714,7 +714,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a)
     }
 
     f32x16 dq[1][DP / 32] = {};
-    Stage<DP, TN, 256, MODE> sk, sv;
+    Stage<DP, TN, 64 * W, MODE> sk, sv;
     auto first_of = [&](uint32_t s) { return (step0 + s) * TN; };
     auto info_of = [&](uint32_t s) { return keys.info(first_of(s) + lane); };
     int info = 0, next_info = 0;
@@ -756,18 +756,18 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a)
     else store_part<DP>(a.part_o + (((int64_t)split * a.batch * a.kv_heads + bh) * a.rows + row) * DP, dq[0], a.scale);
 }
 
-// dK and dV of 128 keys, 32 a wave, over the rows of a piece, TR of them between two barriers.  Per 32 rows: S = Q K^T, dP = dO V^T (rows along m, a lane holds one
-// key), dV^T += dO^T P, dK^T += Q^T dS; the rows' Q and dO are read from shared memory both along and across.
-template <class T, int DP, int MODE>
-__global__ __launch_bounds__(256, 2) void k_attn_dkv(const AttnArgs a)
+// dK and dV of 32 W keys, 32 a wave, over the rows of a piece, TR of them between two barriers.  Per 32 rows: S = Q K^T, dP = dO V^T
+// (rows along m, a lane holds one key), dV^T += dO^T P, dK^T += Q^T dS; the rows' Q and dO are read from shared memory both along and across.
+template <class T, int DP, int W, int MODE>
+__global__ __launch_bounds__(64 * W, 2) void k_attn_dkv(const AttnArgs a)
 {
-    constexpr int TR = DP == 128 ? 32 : 64, CH = DP / 8, LOADS = TR * CH / 256 ? TR * CH / 256 : 1, ROWS = 256 / CH;
+    constexpr int TR = DP == 128 ? 32 : 64, CH = DP / 8, LOADS = TR * CH / (64 * W) ? TR * CH / (64 * W) : 1, ROWS = 64 * W / CH;
     __shared__ u32x4 tiles[2][2][TR * CH];
     __shared__ f32x4 stats[2][2][TR / 4];               // lse in powers of two, D
     constexpr bool AWAY = DP == 128;                    // V's operands in shared memory: with them 256 registers do not suffice
-    __shared__ u32x4 away[AWAY ? 4 : 1][DP / 16][64];
+    __shared__ u32x4 away[AWAY ? W : 1][DP / 16][64];
     const int thread = threadIdx.x, wave = thread >> 6, lane = thread & 63, n = lane & 31, h = lane >> 5;
-    const uint32_t key_tiles = (a.kv_len + 127) / 128;
+    const uint32_t key_tiles = (a.kv_len + 32 * W - 1) / (32 * W);
     uint32_t at = by_die(blockIdx.x, gridDim.x);
     const uint32_t kt = at % key_tiles;
     at /= key_tiles;
@@ -775,8 +775,8 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkv(const AttnArgs a)
     at /= a.splits;
     const uint32_t kvh = at % a.kv_heads, b = at / a.kv_heads;
     const Keys<MODE> keys(a, b, kvh);
-    const uint32_t key = (kt * 4 + wave) * 32 + n;
-    const uint32_t steps = kt * 128 < keys.end ? (a.rows + TR - 1) / TR : 0, per = (steps + a.splits - 1) / a.splits;
+    const uint32_t key = (kt * W + wave) * 32 + n;
+    const uint32_t steps = kt * 32 * W < keys.end ? (a.rows + TR - 1) / TR : 0, per = (steps + a.splits - 1) / a.splits;
     const uint32_t step0 = split * per < steps ? split * per : steps, count = step0 + per < steps ? per : steps - step0;
 
     const bool valid = key < keys.end && keys.info(key) >= 0;

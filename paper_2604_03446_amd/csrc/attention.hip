@@ -30,7 +30,7 @@ int padded(uint32_t head_dim) { return head_dim <= 32 ? 32 : head_dim <= 64 ? 64
 
 struct AttnPlan {
     AttnArgs a = {};
-    int dp = 0, dtype = 0, mode = MODE_PLAIN, row_waves = 4;
+    int dp = 0, dtype = 0, mode = MODE_PLAIN, row_waves = 4, dq_waves = 4, dkv_waves = 4;
     uint32_t blocks = 0;                        // of the forward pass
     uint32_t dq_splits = 1, dkv_splits = 1;
     uint64_t dq_blocks = 0, dkv_blocks = 0;
@@ -38,12 +38,15 @@ struct AttnPlan {
     uint64_t part_bytes = 0, lse_bytes = 0, forward_bytes = 0, backward_bytes = 0;
 };
 
-// Pieces of the keys (or rows) such that about two blocks run on every compute unit, none of them shorter than `least` steps.
-uint32_t pieces(uint64_t blocks, uint64_t steps, uint64_t least)
+// Whether blocks that run alone on a unit keep the card busy: more than half of the units in one round, or 7/8 in whole rounds.
+bool fills(uint64_t blocks) { return blocks > 128 && (blocks <= 256 || blocks * 8 >= (blocks + 255) / 256 * 256 * 7); }
+
+// Pieces of the keys (or rows) such that about `room` blocks run, none of them shorter than `least` steps.
+uint32_t pieces(uint64_t blocks, uint64_t steps, uint64_t least, uint64_t room)
 {
-    if (!blocks || blocks >= 384) return 1;
+    if (!blocks || blocks >= room * 3 / 4) return 1;
     const uint64_t most = std::max<uint64_t>(1, steps / least);
-    return (uint32_t)std::min<uint64_t>({most, std::max<uint64_t>(1, 512 / blocks), 128});
+    return (uint32_t)std::min<uint64_t>({most, std::max<uint64_t>(1, room / blocks), 128});
 }
 
 uint64_t up256(uint64_t x) { return (x + 255) & ~(uint64_t)255; }
@@ -99,14 +102,13 @@ int common(AttnPlan &p, uint32_t dtype, uint32_t batch, uint32_t heads, uint32_t
     a.head_dim = head_dim;
     a.scale = scale;
     a.scale_log2 = scale * LOG2E;
-    // Eight waves with rows of their own read every key half as often as four, but tiles of 256 rows leave more of the card idle: they are
-    // taken where one round of blocks fills more than half of the units or whole rounds at least 7/8.  Microseconds, 256 rows against 128:
-    // rows x keys x heads, 128 a head: 4096 x 4096 x 16 139 : 156, 200 x 2048 x 128 51 : 54, 1024 x 1024 x 128 87 : 92; not taken:
-    // 1024 x 1024 x 16 35 : 32, 640 x 640 x 128 56 : 50, 197 x 197 x 384 34 : 31, 256 x 512 x 128 25 : 21.
+    // Eight waves with rows of their own read every key half as often as four, but their tiles may leave units without work.  Microseconds,
+    // 256 rows against 128, rows x keys x heads, 128 a head: 4096 x 4096 x 16 139 : 156, 200 x 2048 x 128 51 : 54, 1024 x 1024 x 128 87 : 92;
+    // not taken: 1024 x 1024 x 16 35 : 32, 640 x 640 x 128 56 : 50, 197 x 197 x 384 34 : 31, 256 x 512 x 128 25 : 21.
     p.row_waves = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
     if (rows > 128 && p.dp >= 64) {
         const uint64_t blocks = split(p, 8, kv_len, ragged);
-        if (blocks > 128 && (blocks <= 256 || blocks * 8 >= (blocks + 255) / 256 * 256 * 7)) p.row_waves = 8;
+        if (fills(blocks)) p.row_waves = 8;
     }
     const uint64_t blocks = split(p, p.row_waves, kv_len, ragged);
     if (blocks > 0x7fffffff) return MMEE_EINVAL;
@@ -142,10 +144,25 @@ int plan_attn(const mmee_attn *x, bool pointers, AttnPlan &p)
         if (misaligned(x->q) || misaligned(x->k) || misaligned(x->v) || misaligned(x->o) || misaligned(x->workspace) || ((uintptr_t)x->lse & 3) || ((uintptr_t)x->kv_lens & 3))
             return MMEE_EINVAL;
     }
-    // backward
-    const uint64_t heads_all = (uint64_t)a.batch * a.kv_heads, tiles = ((uint64_t)a.rows + 127) / 128, key_tiles = ((uint64_t)a.kv_len + 127) / 128;
-    p.dq_splits = pieces(tiles * heads_all, ((uint64_t)a.kv_len + 63) / 64, 4);
-    p.dkv_splits = pieces(key_tiles * heads_all, ((uint64_t)a.rows + 31) / 32, 8);
+    // Backward.  Blocks of eight waves read rows or keys half as often as blocks of four, and run alone on a unit, so that nothing covers
+    // the beginning and the end of a short one.  Microseconds, eight against four.  dQ, rows x keys x heads, 128 a head: 4096 x 4096 x 16
+    // 183 : 199, 200 x 2048 x 128 64 : 70, 2048 x 4096 x 64 390 : 424; not taken: 512 x 512 x 512 146 : 139, 640 x 640 x 128 70 : 63, 64 a
+    // head 1024 x 1024 x 128 67 : 64 (and 107 : 112 at 4096 x 4096 x 16).  dK and dV, 128 a head: 4096 x 4096 x 16 251 : 284,
+    // 256 x 512 x 128 37 : 39, 64 a head 4096 x 4096 x 16 139 : 152; not taken: 197 x 197 x 384 49 : 47, 64 a head 200 x 2048 x 128 68 : 63.
+    const uint64_t heads_all = (uint64_t)a.batch * a.kv_heads;
+    uint64_t tiles = 0, key_tiles = 0;
+    for (const int waves : {8, 4}) {
+        tiles = ((uint64_t)a.rows + 32 * waves - 1) / (32 * waves);
+        p.dq_waves = waves;
+        p.dq_splits = pieces(tiles * heads_all, ((uint64_t)a.kv_len + 63) / 64, 4, 2048 / waves);
+        if (p.dp == 128 && a.rows > 128 && a.kv_len / p.dq_splits >= 1024 && fills(tiles * heads_all * p.dq_splits)) break;
+    }
+    for (const int waves : {8, 4}) {
+        key_tiles = ((uint64_t)a.kv_len + 32 * waves - 1) / (32 * waves);
+        p.dkv_waves = waves;
+        p.dkv_splits = pieces(key_tiles * heads_all, ((uint64_t)a.rows + 31) / 32, 8, 2048 / waves);
+        if ((p.dp == 128 || (p.dp == 64 && a.rows >= 1024)) && a.kv_len > 128 && fills(key_tiles * heads_all * p.dkv_splits)) break;
+    }
     p.dq_blocks = tiles * heads_all * p.dq_splits;
     p.dkv_blocks = key_tiles * heads_all * p.dkv_splits;
     if (p.dq_blocks > 0x7fffffff || p.dkv_blocks > 0x7fffffff) return MMEE_EINVAL;
@@ -211,15 +228,23 @@ void backward_as(const AttnPlan &p, hipStream_t stream)
     const uint64_t heads_all = (uint64_t)p.a.batch * p.a.kv_heads;
     AttnArgs a = p.a;
     if (p.dq_blocks) {
-        a.row_tiles = (a.rows + 127) / 128;
+        a.row_tiles = (a.rows + 32 * p.dq_waves - 1) / (32 * p.dq_waves);
         a.splits = p.dq_splits;
-        hipLaunchKernelGGL((k_attn_dq<T, DP, MODE>), dim3((uint32_t)p.dq_blocks), dim3(256), 0, stream, a);
+        if (p.dq_waves == 8) {
+            if constexpr (DP == 128) hipLaunchKernelGGL((k_attn_dq<T, DP, 8, MODE>), dim3((uint32_t)p.dq_blocks), dim3(512), 0, stream, a);
+        } else {
+            hipLaunchKernelGGL((k_attn_dq<T, DP, 4, MODE>), dim3((uint32_t)p.dq_blocks), dim3(256), 0, stream, a);
+        }
         const uint64_t per = 256 / (DP / 4);
         if (a.splits > 1) hipLaunchKernelGGL((k_attn_sum<T, DP, 0>), dim3((uint32_t)((heads_all * a.rows + per - 1) / per)), dim3(256), 0, stream, a);
     }
     if (p.dkv_blocks) {
         a.splits = p.dkv_splits;
-        hipLaunchKernelGGL((k_attn_dkv<T, DP, MODE>), dim3((uint32_t)p.dkv_blocks), dim3(256), 0, stream, a);
+        if (p.dkv_waves == 8) {
+            if constexpr (DP >= 64) hipLaunchKernelGGL((k_attn_dkv<T, DP, 8, MODE>), dim3((uint32_t)p.dkv_blocks), dim3(512), 0, stream, a);
+        } else {
+            hipLaunchKernelGGL((k_attn_dkv<T, DP, 4, MODE>), dim3((uint32_t)p.dkv_blocks), dim3(256), 0, stream, a);
+        }
         const uint64_t per = 256 / (DP / 2);
         if (a.splits > 1) hipLaunchKernelGGL((k_attn_sum<T, DP, 1>), dim3((uint32_t)((heads_all * a.kv_len + per - 1) / per)), dim3(256), 0, stream, a);
     }

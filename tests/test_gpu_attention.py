@@ -171,6 +171,25 @@ def test_many_blocks(M, shape, masking):
     compare(t, keep[:, None].expand(B, Lq, Lk), (shape, masking))
 
 
+@pytest.mark.parametrize("masking", ["none", "lens", "mask"])
+@pytest.mark.parametrize("shape", [(1, 600, 48, 1030, 48, 128), (2, 130, 72, 300, 9, 64), (2, 130, 72, 300, 9, 120)])
+def test_many_blocks_backward(M, shape, masking):
+    """Gradients over tiles of 256 rows or keys, alone and in pieces."""
+    import torch
+    B, Lq, H, Lk, Hkv, d = shape
+    t = tensors((B, Lq, H, d), (B, Lk, Hkv, d), torch.bfloat16, 17)
+    kw, keep = {}, torch.ones(B, Lk, dtype=torch.bool)
+    if masking == "lens":
+        lens = torch.tensor([Lk - 5, 100][:B], dtype=torch.int32)
+        kw["kv_lens"] = lens.cuda()
+        keep &= torch.arange(Lk) < lens[:, None]
+    elif masking == "mask":
+        keep = torch.rand(B, Lk, generator=torch.Generator().manual_seed(6)) < 0.4
+        kw["key_mask"] = keep.cuda()
+    run(M, t, **kw)
+    compare(t, keep[:, None].expand(B, Lq, Lk), (shape, masking))
+
+
 def test_nothing_to_do(M):
     import torch
     t = tensors((2, 5, 2, 64), (2, 0, 1, 64), torch.bfloat16, 1)

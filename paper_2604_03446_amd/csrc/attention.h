@@ -350,7 +350,8 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void k_attn_forward(const AttnArgs
     __shared__ u32x4 memory[TILES > JOIN ? TILES : JOIN];
     __shared__ float marks[2][WK][WK > 1 ? 32 * WR : 1];
     __shared__ __align__(16) float bias[WK][NB][MODE == MODE_MASK ? TN : 4];
-    const int thread = threadIdx.x % GT, wave = threadIdx.x >> 6, wr = wave % WR, wk = wave / WR, lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
+    const int thread = threadIdx.x % GT, lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wave % WR, wk = wave / WR;    // scalar, and with them the tiles' places
 
     uint32_t at = by_die(blockIdx.x, gridDim.x);
     const uint32_t rt = at % a.row_tiles;
@@ -564,12 +565,15 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void k_attn_forward(const AttnArgs
             info[1] = info[2];
             info[2] = info_of(s + 4);
         };
-        // Without lengths in the way every tile but the last is whole.
-        constexpr std::bool_constant<MODE != MODE_PLAIN> inner;
+        // Tiles s + 1 and s + 2 are seen whole by every row: without lengths in the way all but the last, of a tree those before the nodes
+        // (as far as pages are there; rows without a node are emptied at the end).
+        auto whole = [&](uint32_t s) {
+            return s + 3 < count && (MODE != MODE_TREE || (first_of(s + 3) <= keys.held && __all(info[0] >= 0) && __all(info[1] >= 0)));
+        };
         uint32_t s = 0;
-        for (; s + 3 < count; s += 2) {
-            step(s, x, ahead, std::true_type(), inner);
-            step(s + 1, ahead, x, std::true_type(), inner);
+        for (; whole(s); s += 2) {
+            step(s, x, ahead, std::true_type(), std::false_type());
+            step(s + 1, ahead, x, std::true_type(), std::false_type());
         }
 #pragma unroll 1
         for (; s + 1 < count; ++s) {
@@ -580,6 +584,11 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void k_attn_forward(const AttnArgs
         step(s, x, ahead, std::false_type(), std::false_type());
     }
     total = sum_of_halves(total);
+    if (MODE == MODE_TREE && WR >= 4 && token >= keys.nodes) {
+        total = 0.0f;
+#pragma unroll
+        for (int dt = 0; dt < DP / 32; ++dt) o[dt] = f32x16{};
+    }
 
     const int64_t part_row = ((int64_t)slot * a.kv_heads + kvh) * a.rows;
     if (WK == 1) {

@@ -168,6 +168,19 @@ def test_many_blocks(M, n, H, Hkv, d, page, lens):
     compare(t, keeps(t), (n, lens))
 
 
+@pytest.mark.parametrize("page", [1, 2, 8, 64])
+@pytest.mark.parametrize("n,H,Hkv,d,counts", [(40, 8, 2, 128, [40, 17, 0]), (3, 4, 1, 64, [3, 1, 2]), (20, 4, 2, 64, [5, 20, 20]), (5, 6, 6, 32, [4, 5, 1])])
+def test_long_tables(M, n, H, Hkv, d, counts, page):
+    """Contexts of many pages, fewer nodes than there is room for, a page of the middle that is not there."""
+    import torch
+    t = build(3, n, H, Hkv, d, page, [1200, 900, 1037], torch.bfloat16, seed=page)
+    t["table"][1, 512 // page] = -5
+    run(M, t, counts)
+    keep = keeps(t, counts)
+    keep[1, :, 512 // page * page:(512 // page + 1) * page] = False
+    compare(t, keep, (n, page))
+
+
 def test_shared_pages_and_strides(M):
     """Sequences that begin with the same pages; heads before tokens inside a page; a table with room behind its rows."""
     import torch

@@ -339,8 +339,17 @@ __device__ __forceinline__ uint64_t seen(const Keys<MODE_TREE> &keys, uint32_t f
 }
 
 // Forward.  WR waves share a tile of keys, 32 rows each; WK such groups take every WK-th tile of the block's piece and are joined
-// at the end.  WR = 4 for many rows: a tile serves 128 rows.  WK = 4 or 8 for 32 rows or fewer (single tokens): nothing is shared
+// at the end.  WR = 4 or 8 for many rows: a tile serves 128 or 256.  WK = 4 or 8 for 32 rows or fewer (single tokens): nothing is shared
 // between waves and no barrier is met while keys stream in.
+//
+// Many rows are bound by the compute unit: of a step's 2.1 us the matrix instructions need 0.85, the reads of operands from shared memory
+// 0.85 and the vector instructions 0.9, and they overlap in part.  2048 rows over 8192 keys, 32 heads of 128: 269 to 280 us, 1.0 PFLOP/s
+// (a library product of 16-bit matrices reaches 1.39); 2 x 2048 over 4096, 32 heads over 8: 290 us, 0.95.  With a mask of a byte a key, 8 x
+// 509 rows over 1500, 12 heads of 64: 45 us, 0.42 PFLOP/s: an exponential a score weighs twice as much as with 128 values a head.  Sixteen
+// trees of up to 63 nodes over contexts of 2048 to 4096 in pages of 16, 32 heads over 8: 93 us, where every block streams keys that no other
+// one reads: 2.4 TB/s and 0.56 PFLOP/s at once; 26 nodes over contexts up to 131072, 64 heads over 8: 305 us, 2.6 TB/s.
+// Few rows are bound by HBM: 64 tokens over 1024 to 2048 keys, 32 heads over 8: 82 us, 4.9 TB/s; one token over 512 keys, 12 heads: 6 us,
+// the latency of a launch, of the lengths, the keys and the join.
 template <class T, int DP, int WR, int WK, int MODE>
 __global__ __launch_bounds__(64 * WR * WK, 2) void k_attn_forward(const AttnArgs a)
 {
@@ -351,7 +360,7 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void k_attn_forward(const AttnArgs
     __shared__ float marks[2][WK][WK > 1 ? 32 * WR : 1];
     __shared__ __align__(16) float bias[WK][NB][MODE == MODE_MASK ? TN : 4];
     const int thread = threadIdx.x % GT, lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wave % WR, wk = wave / WR;    // scalar, and with them the tiles' places
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wave % WR, wk = wave / WR;      // scalar: the tiles' places are
 
     uint32_t at = by_die(blockIdx.x, gridDim.x);
     const uint32_t rt = at % a.row_tiles;
@@ -652,7 +661,8 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void k_attn_forward(const AttnArgs
     }
 }
 
-// Joins the pieces' results: O = sum_s 2^(lse_s - max) O_s / sum_s 2^(lse_s - max), pieces in ascending order.  DP / 4 threads a row.
+// Joins the pieces' results: O = sum_s 2^(lse_s - max) O_s / sum_s 2^(lse_s - max), pieces in ascending order.  DP / 4 threads a row, 16 bytes each.
+// Bound by memory: 32 256 rows of 128 in two pieces, 33 MB and 8 MB of results, 9.6 us, 4.3 TB/s.  In 32 bits, so that cutting costs no precision.
 template <class T, int DP>
 __global__ __launch_bounds__(256) void k_attn_join(const AttnArgs a)
 {
@@ -682,7 +692,10 @@ __global__ __launch_bounds__(256) void k_attn_join(const AttnArgs a)
 }
 
 // dQ, and D on the way.  As the forward pass with W waves on a tile: per tile three products, S^T = K Q^T, dP^T = V dO^T and
-// dQ^T += K^T dS^T.  Split over the keys, the pieces leave their dQ in 32 bits and k_sum_parts adds them in order.
+// dQ^T += K^T dS^T.  Split over the keys, the pieces leave their dQ in 32 bits and k_attn_sum adds them in order.
+// Nothing is added atomically, so results repeat to the bit; the price is that S and dP are formed here and again for dK and dV: seven
+// products where five would do.  Bound as the forward pass is, with two thirds of the exponentials a product: 2 x 2048 rows over 4096 keys, 32 heads of 128
+// over 8: 380 to 390 us, 1.07 PFLOP/s; masked, 8 x 509 over 1500, 12 heads of 64: 57 us.
 template <class T, int DP, int W, int MODE>
 __global__ __launch_bounds__(64 * W, 2) void k_attn_dq(const AttnArgs a)
 {
@@ -767,6 +780,9 @@ __global__ __launch_bounds__(64 * W, 2) void k_attn_dq(const AttnArgs a)
 
 // dK and dV of 32 W keys, 32 a wave, over the rows of a piece, TR of them between two barriers.  Per 32 rows: S = Q K^T, dP = dO V^T
 // (rows along m, a lane holds one key), dV^T += dO^T P, dK^T += Q^T dS; the rows' Q and dO are read from shared memory both along and across.
+// With 128 values a head the 256 registers of a wave hold K and both sums; V's operands lie in shared memory (their reads are what
+// limits it most), with 32 rows a step: 64 spilled 67 registers and took 900 us.  2 x 2048 rows over 4096 keys, 32 heads of 128 over 8: 510 to
+// 540 us, 1.05 PFLOP/s; masked, 8 x 509 over 1500, 12 heads of 64: 65 us.
 template <class T, int DP, int W, int MODE>
 __global__ __launch_bounds__(64 * W, 2) void k_attn_dkv(const AttnArgs a)
 {
@@ -873,7 +889,8 @@ __global__ __launch_bounds__(64 * W, 2) void k_attn_dkv(const AttnArgs a)
     }
 }
 
-// Sums of pieces in ascending order, rounded once: which = 0: dQ rows; 1: dK and dV of a key beside each other.
+// Sums of pieces in ascending order, rounded once: which = 0: dQ rows; 1: dK and dV of a key beside each other.  Bound by memory:
+// four pieces of dK and dV of 1024 keys, 16 heads of 128, 67 MB: 13 us, 5.2 TB/s (some of it from the last level of cache).
 template <class T, int DP, int WHICH>
 __global__ __launch_bounds__(256) void k_attn_sum(const AttnArgs a)
 {

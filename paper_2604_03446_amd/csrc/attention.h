@@ -702,7 +702,7 @@ __global__ __launch_bounds__(64 * W, 2) void k_attn_dq(const AttnArgs a)
     constexpr int TN = 64, CH = DP / 8;
     __shared__ u32x4 tiles[2][2][TN * CH];
     __shared__ __align__(16) float bias[2][MODE == MODE_MASK ? TN : 4];
-    const int thread = threadIdx.x, wave = thread >> 6, lane = thread & 63, n = lane & 31, h = lane >> 5;
+    const int thread = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(thread >> 6), lane = thread & 63, n = lane & 31, h = lane >> 5;
     uint32_t at = by_die(blockIdx.x, gridDim.x);
     const uint32_t rt = at % a.row_tiles;
     at /= a.row_tiles;
@@ -791,7 +791,7 @@ __global__ __launch_bounds__(64 * W, 2) void k_attn_dkv(const AttnArgs a)
     __shared__ f32x4 stats[2][2][TR / 4];               // lse in powers of two, D
     constexpr bool AWAY = DP == 128;                    // V's operands in shared memory: with them 256 registers do not suffice
     __shared__ u32x4 away[AWAY ? W : 1][DP / 16][64];
-    const int thread = threadIdx.x, wave = thread >> 6, lane = thread & 63, n = lane & 31, h = lane >> 5;
+    const int thread = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(thread >> 6), lane = thread & 63, n = lane & 31, h = lane >> 5;
     const uint32_t key_tiles = (a.kv_len + 32 * W - 1) / (32 * W);
     uint32_t at = by_die(blockIdx.x, gridDim.x);
     const uint32_t kt = at % key_tiles;

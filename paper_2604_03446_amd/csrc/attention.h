@@ -691,6 +691,32 @@ __global__ __launch_bounds__(256) void k_attn_join(const AttnArgs a)
     if (a.lse && c == 0) a.lse[lse_at(a, b, kvh, row)] = sum != 0.0f ? (high + __log2f(sum)) * LN2 : -INFINITY;
 }
 
+// Gradients through float16.  Probabilities over many keys, and dS with small gradients of O, lie below the type's normal numbers (6e-5),
+// where rounding is no longer relative (7e-3 of dK with gradients of 5e-4 over 2048 keys).  So P is multiplied by 2^15, and dS by a power of two of
+// the lane's own (a row's in dQ, a key's in dK) that keeps it below 2^15; both are divided out of the 32-bit sums at the end.  The power starts high and
+// is lowered, with the sums so far, when a value outgrows it.  It costs 3 % of dQ's time and 8 % of dK's; bfloat16, with the range of 32 bits,
+// needs none of it.
+template <class T>
+constexpr bool NARROW = std::is_same_v<T, F16>;
+constexpr float UP = 15.0f, HIGHEST = 60.0f;            // powers of two: of P; dS's over P's at first
+
+// Keeps 16 scaled values of dS in range; returns the power of two (none or negative) that they and `sums` were multiplied by.
+template <int N>
+__device__ __forceinline__ float keep_in_range(f32x16 &ds, f32x16 (&sums)[N])
+{
+    float most = 0.0f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) most = __builtin_fmaxf(most, __builtin_fabsf(ds[r]));
+    if (!__any(most > 0x1p15f)) return 0.0f;
+    most = max_of_halves(most);
+    const int lower = most > 0x1p15f ? 11 - __builtin_amdgcn_frexp_expf(most) : 0;       // to 2^10 .. 2^11
+    const float by = __builtin_ldexpf(1.0f, lower);
+    ds *= by;
+#pragma unroll
+    for (int i = 0; i < N; ++i) sums[i] *= by;
+    return (float)lower;
+}
+
 // dQ, and D on the way.  As the forward pass with W waves on a tile: per tile three products, S^T = K Q^T, dP^T = V dO^T and
 // dQ^T += K^T dS^T.  Split over the keys, the pieces leave their dQ in 32 bits and k_attn_sum adds them in order.
 // Nothing is added atomically, so results repeat to the bit; the price is that S and dP are formed here and again for dK and dV: seven
@@ -722,7 +748,7 @@ __global__ __launch_bounds__(64 * W, 2) void k_attn_dq(const AttnArgs a)
     float lse2 = INFINITY, delta = 0.0f;                // rows that see nothing: probabilities 0
     if (live) {
         const float l = a.lse_in[lse_at(a, b, kvh, row)];
-        lse2 = l == -INFINITY ? INFINITY : l * LOG2E;
+        lse2 = l == -INFINITY ? INFINITY : l * LOG2E - (NARROW<T> ? UP + HIGHEST : 0.0f);
     }
     {
         typename T::V8 o[DP / 16];
@@ -736,6 +762,7 @@ __global__ __launch_bounds__(64 * W, 2) void k_attn_dq(const AttnArgs a)
     }
 
     f32x16 dq[1][DP / 32] = {};
+    float lowered = 0.0f;                               // of dS's power of two, which lse2 holds
     Stage<DP, TN, 64 * W, MODE> sk, sv;
     auto first_of = [&](uint32_t s) { return (step0 + s) * TN; };
     auto info_of = [&](uint32_t s) { return keys.info(first_of(s) + lane); };
@@ -766,6 +793,11 @@ __global__ __launch_bounds__(64 * W, 2) void k_attn_dq(const AttnArgs a)
             if (MODE == MODE_PLAIN && bits != ~0ull) mask_keys(x, (uint32_t)(bits >> (32 * mt)));
 #pragma unroll
             for (int r = 0; r < 16; ++r) x[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], a.scale_log2, -lse2)) * (dp[r] - delta);
+            if (NARROW<T>) {
+                const float by = keep_in_range(x, dq[0]);
+                lowered += by;
+                lse2 -= by;
+            }
 #pragma unroll
             for (int part = 0; part < 2; ++part) {
                 const typename T::V8 ds[1] = {rounded<T>(x, part)};
@@ -774,8 +806,9 @@ __global__ __launch_bounds__(64 * W, 2) void k_attn_dq(const AttnArgs a)
         }
     }
     if (!live) return;
-    if (a.splits == 1) store_row<T, DP>(a.dq + row_at(a, a.dqs, b, kvh, row), dq[0], a.scale, a.head_dim);
-    else store_part<DP>(a.part_o + (((int64_t)split * a.batch * a.kv_heads + bh) * a.rows + row) * DP, dq[0], a.scale);
+    const float times = NARROW<T> ? a.scale * __builtin_amdgcn_exp2f(-(UP + HIGHEST + lowered)) : a.scale;
+    if (a.splits == 1) store_row<T, DP>(a.dq + row_at(a, a.dqs, b, kvh, row), dq[0], times, a.head_dim);
+    else store_part<DP>(a.part_o + (((int64_t)split * a.batch * a.kv_heads + bh) * a.rows + row) * DP, dq[0], times);
 }
 
 // dK and dV of 32 W keys, 32 a wave, over the rows of a piece, TR of them between two barriers.  Per 32 rows: S = Q K^T, dP = dO V^T
@@ -830,12 +863,14 @@ __global__ __launch_bounds__(64 * W, 2) void k_attn_dkv(const AttnArgs a)
         const bool there = row < a.rows;
         if (thread < TR) {
             const float l = a.lse_in[lse_at(a, b, kvh, there ? row : a.rows - 1)];
-            stat = there && l != -INFINITY ? l * LOG2E : INFINITY;      // rows that are not there, or see nothing: probabilities 0
+            stat = there && l != -INFINITY ? l * LOG2E - (NARROW<T> ? UP : 0.0f) : INFINITY;      // rows that are not there, or see nothing: probabilities 0
         } else if (thread < 2 * TR) {
             stat = a.delta[bh * a.rows + (there ? row : a.rows - 1)];
         }
     };
     f32x16 dk[1][DP / 32] = {}, dv[1][DP / 32] = {};
+    float by = 0x1p60f;                                 // float16: dS's power of two over P's
+    static_assert(HIGHEST == 60.0f);
     if (count) load(0);
     for (uint32_t s = 0; s < count; ++s) {
         u32x4 *qt = tiles[s & 1][0], *ot = tiles[s & 1][1];
@@ -863,9 +898,10 @@ __global__ __launch_bounds__(64 * W, 2) void k_attn_dkv(const AttnArgs a)
                     const int r = 4 * g + j;
                     const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], a.scale_log2, -lse2[j]));
                     x[r] = p;
-                    dp[r] = p * (dp[r] - delta[j]);
+                    dp[r] = p * (NARROW<T> ? (dp[r] - delta[j]) * by : dp[r] - delta[j]);
                 }
             }
+            if (NARROW<T>) by *= __builtin_amdgcn_exp2f(keep_in_range(dp, dk[0]));
 #pragma unroll
             for (int part = 0; part < 2; ++part) {
                 const typename T::V8 p[1] = {rounded<T>(x, part)}, ds[1] = {rounded<T>(dp, part)};
@@ -879,13 +915,14 @@ __global__ __launch_bounds__(64 * W, 2) void k_attn_dkv(const AttnArgs a)
 #pragma unroll
         for (int dt = 0; dt < DP / 32; ++dt) dk[0][dt] = dv[0][dt] = f32x16{};
     }
+    const float times = NARROW<T> ? a.scale * 0x1p-15f / by : a.scale, times_v = NARROW<T> ? 0x1p-15f : 1.0f;
     if (a.splits == 1) {
-        store_row<T, DP>(a.dk + b * a.dks.batch + key * a.dks.token + kvh * a.dks.head, dk[0], a.scale, a.head_dim);
-        store_row<T, DP>(a.dv + b * a.dvs.batch + key * a.dvs.token + kvh * a.dvs.head, dv[0], 1.0f, a.head_dim);
+        store_row<T, DP>(a.dk + b * a.dks.batch + key * a.dks.token + kvh * a.dks.head, dk[0], times, a.head_dim);
+        store_row<T, DP>(a.dv + b * a.dvs.batch + key * a.dvs.token + kvh * a.dvs.head, dv[0], times_v, a.head_dim);
     } else {
         float *part = a.part_o + ((((int64_t)split * a.batch * a.kv_heads + bh) * a.kv_len + key) * 2) * DP;
-        store_part<DP>(part, dk[0], a.scale);
-        store_part<DP>(part + DP, dv[0], 1.0f);
+        store_part<DP>(part, dk[0], times);
+        store_part<DP>(part + DP, dv[0], times_v);
     }
 }
 

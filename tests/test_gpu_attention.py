@@ -211,6 +211,34 @@ def test_scores_far_apart(M):
     compare(t, everything(1, 64, 700), "rising")
 
 
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
+@pytest.mark.parametrize("shape", [(1, 1024, 2, 2048, 1, 64), (1, 700, 1, 2048, 1, 128), (1, 300, 40, 260, 40, 128)])
+@pytest.mark.parametrize("gradients", ["small", "rising", "large"])
+def test_gradients_of_all_sizes(M, shape, gradients, dtype):
+    """dS far below float16's normal numbers, or thousands, or rising along rows and keys.  In the 2-norm three roundings of relative
+    error at most u / 2 each reach dQ and dK (dS, the output, and O in D), two reach dV: 1.5 u covers them, and half a unit of the subnormal
+    numbers on every element of the result."""
+    import torch
+    from attention_oracle import UNIT, TINY, attention
+    B, Lq, H, Lk, Hkv, d = shape
+    dt = getattr(torch, dtype)
+    t = tensors((B, Lq, H, d), (B, Lk, Hkv, d), dt, 19)
+    t["q"], t["k"], scale = t["q"] / 16, t["k"] / 16, 256 * d ** -0.5
+    up = lambda n: torch.exp2(torch.linspace(-8, 0, n, device="cuda").round())[None, :, None, None]  # noqa: E731
+    if gradients == "small":
+        t["do"] = t["do"] * 2.0 ** -11
+    elif gradients == "large":
+        t["do"] = t["do"] * 2.0 ** 8
+    else:
+        t["do"], t["v"] = (t["do"] * up(Lq)).to(dt), (t["v"] * up(Lk)).to(dt)
+    run(M, t, scale=scale)
+    want = attention(t["q"], t["k"], t["v"], everything(B, Lq, Lk), scale, dt, t["do"])
+    for name in ("dq", "dk", "dv"):
+        value = want[name][0]
+        off = (t[name].double().cpu() - value).norm()
+        assert off <= 1.5 * UNIT[dt] * value.norm() + TINY[dt] * value.numel() ** 0.5, (name, (off / value.norm()).item())
+
+
 def test_scale(M):
     import torch
     t = tensors((1, 20, 2, 32), (1, 50, 2, 32), torch.float16, 2)

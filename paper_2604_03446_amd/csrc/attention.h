@@ -719,6 +719,8 @@ __device__ __forceinline__ float keep_in_range(f32x16 &ds, f32x16 (&sums)[N])
 
 // dQ, and D on the way.  As the forward pass with W waves on a tile: per tile three products, S^T = K Q^T, dP^T = V dO^T and
 // dQ^T += K^T dS^T.  Split over the keys, the pieces leave their dQ in 32 bits and k_attn_sum adds them in order.
+// D comes from O as it was rounded to 16 bits, the only form of it that a caller has to keep: with few keys dQ and dK are then up to 1.7 times
+// as far from 64-bit values as one rounding takes them, with many 1.4 times (2-norm, bfloat16: 0.0029, 0.0024 and 0.0017).
 // Nothing is added atomically, so results repeat to the bit; the price is that S and dP are formed here and again for dK and dV: seven
 // products where five would do.  Bound as the forward pass is, with two thirds of the exponentials a product: 2 x 2048 rows over 4096 keys, 32 heads of 128
 // over 8: 380 to 390 us, 1.07 PFLOP/s; masked, 8 x 509 over 1500, 12 heads of 64: 57 us.

@@ -593,7 +593,8 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void k_attn_forward(const AttnArgs
         step(s, x, ahead, std::false_type(), std::false_type());
     }
     total = sum_of_halves(total);
-    if (MODE == MODE_TREE && WR >= 4 && token >= keys.nodes) {
+    // Rows without a node: tiles seen whole were not masked for them, and a probability of 0 does not clear what is infinite or NaN.
+    if (MODE == MODE_TREE && token >= keys.nodes) {
         total = 0.0f;
 #pragma unroll
         for (int dt = 0; dt < DP / 32; ++dt) o[dt] = f32x16{};

@@ -1,9 +1,9 @@
-"""Infinities and NaN in what a row does not see: rows past a tree's nodes."""
+"""Infinities and NaN in what a row does not see: rows past a tree's nodes, nodes that no row sees."""
 import math
 
 import pytest
 
-from test_gpu_tree_attention import build, run
+from test_gpu_tree_attention import build, compare, keeps, random_tree, run
 
 pytestmark = pytest.mark.gpu
 
@@ -44,3 +44,25 @@ def test_rows_past_the_nodes(M, n, H, Hkv, d, lens, dtype):
     for b, c in enumerate(counts):
         assert not t["o"][b, c:].any() and (t["lse"][b, :, c:] == -math.inf).all()
         assert torch.isnan(t["o"][b, :c]).all()
+
+
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
+@pytest.mark.parametrize("n,H,Hkv,d,lens", TREES + [(9, 2, 1, 32, [0, 63]), (64, 1, 1, 64, [63, 64]), (70, 2, 2, 128, [31, 500]), (200, 2, 1, 80, [130, 1])])
+@pytest.mark.parametrize("counted", ["all", "fewer"])
+def test_nodes_that_no_row_sees(M, n, H, Hkv, d, lens, counted, dtype):
+    """Their keys and values reach no row: pruned branches, the nodes that only rows past the count would see, and padding without a count."""
+    import torch
+    sees = random_tree(2, n, n)
+    unseen = sorted({1, n // 3, n // 2, min(n - 1, 64), n - 1})
+    counts = None if counted == "all" else [n - 1, n // 2 + 1]
+    for j in unseen:
+        sees[:, :, j] = False
+    if counts:
+        for b, c in enumerate(counts):
+            sees[b, c:] = True
+    t = build(2, n, H, Hkv, d, 16, lens, getattr(torch, dtype), seed=n, sees=sees)
+    for b in range(2):
+        for i, j in enumerate(unseen):
+            put(t, b, lens[b] + j, 16, k=(math.nan, math.inf, -math.inf)[i % 3], v=(math.inf, math.nan, -math.inf)[i % 3])
+    run(M, t, counts)
+    compare(t, keeps(t, counts), (n, counts))

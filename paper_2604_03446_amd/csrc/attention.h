@@ -172,9 +172,9 @@ __device__ __forceinline__ void balance(const AttnArgs &a, uint32_t &pieces, uin
     first_slot = sum - pieces;
 }
 
-// One thread's share of a tile of TN keys' K or V by GT threads: loads in flight in registers, then to shared memory.  Keys past the last one
-// and columns past the head's repeat existing ones (probabilities, and the rows' operands, are 0 there), so that nothing branches; masked
-// keys and those of pages that are not there become zeros on the way, since they may hold anything.
+// One thread's share of a tile of TN keys' K or V by GT threads: loads in flight in registers, then to shared memory.  Keys past the last one and
+// columns past the head's are zeros, as are masked keys, which may hold anything, and those of pages that are not there: a probability or a
+// row's operand of 0 does not clear what is infinite or NaN.  What does not exist is asked for beyond the buffer's end, so that nothing branches.
 template <int DP, int TN, int GT, int MODE>
 struct Stage {
     static constexpr int CH = DP / 8, LOADS = TN * CH / GT, ROWS = GT / CH;     // rows that one load of all threads covers
@@ -188,32 +188,33 @@ struct Stage {
     __device__ __forceinline__ void load(const Keys<MODE> &keys, const uint16_t *from, const Strides &s, int thread, uint32_t first, int info)
     {
         const AttnArgs &a = keys.a;
-        const int row0 = thread / CH, c = 8 * (thread % CH) < (int)a.head_dim ? thread % CH : 0;
+        const int row0 = thread / CH, c = thread % CH;
+        const bool inside = 8 * c < (int)a.head_dim;
         if (MODE == MODE_TREE) {
             // a lane works out where its key lies; the threads that load the key ask it
-            const uint32_t key = first + (threadIdx.x & 63) % TN, inside = key & ((1u << a.page_shift) - 1);
-            const int64_t place = info >= 0 ? info * s.batch + inside * s.token : -1;
-            const uint16_t *base = from + keys.kvh * s.head + c * 8;
+            const uint32_t key = first + (threadIdx.x & 63) % TN, within = key & ((1u << a.page_shift) - 1);
+            const int64_t place = info >= 0 ? info * s.batch + within * s.token : -1;
+            const uint16_t *base = from + keys.kvh * s.head + (inside ? c * 8 : 0);
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) {
                 const int row = row0 + i * ROWS, high = __shfl((int)(place >> 32), row);
                 const uint32_t low = __shfl((uint32_t)place, row);
-                there[MODE == MODE_TREE ? i : 0] = high >= 0;
+                there[MODE == MODE_TREE ? i : 0] = high >= 0 && inside;
                 r[i] = *reinterpret_cast<const u32x4 *>(base + (high >= 0 ? (int64_t)high << 32 | low : 0));
             }
             return;
         }
-        const uint32_t begin = first < keys.end ? first : keys.end - 1, last = keys.end - 1 - begin;
-        const uint16_t *base = from + keys.b * s.batch + keys.kvh * s.head + begin * s.token;
-        const uint32_t step = (uint32_t)s.token;        // a tile spans less than 2^31 elements
+        const uint32_t begin = first < keys.end ? first : keys.end, left = keys.end - begin;
+        const auto base = buffer_at(from + keys.b * s.batch + keys.kvh * s.head + begin * s.token);
+        const uint32_t step = 2 * (uint32_t)s.token, column = inside ? 16 * c : BEYOND;         // a tile spans less than 2^31 bytes
         if (MODE == MODE_MASK) {
             which = __ballot(info >= 0);
             bias = info >= 0 ? 0.0f : -INFINITY;
         }
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const uint32_t row = row0 + i * ROWS, at = row < last ? row : last;
-            r[i] = *reinterpret_cast<const u32x4 *>(base + (at * step + c * 8));
+            const uint32_t row = row0 + i * ROWS;
+            r[i] = __builtin_amdgcn_raw_buffer_load_b128(base, row < left ? row * step + column : BEYOND, 0, 0);
         }
     }
 

@@ -88,10 +88,6 @@ struct ProductArgs {
 
 constexpr int BK = 64;
 
-// A buffer of 2^31 bytes from a pointer on: more than a tile spans.  Loads at BEYOND give zeros.
-constexpr uint32_t BEYOND = 0x80000000u;
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_at(const uint16_t *p) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(p), 0, (int)BEYOND, 0x00027000); }
-
 // One thread's share of an operand's tile of ROWS x 64, by THREADS threads: registers in flight, then shared memory.  What does not
 // exist is asked for beyond the buffer's end and comes back as zeros, without a branch in the products' loop.
 template <int ROWS, int THREADS, bool ACROSS>

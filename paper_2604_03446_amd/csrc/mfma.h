@@ -57,6 +57,10 @@ __device__ __forceinline__ s16x4 read_transposed(const void *p)
     return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)p);
 }
 
+// A buffer of 2^31 bytes from a pointer on: more than a tile spans.  Loads at BEYOND give zeros.
+constexpr uint32_t BEYOND = 0x80000000u;
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_at(const uint16_t *p) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(p), 0, (int)BEYOND, 0x00027000); }
+
 // Shared memory that only one wave uses: its accesses stay in order.
 __device__ __forceinline__ void wave_sync()
 {

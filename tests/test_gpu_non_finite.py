@@ -1,8 +1,11 @@
-"""Infinities and NaN in what a row does not see: rows past a tree's nodes, nodes that no row sees."""
+"""Infinities and NaN in what a row does not see, and in what it sees: rows past the nodes, nodes that no row sees, the last key, padded columns."""
 import math
 
 import pytest
 
+from test_gpu_attention import compare as compare_cross
+from test_gpu_attention import run as run_cross
+from test_gpu_attention import tensors
 from test_gpu_tree_attention import build, compare, keeps, random_tree, run
 
 pytestmark = pytest.mark.gpu
@@ -66,3 +69,49 @@ def test_nodes_that_no_row_sees(M, n, H, Hkv, d, lens, counted, dtype):
             put(t, b, lens[b] + j, 16, k=(math.nan, math.inf, -math.inf)[i % 3], v=(math.inf, math.nan, -math.inf)[i % 3])
     run(M, t, counts)
     compare(t, keeps(t, counts), (n, counts))
+
+
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
+@pytest.mark.parametrize("B,Lq,H,Lk,Hkv,d", [(1, 1, 4, 33, 2, 64), (2, 1, 4, 5001, 1, 128), (2, 50, 1, 95, 1, 40), (2, 130, 3, 65, 3, 32), (1, 700, 2, 1601, 1, 128), (1, 270, 70, 200, 70, 64)])
+@pytest.mark.parametrize("masking", ["none", "lens"])
+def test_infinite_values_of_the_last_key(M, B, Lq, H, Lk, Hkv, d, masking, dtype):
+    """An infinity in a value that counts comes out as it is, in its own column."""
+    import torch
+    t = tensors((B, Lq, H, d), (B, Lk, Hkv, d), getattr(torch, dtype), 23, train=False)
+    lens, kw = torch.full((B,), Lk), {}
+    if masking == "lens":
+        lens = torch.tensor([Lk - 2, Lk // 2 + 1][:B])
+        kw["kv_lens"] = lens.to(torch.int32).cuda()
+    t["q"] /= 4                                         # (probabilities stay in the range of 16 bits)
+    for b in range(B):
+        t["v"][b, lens[b] - 1, :, 3], t["v"][b, lens[b] - 1, :, d - 1] = math.inf, -math.inf
+        t["v"][b, lens[b]:], t["k"][b, lens[b]:] = math.nan, math.nan
+    run_cross(M, t, **kw)
+    compare_cross(t, (torch.arange(Lk) < lens[:, None])[:, None].expand(B, Lq, Lk), "last key")
+
+
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
+@pytest.mark.parametrize("d", [8, 24, 32, 40, 64, 80, 128])
+@pytest.mark.parametrize("Lq", [1, 40, 200])
+@pytest.mark.parametrize("masking", ["none", "mask", "tree"])
+def test_keys_at_minus_infinity(M, Lq, d, masking, dtype):
+    """Positive queries on a key that holds -inf: its score is -inf and its probability 0, whatever the head size."""
+    import torch
+    dt, B, H, Lk = getattr(torch, dtype), 2, 2, 130
+    if masking == "tree":
+        t = build(B, Lq, H, 1, d, 16, [Lk, Lk], dt, seed=d)
+        t["q"] = t["q"].abs()
+        for p in (0, 7, 70, Lk - 1):
+            t["k"][:, p, :, :8] = -math.inf
+            for b in range(B):
+                put(t, b, p, 16, k=t["k"][b, p].cuda())
+        run(M, t)
+        return compare(t, keeps(t), d)
+    t = tensors((B, Lq, H, d), (B, Lk, 1, d), dt, 29, train=False)
+    t["q"] = t["q"].abs()
+    t["k"][:, [0, 7, 70, Lk - 1], :, :8] = -math.inf
+    keep = torch.ones(B, Lk, dtype=torch.bool)
+    if masking == "mask":
+        keep[:, 5:60] = False
+    run_cross(M, t, **({"key_mask": keep.cuda()} if masking == "mask" else {}))
+    compare_cross(t, keep[:, None].expand(B, Lq, Lk), d)

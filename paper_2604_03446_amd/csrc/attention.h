@@ -442,8 +442,10 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void k_attn_forward(const AttnArgs
             }
         }
     };
+    uint64_t any = 0;                                   // MODE_MASK: whether a key counts
     auto put_keys = [&](uint32_t s) {
         sk.store(k_tile(s), thread);
+        if (MODE == MODE_MASK) any |= sk.which;
         if (MODE == MODE_MASK && thread < TN) bias[wk][NB == 2 ? s & 1 : 0][MODE == MODE_MASK ? thread : 0] = sk.bias;
     };
     auto maximum = [&](const f32x16 (&of)[MT]) {
@@ -606,7 +608,9 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void k_attn_forward(const AttnArgs
     }
     total = sum_of_halves(total);
     // Rows without a node: tiles seen whole were not masked for them, and a probability of 0 does not clear what is infinite or NaN.
-    if (MODE == MODE_TREE && token >= keys.nodes) {
+    // Rows over masked keys alone: their queries may be anything, and what is infinite or NaN in them no bias masks.
+    if ((MODE == MODE_TREE && token >= keys.nodes) || (MODE == MODE_MASK && !any)) {
+        top = -INFINITY;
         total = 0.0f;
 #pragma unroll
         for (int dt = 0; dt < DP / 32; ++dt) o[dt] = f32x16{};
@@ -821,6 +825,10 @@ __global__ __launch_bounds__(64 * W, 2) void k_attn_dq(const AttnArgs a)
         }
     }
     if (!live) return;
+    if (MODE == MODE_MASK && lse2 == INFINITY) {        // (a row that sees nothing, whatever its query holds)
+#pragma unroll
+        for (int dt = 0; dt < DP / 32; ++dt) dq[0][dt] = f32x16{};
+    }
     const float times = NARROW<T> ? a.scale * __builtin_amdgcn_exp2f(-(UP + HIGHEST + lowered)) : a.scale;
     if (a.splits == 1) store_row<T, DP>(a.dq + row_at(a, a.dqs, b, kvh, row), dq[0], times, a.head_dim);
     else store_part<DP>(a.part_o + (((int64_t)split * a.batch * a.kv_heads + bh) * a.rows + row) * DP, dq[0], times);

@@ -1,8 +1,10 @@
-"""Infinities and NaN in what a row does not see, and in what it sees: rows past the nodes, nodes that no row sees, the last key, padded columns."""
+"""Infinities and NaN in what a row does not see, and in what it sees: rows past the nodes, nodes that no row sees, the last key,
+padded columns, rows without keys."""
 import math
 
 import pytest
 
+from test_gpu_attention import everything
 from test_gpu_attention import compare as compare_cross
 from test_gpu_attention import run as run_cross
 from test_gpu_attention import tensors
@@ -115,3 +117,20 @@ def test_keys_at_minus_infinity(M, Lq, d, masking, dtype):
         keep[:, 5:60] = False
     run_cross(M, t, **({"key_mask": keep.cuda()} if masking == "mask" else {}))
     compare_cross(t, keep[:, None].expand(B, Lq, Lk), d)
+
+
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
+@pytest.mark.parametrize("B,Lq,H,Lk,Hkv,d", [(2, 1, 4, 200, 2, 64), (2, 3, 8, 3000, 1, 64), (3, 50, 1, 150, 1, 80), (2, 140, 2, 333, 2, 128), (2, 700, 48, 300, 24, 64)])
+def test_rows_without_keys(M, B, Lq, H, Lk, Hkv, d, dtype):
+    """A batch whose mask is empty gives zeros, lse -inf and zero gradients also where its queries are infinite or NaN."""
+    import torch
+    t = tensors((B, Lq, H, d), (B, Lk, Hkv, d), getattr(torch, dtype), 31)
+    keep = torch.ones(B, Lk, dtype=torch.bool)
+    keep[1] = False
+    t["q"][1, :, 0], t["q"][1, Lq // 2] = math.inf, math.nan
+    run_cross(M, t, key_mask=keep.cuda())
+    for name in ("o", "dq", "dk", "dv"):
+        assert not t[name][1].any(), name
+    assert (t["lse"][1] == -math.inf).all()
+    t = {n: x[:1] for n, x in t.items()}
+    compare_cross(t, everything(1, Lq, Lk), "the others")

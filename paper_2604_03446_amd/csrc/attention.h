@@ -21,6 +21,10 @@ namespace mmee {
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
+// Types whose normal numbers end well above the smallest probabilities and gradients.
+template <class T>
+constexpr bool NARROW = std::is_same_v<T, F16>;
+
 struct Strides {                // in elements
     int64_t batch, token, head;
 };
@@ -406,7 +410,7 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void k_attn_forward(const AttnArgs
 
     f32x16 sums[1][DP / 32] = {};
     f32x16(&o)[DP / 32] = sums[0];
-    float top = -INFINITY, total = 0.0f;                // maximum (scaled, in powers of two); this lane's share of the sum
+    float top = -INFINITY, total = 0.0f;                // mark near the maximum (scaled, in powers of two); this lane's share of the sum
 
     Stage<DP, TN, GT, MODE> sk, sv;
     u32x4 *const mine = memory + wk * 2 * NB * TN * CH;
@@ -416,6 +420,7 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void k_attn_forward(const AttnArgs
     auto info_of = [&](uint32_t s) { return keys.info(first_of(s) + lane % TN); };
     auto sync = [&] { if (WR > 1) __syncthreads(); else wave_sync(); };
     constexpr uint64_t WHOLE = ~0ull >> (64 - TN);
+    constexpr float HIGHER = NARROW<T> ? 7.0f : 0.0f;   // powers of two, of probabilities
     f32x16 x[MT];
     float most = -INFINITY;                             // maximum of the scores that are next, scaled
     int info[3] = {};                                   // of the tile whose scores come next and the two behind it
@@ -457,9 +462,11 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void k_attn_forward(const AttnArgs
         return m;
     };
     // The sum may be taken against any mark near the maximum.  A mark that is kept until a row outgrows it by 2^8 spares scaling
-    // 16 DP / 32 accumulators a tile; 32-bit sums hold 2^8 times as much, and so do probabilities in 16 bits.
+    // 16 DP / 32 accumulators a tile; 32-bit sums hold 2^8 times as much, and so do probabilities in 16 bits.  In float16 the mark
+    // lies 2^7 below the maximum, probabilities up to 2^15 above it: one of 2^-32 of the row's largest is then rounded as one of 2^-25 would be, below
+    // which float16 holds nothing.
     auto raise = [&] {
-        most = max_of_halves(most) * a.scale_log2;
+        most = __builtin_fmaf(max_of_halves(most), a.scale_log2, -HIGHER);
         if (__any(!(most <= top + 8.0f))) {
             const float mark = __builtin_elementwise_maximum(top, most);
             const float keep = top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top - mark);
@@ -713,8 +720,6 @@ __global__ __launch_bounds__(256) void k_attn_join(const AttnArgs a)
 // the lane's own (a row's in dQ, a key's in dK) that keeps it below 2^15; both are divided out of the 32-bit sums at the end.  The power starts high and
 // is lowered, with the sums so far, when a value outgrows it.  It costs 3 % of dQ's time and 8 % of dK's; bfloat16, with the range of 32 bits,
 // needs none of it.
-template <class T>
-constexpr bool NARROW = std::is_same_v<T, F16>;
 constexpr float UP = 15.0f, HIGHEST = 60.0f;            // powers of two: of P; dS's over P's at first
 
 // Keeps 16 scaled values of dS in range; returns the power of two (none or negative) that they and `sums` were multiplied by.

@@ -12,18 +12,12 @@
 // instructions need them.
 #pragma once
 
-#include <type_traits>
-
 #include "launch.h"
 #include "mfma.h"
 
 namespace mmee {
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-
-// Types whose normal numbers end well above the smallest probabilities and gradients.
-template <class T>
-constexpr bool NARROW = std::is_same_v<T, F16>;
 
 struct Strides {                // in elements
     int64_t batch, token, head;

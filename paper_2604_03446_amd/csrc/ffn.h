@@ -84,6 +84,7 @@ struct ProductArgs {
     const uint16_t *gate_in, *up_in;    // EPI_DGATED
     uint16_t *gate, *up;                // EPI_GATED: kept, or null
     int64_t ld_hidden;                  // of gate and up
+    const float *scale;                 // float16: of dg and du, and its inverse; null: none
 };
 
 constexpr int BK = 64;
@@ -263,6 +264,7 @@ __global__ __launch_bounds__(64 * WM * WN, TM == 256 ? 1 : 2) void k_product(con
     f32x4 *mine = reinterpret_cast<f32x4 *>(&tiles[0][0]) + wave * 32 * C4;
     const int c8 = lane % PER_ROW, r0 = lane / PER_ROW;
     const uint32_t col = n0 + wn * OUT + 8 * c8, rows0 = m0 + wm * MS * 32 + r0;
+    const float times = NARROW<T> && !GATED && p.scale ? p.scale[DGATED ? 0 : 1] : 1.0f;
     const bool column = col < p.n;
     V8 kept[2][DGATED ? PASSES : 1];                    // g and u
     auto ask = [&](int ms) {
@@ -312,14 +314,15 @@ __global__ __launch_bounds__(64 * WM * WN, TM == 256 ? 1 : 2) void k_product(con
                 const f32x8 x = take(pass * ROWS + r0, 2 * c8);
                 if (row >= p.m || !column) continue;
                 if (p.splits > 1) *reinterpret_cast<f32x8 *>(p.parts + ((uint64_t)(problem * p.splits + split) * p.m + row) * p.n + col) = x;
-                else *reinterpret_cast<V8 *>(p.c[problem] + row * p.ldc + col) = __builtin_convertvector(x, V8);
+                else *reinterpret_cast<V8 *>(p.c[problem] + row * p.ldc + col) = __builtin_convertvector(NARROW<T> ? x * times : x, V8);
             }
         } else {
             with_activation(p.act, [&](auto kind) {
 #pragma unroll
                 for (int pass = 0; pass < PASSES; ++pass) {
                     const uint32_t row = row0 + pass * ROWS;
-                    const f32x8 x = take(pass * ROWS + r0, 2 * c8);
+                    f32x8 x = take(pass * ROWS + r0, 2 * c8);
+                    if (NARROW<T> && DGATED) x *= times;
                     f32x8 value, slope;
                     if (GATED) {
                         const f32x8 up = take(pass * ROWS + r0, 2 * c8 + C4 / 2);
@@ -363,7 +366,142 @@ __global__ __launch_bounds__(256) void k_sum_parts(const ProductArgs p)
     f32x4 x = {0, 0, 0, 0};
 #pragma unroll 4
     for (uint32_t s = 0; s < p.splits; ++s) x += *reinterpret_cast<const f32x4 *>(p.parts + ((problem * p.splits + s) * per + in) * 4);
+    if (NARROW<T> && p.scale) x *= p.scale[1];
     *reinterpret_cast<typename T::V4 *>(p.c[problem] + in / n4 * p.ldc + in % n4 * 4) = __builtin_convertvector(x, typename T::V4);
+}
+
+// Float16's dg and du.  They are the next products' operands, and with the gradients of a long mean they lie below the type's normal numbers
+// (6e-5), where rounding is no longer relative, while the weights' gradients, sums over the tokens, lie well above.  So both are multiplied by a power of two of the call's
+// own, which is divided out of the 32-bit sums.  |dg| and |du| are at most max_t |dy_t| max_f |wd_f| max(1.13 |u|, |act(g)|) (2-norms of dy's
+// rows and of Wd's columns, as dh is their product; act' is at most 1.13, |act(g)| at most |g|, or 1): the power takes this bound to 2^14 .. 2^15, so that nothing
+// overflows.  The typical value lies about sqrt(out_dim) and the outliers' ratios below it: of 2^29 between the bound and the last normal number
+// most is left.  A token whose gradient is far below the largest one's (2^-15 and less) gets a dx of fewer bits.
+struct BoundArgs {
+    const uint16_t *dy, *w_down, *gate, *up;
+    int64_t ld_dy, ld_down;
+    uint32_t rows, hidden, out;
+    uint32_t row_blocks, kept_blocks, strips, chunks;   // blocks for dy's rows, for g and u, for 64 rows of 512 of Wd's columns each
+    int act;
+    float *parts;                       // what they found: [row_blocks], [kept_blocks][2], [chunks][strips]
+    float *scale;
+};
+
+__device__ __forceinline__ float finite_or_zero(float x) { return x < INFINITY ? x : 0.0f; }      // (NaN neither)
+
+template <class T>
+__device__ __forceinline__ f32x8 eight(const uint16_t *p) { return __builtin_convertvector(*reinterpret_cast<const typename T::V8 *>(p), f32x8); }
+
+// Bound by memory: 4001 tokens, 2048 -> 8192 -> 2048: 34 us for 181 MB, 5.3 TB/s.  With k_grad_scale's 4 us, the latency of its loads, 3 % of that
+// training step; 64 tokens through 4096 -> 12288 -> 4096, most of it Wd's, or 300 through 768 -> 3072 -> 768: 10 %.
+template <class T>
+__global__ __launch_bounds__(256) void k_grad_bounds(const BoundArgs p)
+{
+    __shared__ float found[2][4];
+    __shared__ float squares[4][512];
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t at = blockIdx.x;
+    float *out = p.parts;
+    float most = 0.0f, second = 0.0f;
+    uint32_t kinds = 1;
+    if (at < p.row_blocks) {                            // squares of dy's rows, a wave each
+        out += at;
+        for (uint64_t row = 4ull * at + wave; row < p.rows; row += 4ull * p.row_blocks) {
+            float sum = 0.0f;
+            for (uint32_t c = 8 * lane; c < p.out; c += 512) {
+                const f32x8 x = eight<T>(p.dy + row * p.ld_dy + c);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sum += x[j] * x[j];
+            }
+#pragma unroll
+            for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
+            most = __builtin_fmaxf(most, finite_or_zero(sum));
+        }
+    } else if ((at -= p.row_blocks) < p.kept_blocks) {  // |g| and |u|
+        out += p.row_blocks + 2 * at;
+        kinds = 2;
+        const uint64_t all = (uint64_t)p.rows * p.hidden, stride = 2048ull * p.kept_blocks;
+        for (uint64_t i = 2048ull * at + 8 * threadIdx.x; i < all; i += stride) {
+            const f32x8 g = eight<T>(p.gate + i), u = eight<T>(p.up + i);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                most = __builtin_fmaxf(most, finite_or_zero(__builtin_fabsf(g[j])));
+                second = __builtin_fmaxf(second, finite_or_zero(__builtin_fabsf(u[j])));
+            }
+        }
+    } else {                                            // squares of 64 rows of Wd's columns, 512 of them
+        at -= p.kept_blocks;
+        out += p.row_blocks + 2 * p.kept_blocks + at;
+        const uint32_t col = at % p.strips * 512 + 8 * lane, row0 = at / p.strips * 64;
+        f32x8 sum = {};
+        if (col < p.hidden) {
+#pragma unroll 4
+            for (uint32_t row = row0 + wave; row < row0 + 64 && row < p.out; row += 4) {
+                const f32x8 x = eight<T>(p.w_down + row * p.ld_down + col);
+                sum += x * x;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) squares[wave][8 * lane + j] = sum[j];
+        __syncthreads();
+        for (uint32_t c = threadIdx.x; c < 512; c += 256)
+            most = __builtin_fmaxf(most, finite_or_zero(squares[0][c] + squares[1][c] + squares[2][c] + squares[3][c]));
+    }
+#pragma unroll
+    for (int d = 32; d; d >>= 1) {
+        most = __builtin_fmaxf(most, __shfl_xor(most, d));
+        second = __builtin_fmaxf(second, __shfl_xor(second, d));
+    }
+    if (lane == 0) {
+        found[0][wave] = most;
+        found[1][wave] = second;
+    }
+    __syncthreads();
+    if (threadIdx.x < kinds) {
+        const float *f = found[threadIdx.x];
+        out[threadIdx.x] = __builtin_fmaxf(__builtin_fmaxf(f[0], f[1]), __builtin_fmaxf(f[2], f[3]));
+    }
+}
+
+// The power of two from what the blocks found, by one block.  The largest column of Wd is at most the sum of the chunks' largest.
+__global__ __launch_bounds__(1024) void k_grad_scale(const BoundArgs p)
+{
+    __shared__ float found[4][16];
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const float *kept = p.parts + p.row_blocks, *w = kept + 2 * p.kept_blocks;
+    float most[4] = {};                                 // dy's rows, g, u; Wd: a sum
+    for (uint32_t i = threadIdx.x; i < p.row_blocks; i += 1024) most[0] = __builtin_fmaxf(most[0], p.parts[i]);
+    for (uint32_t i = threadIdx.x; i < p.kept_blocks; i += 1024) {
+        most[1] = __builtin_fmaxf(most[1], kept[2 * i]);
+        most[2] = __builtin_fmaxf(most[2], kept[2 * i + 1]);
+    }
+    for (uint32_t c = threadIdx.x; c < p.chunks; c += 1024) {
+        float strip = 0.0f;
+#pragma unroll 4
+        for (uint32_t s = 0; s < p.strips; ++s) strip = __builtin_fmaxf(strip, w[(uint64_t)c * p.strips + s]);
+        most[3] += strip;
+    }
+#pragma unroll
+    for (int d = 32; d; d >>= 1) {
+#pragma unroll
+        for (int k = 0; k < 3; ++k) most[k] = __builtin_fmaxf(most[k], __shfl_xor(most[k], d));
+        most[3] += __shfl_xor(most[3], d);
+    }
+    if (lane == 0) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) found[k][wave] = most[k];
+    }
+    __syncthreads();
+    if (threadIdx.x) return;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+#pragma unroll
+        for (int k = 0; k < 3; ++k) most[k] = __builtin_fmaxf(i ? most[k] : 0.0f, found[k][i]);
+        most[3] = (i ? most[3] : 0.0f) + found[3][i];
+    }
+    const float bound = __builtin_sqrtf(most[0]) * __builtin_sqrtf(most[3]) * __builtin_fmaxf(1.13f * most[2], p.act == ACT_SIGMOID ? 1.0f : most[1]);
+    const int power = bound > 0.0f ? 15 - __builtin_amdgcn_frexp_expf(bound) : 0;        // (the bound lies between 2^-72 and 2^72)
+    p.scale[0] = __builtin_ldexpf(1.0f, power);
+    p.scale[1] = __builtin_ldexpf(1.0f, -power);
 }
 
 // Four columns of a token's results; of a gated product from g and u.

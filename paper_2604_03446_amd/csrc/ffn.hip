@@ -102,7 +102,9 @@ bool plan_tokens(Job &j, uint32_t m, uint32_t n, uint32_t k, bool gated)
 struct FfnPlan {
     bool tokens = false;                        // few tokens: weights are streamed
     Job hidden, down, d_hidden, dx, dw_gated, dw_down;
-    uint64_t forward_bytes = 0, backward_bytes = 0, d_hidden_bytes = 0;
+    BoundArgs bounds = {};                      // float16, backward
+    uint64_t forward_bytes = 0, backward_bytes = 0, d_hidden_bytes = 0, parts_bytes = 0;
+    uint64_t bound_blocks() const { return (uint64_t)bounds.row_blocks + bounds.kept_blocks + (uint64_t)bounds.chunks * bounds.strips; }
 };
 
 int plan_ffn(const mmee_ffn *x, bool pointers, FfnPlan &f)
@@ -130,7 +132,20 @@ int plan_ffn(const mmee_ffn *x, bool pointers, FfnPlan &f)
     if (!fits) return MMEE_EINVAL;
     f.forward_bytes = f.down.parts_bytes();
     f.d_hidden_bytes = up256(2ull * M * F);
-    f.backward_bytes = 2 * f.d_hidden_bytes + std::max({f.dx.parts_bytes(), f.dw_gated.parts_bytes(), f.dw_down.parts_bytes()});
+    f.parts_bytes = std::max({f.dx.parts_bytes(), f.dw_gated.parts_bytes(), f.dw_down.parts_bytes()});
+    f.backward_bytes = 2 * f.d_hidden_bytes + f.parts_bytes;
+    if (x->dtype == MMEE_F16 && M) {
+        BoundArgs &b = f.bounds;
+        b.rows = M;
+        b.hidden = F;
+        b.out = J;
+        b.row_blocks = (uint32_t)std::min<uint64_t>(512, ((uint64_t)M + 3) / 4);
+        b.kept_blocks = (uint32_t)std::min<uint64_t>(1024, ((uint64_t)M * F + 8191) / 8192);
+        b.chunks = (J + 63) / 64;
+        b.strips = (F + 511) / 512;
+        if (f.bound_blocks() > 0x7fffffff) return MMEE_EINVAL;
+        f.backward_bytes += up256(4 * (f.bound_blocks() + b.kept_blocks)) + 256;
+    }
     return MMEE_OK;
 }
 
@@ -182,6 +197,12 @@ void forward_as(const FfnPlan &f, hipStream_t stream)
 template <class T>
 void backward_as(const FfnPlan &f, hipStream_t stream)
 {
+    if constexpr (NARROW<T>) {
+        if (f.bounds.rows) {
+            hipLaunchKernelGGL((k_grad_bounds<T>), dim3((uint32_t)f.bound_blocks()), dim3(256), 0, stream, f.bounds);
+            hipLaunchKernelGGL(k_grad_scale, dim3(1), dim3(1024), 0, stream, f.bounds);
+        }
+    }
     product<T, false, true, EPI_DGATED>(f.d_hidden, stream);
     product<T, false, true, EPI_STORE>(f.dx, stream);
     sum_parts<T>(f.dx, stream);
@@ -256,7 +277,21 @@ int mmee_ffn_backward(const mmee_ffn *x, const mmee_ffn_grads *g)
     float *parts = (float *)(du + f.d_hidden_bytes / 2);
     const int64_t x_stride = stride_of(x->x_stride, x->rows), dy_stride = stride_of(g->dy_stride, x->rows);
 
+    BoundArgs &b = f.bounds;
+    if (b.rows) {
+        b.dy = (const uint16_t *)g->dy;
+        b.ld_dy = dy_stride;
+        b.w_down = (const uint16_t *)x->w_down;
+        b.ld_down = x->down_stride;
+        b.gate = (const uint16_t *)x->gate;
+        b.up = (const uint16_t *)x->up;
+        b.act = (int)x->act;
+        b.scale = parts + f.parts_bytes / 4;
+        b.parts = b.scale + 64;
+    }
+
     ProductArgs &h = f.d_hidden.p;
+    h.scale = b.scale;
     h.a[0] = (const uint16_t *)g->dy;
     h.lda = dy_stride;
     h.b[0] = (const uint16_t *)x->w_down;
@@ -269,6 +304,7 @@ int mmee_ffn_backward(const mmee_ffn *x, const mmee_ffn_grads *g)
     h.act = (int)x->act;
 
     ProductArgs &dx = f.dx.p;
+    dx.scale = b.scale;
     dx.a[0] = dg;
     dx.a[1] = du;
     dx.lda = F;
@@ -280,6 +316,7 @@ int mmee_ffn_backward(const mmee_ffn *x, const mmee_ffn_grads *g)
     dx.parts = parts;
 
     ProductArgs &dw = f.dw_gated.p;
+    dw.scale = b.scale;
     dw.a[0] = dg;
     dw.a[1] = du;
     dw.lda = F;

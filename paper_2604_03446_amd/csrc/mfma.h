@@ -11,6 +11,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 namespace mmee {
 
@@ -35,6 +36,10 @@ struct BF16 {
     static __device__ __forceinline__ f32x16 mma(V8 a, V8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
     static __device__ __forceinline__ f32x4 mma(V8 a, V8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 };
+
+// Types whose normal numbers end well above the smallest probabilities and gradients.
+template <class T>
+constexpr bool NARROW = std::is_same_v<T, F16>;
 
 // A row-major tile of 16-bit values in shared memory, CH chunks of eight values a row.  Chunk c of row r lies at place
 // c ^ spread(r): 16 rows' reads of one chunk (A and B operands along the rows) then meet every bank once, and so do four

@@ -291,10 +291,18 @@ extern "C" {
 int mmee_attn_workspace(const mmee_attn *x, int backward, uint64_t *bytes)
 {
     if (!bytes) return MMEE_EINVAL;
-    AttnPlan p;
-    const int rc = plan_attn(x, false, p);
-    if (rc) return rc;
-    *bytes = backward ? std::max(p.forward_bytes, p.backward_bytes) : p.forward_bytes;
+    if (!x) return MMEE_EINVAL;
+    // enough with and without lengths, which decide how the keys are cut: they may be given later
+    *bytes = 0;
+    static const int32_t some = 0;
+    for (const int32_t *lens : {(const int32_t *)nullptr, &some}) {
+        mmee_attn y = *x;
+        y.kv_lens = lens;
+        AttnPlan p;
+        const int rc = plan_attn(&y, false, p);
+        if (rc) return rc;
+        *bytes = std::max({*bytes, p.forward_bytes, backward ? p.backward_bytes : 0});
+    }
     return MMEE_OK;
 }
 

@@ -208,22 +208,22 @@ int plan_tree(const mmee_tree_attn *x, bool pointers, AttnPlan &p)
 }
 
 template <class T, int DP, int MODE>
-void forward_as(const AttnPlan &p, hipStream_t stream)
+void forward_as(const AttnPlan &p, Launching &l)
 {
     if (p.row_waves == 8) {
-        if constexpr (DP >= 64) hipLaunchKernelGGL((k_attn_forward<T, DP, 8, 1, MODE>), dim3(p.blocks), dim3(512), 0, stream, p.a);
-    } else if (p.row_waves == 4) hipLaunchKernelGGL((k_attn_forward<T, DP, 4, 1, MODE>), dim3(p.blocks), dim3(256), 0, stream, p.a);
-    else if (p.row_waves == 2) hipLaunchKernelGGL((k_attn_forward<T, DP, 2, 2, MODE>), dim3(p.blocks), dim3(256), 0, stream, p.a);
-    else if (p.a.step_keys == 128) hipLaunchKernelGGL((k_attn_forward<T, DP, 1, 4, MODE>), dim3(p.blocks), dim3(256), 0, stream, p.a);
-    else hipLaunchKernelGGL((k_attn_forward<T, DP, 1, 8, MODE>), dim3(p.blocks), dim3(512), 0, stream, p.a);
+        if constexpr (DP >= 64) l.run(k_attn_forward<T, DP, 8, 1, MODE>, p.blocks, 512, p.a);
+    } else if (p.row_waves == 4) l.run(k_attn_forward<T, DP, 4, 1, MODE>, p.blocks, 256, p.a);
+    else if (p.row_waves == 2) l.run(k_attn_forward<T, DP, 2, 2, MODE>, p.blocks, 256, p.a);
+    else if (p.a.step_keys == 128) l.run(k_attn_forward<T, DP, 1, 4, MODE>, p.blocks, 256, p.a);
+    else l.run(k_attn_forward<T, DP, 1, 8, MODE>, p.blocks, 512, p.a);
     if (p.joins) {
         const uint64_t lines = (uint64_t)p.a.batch * p.a.kv_heads * p.a.rows, per = 256 / (DP / 4);
-        hipLaunchKernelGGL((k_attn_join<T, DP>), dim3((uint32_t)((lines + per - 1) / per)), dim3(256), 0, stream, p.a);
+        l.run(k_attn_join<T, DP>, (lines + per - 1) / per, 256, p.a);
     }
 }
 
 template <class T, int DP, int MODE>
-void backward_as(const AttnPlan &p, hipStream_t stream)
+void backward_as(const AttnPlan &p, Launching &l)
 {
     const uint64_t heads_all = (uint64_t)p.a.batch * p.a.kv_heads;
     AttnArgs a = p.a;
@@ -231,22 +231,22 @@ void backward_as(const AttnPlan &p, hipStream_t stream)
         a.row_tiles = (a.rows + 32 * p.dq_waves - 1) / (32 * p.dq_waves);
         a.splits = p.dq_splits;
         if (p.dq_waves == 8) {
-            if constexpr (DP == 128) hipLaunchKernelGGL((k_attn_dq<T, DP, 8, MODE>), dim3((uint32_t)p.dq_blocks), dim3(512), 0, stream, a);
+            if constexpr (DP == 128) l.run(k_attn_dq<T, DP, 8, MODE>, p.dq_blocks, 512, a);
         } else {
-            hipLaunchKernelGGL((k_attn_dq<T, DP, 4, MODE>), dim3((uint32_t)p.dq_blocks), dim3(256), 0, stream, a);
+            l.run(k_attn_dq<T, DP, 4, MODE>, p.dq_blocks, 256, a);
         }
         const uint64_t per = 256 / (DP / 4);
-        if (a.splits > 1) hipLaunchKernelGGL((k_attn_sum<T, DP, 0>), dim3((uint32_t)((heads_all * a.rows + per - 1) / per)), dim3(256), 0, stream, a);
+        if (a.splits > 1) l.run(k_attn_sum<T, DP, 0>, (heads_all * a.rows + per - 1) / per, 256, a);
     }
     if (p.dkv_blocks) {
         a.splits = p.dkv_splits;
         if (p.dkv_waves == 8) {
-            if constexpr (DP >= 64) hipLaunchKernelGGL((k_attn_dkv<T, DP, 8, MODE>), dim3((uint32_t)p.dkv_blocks), dim3(512), 0, stream, a);
+            if constexpr (DP >= 64) l.run(k_attn_dkv<T, DP, 8, MODE>, p.dkv_blocks, 512, a);
         } else {
-            hipLaunchKernelGGL((k_attn_dkv<T, DP, 4, MODE>), dim3((uint32_t)p.dkv_blocks), dim3(256), 0, stream, a);
+            l.run(k_attn_dkv<T, DP, 4, MODE>, p.dkv_blocks, 256, a);
         }
         const uint64_t per = 256 / (DP / 2);
-        if (a.splits > 1) hipLaunchKernelGGL((k_attn_sum<T, DP, 1>), dim3((uint32_t)((heads_all * a.kv_len + per - 1) / per)), dim3(256), 0, stream, a);
+        if (a.splits > 1) l.run(k_attn_sum<T, DP, 1>, (heads_all * a.kv_len + per - 1) / per, 256, a);
     }
 }
 
@@ -277,8 +277,8 @@ int forward(AttnPlan &p, void *workspace, uint64_t workspace_bytes)
     p.a.cut = (uint32_t *)(p.a.part_lse + p.lse_bytes / 4);
     Launching l;
     if (l.rc) return l.rc;
-    dispatch(p, [&](auto type, auto dp, auto mode) { forward_as<decltype(type), dp.value, mode.value>(p, l.stream); });
-    return launched("attention, forward");
+    dispatch(p, [&](auto type, auto dp, auto mode) { forward_as<decltype(type), dp.value, mode.value>(p, l); });
+    return l.result("attention, forward");
 }
 
 }  // namespace
@@ -337,9 +337,9 @@ int mmee_attn_backward(const mmee_attn *x, const mmee_attn_grads *g)
     Launching l;
     if (l.rc) return l.rc;
     dispatch(p, [&](auto type, auto dp, auto mode) {
-        if constexpr (mode.value != MODE_TREE) backward_as<decltype(type), dp.value, mode.value>(p, l.stream);
+        if constexpr (mode.value != MODE_TREE) backward_as<decltype(type), dp.value, mode.value>(p, l);
     });
-    return launched("attention, backward");
+    return l.result("attention, backward");
 }
 
 int mmee_tree_attn_workspace(const mmee_tree_attn *x, uint64_t *bytes)

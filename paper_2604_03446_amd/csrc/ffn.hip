@@ -150,30 +150,30 @@ int plan_ffn(const mmee_ffn *x, bool pointers, FfnPlan &f)
 }
 
 template <class T, bool A_ACROSS, bool B_ACROSS, int EPI>
-void product(const Job &j, hipStream_t stream)
+void product(const Job &j, Launching &l)
 {
     if (!j.blocks) return;
-    if (j.big) hipLaunchKernelGGL((k_product<T, 256, 256, 2, 2, A_ACROSS, B_ACROSS, EPI>), dim3(j.blocks), dim3(256), 0, stream, j.p);
-    else hipLaunchKernelGGL((k_product<T, 128, 128, 2, 2, A_ACROSS, B_ACROSS, EPI>), dim3(j.blocks), dim3(256), 0, stream, j.p);
+    if (j.big) l.run(k_product<T, 256, 256, 2, 2, A_ACROSS, B_ACROSS, EPI>, j.blocks, 256, j.p);
+    else l.run(k_product<T, 128, 128, 2, 2, A_ACROSS, B_ACROSS, EPI>, j.blocks, 256, j.p);
 }
 
 template <class T>
-void sum_parts(const Job &j, hipStream_t stream)
+void sum_parts(const Job &j, Launching &l)
 {
     if (j.blocks && j.p.splits > 1)
-        hipLaunchKernelGGL((k_sum_parts<T>), dim3((uint32_t)(((uint64_t)j.p.problems * j.p.m * (j.p.n / 4) + 255) / 256)), dim3(256), 0, stream, j.p);
+        l.run(k_sum_parts<T>, ((uint64_t)j.p.problems * j.p.m * (j.p.n / 4) + 255) / 256, 256, j.p);
 }
 
 template <class T, bool GATED>
-void tokens(const Job &j, hipStream_t stream)
+void tokens(const Job &j, Launching &l)
 {
     auto with = [&](auto mt) {
         constexpr int MT = mt.value;
-        if (j.shared && j.columns == 64) hipLaunchKernelGGL((k_tokens_shared<T, MT, 2, 2, GATED>), dim3(j.blocks), dim3(512), 0, stream, j.p);
-        else if (j.shared) hipLaunchKernelGGL((k_tokens_shared<T, MT, 1, 2, GATED>), dim3(j.blocks), dim3(512), 0, stream, j.p);
-        else if (GATED && j.columns == 16) hipLaunchKernelGGL((k_tokens<T, GATED ? MT : 1, 1, GATED>), dim3(j.blocks), dim3(512), 0, stream, j.p);
-        else if (j.columns == 16) hipLaunchKernelGGL((k_tokens<T, 1, 1, GATED>), dim3(j.blocks), dim3(512), 0, stream, j.p);
-        else hipLaunchKernelGGL((k_tokens<T, 1, 2, GATED>), dim3(j.blocks), dim3(512), 0, stream, j.p);          // (up to 8 tokens)
+        if (j.shared && j.columns == 64) l.run(k_tokens_shared<T, MT, 2, 2, GATED>, j.blocks, 512, j.p);
+        else if (j.shared) l.run(k_tokens_shared<T, MT, 1, 2, GATED>, j.blocks, 512, j.p);
+        else if (GATED && j.columns == 16) l.run(k_tokens<T, GATED ? MT : 1, 1, GATED>, j.blocks, 512, j.p);
+        else if (j.columns == 16) l.run(k_tokens<T, 1, 1, GATED>, j.blocks, 512, j.p);
+        else l.run(k_tokens<T, 1, 2, GATED>, j.blocks, 512, j.p);          // (up to 8 tokens)
     };
     if (j.p.m <= 16) with(std::integral_constant<int, 1>());
     else if (j.p.m <= 32) with(std::integral_constant<int, 2>());
@@ -182,34 +182,34 @@ void tokens(const Job &j, hipStream_t stream)
 }
 
 template <class T>
-void forward_as(const FfnPlan &f, hipStream_t stream)
+void forward_as(const FfnPlan &f, Launching &l)
 {
     if (f.tokens) {
-        tokens<T, true>(f.hidden, stream);
-        tokens<T, false>(f.down, stream);
+        tokens<T, true>(f.hidden, l);
+        tokens<T, false>(f.down, l);
     } else {
-        product<T, false, false, EPI_GATED>(f.hidden, stream);
-        product<T, false, false, EPI_STORE>(f.down, stream);
+        product<T, false, false, EPI_GATED>(f.hidden, l);
+        product<T, false, false, EPI_STORE>(f.down, l);
     }
-    sum_parts<T>(f.down, stream);
+    sum_parts<T>(f.down, l);
 }
 
 template <class T>
-void backward_as(const FfnPlan &f, hipStream_t stream)
+void backward_as(const FfnPlan &f, Launching &l)
 {
     if constexpr (NARROW<T>) {
         if (f.bounds.rows) {
-            hipLaunchKernelGGL((k_grad_bounds<T>), dim3((uint32_t)f.bound_blocks()), dim3(256), 0, stream, f.bounds);
-            hipLaunchKernelGGL(k_grad_scale, dim3(1), dim3(1024), 0, stream, f.bounds);
+            l.run(k_grad_bounds<T>, f.bound_blocks(), 256, f.bounds);
+            l.run(k_grad_scale, 1, 1024, f.bounds);
         }
     }
-    product<T, false, true, EPI_DGATED>(f.d_hidden, stream);
-    product<T, false, true, EPI_STORE>(f.dx, stream);
-    sum_parts<T>(f.dx, stream);
-    product<T, true, true, EPI_STORE>(f.dw_gated, stream);
-    sum_parts<T>(f.dw_gated, stream);
-    product<T, true, true, EPI_STORE>(f.dw_down, stream);
-    sum_parts<T>(f.dw_down, stream);
+    product<T, false, true, EPI_DGATED>(f.d_hidden, l);
+    product<T, false, true, EPI_STORE>(f.dx, l);
+    sum_parts<T>(f.dx, l);
+    product<T, true, true, EPI_STORE>(f.dw_gated, l);
+    sum_parts<T>(f.dw_gated, l);
+    product<T, true, true, EPI_STORE>(f.dw_down, l);
+    sum_parts<T>(f.dw_down, l);
 }
 
 int64_t stride_of(int64_t given, uint64_t rows) { return rows > 1 ? given : 0; }
@@ -258,9 +258,9 @@ int mmee_ffn_forward(const mmee_ffn *x)
     d.parts = (float *)x->workspace;
     Launching l;
     if (l.rc) return l.rc;
-    if (x->dtype == MMEE_F16) forward_as<F16>(f, l.stream);
-    else forward_as<BF16>(f, l.stream);
-    return launched("gated feed-forward block, forward");
+    if (x->dtype == MMEE_F16) forward_as<F16>(f, l);
+    else forward_as<BF16>(f, l);
+    return l.result("gated feed-forward block, forward");
 }
 
 int mmee_ffn_backward(const mmee_ffn *x, const mmee_ffn_grads *g)
@@ -338,9 +338,9 @@ int mmee_ffn_backward(const mmee_ffn *x, const mmee_ffn_grads *g)
 
     Launching l;
     if (l.rc) return l.rc;
-    if (x->dtype == MMEE_F16) backward_as<F16>(f, l.stream);
-    else backward_as<BF16>(f, l.stream);
-    return launched("gated feed-forward block, backward");
+    if (x->dtype == MMEE_F16) backward_as<F16>(f, l);
+    else backward_as<BF16>(f, l);
+    return l.result("gated feed-forward block, backward");
 }
 
 }  // extern "C"

@@ -13,15 +13,23 @@ namespace mmee {
 // Holds the library's lock for one call that enqueues kernels on the library's stream.
 class Launching {
     std::unique_lock<std::mutex> held;
+    hipStream_t stream;
+    hipError_t error = hipSuccess;      // the first of this call's launches.  (hipGetLastError would report, and clear, what the program met before.)
 
 public:
     Launching();
-    hipStream_t stream;
-    int rc;                     // MMEE_OK, or MMEE_EDEVICE without a device
-};
+    int rc;                             // MMEE_OK, or MMEE_EDEVICE without a device
 
-// MMEE_OK after a successful launch; otherwise keeps the error's text for mmee_strerror.  Under the lock.
-int launched(const char *what);
+    template <class Args>
+    void run(void (*kernel)(Args), uint64_t blocks, uint32_t threads, Args args)
+    {
+        void *list[] = {&args};
+        const hipError_t e = hipLaunchKernel(reinterpret_cast<const void *>(kernel), dim3((uint32_t)blocks), dim3(threads), list, 0, stream);
+        if (error == hipSuccess) error = e;
+    }
+
+    int result(const char *what);       // MMEE_OK if every launch went well; otherwise keeps the error's text for mmee_strerror
+};
 
 // Blocks whose numbers agree modulo 8 run on one of the eight dies and share its L2: block `at` of n takes a number such that the
 // blocks of a die are neighbours.  A permutation of 0 .. n-1 for any n.

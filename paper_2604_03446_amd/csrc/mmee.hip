@@ -1567,11 +1567,11 @@ Launching::Launching() : held(g_lock), stream(S.stream), rc(MMEE_OK)
     rc = MMEE_EDEVICE;
 }
 
-int launched(const char *what)
+int Launching::result(const char *what)
 {
-    const hipError_t e = hipGetLastError();
-    if (e == hipSuccess) return MMEE_OK;
-    std::snprintf(g_last_error, sizeof(g_last_error), "%s: %s", what, hipGetErrorString(e));
+    if (error == hipSuccess) return MMEE_OK;
+    std::snprintf(g_last_error, sizeof(g_last_error), "%s: %s", what, hipGetErrorString(error));
+    (void)hipGetLastError();
     return MMEE_EDEVICE;
 }
 

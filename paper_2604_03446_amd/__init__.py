@@ -78,6 +78,9 @@ class _Call(C.Structure):
 
     def use_workspace(self, tensor):
         """Give the call a contiguous device buffer as its workspace."""
+        _on_device("use_workspace", "the workspace", tensor)
+        if not tensor.is_contiguous():
+            raise _invalid("use_workspace", "the workspace has to be contiguous")
         self.workspace, self.workspace_bytes = tensor.data_ptr(), tensor.numel() * tensor.element_size()
         self._workspace = tensor
         return self

@@ -18,3 +18,14 @@ def test_lengths_do_not_change_the_room(B, Lq, H, Hkv, d, Lk, backward):
         setattr(without, name, None)
     assert size == A.M.mmee_attn_workspace(without, backward)
     assert A.M._lib.mmee_attn_workspace(None, 0, C.byref(C.c_uint64())) == A.M.EINVAL
+
+
+def test_workspaces_that_are_refused():
+    """Host memory, which no kernel may be given, and a view whose elements do not lie one behind the other: it is longer than it says."""
+    from test_operator_arguments import block, refused, tree
+    on_host = Fake(1 << 20, dtype="torch.uint8")
+    on_host.is_cuda = False
+    for call in (cross, tree, block):
+        refused(lambda: call().use_workspace(on_host))
+        refused(lambda: call().use_workspace(Fake(1 << 10, 1 << 10, dtype="torch.uint8", stride=(1 << 12, 4))))
+        call().use_workspace(Fake(1 << 20, dtype="torch.uint8"))

@@ -446,6 +446,12 @@ def _whole(where, name, t, shape, kinds, contiguous=True):
     return t.data_ptr()
 
 
+def _scale(where, head_dim, given):
+    if head_dim == 0:
+        raise _invalid(where, "the head size is 0")
+    return head_dim ** -0.5 if given is None else given
+
+
 def _three(t):
     return _Strides(*t.stride()[:3])
 
@@ -466,7 +472,7 @@ def attn(q, k, v, o, lse=None, scale: float | None = None, kv_lens=None, key_mas
     mask = _whole(where, "key_mask", key_mask, (B, Lk), ("torch.uint8", "torch.bool"), contiguous=False)
     if mask and Lk > 1 and key_mask.stride()[1] != 1:
         raise _invalid(where, "key_mask: the last dimension has to be contiguous")
-    a = Attn(dtype, B, H, Hkv, d, Lq, Lk, d ** -0.5 if scale is None else scale, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
+    a = Attn(dtype, B, H, Hkv, d, Lq, Lk, _scale(where, d, scale), q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
              _three(q), _three(k), _three(v), _three(o), _whole(where, "lse", lse, (B, H, Lq), ("torch.float32",)),
              _whole(where, "kv_lens", kv_lens, (B,), ("torch.int32",)), mask, key_mask.stride()[0] if mask else 0)
     a._tensors = (q, k, v, o, lse, kv_lens, key_mask)
@@ -520,7 +526,7 @@ def tree_attn(q, k_pages, v_pages, page_table, cache_lens, ancestors, o, node_co
     table = _whole(where, "page_table", page_table, (B, width), ("torch.int32",), contiguous=False)
     if width > 1 and page_table.stride()[1] != 1:
         raise _invalid(where, "page_table: the last dimension has to be contiguous")
-    t = TreeAttn(dtype, B, H, Hkv, d, n, page, width, P, d ** -0.5 if scale is None else scale,
+    t = TreeAttn(dtype, B, H, Hkv, d, n, page, width, P, _scale(where, d, scale),
                  q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), o.data_ptr(), _three(q), _three(k_pages), _three(v_pages), _three(o),
                  table, page_table.stride()[0], _whole(where, "cache_lens", cache_lens, (B,), ("torch.int32",)),
                  _whole(where, "node_counts", node_counts, (B,), ("torch.int32",)),

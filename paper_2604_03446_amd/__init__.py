@@ -550,6 +550,8 @@ def ffn(x, w_gate, w_up, w_down, y, hidden, act: str = "silu", gate=None, up=Non
     """Arguments of mmee_ffn_forward and mmee_ffn_backward.  x [rows, in_dim], w_gate and w_up [hidden_dim, in_dim], w_down [out_dim,
     hidden_dim], y [rows, out_dim]; hidden, and gate and up (wanted for the backward call), [rows, hidden_dim] contiguous."""
     where = "ffn"
+    if hidden is None:
+        raise _invalid(where, "hidden is wanted")
     kept = {name: t for name, t in (("hidden", hidden), ("gate", gate), ("up", up)) if t is not None}
     dtype = _float_type(where, {"x": x, "w_gate": w_gate, "w_up": w_up, "w_down": w_down, "y": y, **kept})
     if act not in ACTS:

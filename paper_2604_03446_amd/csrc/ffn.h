@@ -39,8 +39,9 @@ __device__ __forceinline__ void activate(float g, float &value, float &slope)
         slope = e + g * 0.3989422804014327f * bell;
     } else if (KIND == ACT_GELU_TANH) {                 // (1 + tanh z) / 2 = sigmoid(2 z)
         const float e = sigmoid_of(1.5957691216057308f * (g + 0.044715f * g * g * g));
+        const float near = __builtin_amdgcn_fmed3f(g, -16.0f, 16.0f);          // beyond it e is 0 or 1, and the square of g may be beyond 32 bits
         value = g * e;
-        slope = e + g * e * (1.0f - e) * 1.5957691216057308f * (1.0f + 0.134145f * g * g);
+        slope = e + near * e * (1.0f - e) * 1.5957691216057308f * (1.0f + 0.134145f * near * near);
     } else if (KIND == ACT_RELU) {
         value = __builtin_elementwise_maximum(g, 0.0f);
         slope = g > 0.0f ? 1.0f : 0.0f;

@@ -1,5 +1,5 @@
 """Infinities and NaN in what a row does not see, and in what it sees: rows past the nodes, nodes that no row sees, the last key,
-padded columns, rows without keys."""
+padded columns, rows without keys; gates near the largest numbers."""
 import math
 
 import pytest
@@ -134,3 +134,23 @@ def test_rows_without_keys(M, B, Lq, H, Lk, Hkv, d, dtype):
     assert (t["lse"][1] == -math.inf).all()
     t = {n: x[:1] for n, x in t.items()}
     compare_cross(t, everything(1, Lq, Lk), "the others")
+
+
+@pytest.mark.parametrize("rows", [40, 200])
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh", "relu"])
+def test_large_gates(M, act, rows):
+    """Gates of up to 2^72, whose squares and cubes are beyond 32 bits: the activations are the identity or 0 there, with slopes of 1 and 0."""
+    import torch
+    from test_gpu_ffn import run as run_ffn
+    from test_gpu_ffn import tensors as block
+    t = block(rows, 64, 72, 40, torch.bfloat16, 53)
+    t["x"], t["w_up"], t["dy"] = t["x"] * 2.0 ** 70, t["w_up"] * 2.0 ** -70, t["dy"] * 2.0 ** -60
+    run_ffn(M, t, act)
+    x, wg, wu, wd, dy = (t[n].double().cpu() for n in ("x", "w_gate", "w_up", "w_down", "dy"))
+    g, up = x @ wg.t(), x @ wu.t()
+    dh, on = dy @ wd, (g > 0).double()
+    dg, du = dh * up * on, dh * g * on
+    want = {"y": (g * on * up) @ wd.t(), "dx": dg @ wg + du @ wu, "dw_gate": dg.t() @ x, "dw_up": du.t() @ x, "dw_down": dy.t() @ (g * on * up)}
+    assert all(value.abs().max() < 2.0 ** 127 for value in want.values())
+    for name, value in want.items():                    # (four roundings of at most u / 2 each, in the 2-norm)
+        assert (t[name].double().cpu() - value).norm() <= 1.5 * 2.0 ** -8 * value.norm(), name

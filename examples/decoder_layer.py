@@ -100,7 +100,7 @@ def main():
     batch_in = inputs(layer, cache, encoder)
     stream = torch.cuda.Stream()
     stream.wait_stream(torch.cuda.current_stream())
-    M.mmee_set_stream(stream.cuda_stream)               # once: a change of streams waits for the old one
+    M.mmee_set_stream(stream.cuda_stream)               # once for all calls
     with torch.cuda.stream(stream):
         y = layer.step(**batch_in)
         begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)

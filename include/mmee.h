@@ -392,7 +392,9 @@ int mmee_ffn_forward(const mmee_ffn *f);
 /* Reads hidden, gate and up as the forward call left them. */
 int mmee_ffn_backward(const mmee_ffn *f, const mmee_ffn_grads *g);
 
-/* Use this HIP stream (a hipStream_t passed as void*) for all later launches; NULL = default. */
+/* Use this HIP stream (a hipStream_t passed as void*) for all later launches; NULL = default.  Once a search, evaluation or front has
+ * run, the call first waits for the stream used so far, whose scratch later launches share; before that, in a program that runs the
+ * chains alone, it waits for nothing. */
 int mmee_set_stream(void *hip_stream);
 
 /* Free all cached device memory.  The library re-initialises itself on the next call. */

@@ -353,11 +353,12 @@ __device__ __forceinline__ uint64_t seen(const Keys<MODE_TREE> &keys, uint32_t f
 // between waves and no barrier is met while keys stream in.
 //
 // Many rows are bound by the compute unit: of a step's 2.1 us the matrix instructions need 0.85, the reads of operands from shared memory
-// 0.85 and the vector instructions 0.9, and they overlap in part.  2048 rows over 8192 keys, 32 heads of 128: 269 to 280 us, 1.0 PFLOP/s
-// (a library product of 16-bit matrices reaches 1.39); 2 x 2048 over 4096, 32 heads over 8: 290 us, 0.95.  With a mask of a byte a key, 8 x
-// 509 rows over 1500, 12 heads of 64: 45 us, 0.42 PFLOP/s: an exponential a score weighs twice as much as with 128 values a head.  Sixteen
-// trees of up to 63 nodes over contexts of 2048 to 4096 in pages of 16, 32 heads over 8: 93 us, where every block streams keys that no other
-// one reads: 2.4 TB/s and 0.56 PFLOP/s at once; 26 nodes over contexts up to 131072, 64 heads over 8: 305 us, 2.6 TB/s.
+// 0.85 and the vector instructions 0.9, and they overlap in part.  2048 rows over 8192 keys, 32 heads of 128: 257 to 280 us, 1.0 PFLOP/s
+// (a library product of 16-bit matrices reaches 1.39); 2 x 2048 over 4096, 32 heads over 8: 278 to 300 us, 0.95.  With a mask of a byte a key, 8 x
+// 509 rows over 1500, 12 heads of 64: 47 to 50 us, 0.4 PFLOP/s: an exponential a score weighs twice as much as with 128 values a head.  Sixteen
+// trees of up to 63 nodes over contexts of 2048 to 4096 in pages of 16, 32 heads over 8: 94 us, where every block streams keys that no other
+// one reads: 2.4 TB/s and 0.56 PFLOP/s at once; 26 nodes over contexts up to 131072, 64 heads over 8: 309 to 375 us, 2.1 to 2.6 TB/s.
+// With 128 values a head all 256 registers of a wave are in use: eight waves without a mask spill 3 or 4 more, four waves with a mask or a tree 12 to 14.
 // Few rows are bound by HBM: 64 tokens over 1024 to 2048 keys, 32 heads over 8: 82 us, 4.9 TB/s; one token over 512 keys, 12 heads: 6 us,
 // the latency of a launch, of the lengths, the keys and the join.
 template <class T, int DP, int WR, int WK, int MODE>
@@ -739,7 +740,8 @@ __device__ __forceinline__ float keep_in_range(f32x16 &ds, f32x16 (&sums)[N])
 // as far from 64-bit values as one rounding takes them, with many 1.4 times (2-norm, bfloat16: 0.0029, 0.0024 and 0.0017).
 // Nothing is added atomically, so results repeat to the bit; the price is that S and dP are formed here and again for dK and dV: seven
 // products where five would do.  Bound as the forward pass is, with two thirds of the exponentials a product: 2 x 2048 rows over 4096 keys, 32 heads of 128
-// over 8: 380 to 390 us, 1.07 PFLOP/s; masked, 8 x 509 over 1500, 12 heads of 64: 57 us.
+// over 8: 376 to 392 us, 1.07 PFLOP/s; masked, 8 x 509 over 1500, 12 heads of 64: 57 to 60 us.  Four waves with a mask over 128 values a head in
+// float16 spill 2 registers, the others none.
 template <class T, int DP, int W, int MODE>
 __global__ __launch_bounds__(64 * W, 2) void k_attn_dq(const AttnArgs a)
 {
@@ -837,11 +839,13 @@ __global__ __launch_bounds__(64 * W, 2) void k_attn_dq(const AttnArgs a)
 // (rows along m, a lane holds one key), dV^T += dO^T P, dK^T += Q^T dS; the rows' Q and dO are read from shared memory both along and across.
 // With 128 values a head the 256 registers of a wave hold K and both sums; V's operands lie in shared memory (their reads are what
 // limits it most), with 32 rows a step: 64 spilled 67 registers and took 900 us.  2 x 2048 rows over 4096 keys, 32 heads of 128 over 8: 510 to
-// 540 us, 1.05 PFLOP/s; masked, 8 x 509 over 1500, 12 heads of 64: 65 us.
+// 540 us, 1.05 PFLOP/s; masked, 8 x 509 over 1500, 12 heads of 64: 65 to 69 us.  With four waves 10 registers are spilled in bfloat16 and 18 in
+// float16 (some of them read again in the loop), with eight none and 8.
 template <class T, int DP, int W, int MODE>
 __global__ __launch_bounds__(64 * W, 2) void k_attn_dkv(const AttnArgs a)
 {
-    constexpr int TR = DP == 128 ? 32 : 64, CH = DP / 8, LOADS = TR * CH / (64 * W) ? TR * CH / (64 * W) : 1, ROWS = 64 * W / CH;
+    constexpr int TR = DP == 128 ? 32 : 64, CH = DP / 8, LOADS = TR * CH / (64 * W), ROWS = 64 * W / CH;
+    static_assert(LOADS * 64 * W == TR * CH && 2 * TR <= 64 * W, "a tile is dealt out evenly, its statistics to two threads a row");
     __shared__ u32x4 tiles[2][2][TR * CH];
     __shared__ f32x4 stats[2][2][TR / 4];               // lse in powers of two, D
     constexpr bool AWAY = DP == 128;                    // V's operands in shared memory: with them 256 registers do not suffice
@@ -872,7 +876,7 @@ __global__ __launch_bounds__(64 * W, 2) void k_attn_dkv(const AttnArgs a)
     // Rows past the last one and columns past the head's repeat existing ones: probabilities are 0 there, K and V are.
     u32x4 rq[LOADS], ro[LOADS];
     float stat = 0.0f;
-    const int row0 = thread / CH % TR, c = 8 * (thread % CH) < (int)a.head_dim ? thread % CH : 0;
+    const int row0 = thread / CH, c = 8 * (thread % CH) < (int)a.head_dim ? thread % CH : 0;
     auto load = [&](uint32_t s) {
         const uint32_t first = (step0 + s) * TR;
 #pragma unroll
@@ -897,7 +901,7 @@ __global__ __launch_bounds__(64 * W, 2) void k_attn_dkv(const AttnArgs a)
     for (uint32_t s = 0; s < count; ++s) {
         u32x4 *qt = tiles[s & 1][0], *ot = tiles[s & 1][1];
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) {               // (with 32 values a head two threads store the same)
+        for (int i = 0; i < LOADS; ++i) {
             qt[chunk_at<CH>(row0 + i * ROWS, thread % CH)] = rq[i];
             ot[chunk_at<CH>(row0 + i * ROWS, thread % CH)] = ro[i];
         }

@@ -91,7 +91,7 @@ struct ProductArgs {
 constexpr int BK = 64;
 
 // One thread's share of an operand's tile of ROWS x 64, by THREADS threads: registers in flight, then shared memory.  What does not
-// exist is asked for beyond the buffer's end and comes back as zeros, without a branch in the products' loop.
+// exist is asked for beyond the buffer's end and comes back as zeros, without a branch of its own.
 template <int ROWS, int THREADS, bool ACROSS>
 struct OperandStage {
     static constexpr int CH = ACROSS ? ROWS / 8 : BK / 8, LINES = ACROSS ? BK : ROWS, LOADS = LINES * CH / THREADS, PER = THREADS / CH;
@@ -149,8 +149,11 @@ __device__ __forceinline__ typename T::V8 operand(const u32x4 *tile, int first, 
 // when it begins.  A wave of a 256 x 256 tile holds 128 x 128 results in 256 registers, for which it reads half as much from shared memory a
 // product as with 64 x 64; it is then alone on its unit's quarter.
 // Bound by the matrix instructions, at the clock that the card holds under them (1.8 to 2.1 GHz of 2.4).  4001 tokens, 2048 -> 8192 -> 2048, bfloat16,
-// all six products: gate and up with their epilogue (h, g and u, 197 MB, leave at its end) 305 to 325 us, 0.85 PFLOP/s; y 140, 0.96; dg and du
-// (g and u read, two results) 205 to 215, 0.64; dx 228 and its pieces 14, 1.11; dWg and dWu together 230, 1.16; dWd 117, 1.15.
+// all six products: gate and up with their epilogue (h, g and u, 197 MB, leave at its end) 306 to 331 us, 0.85 PFLOP/s; y 141 to 146, 0.95; dg and du
+// (g and u read, two results) 204 to 217, 0.64; dx 231 to 241 and its pieces 14, 1.1; dWg and dWu together 232 to 246, 1.1; dWd 117 to 122, 1.1.
+// The instances with an epilogue (gate and up, dg and du) keep the choice of A in vector registers, so that each load of A is a loop over the
+// lanes that cuts the quarter's instructions into pieces which nothing orders: with a scalar choice a training step of that size took 1138 us
+// instead of 1216, the forward pass of 2048 tokens through 768 -> 3072 -> 768 52 instead of 57.
 template <class T, int TM, int TN, int WM, int WN, bool A_ACROSS, bool B_ACROSS, int EPI>
 __global__ __launch_bounds__(64 * WM * WN, TM == 256 ? 1 : 2) void k_product(const ProductArgs p)
 {
@@ -611,10 +614,11 @@ __global__ __launch_bounds__(512, 2) void k_tokens(const ProductArgs p)
     }
 }
 
-// As k_tokens, for more than 16 tokens, whose operands would be read as often as the weights': WR waves with 16 NT rows each share a
+// As k_tokens, for more than 8 tokens, whose operands would be read as often as the weights': WR waves with 16 NT rows each share a
 // chunk of 64 values of k of all tokens in shared memory, 8 / WR such groups take every (8 / WR)-th chunk.  Weights are asked for two chunks ahead,
 // straight into operands; the tokens' next chunk is on its way meanwhile.  Bound by HBM: 37 tokens, 4096 -> 12288 -> 4096: 45 us for 201 MB, 4.5 TB/s
-// (a copy reaches 4.7), and 25 for 101 MB with its pieces, 4.0.
+// (a copy reaches 4.7), and 25 for 101 MB with its pieces, 4.0.  The wave's number is in vector registers here, and with it the buffers that loads
+// name: each load is a loop over the lanes (both products took 71 us with it in a scalar one, 75 as it is).
 template <class T, int MT, int NT, int WR, bool GATED>
 __global__ __launch_bounds__(512, 2) void k_tokens_shared(const ProductArgs p)
 {

@@ -49,10 +49,10 @@ HBM_PEAK_GBS = 8000.0
 # HBM bytes per launch from rocprofv3 --pmc FETCH_SIZE / WRITE_SIZE (summaries under profiles/), scaled by
 # what the same counters read for a 1 GiB device-to-device copy (x2.0 and x1.0).  Valid only for the kernel
 # sources they were taken with: any change to the sources turns "traffic" into null.
-COUNTERS_TAKEN_WITH = "fbe43663f79a63a434c2da2d9d90d8e73814079b326dec3a25c16aa8659ca006"
+COUNTERS_TAKEN_WITH = "eb92d95443cff0fefc322b7ba5e2df2486bfc7eeefda0da2773f77bed9146a44"
 TRAFFIC = {"k_search_dense_long": (2 * 265.0 + 161.0) * 1024.0,      # FETCH_SIZE x 2.0 + WRITE_SIZE x 1.0, KiB per dispatch
-           "k_search_dense_bert": (2 * 258.0 + 196.0) * 1024.0,
-           "k_eval_batch": (2 * 19961.0 + 4195078.0) * 1024.0}
+           "k_search_dense_bert": (2 * 257.0 + 196.0) * 1024.0,
+           "k_eval_batch": (2 * 19966.0 + 4195099.0) * 1024.0}
 TRAFFIC_SOURCE = {"k_search_dense_long": "profiles/k_search_dense_long.md", "k_search_dense_bert": "profiles/k_search_dense_bert.md",
                   "k_eval_batch": "profiles/k_eval_batch_bert.md"}
 

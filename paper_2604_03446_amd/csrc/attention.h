@@ -873,7 +873,8 @@ __global__ __launch_bounds__(64 * W, 2) void k_attn_dkv(const AttnArgs a)
     }
     const int64_t bh = (int64_t)b * a.kv_heads + kvh;
 
-    // Rows past the last one and columns past the head's repeat existing ones: probabilities are 0 there, K and V are.
+    // Rows past the last one repeat its Q, and their dO is zeros, as their probabilities do not clear an infinite gradient.  Columns past the
+    // head's repeat the first ones: K and V are 0 there.
     u32x4 rq[LOADS], ro[LOADS];
     float stat = 0.0f;
     const int row0 = thread / CH, c = 8 * (thread % CH) < (int)a.head_dim ? thread % CH : 0;
@@ -883,7 +884,8 @@ __global__ __launch_bounds__(64 * W, 2) void k_attn_dkv(const AttnArgs a)
         for (int i = 0; i < LOADS; ++i) {
             const uint32_t row = first + row0 + i * ROWS, token = token_of(a, row < a.rows ? row : a.rows - 1), head = kvh * a.group + ((row < a.rows ? row : a.rows - 1) - token * a.group);
             rq[i] = *reinterpret_cast<const u32x4 *>(a.q + (b * a.qs.batch + token * a.qs.token + head * a.qs.head + c * 8));
-            ro[i] = *reinterpret_cast<const u32x4 *>(a.d_o + (b * a.dos.batch + token * a.dos.token + head * a.dos.head + c * 8));
+            ro[i] = zeros();
+            if (row < a.rows) ro[i] = *reinterpret_cast<const u32x4 *>(a.d_o + (b * a.dos.batch + token * a.dos.token + head * a.dos.head + c * 8));
         }
         const uint32_t row = first + thread % TR;
         const bool there = row < a.rows;

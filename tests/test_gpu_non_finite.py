@@ -154,3 +154,18 @@ def test_large_gates(M, act, rows):
     assert all(value.abs().max() < 2.0 ** 127 for value in want.values())
     for name, value in want.items():                    # (four roundings of at most u / 2 each, in the 2-norm)
         assert (t[name].double().cpu() - value).norm() <= 1.5 * 2.0 ** -8 * value.norm(), name
+
+
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
+@pytest.mark.parametrize("Lq,H,Hkv,Lk,d", [(5, 2, 2, 70, 64), (33, 3, 1, 100, 128), (700, 24, 24, 300, 128), (65, 2, 2, 2000, 32), (1100, 40, 40, 270, 64)])
+def test_infinite_gradient_of_the_last_row(M, Lq, H, Hkv, Lk, d, dtype):
+    """It comes out as it is in the values' gradients, in its own column: dV = P^T dO."""
+    import torch
+    from attention_oracle import attention, check
+    t = tensors((1, Lq, H, d), (1, Lk, Hkv, d), getattr(torch, dtype), 61)
+    t["q"] /= 4
+    t["do"][:, -1, -1, 5] = math.inf
+    run_cross(M, t)
+    want = attention(t["q"], t["k"], t["v"], everything(1, Lq, Lk), d ** -0.5, t["q"].dtype, t["do"])
+    assert torch.isinf(want["dv"][0]).any()
+    check(t["dv"], want["dv"], (Lq, d))

@@ -73,6 +73,20 @@ def test_nodes_that_no_row_sees(M, n, H, Hkv, d, lens, counted, dtype):
     compare(t, keeps(t, counts), (n, counts))
 
 
+@pytest.mark.parametrize("n,used,H,Hkv,lens", [(700, 30, 2, 2, [100, 70]), (1024, 1, 2, 1, [64, 5]), (600, 599, 1, 1, [0, 33]), (64, 20, 32, 8, [500, 129])])
+def test_room_that_is_not_used(M, n, used, H, Hkv, lens):
+    """Rows and nodes past those used are left empty by their bits alone, without a count; their cache slots hold anything."""
+    import torch
+    sees = random_tree(2, n, 5)
+    sees[:, used:], sees[:, :, used:] = False, False
+    t = build(2, n, H, Hkv, 64, 16, lens, torch.bfloat16, seed=n, sees=sees)
+    for b in range(2):
+        for j in range(used, n):
+            put(t, b, lens[b] + j, 16, k=math.nan, v=math.nan if j % 2 else math.inf)
+    run(M, t)
+    compare(t, keeps(t), (n, used))
+
+
 @pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
 @pytest.mark.parametrize("B,Lq,H,Lk,Hkv,d", [(1, 1, 4, 33, 2, 64), (2, 1, 4, 5001, 1, 128), (2, 50, 1, 95, 1, 40), (2, 130, 3, 65, 3, 32), (1, 700, 2, 1601, 1, 128), (1, 270, 70, 200, 70, 64)])
 @pytest.mark.parametrize("masking", ["none", "lens"])

@@ -337,6 +337,7 @@ int mmee_attn_backward(const mmee_attn *a, const mmee_attn_grads *g);
  * sees itself), j < node_counts[b].  ancestors is [batch][nodes][(nodes + 63) / 64] contiguous.  Rows i >= node_counts[b] give zeros, and lse -inf.
  * Lengths and counts are clamped to what there is room for; positions in a page outside 0 .. n_pages-1 are not read and count as masked, like those
  * past the last node and nodes that no row i < node_counts[b] sees.  The values of a node that some row sees must be finite also for the rows that do not see it.
+ * Room that a batch leaves unused is best left out by node_counts: nodes that only their empty bits leave out are looked for among the rows.
  * nodes at most 1024. */
 typedef struct mmee_tree_attn {
     uint32_t dtype;

@@ -366,7 +366,7 @@ __device__ __forceinline__ uint64_t seen(const Keys<MODE_TREE> &keys, uint32_t f
 // 509 rows over 1500, 12 heads of 64: 47 to 50 us, 0.4 PFLOP/s: an exponential a score weighs twice as much as with 128 values a head.  Sixteen
 // trees of up to 63 nodes over contexts of 2048 to 4096 in pages of 16, 32 heads over 8: 94 us, where every block streams keys that no other
 // one reads: 2.4 TB/s and 0.56 PFLOP/s at once; 26 nodes over contexts up to 131072, 64 heads over 8: 309 to 375 us, 2.1 to 2.6 TB/s.
-// With 128 values a head all 256 registers of a wave are in use: eight waves without a mask spill 3 or 4 more, four waves with a mask or a tree 12 to 14.
+// With 128 values a head all 256 registers of a wave are in use: eight waves without a mask spill 3 or 4 more, four waves with a mask or a tree 10 to 14.
 // Few rows are bound by HBM: 64 tokens over 1024 to 2048 keys, 32 heads over 8: 82 us, 4.9 TB/s; one token over 512 keys, 12 heads: 6 us,
 // the latency of a launch, of the lengths, the keys and the join.
 template <class T, int DP, int WR, int WK, int MODE>

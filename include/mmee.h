@@ -393,6 +393,81 @@ int mmee_ffn_forward(const mmee_ffn *f);
 /* Reads hidden, gate and up as the forward call left them. */
 int mmee_ffn_backward(const mmee_ffn *f, const mmee_ffn_grads *g);
 
+/* Norm of queries and keys per head and their rotation by position, in one pass over both: tokens rows, q [tokens][heads][head_dim], k
+ * [tokens][kv_heads][head_dim], outputs likewise; strides of the first two dimensions.  With weights (both or none)
+ *   z = x weight / sqrt(mean of the head's x^2 + eps),     without: z = x
+ * and the first rot_dim values of a head turn in pairs by angle[i] = position * freqs[i]:
+ *   (y_a, y_b) = (z_a cos - z_b sin, z_a sin + z_b cos)    (a, b) = (i, i + rot_dim / 2), or (2 i, 2 i + 1) with MMEE_PAIRS_NEIGHBOURS
+ * the rest of the head is z.  freqs are radians a position in 64 bits, and so are the angles, whatever the position.  Positions may have several
+ * axes (time, height, width): pair i turns by the position along axis axis_of[i] (clamped to axes - 1; null: all along the first).  head_dim: a
+ * multiple of 8 up to 256; rot_dim: a multiple of 16 up to head_dim, 0: no rotation (freqs and positions may then be null).  eps at least 1e-30.
+ * An output may be its input's own buffer with the same strides, not one that overlaps it otherwise. */
+enum { MMEE_PAIRS_HALVES = 0, MMEE_PAIRS_NEIGHBOURS = 1 };
+
+typedef struct mmee_qk_rotate {
+    uint32_t dtype, pairs;
+    uint32_t tokens, heads, kv_heads, head_dim, rot_dim;
+    uint32_t axes;                  /* 1 to 4 */
+    float eps;
+    const void *q, *k;
+    void *q_out, *k_out;
+    int64_t q_stride[2], k_stride[2], q_out_stride[2], k_out_stride[2];     /* token, head */
+    const void *q_weight, *k_weight;                                        /* [head_dim], of the tensors' type, or null */
+    const double *freqs;            /* [rot_dim / 2] */
+    const int32_t *positions;       /* [axes][tokens] */
+    int64_t axis_stride;            /* positions from one axis to the next */
+    const uint8_t *axis_of;         /* [rot_dim / 2] or null */
+    void *workspace;                /* of the backward call */
+    uint64_t workspace_bytes;
+    uint64_t reserved;              /* must be 0 */
+} mmee_qk_rotate;
+
+/* Gradients: dq_out and dk_out of the outputs, dq and dk as q and k, the weights' as the weights (null without weights).  dq may be dq_out's own
+ * buffer, dk dk_out's, with the same strides. */
+typedef struct mmee_qk_rotate_grads {
+    const void *dq_out, *dk_out;
+    void *dq, *dk, *dq_weight, *dk_weight;
+    int64_t dq_out_stride[2], dk_out_stride[2], dq_stride[2], dk_stride[2];
+} mmee_qk_rotate_grads;
+
+/* Of the backward call; the forward call needs none. */
+int mmee_qk_rotate_workspace(const mmee_qk_rotate *r, uint64_t *bytes);
+int mmee_qk_rotate_forward(const mmee_qk_rotate *r);
+/* Reads q and k as the forward call did, not its outputs. */
+int mmee_qk_rotate_backward(const mmee_qk_rotate *r, const mmee_qk_rotate_grads *g);
+
+/* Appends keys and values to a paged cache (pages, table and lengths as of mmee_tree_attn), the keys normed and rotated on the way as by
+ * mmee_qk_rotate, the values as they are, and norms and rotates the queries beside them (q null: none; heads is then 0).  The new tokens of
+ * `seqs` sequences lie one behind the other: sequence b's are starts[b] .. starts[b + 1] - 1, or, with starts null, tokens / seqs of each (without a
+ * remainder).  Its j-th goes to position cache_lens[b] + j, which is also what it is rotated by unless positions are given.  Tokens
+ * j >= counts[b] (when given) and tokens of no sequence leave everything as it was.  Positions past the page table and pages outside 0 .. n_pages-1 are
+ * not written; the token's query is.  cache_lens stay as they are (clamped to 0 where they are below).  starts ascend and lie within 0 .. tokens.  Two new tokens at one place of the pool
+ * (sequences that share the page they write to) leave either's key and value there. */
+typedef struct mmee_cache_append {
+    uint32_t dtype, pairs;
+    uint32_t tokens, seqs, heads, kv_heads, head_dim, rot_dim;
+    uint32_t axes;
+    uint32_t page_tokens, pages_per_seq, n_pages;
+    float eps;
+    const void *q, *k, *v;
+    void *q_out, *k_pages, *v_pages;
+    int64_t q_stride[2], k_stride[2], v_stride[2], q_out_stride[2];         /* token, head */
+    int64_t k_pages_stride[3], v_pages_stride[3];                           /* page, token, head */
+    const void *q_weight, *k_weight;
+    const double *freqs;
+    const int32_t *positions;       /* [axes][tokens], or null: positions in the cache (axes 1) */
+    int64_t axis_stride;
+    const uint8_t *axis_of;
+    const int32_t *starts;          /* [seqs + 1] or null */
+    const int32_t *counts;          /* [seqs] or null */
+    const int32_t *cache_lens;      /* [seqs] */
+    const int32_t *page_table;      /* [seqs][pages_per_seq] */
+    int64_t table_stride;
+    uint64_t reserved;              /* must be 0 */
+} mmee_cache_append;
+
+int mmee_cache_append_forward(const mmee_cache_append *c);
+
 /* Use this HIP stream (a hipStream_t passed as void*) for all later launches; NULL = default.  Once a search, evaluation or front has
  * run, the call first waits for the stream used so far, whose scratch later launches share; before that, in a program that runs the
  * chains alone, it waits for nothing. */

@@ -21,6 +21,7 @@ OBJ_ENERGY, OBJ_LATENCY, OBJ_LATENCY_THEN_ENERGY, OBJ_EDP = 0, 1, 2, 3
 SEARCH_PRUNED, SEARCH_EXHAUSTIVE, SEARCH_ORDERED_SUM = 0, 1, 2
 OK, EINVAL, ERANGE, ENOFEASIBLE, EDEVICE, EOVERFLOW, ETOOBIG, EWORKSPACE = 0, -1, -2, -3, -4, -5, -6, -7
 F16, BF16 = 0, 1
+PAIRS = {"halves": 0, "neighbours": 1}
 ACTS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3, "sigmoid": 4}
 
 
@@ -127,6 +128,34 @@ class FfnGrads(_Call):
                 ("dy_stride", C.c_int64), ("dx_stride", C.c_int64)]
 
 
+_Two = C.c_int64 * 2
+
+
+class QkRotate(_Call):
+    _fields_ = [("dtype", C.c_uint32), ("pairs", C.c_uint32), ("tokens", C.c_uint32), ("heads", C.c_uint32), ("kv_heads", C.c_uint32),
+                ("head_dim", C.c_uint32), ("rot_dim", C.c_uint32), ("axes", C.c_uint32), ("eps", C.c_float),
+                ("q", C.c_void_p), ("k", C.c_void_p), ("q_out", C.c_void_p), ("k_out", C.c_void_p),
+                ("q_stride", _Two), ("k_stride", _Two), ("q_out_stride", _Two), ("k_out_stride", _Two),
+                ("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("freqs", C.c_void_p), ("positions", C.c_void_p), ("axis_stride", C.c_int64),
+                ("axis_of", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64), ("reserved", C.c_uint64)]
+
+
+class QkRotateGrads(_Call):
+    _fields_ = [("dq_out", C.c_void_p), ("dk_out", C.c_void_p), ("dq", C.c_void_p), ("dk", C.c_void_p), ("dq_weight", C.c_void_p),
+                ("dk_weight", C.c_void_p), ("dq_out_stride", _Two), ("dk_out_stride", _Two), ("dq_stride", _Two), ("dk_stride", _Two)]
+
+
+class CacheAppend(_Call):
+    _fields_ = [("dtype", C.c_uint32), ("pairs", C.c_uint32), ("tokens", C.c_uint32), ("seqs", C.c_uint32), ("heads", C.c_uint32),
+                ("kv_heads", C.c_uint32), ("head_dim", C.c_uint32), ("rot_dim", C.c_uint32), ("axes", C.c_uint32), ("page_tokens", C.c_uint32),
+                ("pages_per_seq", C.c_uint32), ("n_pages", C.c_uint32), ("eps", C.c_float),
+                ("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("q_out", C.c_void_p), ("k_pages", C.c_void_p), ("v_pages", C.c_void_p),
+                ("q_stride", _Two), ("k_stride", _Two), ("v_stride", _Two), ("q_out_stride", _Two), ("k_pages_stride", _Strides),
+                ("v_pages_stride", _Strides), ("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("freqs", C.c_void_p), ("positions", C.c_void_p),
+                ("axis_stride", C.c_int64), ("axis_of", C.c_void_p), ("starts", C.c_void_p), ("counts", C.c_void_p), ("cache_lens", C.c_void_p),
+                ("page_table", C.c_void_p), ("table_stride", C.c_int64), ("reserved", C.c_uint64)]
+
+
 COST_DTYPE = np.dtype([("bs_words", "<u8"), ("da_words", "<u8"), ("br_words", "<u8"),
                        ("mac_total", "<u8"), ("comp_cycles", "<u8"),
                        ("energy_pj", "<f8"), ("latency_cycles", "<f8"),
@@ -172,6 +201,10 @@ def _load() -> C.CDLL:
     L.mmee_ffn_workspace.argtypes = [P(Ffn), C.c_int, P(C.c_uint64)]
     L.mmee_ffn_forward.argtypes = [P(Ffn)]
     L.mmee_ffn_backward.argtypes = [P(Ffn), P(FfnGrads)]
+    L.mmee_qk_rotate_workspace.argtypes = [P(QkRotate), P(C.c_uint64)]
+    L.mmee_qk_rotate_forward.argtypes = [P(QkRotate)]
+    L.mmee_qk_rotate_backward.argtypes = [P(QkRotate), P(QkRotateGrads)]
+    L.mmee_cache_append_forward.argtypes = [P(CacheAppend)]
     L.mmee_set_stream.argtypes = [C.c_void_p]
     L.mmee_shutdown.argtypes = []
     L.mmee_shutdown.restype = None
@@ -183,7 +216,8 @@ def _load() -> C.CDLL:
                  "mmee_chain_search_multi", "mmee_chain_search_many", "mmee_pareto", "mmee_chain_pareto",
                  "mmee_front_bs_da", "mmee_chain_front_bs_da",
                  "mmee_attn_workspace", "mmee_attn_forward", "mmee_attn_backward", "mmee_tree_attn_workspace", "mmee_tree_attn_forward",
-                 "mmee_ffn_workspace", "mmee_ffn_forward", "mmee_ffn_backward"):
+                 "mmee_ffn_workspace", "mmee_ffn_forward", "mmee_ffn_backward",
+                 "mmee_qk_rotate_workspace", "mmee_qk_rotate_forward", "mmee_qk_rotate_backward", "mmee_cache_append_forward"):
         getattr(L, name).restype = C.c_int
     return L
 
@@ -604,6 +638,148 @@ def mmee_ffn_backward(f: Ffn, g: FfnGrads) -> None:
         if t.dtype != like.dtype:
             raise _invalid("mmee_ffn_backward", f"{name} is {t.dtype}, {like.dtype} is wanted")
     _check(_lib.mmee_ffn_backward(C.byref(f), C.byref(g)), "mmee_ffn_backward")
+
+
+def _two(t):
+    return _Two(*t.stride()[:2])
+
+
+def _rotation(where, tokens, head_dim, freqs, positions, axis_of, pairs):
+    """rot_dim, axes, and freqs, positions, axis stride and axis_of as pointers, of a rotation (none without freqs)."""
+    if pairs not in PAIRS:
+        raise _invalid(where, f"pairs is one of {', '.join(PAIRS)}")
+    if freqs is None:
+        if positions is not None or axis_of is not None:
+            raise _invalid(where, "positions without freqs")
+        return 0, 1, None, None, 0, None
+    if len(freqs.shape) != 1 or 2 * freqs.shape[0] > head_dim:
+        raise _invalid(where, f"freqs has shape {tuple(freqs.shape)}, (rot_dim / 2,) is wanted")
+    rot = 2 * freqs.shape[0]
+    axes, stride = 1, 0
+    if positions is not None:
+        if len(positions.shape) == 2:
+            axes, stride = positions.shape[0], positions.stride()[0]
+        _whole(where, "positions", positions, (axes, tokens) if len(positions.shape) == 2 else (tokens,), ("torch.int32",), contiguous=False)
+        if tokens > 1 and positions.stride()[-1] != 1:
+            raise _invalid(where, "positions: the last dimension has to be contiguous")
+    return (rot, axes, _whole(where, "freqs", freqs, (rot // 2,), ("torch.float64",)), None if positions is None else positions.data_ptr(), stride,
+            _whole(where, "axis_of", axis_of, (rot // 2,), ("torch.uint8",)))
+
+
+def _norm_weights(where, head_dim, given):
+    """Norm weights by name -> pointers, of the tensors' type (which _float_type has seen to)."""
+    for name, t in given.items():
+        if t is not None:
+            _shaped(where, name, t, head_dim)
+    return [None if t is None else t.data_ptr() for t in given.values()]
+
+
+def qk_rotate(q, k, q_out, k_out, freqs, positions, axis_of=None, q_weight=None, k_weight=None, eps: float = 1e-6, pairs: str = "halves") -> QkRotate:
+    """Arguments of mmee_qk_rotate_forward and mmee_qk_rotate_backward.  q, q_out [tokens, heads, head_dim]; k, k_out [tokens, kv_heads,
+    head_dim], any strides but of the last dimension; freqs float64 [rot_dim / 2] in radians a position, or None: no rotation; positions int32
+    [tokens] or [axes, tokens], with axis_of uint8 [rot_dim / 2]; q_weight, k_weight [head_dim]: the norms' weights, or None: no norms."""
+    where = "qk_rotate"
+    kept = {name: t for name, t in (("q_weight", q_weight), ("k_weight", k_weight)) if t is not None}
+    dtype = _float_type(where, {"q": q, "k": k, "q_out": q_out, "k_out": k_out, **kept})
+    if len(q.shape) != 3 or len(k.shape) != 3:
+        raise _invalid(where, "q and k have three dimensions")
+    T, H, d = q.shape
+    Hkv = k.shape[1]
+    _shaped(where, "k", k, T, Hkv, d)
+    _shaped(where, "q_out", q_out, T, H, d)
+    _shaped(where, "k_out", k_out, T, Hkv, d)
+    if (q_weight is None) != (k_weight is None):
+        raise _invalid(where, "q_weight and k_weight come together")
+    if freqs is not None and positions is None:
+        raise _invalid(where, "positions are wanted")
+    rot, axes, freq_at, positions_at, axis_stride, axis_at = _rotation(where, T, d, freqs, positions, axis_of, pairs)
+    r = QkRotate(dtype, PAIRS[pairs], T, H, Hkv, d, rot, axes, eps, q.data_ptr(), k.data_ptr(), q_out.data_ptr(), k_out.data_ptr(), _two(q), _two(k), _two(q_out),
+                 _two(k_out), *_norm_weights(where, d, {"q_weight": q_weight, "k_weight": k_weight}), freq_at, positions_at, axis_stride, axis_at)
+    r._tensors = (q, k, q_weight, k_weight, q_out, k_out, freqs, positions, axis_of)
+    return r
+
+
+def qk_rotate_grads(dq_out, dk_out, dq, dk, dq_weight=None, dk_weight=None) -> QkRotateGrads:
+    """Output gradients and gradients of mmee_qk_rotate_backward, shaped as q_out, k_out, q, k and the weights."""
+    where = "qk_rotate_grads"
+    kept = {name: t for name, t in (("dq_weight", dq_weight), ("dk_weight", dk_weight)) if t is not None}
+    _float_type(where, {"dq_out": dq_out, "dk_out": dk_out, "dq": dq, "dk": dk, **kept})
+    if len(dq_out.shape) != 3 or len(dk_out.shape) != 3:
+        raise _invalid(where, "dq_out and dk_out have three dimensions")
+    _shaped(where, "dq", dq, *dq_out.shape)
+    _shaped(where, "dk", dk, *dk_out.shape)
+    g = QkRotateGrads(dq_out.data_ptr(), dk_out.data_ptr(), dq.data_ptr(), dk.data_ptr(),
+                      *_norm_weights(where, dq_out.shape[2], {"dq_weight": dq_weight, "dk_weight": dk_weight}), _two(dq_out), _two(dk_out), _two(dq), _two(dk))
+    g._tensors = (dq_out, dk_out, dq, dk, dq_weight, dk_weight)
+    return g
+
+
+def mmee_qk_rotate_workspace(r: QkRotate) -> int:
+    out = C.c_uint64()
+    _check(_lib.mmee_qk_rotate_workspace(C.byref(r), C.byref(out)), "mmee_qk_rotate_workspace")
+    return out.value
+
+
+def mmee_qk_rotate_forward(r: QkRotate) -> None:
+    _check(_lib.mmee_qk_rotate_forward(C.byref(r)), "mmee_qk_rotate_forward")
+
+
+def mmee_qk_rotate_backward(r: QkRotate, g: QkRotateGrads) -> None:
+    where = "mmee_qk_rotate_backward"
+    for name, t, like in zip(("dq", "dk", "dq_weight", "dk_weight"), g._tensors[2:], r._tensors):
+        if (t is None) != (like is None):
+            raise _invalid(where, f"{name} is {'wanted' if t is None else 'not wanted'}")
+        if t is not None:
+            _shaped(where, name, t, *like.shape)
+            if t.dtype != like.dtype:
+                raise _invalid(where, f"{name} is {t.dtype}, {like.dtype} is wanted")
+    _check(_lib.mmee_qk_rotate_backward(C.byref(r), C.byref(g)), where)
+
+
+def cache_append(k, v, k_pages, v_pages, page_table, cache_lens, starts=None, counts=None, q=None, q_out=None, freqs=None, positions=None, axis_of=None,
+                 q_weight=None, k_weight=None, eps: float = 1e-6, pairs: str = "halves") -> CacheAppend:
+    """Arguments of mmee_cache_append_forward.  k, v [tokens, kv_heads, head_dim]; k_pages, v_pages [n_pages, page_tokens, kv_heads, head_dim];
+    page_table int32 [seqs, pages_per_seq]; cache_lens, counts int32 [seqs]; starts int32 [seqs + 1], or None: as many tokens of every
+    sequence; q, q_out [tokens, heads, head_dim] or None; the rest as for qk_rotate, positions None: those in the cache."""
+    where = "cache_append"
+    if (q is None) != (q_out is None):
+        raise _invalid(where, "q and q_out come together")
+    kept = {name: t for name, t in (("q", q), ("q_out", q_out), ("q_weight", q_weight), ("k_weight", k_weight)) if t is not None}
+    dtype = _float_type(where, {"k": k, "v": v, "k_pages": k_pages, "v_pages": v_pages, **kept})
+    if len(k.shape) != 3 or len(k_pages.shape) != 4 or len(page_table.shape) != 2:
+        raise _invalid(where, "k has three dimensions, k_pages four, page_table two")
+    T, Hkv, d = k.shape
+    P, page = k_pages.shape[:2]
+    B, width = page_table.shape
+    _shaped(where, "v", v, T, Hkv, d)
+    _shaped(where, "k_pages", k_pages, P, page, Hkv, d)
+    _shaped(where, "v_pages", v_pages, P, page, Hkv, d)
+    H = 0
+    if q is not None:
+        if len(q.shape) != 3:
+            raise _invalid(where, "q has three dimensions")
+        H = q.shape[1]
+        _shaped(where, "q", q, T, H, d)
+        _shaped(where, "q_out", q_out, T, H, d)
+    if (q_weight is None) != (k_weight is None or q is None):
+        raise _invalid(where, "q_weight and k_weight come together, q_weight with q alone")
+    table = _whole(where, "page_table", page_table, (B, width), ("torch.int32",), contiguous=False)
+    if width > 1 and page_table.stride()[1] != 1:
+        raise _invalid(where, "page_table: the last dimension has to be contiguous")
+    rot, axes, freq_at, positions_at, axis_stride, axis_at = _rotation(where, T, d, freqs, positions, axis_of, pairs)
+    none = _Two(0, 0)
+    c = CacheAppend(dtype, PAIRS[pairs], T, B, H, Hkv, d, rot, axes, page, width, P, eps, None if q is None else q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                    None if q is None else q_out.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), none if q is None else _two(q), _two(k), _two(v),
+                    none if q is None else _two(q_out), _three(k_pages), _three(v_pages), *_norm_weights(where, d, {"q_weight": q_weight, "k_weight": k_weight}),
+                    freq_at, positions_at, axis_stride, axis_at, _whole(where, "starts", starts, (B + 1,), ("torch.int32",)),
+                    _whole(where, "counts", counts, (B,), ("torch.int32",)), _whole(where, "cache_lens", cache_lens, (B,), ("torch.int32",)),
+                    table, page_table.stride()[0])
+    c._tensors = (k, v, k_pages, v_pages, page_table, cache_lens, starts, counts, q, q_out, freqs, positions, axis_of, q_weight, k_weight)
+    return c
+
+
+def mmee_cache_append_forward(c: CacheAppend) -> None:
+    _check(_lib.mmee_cache_append_forward(C.byref(c)), "mmee_cache_append_forward")
 
 
 def mmee_set_stream(stream_ptr: int | None):

@@ -1,0 +1,339 @@
+// Norm of queries and keys per head and their rotation by position, forward and backward; the same on the way into a paged cache.
+//
+//   z = x r w,  r = (mean of the head's x^2 + eps)^-1/2      (without a weight: z = x)
+//   (y_a, y_b) = (z_a cos - z_b sin, z_a sin + z_b cos)      for the pairs (a, b) of the first `rot` values, angle = position * frequency
+//   backward: dz = dy turned back;  dw = sum of dz x r over tokens and heads;  dx = r (w dz - x r * mean(w dz x r))
+//
+// A head is at most 32 chunks of eight values.  G lanes share it, two chunks each: the chunks of a pair's two halves, so that a pair never
+// leaves its lane, and the rest beside each other.  What a wave's lanes need of angles is the same for every head of a token: it is
+// worked out once a token.  Everything between the 16-bit input and the 16-bit output is 32 bits, angles 64.
+#pragma once
+
+#include "launch.h"
+#include "mfma.h"
+
+namespace mmee {
+
+struct Rows {                   // a tensor's strides in elements
+    int64_t token, head;
+};
+
+struct RotateArgs {
+    uint32_t tokens, heads, kv_heads, head_dim, rot;
+    uint32_t axes, shares;      // shares: waves that share a token's heads
+    float eps;
+    const uint16_t *q, *k, *v;
+    uint16_t *q_out, *k_out, *v_out;            // k_out, v_out: tensors, or pages
+    Rows qs, ks, vs, qos, kos, vos;
+    const uint16_t *q_weight, *k_weight;
+    const double *freqs;
+    const int32_t *positions;
+    int64_t axis_stride;
+    const uint8_t *axis_of;
+    // paged cache
+    int64_t k_page, v_page, table_stride;       // from one page, and from one sequence's entries, to the next
+    const int32_t *starts, *counts, *cache_lens, *page_table;
+    uint32_t seqs, per_seq, page_shift, pages_per_seq, n_pages;
+    // backward
+    const uint16_t *dq_out, *dk_out;
+    uint16_t *dq, *dk, *dq_weight, *dk_weight;
+    Rows dqos, dkos, dqs, dks;
+    float *parts;               // [block][2][head_dim]
+    uint32_t blocks;
+};
+
+// The largest i < n with value(i) <= x, or -1; value ascends.  64 at a time, asked by a whole wave.
+template <class F>
+__device__ __forceinline__ int last_at_most(uint32_t n, int64_t x, F value)
+{
+    const uint32_t lane = threadIdx.x & 63;
+    uint32_t lo = 0;
+    bool first = true;
+    while (n > 0) {
+        const uint32_t step = (n + 63) / 64, at = lane * step;
+        const uint64_t below = __ballot(at < n && value(lo + at) <= x);
+        if (!below) return first ? -1 : (int)lo;
+        const uint32_t last = 63 - __builtin_clzll(below);
+        lo += last * step;
+        n = step == 1 ? 0 : (n - last * step < step ? n - last * step : step);
+        first = false;
+    }
+    return first ? -1 : (int)lo;
+}
+
+__device__ __forceinline__ int64_t within(int64_t x, int64_t lo, int64_t hi) { return x < lo ? lo : x > hi ? hi : x; }
+
+// cos and sin of position * frequency.  The product in turns in 64 bits, which a million turns away still tell 2^-33 of a turn apart; the
+// eighth of a turn that is left, in 32 bits, by the Taylor series, whose next terms are below 2^-28.
+__device__ __forceinline__ void turn(double position, double freq, float &cos, float &sin)
+{
+    constexpr double PER_TURN = 0.15915494309189533577;
+    const double turns = position * (freq * PER_TURN);
+    const float part = (float)(turns - __builtin_rint(turns));              // -1/2 .. 1/2
+    const float quarters = __builtin_rintf(4.0f * part);
+    const float x = (part - 0.25f * quarters) * 6.2831853071795865f, x2 = x * x;            // |x| <= pi / 4
+    const float s = x + x * x2 * (-1.0f / 6 + x2 * (1.0f / 120 + x2 * (-1.0f / 5040 + x2 * (1.0f / 362880))));
+    const float c = 1.0f + x2 * (-0.5f + x2 * (1.0f / 24 + x2 * (-1.0f / 720 + x2 * (1.0f / 40320 - x2 * (1.0f / 3628800)))));
+    const int n = (int)quarters & 3;
+    const float a = n & 1 ? s : c, b = n & 1 ? c : s;
+    cos = n == 1 || n == 2 ? -a : a;
+    sin = n & 2 ? -b : b;
+}
+
+// What a lane holds of a head: chunks at[0] and at[1] (of eight values), values a[0..7], b[0..7].
+template <class T, int G, bool NEIGHBOURS>
+struct Head {
+    uint32_t at[2];
+    bool there[2], turned[2];
+    float cos[8], sin[8];       // halves: of the pairs (a[j], b[j]); neighbours: 0..3 of a's pairs, 4..7 of b's
+
+    __device__ __forceinline__ explicit Head(const RotateArgs &r)
+    {
+        const uint32_t p = threadIdx.x % G, chunks = r.head_dim / 8, half = NEIGHBOURS ? 0 : r.rot / 16, lanes = (chunks + 1) / 2;
+        at[0] = p < half ? p : half + p;                                    // (2 half + p - half)
+        at[1] = p < half ? p + half : at[0] + (lanes - half);
+        there[0] = p < lanes;
+        there[1] = p < lanes && at[1] < chunks;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            turned[i] = there[i] && 8 * at[i] < r.rot;
+            if (!there[i]) at[i] = 0;
+        }
+    }
+
+    __device__ __forceinline__ void angles(const RotateArgs &r, uint32_t token, int64_t place)
+    {
+        const double first = r.positions ? (double)r.positions[token] : (double)place;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int i = NEIGHBOURS ? j / 4 : 0;
+            cos[j] = sin[j] = 0.0f;
+            if (turned[i]) {
+                const uint32_t pair = NEIGHBOURS ? 4 * at[i] + j % 4 : 8 * at[0] + j;
+                double position = first;
+                if (r.axis_of) {
+                    const uint32_t axis = r.axis_of[pair];
+                    position = r.positions[(axis < r.axes ? axis : r.axes - 1) * r.axis_stride + token];
+                }
+                turn(position, r.freqs[pair], cos[j], sin[j]);
+            }
+        }
+    }
+
+    __device__ __forceinline__ void load(const uint16_t *head, u32x4 (&raw)[2]) const
+    {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            raw[i] = u32x4{0, 0, 0, 0};
+            if (there[i]) raw[i] = *reinterpret_cast<const u32x4 *>(head + 8 * at[i]);
+        }
+    }
+
+    static __device__ __forceinline__ void widen(const u32x4 (&raw)[2], float (&x)[16])
+    {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const f32x8 y = __builtin_convertvector(as_operand<T>(raw[i]), f32x8);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[8 * i + j] = y[j];
+        }
+    }
+
+    __device__ __forceinline__ void store(uint16_t *head, const float (&x)[16]) const
+    {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            f32x8 y;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = x[8 * i + j];
+            if (there[i]) *reinterpret_cast<typename T::V8 *>(head + 8 * at[i]) = __builtin_convertvector(y, typename T::V8);
+        }
+    }
+
+    // sign = 1: by the angles; -1: back.
+    __device__ __forceinline__ void rotate(float (&x)[16], float sign) const
+    {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int a = NEIGHBOURS ? 8 * (j / 4) + 2 * (j % 4) : j, b = NEIGHBOURS ? a + 1 : 8 + j;
+            const float s = sign * sin[j], u = x[a] * cos[j] - x[b] * s, w = x[a] * s + x[b] * cos[j];
+            const bool yes = turned[NEIGHBOURS ? j / 4 : 0];
+            x[a] = yes ? u : x[a];
+            x[b] = yes ? w : x[b];
+        }
+    }
+
+    static __device__ __forceinline__ float sum(float x)
+    {
+#pragma unroll
+        for (int d = 1; d < G; d <<= 1) x += __shfl_xor(x, d);
+        return x;
+    }
+
+    static __device__ __forceinline__ float squares(const float (&x)[16])
+    {
+        float s = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) s += x[j] * x[j];
+        return sum(s);
+    }
+};
+
+// Forward: a wave takes 64 / G heads of a token at a time.  CACHE: keys and values go to the pages, values as they are.
+template <class T, int G, bool NEIGHBOURS, bool CACHE>
+__global__ __launch_bounds__(256) void k_rotate(const RotateArgs r)
+{
+    constexpr uint32_t PER = 64 / G;
+    const uint64_t wave = (uint64_t)blockIdx.x * (blockDim.x / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t token = (uint32_t)(wave / r.shares), share = (uint32_t)(wave % r.shares);
+    if (token >= r.tokens) return;
+    int64_t place = 0;
+    int32_t page = -1;
+    if (CACHE) {
+        int seq = r.starts ? last_at_most(r.seqs, token, [&](uint32_t i) { return (int64_t)r.starts[i]; }) : (int)(token / r.per_seq);
+        seq = __builtin_amdgcn_readfirstlane(seq);
+        if (seq < 0 || (r.starts && (int64_t)token >= r.starts[seq + 1])) return;           // a token of no sequence
+        const int64_t nth = r.starts ? (int64_t)token - r.starts[seq] : token % r.per_seq;
+        if (r.counts && nth >= r.counts[seq]) return;
+        place = within(r.cache_lens[seq], 0, INT32_MAX) + nth;
+        if (place >> r.page_shift < r.pages_per_seq) page = r.page_table[seq * r.table_stride + (place >> r.page_shift)];
+        if ((uint32_t)page >= r.n_pages) page = -1;
+    }
+    Head<T, G, NEIGHBOURS> h(r);
+    h.angles(r, token, place);
+    float w[2][16];
+    const bool norm = r.q_weight || r.k_weight;
+    if (norm) {
+        u32x4 raw[2];
+        h.load(r.q_weight, raw);
+        h.widen(raw, w[0]);
+        h.load(r.k_weight, raw);
+        h.widen(raw, w[1]);
+    }
+    const uint32_t all = r.heads + r.kv_heads * (CACHE ? 2 : 1);
+    const int64_t inside = CACHE ? place & ((1u << r.page_shift) - 1) : 0;
+    for (uint32_t at = share * PER + (threadIdx.x & 63) / G; at - (threadIdx.x & 63) / G < all; at += r.shares * PER) {
+        if (at >= all) continue;
+        const bool is_q = at < r.heads, is_v = CACHE && at >= r.heads + r.kv_heads;
+        const uint32_t head = is_q ? at : is_v ? at - r.heads - r.kv_heads : at - r.heads;
+        const uint16_t *from = is_q ? r.q + token * r.qs.token + head * r.qs.head : is_v ? r.v + token * r.vs.token + head * r.vs.head : r.k + token * r.ks.token + head * r.ks.head;
+        uint16_t *to;
+        if (is_q) to = r.q_out + token * r.qos.token + head * r.qos.head;
+        else if (!CACHE) to = r.k_out + token * r.kos.token + head * r.kos.head;
+        else if (is_v) to = r.v_out + page * r.v_page + inside * r.vos.token + head * r.vos.head;
+        else to = r.k_out + page * r.k_page + inside * r.kos.token + head * r.kos.head;
+        u32x4 raw[2];
+        h.load(from, raw);
+        if (is_v) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (page >= 0 && h.there[i]) *reinterpret_cast<u32x4 *>(to + 8 * h.at[i]) = raw[i];
+            continue;
+        }
+        float x[16];
+        h.widen(raw, x);
+        if (norm) {
+            const float inverse = __builtin_amdgcn_rsqf(h.squares(x) / (float)r.head_dim + r.eps);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) x[j] *= inverse * (is_q ? w[0][j] : w[1][j]);
+        }
+        h.rotate(x, 1.0f);
+        if (is_q || !CACHE || page >= 0) h.store(to, x);
+    }
+}
+
+// Backward.  A wave takes heads as in the forward pass, and further tokens; the weights' gradients of its lanes' columns stay in registers and
+// leave the block as one line of 32-bit sums.
+template <class T, int G, bool NEIGHBOURS>
+__global__ __launch_bounds__(256) void k_rotate_back(const RotateArgs r)
+{
+    constexpr uint32_t PER = 64 / G;
+    __shared__ float sums[4][2][16 * G];
+    const uint32_t w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const bool norm = r.q_weight != nullptr;
+    Head<T, G, NEIGHBOURS> h(r);
+    float weight[2][16], dw[2][16] = {};
+    if (norm) {
+        u32x4 raw[2];
+        h.load(r.q_weight, raw);
+        h.widen(raw, weight[0]);
+        h.load(r.k_weight, raw);
+        h.widen(raw, weight[1]);
+    }
+    const uint64_t step = (uint64_t)gridDim.x * 4, all_items = (uint64_t)r.tokens * r.shares;
+    const uint32_t all = r.heads + r.kv_heads;
+    for (uint64_t item = (uint64_t)blockIdx.x * 4 + w; item < all_items; item += step) {
+        const uint32_t token = (uint32_t)(item / r.shares), share = (uint32_t)(item % r.shares);
+        h.angles(r, token, 0);
+        for (uint32_t at = share * PER + lane / G; at - lane / G < all; at += r.shares * PER) {
+            if (at >= all) continue;
+            const bool is_q = at < r.heads;
+            const uint32_t head = is_q ? at : at - r.heads;
+            u32x4 raw[2], raw_d[2];
+            h.load(is_q ? r.dq_out + token * r.dqos.token + head * r.dqos.head : r.dk_out + token * r.dkos.token + head * r.dkos.head, raw_d);
+            float d[16];
+            h.widen(raw_d, d);
+            h.rotate(d, -1.0f);
+            if (norm) {
+                h.load(is_q ? r.q + token * r.qs.token + head * r.qs.head : r.k + token * r.ks.token + head * r.ks.head, raw);
+                float x[16];
+                h.widen(raw, x);
+                const float inverse = __builtin_amdgcn_rsqf(h.squares(x) / (float)r.head_dim + r.eps);
+                float along = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    x[j] *= inverse;
+                    const float part = d[j] * x[j];
+                    dw[0][j] += is_q ? part : 0.0f;
+                    dw[1][j] += is_q ? 0.0f : part;
+                    d[j] *= is_q ? weight[0][j] : weight[1][j];
+                    along += d[j] * x[j];
+                }
+                along = h.sum(along) / (float)r.head_dim;
+#pragma unroll
+                for (int j = 0; j < 16; ++j) d[j] = inverse * (d[j] - x[j] * along);
+            }
+            h.store(is_q ? r.dq + token * r.dqs.token + head * r.dqs.head : r.dk + token * r.dks.token + head * r.dks.head, d);
+        }
+    }
+    if (!norm) return;
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            float x = dw[n][j];
+#pragma unroll
+            for (int d = G; d < 64; d <<= 1) x += __shfl_xor(x, d);
+            if (lane < G) sums[w][n][16 * lane + j] = x;
+        }
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < 2 * 16 * G; i += 256) {
+        const uint32_t n = i / (16 * G), c = i % (16 * G), chunk = c / 8 % 2, p = c / 16;
+        const float x = (sums[0][n][c] + sums[1][n][c]) + (sums[2][n][c] + sums[3][n][c]);
+        // lane p's chunk of the head, as Head has it
+        const uint32_t chunks = r.head_dim / 8, half = NEIGHBOURS ? 0 : r.rot / 16, lanes = (chunks + 1) / 2;
+        const uint32_t first = p < half ? p : half + p, at = !chunk ? first : p < half ? p + half : first + (lanes - half);
+        if (p < lanes && at < chunks) r.parts[((uint64_t)blockIdx.x * 2 + n) * r.head_dim + 8 * at + c % 8] = x;
+    }
+}
+
+// The weights' gradients: the blocks' lines in ascending order, 32 columns a block, 32 slices of the lines.
+template <class T>
+__global__ __launch_bounds__(1024) void k_rotate_weights(const RotateArgs r)
+{
+    __shared__ float slices[32][33];
+    const uint32_t column = blockIdx.x * 32 + threadIdx.x % 32, slice = threadIdx.x / 32, width = 2 * r.head_dim;
+    float x = 0.0f;
+    if (column < width)
+        for (uint32_t i = slice; i < r.blocks; i += 32) x += r.parts[(uint64_t)i * width + column];
+    slices[slice][threadIdx.x % 32] = x;
+    __syncthreads();
+    if (slice || column >= width) return;
+    float total = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) total += slices[i][threadIdx.x];
+    uint16_t *to = column < r.head_dim ? r.dq_weight + column : r.dk_weight + (column - r.head_dim);
+    *reinterpret_cast<typename T::Scalar *>(to) = (typename T::Scalar)total;
+}
+
+}  // namespace mmee

@@ -468,6 +468,42 @@ typedef struct mmee_cache_append {
 
 int mmee_cache_append_forward(const mmee_cache_append *c);
 
+/* Attention of packed prompts: rows of sequence b are tokens q_starts[b] .. q_starts[b + 1] - 1 of q and o [q_tokens][heads][head_dim], its keys
+ * tokens kv_starts[b] .. kv_starts[b + 1] - 1 of k and v [kv_tokens][kv_heads][head_dim] (kv_starts null: q_starts, and kv_tokens = q_tokens).
+ * Heads, head_dim, scale as of mmee_attn; strides of the first two dimensions.  causal != 0: row i of a sequence of m rows and n keys sees the
+ * keys j <= i + n - m (the last row at the last key: a prompt over itself, or a prompt's next rows over all keys so far); 0: all n.  A row without keys
+ * gives zeros, and lse -inf.  Starts ascend and lie within 0 .. tokens (beyond, they are clamped; a sequence whose end lies before its start is empty;
+ * sequences that overlap are not looked for: which of them an output belongs to is then undefined).
+ * What is not finite in a token may reach all rows of its sequence, none of another one.  Tokens of no sequence are not read, and outputs there are
+ * left as they were; keys of a sequence without rows get zero gradients. */
+typedef struct mmee_prompt_attn {
+    uint32_t dtype, causal;
+    uint32_t seqs, heads, kv_heads, head_dim;
+    uint32_t q_tokens, kv_tokens;
+    float scale;
+    const void *q, *k, *v;
+    void *o;
+    int64_t q_stride[2], k_stride[2], v_stride[2], o_stride[2];             /* token, head */
+    const int32_t *q_starts, *kv_starts;                                    /* [seqs + 1]  */
+    float *lse;                     /* [heads][q_tokens] contiguous; may be null for forward */
+    void *workspace;
+    uint64_t workspace_bytes;
+    uint64_t reserved;              /* must be 0 */
+} mmee_prompt_attn;
+
+/* d_o as o; dq as q, dk and dv as k and v. */
+typedef struct mmee_prompt_attn_grads {
+    const void *d_o;
+    void *dq, *dk, *dv;
+    int64_t do_stride[2], dq_stride[2], dk_stride[2], dv_stride[2];
+} mmee_prompt_attn_grads;
+
+/* backward != 0: enough for the forward and the backward call. */
+int mmee_prompt_attn_workspace(const mmee_prompt_attn *a, int backward, uint64_t *bytes);
+int mmee_prompt_attn_forward(const mmee_prompt_attn *a);
+/* Reads o and lse as the forward call left them. */
+int mmee_prompt_attn_backward(const mmee_prompt_attn *a, const mmee_prompt_attn_grads *g);
+
 /* Use this HIP stream (a hipStream_t passed as void*) for all later launches; NULL = default.  Once a search, evaluation or front has
  * run, the call first waits for the stream used so far, whose scratch later launches share; before that, in a program that runs the
  * chains alone, it waits for nothing. */

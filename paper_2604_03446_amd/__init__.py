@@ -156,6 +156,19 @@ class CacheAppend(_Call):
                 ("page_table", C.c_void_p), ("table_stride", C.c_int64), ("reserved", C.c_uint64)]
 
 
+class PromptAttn(_Call):
+    _fields_ = [("dtype", C.c_uint32), ("causal", C.c_uint32), ("seqs", C.c_uint32), ("heads", C.c_uint32), ("kv_heads", C.c_uint32),
+                ("head_dim", C.c_uint32), ("q_tokens", C.c_uint32), ("kv_tokens", C.c_uint32), ("scale", C.c_float),
+                ("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("o", C.c_void_p),
+                ("q_stride", _Two), ("k_stride", _Two), ("v_stride", _Two), ("o_stride", _Two), ("q_starts", C.c_void_p), ("kv_starts", C.c_void_p),
+                ("lse", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64), ("reserved", C.c_uint64)]
+
+
+class PromptAttnGrads(_Call):
+    _fields_ = [("d_o", C.c_void_p), ("dq", C.c_void_p), ("dk", C.c_void_p), ("dv", C.c_void_p),
+                ("do_stride", _Two), ("dq_stride", _Two), ("dk_stride", _Two), ("dv_stride", _Two)]
+
+
 COST_DTYPE = np.dtype([("bs_words", "<u8"), ("da_words", "<u8"), ("br_words", "<u8"),
                        ("mac_total", "<u8"), ("comp_cycles", "<u8"),
                        ("energy_pj", "<f8"), ("latency_cycles", "<f8"),
@@ -205,6 +218,9 @@ def _load() -> C.CDLL:
     L.mmee_qk_rotate_forward.argtypes = [P(QkRotate)]
     L.mmee_qk_rotate_backward.argtypes = [P(QkRotate), P(QkRotateGrads)]
     L.mmee_cache_append_forward.argtypes = [P(CacheAppend)]
+    L.mmee_prompt_attn_workspace.argtypes = [P(PromptAttn), C.c_int, P(C.c_uint64)]
+    L.mmee_prompt_attn_forward.argtypes = [P(PromptAttn)]
+    L.mmee_prompt_attn_backward.argtypes = [P(PromptAttn), P(PromptAttnGrads)]
     L.mmee_set_stream.argtypes = [C.c_void_p]
     L.mmee_shutdown.argtypes = []
     L.mmee_shutdown.restype = None
@@ -217,7 +233,8 @@ def _load() -> C.CDLL:
                  "mmee_front_bs_da", "mmee_chain_front_bs_da",
                  "mmee_attn_workspace", "mmee_attn_forward", "mmee_attn_backward", "mmee_tree_attn_workspace", "mmee_tree_attn_forward",
                  "mmee_ffn_workspace", "mmee_ffn_forward", "mmee_ffn_backward",
-                 "mmee_qk_rotate_workspace", "mmee_qk_rotate_forward", "mmee_qk_rotate_backward", "mmee_cache_append_forward"):
+                 "mmee_qk_rotate_workspace", "mmee_qk_rotate_forward", "mmee_qk_rotate_backward", "mmee_cache_append_forward",
+                 "mmee_prompt_attn_workspace", "mmee_prompt_attn_forward", "mmee_prompt_attn_backward"):
         getattr(L, name).restype = C.c_int
     return L
 
@@ -780,6 +797,64 @@ def cache_append(k, v, k_pages, v_pages, page_table, cache_lens, starts=None, co
 
 def mmee_cache_append_forward(c: CacheAppend) -> None:
     _check(_lib.mmee_cache_append_forward(C.byref(c)), "mmee_cache_append_forward")
+
+
+def prompt_attn(q, k, v, o, q_starts, kv_starts=None, lse=None, scale: float | None = None, causal: bool = True) -> PromptAttn:
+    """Arguments of mmee_prompt_attn_forward and mmee_prompt_attn_backward.  q, o [q_tokens, heads, head_dim]; k, v [kv_tokens, kv_heads,
+    head_dim], any strides but of the last dimension; q_starts, kv_starts int32 [seqs + 1], kv_starts None: q_starts; lse float32 [heads,
+    q_tokens] (wanted for the backward call).  scale: 1 / sqrt(head_dim) unless given."""
+    where = "prompt_attn"
+    dtype = _float_type(where, {"q": q, "k": k, "v": v, "o": o})
+    if len(q.shape) != 3 or len(k.shape) != 3 or len(q_starts.shape) != 1:
+        raise _invalid(where, "q and k have three dimensions, q_starts one")
+    Tq, H, d = q.shape
+    Tk, Hkv = k.shape[:2]
+    _shaped(where, "k", k, Tk, Hkv, d)
+    _shaped(where, "v", v, Tk, Hkv, d)
+    _shaped(where, "o", o, Tq, H, d)
+    if kv_starts is None and Tk != Tq:
+        raise _invalid(where, "kv_starts are wanted where there are not as many keys as rows")
+    seqs = q_starts.shape[0] - 1
+    if seqs < 1:
+        raise _invalid(where, "q_starts has a start and an end at least")
+    a = PromptAttn(dtype, bool(causal), seqs, H, Hkv, d, Tq, Tk, _scale(where, d, scale), q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), _two(q), _two(k),
+                   _two(v), _two(o), _whole(where, "q_starts", q_starts, (seqs + 1,), ("torch.int32",)), _whole(where, "kv_starts", kv_starts, (seqs + 1,), ("torch.int32",)),
+                   _whole(where, "lse", lse, (H, Tq), ("torch.float32",)))
+    a._tensors = (q, k, v, o, q_starts, kv_starts, lse)
+    return a
+
+
+def prompt_attn_grads(do, dq, dk, dv) -> PromptAttnGrads:
+    """Output gradient and gradients of mmee_prompt_attn_backward, shaped as o, q, k and v."""
+    where = "prompt_attn_grads"
+    _float_type(where, {"do": do, "dq": dq, "dk": dk, "dv": dv})
+    if len(do.shape) != 3 or len(dk.shape) != 3:
+        raise _invalid(where, "do and dk have three dimensions")
+    _shaped(where, "dq", dq, *do.shape)
+    _shaped(where, "dv", dv, *dk.shape)
+    g = PromptAttnGrads(do.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), _two(do), _two(dq), _two(dk), _two(dv))
+    g._tensors = (do, dq, dk, dv)
+    return g
+
+
+def mmee_prompt_attn_workspace(a: PromptAttn, backward: bool = False) -> int:
+    out = C.c_uint64()
+    _check(_lib.mmee_prompt_attn_workspace(C.byref(a), int(backward), C.byref(out)), "mmee_prompt_attn_workspace")
+    return out.value
+
+
+def mmee_prompt_attn_forward(a: PromptAttn) -> None:
+    _check(_lib.mmee_prompt_attn_forward(C.byref(a)), "mmee_prompt_attn_forward")
+
+
+def mmee_prompt_attn_backward(a: PromptAttn, g: PromptAttnGrads) -> None:
+    do, dq, dk, dv = g._tensors
+    q, k = a._tensors[:2]
+    for name, t, like in (("do", do, q), ("dk", dk, k)):
+        _shaped("mmee_prompt_attn_backward", name, t, *like.shape)
+        if t.dtype != like.dtype:
+            raise _invalid("mmee_prompt_attn_backward", f"{name} is {t.dtype}, {like.dtype} is wanted")
+    _check(_lib.mmee_prompt_attn_backward(C.byref(a), C.byref(g)), "mmee_prompt_attn_backward")
 
 
 def mmee_set_stream(stream_ptr: int | None):

@@ -1,0 +1,232 @@
+// Host side of the attention of packed prompts: argument checks, the choice of tiles and pieces, launches.
+#include <algorithm>
+#include <cmath>
+
+#include "prompt.h"
+
+namespace mmee {
+namespace {
+
+constexpr uint64_t MOST_ROWS = 1u << 28;        // rows of one key/value head, keys: token_of() and row numbers stay exact
+constexpr int64_t MOST_TOKEN_STRIDE = 1 << 24;  // a tile's offsets fit 32 bits
+
+bool misaligned(const void *p, uintptr_t to = 16) { return ((uintptr_t)p & (to - 1)) != 0; }
+
+// Strides of a tensor of `tokens` x `heads` rows: 16-byte aligned rows, nothing negative; an output's rows are rows of their own.
+bool take_strides(const int64_t *given, uint64_t tokens, uint64_t heads, bool output, Strides &out)
+{
+    const uint64_t extent[2] = {tokens, heads};
+    int64_t s[2];
+    for (int k = 0; k < 2; ++k) {
+        s[k] = extent[k] > 1 ? given[k] : 0;
+        if (s[k] < 0 || s[k] % 8 || s[k] > (int64_t)1 << 46 || (output && extent[k] > 1 && s[k] == 0)) return false;
+    }
+    if (s[0] > MOST_TOKEN_STRIDE) return false;
+    out = {0, s[0], s[1]};
+    return true;
+}
+
+uint64_t up256(uint64_t x) { return (x + 255) & ~(uint64_t)255; }
+
+// One of the three kernels: waves, slots of tiles, pieces, blocks.
+struct Launch {
+    int waves = 4;
+    uint64_t slots = 0, splits = 1, blocks = 0;
+};
+
+struct Plan {
+    PromptArgs p = {};
+    int dp = 0, dtype = 0;
+    Launch forward, dq, dkv;
+    uint64_t part_bytes = 0, forward_bytes = 0, backward_bytes = 0;
+};
+
+// Whether blocks that run alone on a unit keep the card busy: more than half of the units in one round, or 7/8 in whole rounds.
+bool fills(uint64_t blocks) { return blocks > 128 && (blocks <= 256 || blocks * 8 >= (blocks + 255) / 256 * 256 * 7); }
+
+// Tiles of 32 rows (or keys) a wave; pieces of at least `least` steps of `across` elements on average (the lengths are not known here), where there
+// are not enough tiles for one round of blocks.
+Launch plan_launch(uint64_t lines, uint64_t seqs, uint64_t kv_heads, uint64_t across, uint64_t step, uint64_t least, bool eight)
+{
+    Launch l;
+    for (const int waves : {8, 4}) {
+        l.waves = waves;
+        l.slots = lines / (32 * waves) + seqs;
+        const uint64_t blocks = l.slots * kv_heads, room = 2048 / waves, steps = (across / seqs + step - 1) / step;
+        l.splits = blocks * 4 >= room * 3 ? 1 : std::min<uint64_t>({std::max<uint64_t>(1, steps / least), std::max<uint64_t>(1, room / blocks), 128});
+        l.blocks = blocks * l.splits;
+        if (waves == 8 && eight && lines / seqs >= 256 && fills(l.blocks)) break;
+    }
+    return l;
+}
+
+int make_plan(const mmee_prompt_attn *x, bool pointers, Plan &plan)
+{
+    if (!x || x->reserved) return MMEE_EINVAL;
+    if (x->dtype != MMEE_F16 && x->dtype != MMEE_BF16) return MMEE_EINVAL;
+    if (!x->seqs || !x->heads || !x->kv_heads || x->heads % x->kv_heads || !x->head_dim || x->head_dim % 8 || x->head_dim > 128) return MMEE_EINVAL;
+    if (!(x->scale > 0.0f) || !std::isfinite(x->scale)) return MMEE_EINVAL;
+    const uint64_t group = x->heads / x->kv_heads, rows = group * x->q_tokens;
+    if (rows > MOST_ROWS || group > 4096 || x->kv_tokens > MOST_ROWS || x->heads > 1u << 24 || x->seqs > 1u << 24) return MMEE_EINVAL;
+    PromptArgs &p = plan.p;
+    AttnArgs &a = p.a;
+    if (!take_strides(x->q_stride, x->q_tokens, x->heads, false, a.qs) || !take_strides(x->k_stride, x->kv_tokens, x->kv_heads, false, a.ks) ||
+        !take_strides(x->v_stride, x->kv_tokens, x->kv_heads, false, a.vs) || !take_strides(x->o_stride, x->q_tokens, x->heads, true, a.os))
+        return MMEE_EINVAL;
+    if (pointers) {
+        if (!x->q_starts || (!x->kv_starts && x->kv_tokens != x->q_tokens) || (rows && (!x->q || !x->o)) || (x->kv_tokens && (!x->k || !x->v))) return MMEE_EINVAL;
+        if (misaligned(x->q) || misaligned(x->k) || misaligned(x->v) || misaligned(x->o) || misaligned(x->workspace) || misaligned(x->lse, 4) || misaligned(x->q_starts, 4) ||
+            misaligned(x->kv_starts, 4))
+            return MMEE_EINVAL;
+    }
+    plan.dtype = (int)x->dtype;
+    plan.dp = x->head_dim <= 32 ? 32 : x->head_dim <= 64 ? 64 : 128;
+    a.batch = 1;
+    a.heads = x->heads;
+    a.kv_heads = x->kv_heads;
+    a.group = (uint32_t)group;
+    // r / group = r * ceil(2^shift / group) >> shift for every r < 2^28, as in attention.hip
+    a.group_shift = 32;
+    while ((uint64_t)1 << (a.group_shift - 32) < group) ++a.group_shift;
+    a.group_inverse = (((uint64_t)1 << a.group_shift) + group - 1) / group;
+    a.q_len = x->q_tokens;
+    a.rows = (uint32_t)rows;
+    a.kv_len = x->kv_tokens;
+    a.head_dim = x->head_dim;
+    a.scale = x->scale;
+    a.scale_log2 = x->scale * LOG2E;
+    a.q = (const uint16_t *)x->q;
+    a.k = (const uint16_t *)x->k;
+    a.v = (const uint16_t *)x->v;
+    a.o = (uint16_t *)x->o;
+    a.lse = x->lse;
+    p.q_starts = x->q_starts;
+    p.kv_starts = x->kv_starts ? x->kv_starts : x->q_starts;
+    p.seqs = x->seqs;
+    p.causal = x->causal != 0;
+    p.dies = x->kv_heads % 8 == 0;
+    plan.forward = plan_launch(rows, x->seqs, x->kv_heads, x->kv_tokens, 64, 8, plan.dp >= 64);
+    plan.dq = plan_launch(rows, x->seqs, x->kv_heads, x->kv_tokens, 64, 8, plan.dp == 128);
+    plan.dkv = plan_launch(x->kv_tokens, x->seqs, x->kv_heads, rows, 64, 8, plan.dp >= 64);
+    for (const Launch *l : {&plan.forward, &plan.dq, &plan.dkv})
+        if (l->blocks > 0x7fffffff) return MMEE_EINVAL;
+    const auto parts = [&](const Launch &l, uint64_t lines) { return l.splits > 1 ? 4 * l.splits * x->kv_heads * lines * plan.dp : 0; };
+    plan.part_bytes = up256(parts(plan.forward, rows));
+    plan.forward_bytes = plan.part_bytes ? plan.part_bytes + 4 * plan.forward.splits * x->kv_heads * rows : 0;
+    plan.backward_bytes = up256(4ull * x->kv_heads * rows) + std::max(parts(plan.dq, rows), parts(plan.dkv, 2ull * x->kv_tokens));
+    return MMEE_OK;
+}
+
+// Calls f(type, padded head size).
+template <class F>
+void dispatch(const Plan &plan, F f)
+{
+    auto with_dp = [&](auto type) {
+        if (plan.dp == 32) f(type, std::integral_constant<int, 32>());
+        else if (plan.dp == 64) f(type, std::integral_constant<int, 64>());
+        else f(type, std::integral_constant<int, 128>());
+    };
+    if (plan.dtype == MMEE_F16) with_dp(F16());
+    else with_dp(BF16());
+}
+
+PromptArgs with(const PromptArgs &p, const Launch &l)
+{
+    PromptArgs q = p;
+    q.slots = (uint32_t)l.slots;
+    q.a.splits = (uint32_t)l.splits;
+    return q;
+}
+
+}  // namespace
+}  // namespace mmee
+
+using namespace mmee;
+
+extern "C" {
+
+int mmee_prompt_attn_workspace(const mmee_prompt_attn *x, int backward, uint64_t *bytes)
+{
+    if (!bytes) return MMEE_EINVAL;
+    Plan plan;
+    const int rc = make_plan(x, false, plan);
+    if (rc) return rc;
+    *bytes = std::max(plan.forward_bytes, backward ? plan.backward_bytes : 0);
+    return MMEE_OK;
+}
+
+int mmee_prompt_attn_forward(const mmee_prompt_attn *x)
+{
+    Plan plan;
+    const int rc = make_plan(x, true, plan);
+    if (rc) return rc;
+    if (plan.forward_bytes && (!x->workspace || x->workspace_bytes < plan.forward_bytes)) return MMEE_EWORKSPACE;
+    if (!plan.p.a.rows) return MMEE_OK;
+    PromptArgs p = with(plan.p, plan.forward);
+    p.a.part_o = (float *)x->workspace;
+    p.a.part_lse = p.a.part_o + plan.part_bytes / 4;
+    Launching l;
+    if (l.rc) return l.rc;
+    dispatch(plan, [&](auto type, auto dp) {
+        using T = decltype(type);
+        if (plan.forward.waves == 8) {
+            if constexpr (dp.value >= 64) l.run(k_prompt_forward<T, dp.value, 8>, plan.forward.blocks, 512, p);
+        } else {
+            l.run(k_prompt_forward<T, dp.value, 4>, plan.forward.blocks, 256, p);
+        }
+        const uint64_t per = 256 / (dp.value / 4);
+        if (p.a.splits > 1) l.run(k_prompt_join<T, dp.value>, ((uint64_t)p.a.kv_heads * p.a.rows + per - 1) / per, 256, p);
+    });
+    return l.result("prompt attention, forward");
+}
+
+int mmee_prompt_attn_backward(const mmee_prompt_attn *x, const mmee_prompt_attn_grads *g)
+{
+    Plan plan;
+    const int rc = make_plan(x, true, plan);
+    if (rc) return rc;
+    AttnArgs &a = plan.p.a;
+    if (!g || (a.rows && (!x->lse || !g->d_o || !g->dq)) || (a.kv_len && (!g->dk || !g->dv))) return MMEE_EINVAL;
+    if (misaligned(g->d_o) || misaligned(g->dq) || misaligned(g->dk) || misaligned(g->dv)) return MMEE_EINVAL;
+    if (!take_strides(g->do_stride, a.q_len, a.heads, false, a.dos) || !take_strides(g->dq_stride, a.q_len, a.heads, true, a.dqs) ||
+        !take_strides(g->dk_stride, a.kv_len, a.kv_heads, true, a.dks) || !take_strides(g->dv_stride, a.kv_len, a.kv_heads, true, a.dvs))
+        return MMEE_EINVAL;
+    if (plan.backward_bytes && (!x->workspace || x->workspace_bytes < plan.backward_bytes)) return MMEE_EWORKSPACE;
+    if (!a.rows && !a.kv_len) return MMEE_OK;
+    a.o_in = (const uint16_t *)x->o;
+    a.lse_in = x->lse;
+    a.d_o = (const uint16_t *)g->d_o;
+    a.dq = (uint16_t *)g->dq;
+    a.dk = (uint16_t *)g->dk;
+    a.dv = (uint16_t *)g->dv;
+    a.delta = (float *)x->workspace;
+    a.part_o = a.delta + up256(4ull * a.kv_heads * a.rows) / 4;
+    const PromptArgs dq = with(plan.p, plan.dq), dkv = with(plan.p, plan.dkv);
+    Launching l;
+    if (l.rc) return l.rc;
+    dispatch(plan, [&](auto type, auto dp) {
+        using T = decltype(type);
+        constexpr int DP = dp.value;
+        if (a.rows) {
+            if (plan.dq.waves == 8) {
+                if constexpr (DP == 128) l.run(k_prompt_dq<T, DP, 8>, plan.dq.blocks, 512, dq);
+            } else {
+                l.run(k_prompt_dq<T, DP, 4>, plan.dq.blocks, 256, dq);
+            }
+            const uint64_t per = 256 / (DP / 4);
+            if (dq.a.splits > 1) l.run(k_prompt_sum<T, DP, 0>, ((uint64_t)a.kv_heads * a.rows + per - 1) / per, 256, dq);
+        }
+        if (a.kv_len) {
+            if (plan.dkv.waves == 8) {
+                if constexpr (DP >= 64) l.run(k_prompt_dkv<T, DP, 8>, plan.dkv.blocks, 512, dkv);
+            } else {
+                l.run(k_prompt_dkv<T, DP, 4>, plan.dkv.blocks, 256, dkv);
+            }
+            const uint64_t per = 256 / (DP / 2);
+            if (dkv.a.splits > 1) l.run(k_prompt_sum<T, DP, 1>, ((uint64_t)a.kv_heads * a.kv_len + per - 1) / per, 256, dkv);
+        }
+    });
+    return l.result("prompt attention, backward");
+}
+
+}  // extern "C"

@@ -1,9 +1,12 @@
 // Attention of packed prompts: sequences of different lengths one behind the other, each row over its own sequence's keys, all of them or those
 // up to its own.  Formulas, the folding of query heads into rows, the transposed scores and what is rounded are those of attention.h.
 //
-// A sequence's rows are cut into tiles, and tile t of sequence b has slot (first row of b) / TILE + b + t: slots of different tiles differ
-// whatever the lengths, so that blocks find their tile from the starts alone (64 of them at a time) and the host, which does not know the
-// lengths, launches rows / TILE + seqs slots a head.  Slots without a tile end at once.
+// A sequence's rows (for dK and dV its keys) are cut into tiles of a block each.  Blocks find theirs from the starts alone, and the host, which
+// does not know the lengths, launches as many as any lengths can need, rows / TILE + seqs a head; those without a tile end at once.
+//   Up to 64 sequences (a lane holds one): tiles in the order of their work, the longest first, whatever sequence they are of, so that the short
+//   ones fill up the end; where there are few tiles, or some far longer than a unit's share, they are cut into pieces of equal length that are
+//   joined afterwards (`pieces_of`).
+//   More sequences: tile t of sequence b has slot (first row of b) / TILE + b + t, which differ whatever the lengths.
 #pragma once
 
 #include "attention.h"
@@ -12,45 +15,152 @@
 namespace mmee {
 
 struct PromptArgs {
-    AttnArgs a;                 // batch 1, q_len: all tokens, rows: of all tokens, kv_len: all keys, splits: pieces of every tile
+    AttnArgs a;                 // batch 1, q_len: all tokens, rows: of all tokens, kv_len: all keys, splits: pieces of a tile at most
     const int32_t *q_starts, *kv_starts;
     uint32_t seqs, slots;
+    uint32_t room_shift, least; // blocks that run at once (a power of two), steps of a piece at least
     bool causal;
     bool dies;                  // heads are dealt out to the dies, whose L2 then holds their keys
 };
 
-// A block's tile: rows (or, with KEYS, keys) index * TILE .. of a sequence of m tokens from q0 on over n keys from k0 on.
-template <uint32_t TILE, bool KEYS>
+// A block's tile: rows (or, with KEYS, keys) index * TILE .. of a sequence of m tokens from q0 on over n keys from k0 on, and the steps step0 .. of
+// STEP keys (or rows) that are the block's piece of it.
+template <uint32_t TILE, uint32_t STEP, bool KEYS>
 struct Tile {
-    uint32_t index = 0, q0 = 0, m = 0, k0 = 0, n = 0, kvh, split;
+    uint32_t index = 0, q0 = 0, m = 0, k0 = 0, n = 0, kvh, piece, pieces = 1, step0 = 0, count = 0;
     bool there = false;
 
-    __device__ __forceinline__ explicit Tile(const PromptArgs &p)
+    // at: place among heads, tiles and pieces.
+    __device__ __forceinline__ Tile(const PromptArgs &p, uint32_t at)
     {
-        uint32_t at = p.dies ? by_die(blockIdx.x, gridDim.x) : blockIdx.x;
-        // the last rows see most keys, the first keys are seen by most rows: those tiles first
-        const uint32_t slot = KEYS ? at % p.slots : p.slots - 1 - at % p.slots;
-        at /= p.slots;
-        split = at % p.a.splits;
-        kvh = at / p.a.splits;
-        const int32_t *starts = KEYS ? p.kv_starts : p.q_starts;
-        const uint32_t tokens = KEYS ? p.a.kv_len : p.a.q_len, each = KEYS ? 1 : p.a.group;
-        const auto slot_of = [&](uint32_t i) { return (int64_t)((uint32_t)within(starts[i], 0, tokens) * each / TILE + i); };
-        int seq = last_at_most(p.seqs, slot, slot_of);
-        if (seq < 0) return;
-        seq = __builtin_amdgcn_readfirstlane(seq);
+        piece = at % p.a.splits;
+        at /= p.a.splits;
+        const uint32_t order = at % p.slots;
+        kvh = at / p.slots;
+        uint32_t longest = p.least;                     // of a piece, in steps
+        if (p.seqs <= 64) there = by_work(p, order, longest);
+        else there = by_slot(p, p.slots - 1 - order);
+        if (!there) return;
+        const uint32_t steps = steps_of(p, m, n, index);
+        if (p.a.splits > 1) {
+            pieces = (steps + longest - 1) / longest;
+            pieces = pieces < 1 ? 1 : pieces < p.a.splits ? pieces : p.a.splits;
+        }
+        const uint32_t per = pieces > 1 ? (steps + pieces - 1) / pieces : steps;
+        step0 = piece * per < steps ? piece * per : steps;
+        count = step0 + per < steps ? per : steps - step0;
+        there = piece < pieces;
+    }
+
+    // Of a tile that is there: the same in all lanes, so that loops on its numbers are scalar, and so are the buffers that it is loaded from.  (Said once it is
+    // known to be there; in the constructor, where lanes held numbers of their own, the compiler still made loops over the lanes of every load.)
+    __device__ __forceinline__ void settle()
+    {
+        for (uint32_t *x : {&index, &q0, &m, &k0, &n, &kvh, &piece, &pieces, &step0, &count}) *x = __builtin_amdgcn_readfirstlane(*x);
+    }
+
+    static __device__ __forceinline__ uint32_t tiles_of(const PromptArgs &p, uint32_t m, uint32_t n) { return ((KEYS ? n : m * p.a.group) + TILE - 1) / TILE; }
+
+    // Keys 0 .. that a token sees.
+    static __device__ __forceinline__ uint32_t limit(const PromptArgs &p, uint32_t m, uint32_t n, uint32_t token)
+    {
+        return p.causal ? (uint32_t)within((int64_t)token + 1 + n - m, 0, n) : n;
+    }
+
+    // The first row that sees a key, which may lie before the first or behind the last one.
+    static __device__ __forceinline__ int first_row(const PromptArgs &p, uint32_t m, uint32_t n, uint32_t key)
+    {
+        return p.causal ? (int)within(((int64_t)key + m - n) * p.a.group, -(1 << 29), (int64_t)m * p.a.group) : 0;
+    }
+
+    static __device__ __forceinline__ uint32_t steps_of(const PromptArgs &p, uint32_t m, uint32_t n, uint32_t index)
+    {
+        const uint32_t rows = m * p.a.group;
+        if (KEYS) {
+            const int begin = first_row(p, m, n, index * TILE);
+            return (rows - (begin < 0 ? 0 : begin) + STEP - 1) / STEP;
+        }
+        const uint32_t behind = (index + 1) * TILE < rows ? (index + 1) * TILE : rows;
+        return (limit(p, m, n, token_of(p.a, behind - 1)) + STEP - 1) / STEP;
+    }
+
+    __device__ __forceinline__ void take(const PromptArgs &p, uint32_t seq)
+    {
         q0 = (uint32_t)within(p.q_starts[seq], 0, p.a.q_len);
         m = (uint32_t)within(p.q_starts[seq + 1], q0, p.a.q_len) - q0;
         k0 = (uint32_t)within(p.kv_starts[seq], 0, p.a.kv_len);
         n = (uint32_t)within(p.kv_starts[seq + 1], k0, p.a.kv_len) - k0;
-        index = slot - (uint32_t)slot_of(seq);
-        there = (uint64_t)index * TILE < (KEYS ? n : m * each);
     }
 
-    // Keys 0 .. that a token of the sequence sees.
-    __device__ __forceinline__ uint32_t limit(const PromptArgs &p, uint32_t token) const
+    __device__ __forceinline__ bool by_slot(const PromptArgs &p, uint32_t slot)
     {
-        return p.causal ? (uint32_t)within((int64_t)token + 1 + n - m, 0, n) : n;
+        const int32_t *starts = KEYS ? p.kv_starts : p.q_starts;
+        const uint32_t tokens = KEYS ? p.a.kv_len : p.a.q_len, each = KEYS ? 1 : p.a.group;
+        const auto slot_of = [&](uint32_t i) { return (int64_t)((uint32_t)within(starts[i], 0, tokens) * each / TILE + i); };
+        const int seq = __builtin_amdgcn_readfirstlane(last_at_most(p.seqs, slot, slot_of));
+        if (seq < 0) return false;
+        take(p, seq);
+        index = slot - (uint32_t)slot_of(seq);
+        return index < tiles_of(p, m, n);
+    }
+
+    // Tiles have levels, about their length in tiles: with a causal mask those of a sequence are neighbours, else they are the same.
+    __device__ __forceinline__ bool by_work(const PromptArgs &p, uint32_t order, uint32_t &longest)
+    {
+        const uint32_t lane = threadIdx.x & 63;
+        uint32_t tiles = 0, base = 0;
+        if (lane < p.seqs) {
+            take(p, lane);
+            tiles = tiles_of(p, m, n);
+            if (KEYS) base = p.causal ? 0 : m * p.a.group / STEP;
+            else base = p.causal ? (n > m ? (n - m) * p.a.group / TILE : 0) : n / STEP;
+        }
+        if (order >= sum_of_lanes(tiles)) return false;
+        // tiles of a sequence at this level or above
+        const auto above = [&](uint32_t level) {
+            if (!p.causal) return base >= level ? tiles : 0;
+            return level <= base ? tiles : level < base + tiles ? base + tiles - level : 0;
+        };
+        uint32_t low = 0, high = p.seqs == 1 && p.causal ? base + tiles : most_of_lanes(p.causal ? base + tiles : base + 1);
+        high = __builtin_amdgcn_readfirstlane(high);
+        while (high - low > 1) {
+            const uint32_t mid = (low + high) / 2;
+            if (sum_of_lanes(above(mid)) > order) low = mid;
+            else high = mid;
+        }
+        const uint32_t here = above(low) - above(low + 1), rank = order - sum_of_lanes(above(low + 1)), below = sums_below(here) - here;
+        const uint64_t owner = __ballot(rank >= below && rank < below + here);
+        const uint32_t seq = (uint32_t)__builtin_ctzll(owner);
+        index = p.causal ? (KEYS ? tiles - 1 - (low - base) : low - base) : rank - below;
+        if (p.a.splits > 1) longest = pieces_of(p, tiles);
+        index = __builtin_amdgcn_readlane(index, seq);
+        q0 = __builtin_amdgcn_readlane(q0, seq);
+        m = __builtin_amdgcn_readlane(m, seq);
+        k0 = __builtin_amdgcn_readlane(k0, seq);
+        n = __builtin_amdgcn_readlane(n, seq);
+        return true;
+    }
+
+    // The length that pieces may have: what each of the blocks that run at once gets of all steps.  Where there are fewer tiles than such blocks, the least
+    // up to three times that with which all pieces run at once.  (The kernels that join the pieces come to the same ones: whole numbers, and products of
+    // floats that nothing is added to.)
+    __device__ __forceinline__ uint32_t pieces_of(const PromptArgs &p, uint32_t tiles) const
+    {
+        const uint32_t a = tiles ? steps_of(p, m, n, 0) : 0, b = tiles ? steps_of(p, m, n, tiles - 1) : 0;
+        const uint32_t most = a > b ? a : b, least = a > b ? b : a;
+        const uint32_t own = (uint32_t)((uint64_t)tiles * (a + b) >> 4);                // in 8 steps, on average over the tiles: below 2^31 in all
+        const uint64_t share = (uint64_t)sum_of_lanes(own) * p.a.kv_heads * 8 >> p.room_shift, blocks = (uint64_t)sum_of_lanes(tiles) * p.a.kv_heads;
+        const uint32_t low = share > p.least ? (uint32_t)share : p.least;
+        if (blocks >> p.room_shift) return low;
+        uint32_t no = low - 1, yes = 3 * low;
+        while (yes - no > 1 + low / 16) {
+            const uint32_t mid = (no + yes) / 2;
+            const float inverse = 1.0f / (float)mid;
+            const uint32_t wanted = most - least < mid ? tiles * ((most + mid - 1) / mid) : (uint32_t)((float)own * (8.0f * inverse)) + tiles / 2 + 1;
+            if (((uint64_t)sum_of_lanes(tiles ? wanted : 0) * p.a.kv_heads - 1) >> p.room_shift == 0) yes = mid;
+            else no = mid;
+        }
+        return yes;
     }
 
     // Keys of the sequence as the tiles' loads want them.
@@ -61,6 +171,8 @@ struct Tile {
         return k;
     }
 };
+
+__device__ __forceinline__ uint32_t block_place(const PromptArgs &p) { return p.dies ? by_die(blockIdx.x, gridDim.x) : blockIdx.x; }
 
 // Scores of keys first + {8 (r / 4) + 4 h + r % 4} that a row with so many keys left does not see become -inf.
 __device__ __forceinline__ void mask_behind(f32x16 &x, int left)
@@ -78,16 +190,13 @@ __global__ __launch_bounds__(64 * W, 2) void k_prompt_forward(const PromptArgs p
     constexpr int TN = 64, MT = 2, CH = DP / 8, GT = 64 * W;
     __shared__ u32x4 memory[4 * TN * CH];
     const AttnArgs &a = p.a;
-    const Tile<32 * W, false> tile(p);
+    Tile<32 * W, TN, false> tile(p, block_place(p));
     if (!tile.there) return;
+    tile.settle();
     const int thread = threadIdx.x, lane = thread & 63, n = lane & 31, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
-    const uint32_t rows = tile.m * a.group, row0 = tile.index * 32 * W, row1 = row0 + 32 * W < rows ? row0 + 32 * W : rows;
-    const uint32_t row = row0 + 32 * wave + n;
+    const uint32_t rows = tile.m * a.group, row0 = tile.index * 32 * W, row = row0 + 32 * wave + n, step0 = tile.step0, count = tile.count;
     const bool live = row < rows;
-    const uint32_t token = token_of(a, live ? row : rows - 1), limit = tile.limit(p, token);
-    const uint32_t all_see = tile.limit(p, token_of(a, row0)), end = tile.limit(p, token_of(a, row1 - 1));
-    const uint32_t steps = (end + TN - 1) / TN, per = (steps + a.splits - 1) / a.splits;
-    const uint32_t step0 = tile.split * per < steps ? tile.split * per : steps, count = step0 + per < steps ? per : steps - step0;
+    const uint32_t limit = tile.limit(p, tile.m, tile.n, token_of(a, live ? row : rows - 1)), all_see = tile.limit(p, tile.m, tile.n, token_of(a, row0));
 
     const Keys<MODE_PLAIN> keys = tile.keys(p);
     const uint16_t *const k_at = a.k + tile.k0 * a.ks.token, *const v_at = a.v + tile.k0 * a.vs.token;
@@ -232,43 +341,44 @@ __global__ __launch_bounds__(64 * W, 2) void k_prompt_forward(const PromptArgs p
     total = sum_of_halves(total);
     if (!live) return;
     const float times = total != 0.0f ? 1.0f / total : 0.0f, sum2 = total != 0.0f ? top + __log2f(total) : -INFINITY;
-    if (a.splits == 1) {
+    if (tile.pieces == 1) {
         store_row<T, DP>(a.o + tile.q0 * a.os.token + row_at(a, a.os, 0, tile.kvh, row), o, times, a.head_dim);
         if (a.lse && h == 0) a.lse[lse_at(a, 0, tile.kvh, row) + tile.q0] = sum2 * LN2;
     } else {
-        const int64_t line = ((int64_t)tile.split * a.kv_heads + tile.kvh) * a.rows + tile.q0 * a.group + row;
+        const int64_t line = ((int64_t)tile.piece * a.kv_heads + tile.kvh) * a.rows + tile.q0 * a.group + row;
         store_part<DP>(a.part_o + line * DP, o, times);
         if (h == 0) a.part_lse[line] = sum2;
     }
 }
 
-// Whether a token belongs to a sequence.
-__device__ __forceinline__ bool belongs(const int32_t *starts, uint32_t seqs, uint32_t token) { return (int64_t)token >= starts[0] && (int64_t)token < starts[seqs]; }
-
-// Joins the pieces' results in ascending order, as k_attn_join does, of tokens that belong to a sequence.
-template <class T, int DP>
+// Joins the pieces of the tiles of 32 W rows that were cut, in ascending order, as k_attn_join does: 32 rows a block.
+template <class T, int DP, int W>
 __global__ __launch_bounds__(256) void k_prompt_join(const PromptArgs p)
 {
-    constexpr int C4 = DP / 4, ROWS = 256 / C4;
+    constexpr int C4 = DP / 4;
     const AttnArgs &a = p.a;
-    const int64_t all = (int64_t)a.kv_heads * a.rows, at = (int64_t)blockIdx.x * ROWS + threadIdx.x / C4;
-    const int c = threadIdx.x % C4;
-    if (at >= all) return;
-    const uint32_t row = (uint32_t)(at % a.rows), kvh = (uint32_t)(at / a.rows);
-    if (!belongs(p.q_starts, p.seqs, token_of(a, row))) return;
-    float high = -INFINITY, sum = 0.0f;
-    for (uint32_t s = 0; s < a.splits; ++s) high = __builtin_elementwise_maximum(high, a.part_lse[s * all + at]);
-    const float off = high == -INFINITY ? 0.0f : high;
-    f32x4 x = {0, 0, 0, 0};
+    Tile<32 * W, 64, false> tile(p, blockIdx.x / W * a.splits);
+    if (!tile.there || tile.pieces == 1) return;
+    tile.settle();
+    const int64_t next = (int64_t)a.kv_heads * a.rows;
+    for (uint32_t i = threadIdx.x; i < 32 * C4; i += 256) {
+        const uint32_t row = tile.index * 32 * W + blockIdx.x % W * 32 + i / C4, c = i % C4;
+        if (row >= tile.m * a.group) return;
+        const int64_t line = (int64_t)tile.kvh * a.rows + tile.q0 * a.group + row;
+        float high = -INFINITY, sum = 0.0f;
+        for (uint32_t s = 0; s < tile.pieces; ++s) high = __builtin_elementwise_maximum(high, a.part_lse[s * next + line]);
+        const float off = high == -INFINITY ? 0.0f : high;
+        f32x4 x = {0, 0, 0, 0};
 #pragma unroll 4
-    for (uint32_t s = 0; s < a.splits; ++s) {
-        const float w = __builtin_amdgcn_exp2f(a.part_lse[s * all + at] - off);
-        sum += w;
-        x += *reinterpret_cast<const f32x4 *>(a.part_o + (s * all + at) * DP + 4 * c) * w;
+        for (uint32_t s = 0; s < tile.pieces; ++s) {
+            const float w = __builtin_amdgcn_exp2f(a.part_lse[s * next + line] - off);
+            sum += w;
+            x += *reinterpret_cast<const f32x4 *>(a.part_o + (s * next + line) * DP + 4 * c) * w;
+        }
+        x *= sum != 0.0f ? 1.0f / sum : 0.0f;
+        if (4 * c < a.head_dim) *reinterpret_cast<typename T::V4 *>(a.o + tile.q0 * a.os.token + row_at(a, a.os, 0, tile.kvh, row) + 4 * c) = __builtin_convertvector(x, typename T::V4);
+        if (a.lse && c == 0) a.lse[lse_at(a, 0, tile.kvh, row) + tile.q0] = sum != 0.0f ? (high + __log2f(sum)) * LN2 : -INFINITY;
     }
-    x *= sum != 0.0f ? 1.0f / sum : 0.0f;
-    if (4 * c < (int)a.head_dim) *reinterpret_cast<typename T::V4 *>(a.o + row_at(a, a.os, 0, kvh, row) + 4 * c) = __builtin_convertvector(x, typename T::V4);
-    if (a.lse && c == 0) a.lse[lse_at(a, 0, kvh, row)] = sum != 0.0f ? (high + __log2f(sum)) * LN2 : -INFINITY;
 }
 
 // dQ, and D on the way, as k_attn_dq.
@@ -278,15 +388,13 @@ __global__ __launch_bounds__(64 * W, 2) void k_prompt_dq(const PromptArgs p)
     constexpr int TN = 64, CH = DP / 8;
     __shared__ u32x4 tiles[2][2][TN * CH];
     const AttnArgs &a = p.a;
-    const Tile<32 * W, false> tile(p);
+    Tile<32 * W, TN, false> tile(p, block_place(p));
     if (!tile.there) return;
+    tile.settle();
     const int thread = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(thread >> 6), lane = thread & 63, n = lane & 31, h = lane >> 5;
-    const uint32_t rows = tile.m * a.group, row0 = tile.index * 32 * W, row1 = row0 + 32 * W < rows ? row0 + 32 * W : rows;
-    const uint32_t row = row0 + 32 * wave + n;
+    const uint32_t rows = tile.m * a.group, row = tile.index * 32 * W + 32 * wave + n, step0 = tile.step0, count = tile.count;
     const bool live = row < rows;
-    const uint32_t limit = tile.limit(p, token_of(a, live ? row : rows - 1)), end = tile.limit(p, token_of(a, row1 - 1));
-    const uint32_t steps = (end + TN - 1) / TN, per = (steps + a.splits - 1) / a.splits;
-    const uint32_t step0 = tile.split * per < steps ? tile.split * per : steps, count = step0 + per < steps ? per : steps - step0;
+    const uint32_t limit = tile.limit(p, tile.m, tile.n, token_of(a, live ? row : rows - 1));
 
     const Keys<MODE_PLAIN> keys = tile.keys(p);
     const uint16_t *const k_at = a.k + tile.k0 * a.ks.token, *const v_at = a.v + tile.k0 * a.vs.token;
@@ -307,7 +415,7 @@ __global__ __launch_bounds__(64 * W, 2) void k_prompt_dq(const PromptArgs p)
 #pragma unroll
             for (int j = 0; j < 8; ++j) delta += (float)o[t][j] * (float)d_o[t][j];
         delta = sum_of_halves(delta);
-        if (live && h == 0 && tile.split == 0) a.delta[line] = delta;
+        if (live && h == 0 && tile.piece == 0) a.delta[line] = delta;
     }
 
     f32x16 dq[1][DP / 32] = {};
@@ -354,8 +462,8 @@ __global__ __launch_bounds__(64 * W, 2) void k_prompt_dq(const PromptArgs p)
         for (int dt = 0; dt < DP / 32; ++dt) dq[0][dt] = f32x16{};
     }
     const float times = NARROW<T> ? a.scale * __builtin_amdgcn_exp2f(-(UP + HIGHEST + lowered)) : a.scale;
-    if (a.splits == 1) store_row<T, DP>(a.dq + tile.q0 * a.dqs.token + row_at(a, a.dqs, 0, tile.kvh, row), dq[0], times, a.head_dim);
-    else store_part<DP>(a.part_o + ((int64_t)tile.split * a.kv_heads * a.rows + line) * DP, dq[0], times);
+    if (tile.pieces == 1) store_row<T, DP>(a.dq + tile.q0 * a.dqs.token + row_at(a, a.dqs, 0, tile.kvh, row), dq[0], times, a.head_dim);
+    else store_part<DP>(a.part_o + ((int64_t)tile.piece * a.kv_heads * a.rows + line) * DP, dq[0], times);
 }
 
 // dK and dV of 32 W keys, 32 a wave, over the rows that see them, as k_attn_dkv.
@@ -369,16 +477,14 @@ __global__ __launch_bounds__(64 * W, 2) void k_prompt_dkv(const PromptArgs p)
     constexpr bool AWAY = DP == 128;                    // V's operands in shared memory: with them 256 registers do not suffice
     __shared__ u32x4 away[AWAY ? W : 1][DP / 16][64];
     const AttnArgs &a = p.a;
-    const Tile<32 * W, true> tile(p);
+    Tile<32 * W, TR, true> tile(p, block_place(p));
     if (!tile.there) return;
+    tile.settle();
     const int thread = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(thread >> 6), lane = thread & 63, n = lane & 31, h = lane >> 5;
     const uint32_t rows = tile.m * a.group, key0 = tile.index * 32 * W, key = key0 + 32 * wave + n;
-    // the first row that sees a key, of the block's first key and of its last one
-    const auto first_row = [&](uint32_t of) { return p.causal ? (int)within(((int64_t)of + tile.m - tile.n) * a.group, INT32_MIN / 2, rows) : 0; };
-    const uint32_t begin = (uint32_t)(first_row(key0) < 0 ? 0 : first_row(key0));
-    const int all_see = first_row(key0 + 32 * W - 1), own = first_row(key);
-    const uint32_t steps = (rows - begin + TR - 1) / TR, per = (steps + a.splits - 1) / a.splits;
-    const uint32_t step0 = tile.split * per < steps ? tile.split * per : steps, count = step0 + per < steps ? per : steps - step0;
+    const int own = tile.first_row(p, tile.m, tile.n, key), all_see = tile.first_row(p, tile.m, tile.n, key0 + 32 * W - 1);
+    const int first_seen = tile.first_row(p, tile.m, tile.n, key0);
+    const uint32_t begin = first_seen < 0 ? 0 : first_seen, step0 = tile.step0, count = tile.count;
 
     const bool valid = key < tile.n;
     const int64_t key_at = (int64_t)tile.k0 + (valid ? key : 0);
@@ -465,36 +571,41 @@ __global__ __launch_bounds__(64 * W, 2) void k_prompt_dkv(const PromptArgs p)
     }
     if (!valid) return;
     const float times = NARROW<T> ? a.scale * 0x1p-15f / by : a.scale, times_v = NARROW<T> ? 0x1p-15f : 1.0f;
-    if (a.splits == 1) {
+    if (tile.pieces == 1) {
         store_row<T, DP>(a.dk + key_at * a.dks.token + tile.kvh * a.dks.head, dk[0], times, a.head_dim);
         store_row<T, DP>(a.dv + key_at * a.dvs.token + tile.kvh * a.dvs.head, dv[0], times_v, a.head_dim);
     } else {
-        float *part = a.part_o + ((((int64_t)tile.split * a.kv_heads + tile.kvh) * a.kv_len + key_at) * 2) * DP;
+        float *part = a.part_o + ((((int64_t)tile.piece * a.kv_heads + tile.kvh) * a.kv_len + key_at) * 2) * DP;
         store_part<DP>(part, dk[0], times);
         store_part<DP>(part + DP, dv[0], times_v);
     }
 }
 
-// Sums of pieces in ascending order, rounded once, as k_attn_sum: WHICH = 0: dQ rows; 1: dK and dV of a key.
-template <class T, int DP, int WHICH>
+// Sums of the pieces of tiles that were cut, in ascending order, rounded once, as k_attn_sum: dQ of 32 rows a block, or, with KEYS, dK and dV of 32 keys.
+template <class T, int DP, int W, int STEP, bool KEYS>
 __global__ __launch_bounds__(256) void k_prompt_sum(const PromptArgs p)
 {
-    constexpr int C4 = DP / 4 * (WHICH + 1), LINES = 256 / C4;
+    constexpr int C4 = DP / 4 * (KEYS ? 2 : 1);
     const AttnArgs &a = p.a;
-    const uint32_t lines = WHICH ? a.kv_len : a.rows;
-    const int64_t all = (int64_t)a.kv_heads * lines, at = (int64_t)blockIdx.x * LINES + threadIdx.x / C4;
-    const int c = threadIdx.x % C4, d = 4 * c % DP;
-    if (at >= all || d >= (int)a.head_dim) return;
-    const uint32_t line = (uint32_t)(at % lines), kvh = (uint32_t)(at / lines);
-    if (!belongs(WHICH ? p.kv_starts : p.q_starts, p.seqs, WHICH ? line : token_of(a, line))) return;
-    f32x4 x = {0, 0, 0, 0};
+    Tile<32 * W, STEP, KEYS> tile(p, blockIdx.x / W * a.splits);
+    if (!tile.there || tile.pieces == 1) return;
+    tile.settle();
+    const uint32_t lines = KEYS ? tile.n : tile.m * a.group;
+    const int64_t next = (int64_t)a.kv_heads * (KEYS ? a.kv_len : a.rows);
+    for (uint32_t i = threadIdx.x; i < 32 * C4; i += 256) {
+        const uint32_t own = tile.index * 32 * W + blockIdx.x % W * 32 + i / C4, c = i % C4, d = 4 * c % DP;
+        if (own >= lines) return;
+        if (d >= a.head_dim) continue;
+        const int64_t line = KEYS ? (int64_t)tile.kvh * a.kv_len + tile.k0 + own : (int64_t)tile.kvh * a.rows + tile.q0 * a.group + own;
+        f32x4 x = {0, 0, 0, 0};
 #pragma unroll 4
-    for (uint32_t s = 0; s < a.splits; ++s) x += *reinterpret_cast<const f32x4 *>(a.part_o + ((s * all + at) * C4 + c) * 4);
-    uint16_t *to;
-    if (!WHICH) to = a.dq + row_at(a, a.dqs, 0, kvh, line);
-    else if (4 * c < DP) to = a.dk + line * a.dks.token + kvh * a.dks.head;
-    else to = a.dv + line * a.dvs.token + kvh * a.dvs.head;
-    *reinterpret_cast<typename T::V4 *>(to + d) = __builtin_convertvector(x, typename T::V4);
+        for (uint32_t s = 0; s < tile.pieces; ++s) x += *reinterpret_cast<const f32x4 *>(a.part_o + ((s * next + line) * C4 + c) * 4);
+        uint16_t *to;
+        if (!KEYS) to = a.dq + tile.q0 * a.dqs.token + row_at(a, a.dqs, 0, tile.kvh, own);
+        else if (4 * c < DP) to = a.dk + (int64_t)(tile.k0 + own) * a.dks.token + tile.kvh * a.dks.head;
+        else to = a.dv + (int64_t)(tile.k0 + own) * a.dvs.token + tile.kvh * a.dvs.head;
+        *reinterpret_cast<typename T::V4 *>(to + d) = __builtin_convertvector(x, typename T::V4);
+    }
 }
 
 }  // namespace mmee

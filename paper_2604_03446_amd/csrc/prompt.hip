@@ -28,10 +28,10 @@ bool take_strides(const int64_t *given, uint64_t tokens, uint64_t heads, bool ou
 
 uint64_t up256(uint64_t x) { return (x + 255) & ~(uint64_t)255; }
 
-// One of the three kernels: waves, slots of tiles, pieces, blocks.
+// One of the three kernels: waves, slots of tiles, pieces of a tile at most, blocks.
 struct Launch {
     int waves = 4;
-    uint64_t slots = 0, splits = 1, blocks = 0;
+    uint64_t slots = 0, splits = 1, blocks = 0, room = 0, least = 0;
 };
 
 struct Plan {
@@ -41,22 +41,18 @@ struct Plan {
     uint64_t part_bytes = 0, forward_bytes = 0, backward_bytes = 0;
 };
 
-// Whether blocks that run alone on a unit keep the card busy: more than half of the units in one round, or 7/8 in whole rounds.
-bool fills(uint64_t blocks) { return blocks > 128 && (blocks <= 256 || blocks * 8 >= (blocks + 255) / 256 * 256 * 7); }
-
-// Tiles of 32 rows (or keys) a wave; pieces of at least `least` steps of `across` elements on average (the lengths are not known here), where there
-// are not enough tiles for one round of blocks.
-Launch plan_launch(uint64_t lines, uint64_t seqs, uint64_t kv_heads, uint64_t across, uint64_t step, uint64_t least, bool eight)
+// Tiles of 32 rows (or keys) a wave, `lines` of them in all; `across`: keys (or rows) in all, `step` of them a step.
+Launch plan_launch(uint64_t lines, uint64_t seqs, uint64_t kv_heads, uint64_t across, uint64_t step, bool eight)
 {
     Launch l;
-    for (const int waves : {8, 4}) {
-        l.waves = waves;
-        l.slots = lines / (32 * waves) + seqs;
-        const uint64_t blocks = l.slots * kv_heads, room = 2048 / waves, steps = (across / seqs + step - 1) / step;
-        l.splits = blocks * 4 >= room * 3 ? 1 : std::min<uint64_t>({std::max<uint64_t>(1, steps / least), std::max<uint64_t>(1, room / blocks), 128});
-        l.blocks = blocks * l.splits;
-        if (waves == 8 && eight && lines / seqs >= 256 && fills(l.blocks)) break;
-    }
+    l.waves = eight && lines / seqs >= 256 && (lines / 256 + seqs / 2) * kv_heads > 128 ? 8 : 4;
+    l.slots = lines / (32 * l.waves) + seqs;
+    l.room = 2048 / l.waves;
+    l.least = 512 / step;
+    // Pieces: with four times as many tiles as run at once the last ones fill up what the long ones leave.
+    const uint64_t tiles = std::max<uint64_t>(1, lines / (32 * l.waves) + seqs / 2) * kv_heads;
+    l.splits = tiles >= 4 * l.room ? 1 : std::min<uint64_t>({(3 * l.room + tiles - 1) / tiles, std::max<uint64_t>(1, 4 * across / seqs / step / l.least), 128});
+    l.blocks = l.slots * kv_heads * l.splits;
     return l;
 }
 
@@ -105,11 +101,11 @@ int make_plan(const mmee_prompt_attn *x, bool pointers, Plan &plan)
     p.seqs = x->seqs;
     p.causal = x->causal != 0;
     p.dies = x->kv_heads % 8 == 0;
-    plan.forward = plan_launch(rows, x->seqs, x->kv_heads, x->kv_tokens, 64, 8, plan.dp >= 64);
-    plan.dq = plan_launch(rows, x->seqs, x->kv_heads, x->kv_tokens, 64, 8, plan.dp == 128);
-    plan.dkv = plan_launch(x->kv_tokens, x->seqs, x->kv_heads, rows, 64, 8, plan.dp >= 64);
+    plan.forward = plan_launch(rows, x->seqs, x->kv_heads, x->kv_tokens, 64, plan.dp >= 64);
+    plan.dq = plan_launch(rows, x->seqs, x->kv_heads, x->kv_tokens, 64, plan.dp == 128);
+    plan.dkv = plan_launch(x->kv_tokens, x->seqs, x->kv_heads, rows, plan.dp == 128 ? 32 : 64, plan.dp >= 64);
     for (const Launch *l : {&plan.forward, &plan.dq, &plan.dkv})
-        if (l->blocks > 0x7fffffff) return MMEE_EINVAL;
+        if (l->blocks > 0x7fffffff || l->slots * x->kv_heads * l->waves > 0x7fffffff) return MMEE_EINVAL;
     const auto parts = [&](const Launch &l, uint64_t lines) { return l.splits > 1 ? 4 * l.splits * x->kv_heads * lines * plan.dp : 0; };
     plan.part_bytes = up256(parts(plan.forward, rows));
     plan.forward_bytes = plan.part_bytes ? plan.part_bytes + 4 * plan.forward.splits * x->kv_heads * rows : 0;
@@ -135,7 +131,39 @@ PromptArgs with(const PromptArgs &p, const Launch &l)
     PromptArgs q = p;
     q.slots = (uint32_t)l.slots;
     q.a.splits = (uint32_t)l.splits;
+    q.room_shift = l.waves == 8 ? 8 : 9;
+    q.least = (uint32_t)l.least;
     return q;
+}
+
+// Calls f(8 or 4 waves), 8 where there is such a kernel.
+template <bool EIGHT, class F>
+void with_waves(int waves, F f)
+{
+    if constexpr (EIGHT)
+        if (waves == 8) return f(std::integral_constant<int, 8>());
+    f(std::integral_constant<int, 4>());
+}
+
+template <class T, int DP, int W>
+void forward_as(const PromptArgs &p, const Launch &at, Launching &l)
+{
+    l.run(k_prompt_forward<T, DP, W>, at.blocks, 64 * W, p);
+    if (at.splits > 1) l.run(k_prompt_join<T, DP, W>, at.slots * p.a.kv_heads * W, 256, p);
+}
+
+template <class T, int DP, int W>
+void dq_as(const PromptArgs &p, const Launch &at, Launching &l)
+{
+    l.run(k_prompt_dq<T, DP, W>, at.blocks, 64 * W, p);
+    if (at.splits > 1) l.run(k_prompt_sum<T, DP, W, 64, false>, at.slots * p.a.kv_heads * W, 256, p);
+}
+
+template <class T, int DP, int W>
+void dkv_as(const PromptArgs &p, const Launch &at, Launching &l)
+{
+    l.run(k_prompt_dkv<T, DP, W>, at.blocks, 64 * W, p);
+    if (at.splits > 1) l.run(k_prompt_sum<T, DP, W, DP == 128 ? 32 : 64, true>, at.slots * p.a.kv_heads * W, 256, p);
 }
 
 }  // namespace
@@ -168,14 +196,7 @@ int mmee_prompt_attn_forward(const mmee_prompt_attn *x)
     Launching l;
     if (l.rc) return l.rc;
     dispatch(plan, [&](auto type, auto dp) {
-        using T = decltype(type);
-        if (plan.forward.waves == 8) {
-            if constexpr (dp.value >= 64) l.run(k_prompt_forward<T, dp.value, 8>, plan.forward.blocks, 512, p);
-        } else {
-            l.run(k_prompt_forward<T, dp.value, 4>, plan.forward.blocks, 256, p);
-        }
-        const uint64_t per = 256 / (dp.value / 4);
-        if (p.a.splits > 1) l.run(k_prompt_join<T, dp.value>, ((uint64_t)p.a.kv_heads * p.a.rows + per - 1) / per, 256, p);
+        with_waves<(dp.value >= 64)>(plan.forward.waves, [&](auto w) { forward_as<decltype(type), dp.value, w.value>(p, plan.forward, l); });
     });
     return l.result("prompt attention, forward");
 }
@@ -205,26 +226,8 @@ int mmee_prompt_attn_backward(const mmee_prompt_attn *x, const mmee_prompt_attn_
     Launching l;
     if (l.rc) return l.rc;
     dispatch(plan, [&](auto type, auto dp) {
-        using T = decltype(type);
-        constexpr int DP = dp.value;
-        if (a.rows) {
-            if (plan.dq.waves == 8) {
-                if constexpr (DP == 128) l.run(k_prompt_dq<T, DP, 8>, plan.dq.blocks, 512, dq);
-            } else {
-                l.run(k_prompt_dq<T, DP, 4>, plan.dq.blocks, 256, dq);
-            }
-            const uint64_t per = 256 / (DP / 4);
-            if (dq.a.splits > 1) l.run(k_prompt_sum<T, DP, 0>, ((uint64_t)a.kv_heads * a.rows + per - 1) / per, 256, dq);
-        }
-        if (a.kv_len) {
-            if (plan.dkv.waves == 8) {
-                if constexpr (DP >= 64) l.run(k_prompt_dkv<T, DP, 8>, plan.dkv.blocks, 512, dkv);
-            } else {
-                l.run(k_prompt_dkv<T, DP, 4>, plan.dkv.blocks, 256, dkv);
-            }
-            const uint64_t per = 256 / (DP / 2);
-            if (dkv.a.splits > 1) l.run(k_prompt_sum<T, DP, 1>, ((uint64_t)a.kv_heads * a.kv_len + per - 1) / per, 256, dkv);
-        }
+        if (a.rows) with_waves<(dp.value == 128)>(plan.dq.waves, [&](auto w) { dq_as<decltype(type), dp.value, w.value>(dq, plan.dq, l); });
+        if (a.kv_len) with_waves<(dp.value >= 64)>(plan.dkv.waves, [&](auto w) { dkv_as<decltype(type), dp.value, w.value>(dkv, plan.dkv, l); });
     });
     return l.result("prompt attention, backward");
 }

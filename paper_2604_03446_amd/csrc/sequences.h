@@ -28,4 +28,28 @@ __device__ __forceinline__ int last_at_most(uint32_t n, int64_t x, F value)
 
 __device__ __forceinline__ int64_t within(int64_t x, int64_t lo, int64_t hi) { return x < lo ? lo : x > hi ? hi : x; }
 
+// Sum over the lanes up to a lane's own, and over all of them; the largest of all.
+template <class F>
+__device__ __forceinline__ uint32_t scan_lanes(uint32_t x, F join)
+{
+    x = join(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, false));        // from 1, 2, 4, 8 lanes below within a row of 16
+    x = join(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, false));
+    x = join(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, false));
+    x = join(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, false));
+    x = join(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false));        // row 0's last lane to row 1, row 2's to row 3
+    return join(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false));     // the lower half's last lane to the upper half
+}
+
+__device__ __forceinline__ uint32_t sums_below(uint32_t x)
+{
+    return scan_lanes(x, [](uint32_t a, uint32_t b) { return a + b; });
+}
+
+__device__ __forceinline__ uint32_t sum_of_lanes(uint32_t x) { return __builtin_amdgcn_readlane(sums_below(x), 63); }
+
+__device__ __forceinline__ uint32_t most_of_lanes(uint32_t x)
+{
+    return __builtin_amdgcn_readlane(scan_lanes(x, [](uint32_t a, uint32_t b) { return a > b ? a : b; }), 63);
+}
+
 }  // namespace mmee

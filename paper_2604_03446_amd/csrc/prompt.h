@@ -1,12 +1,11 @@
 // Attention of packed prompts: sequences of different lengths one behind the other, each row over its own sequence's keys, all of them or those
 // up to its own.  Formulas, the folding of query heads into rows, the transposed scores and what is rounded are those of attention.h.
 //
-// A sequence's rows (for dK and dV its keys) are cut into tiles of a block each.  Blocks find theirs from the starts alone, and the host, which
-// does not know the lengths, launches as many as any lengths can need, rows / TILE + seqs a head; those without a tile end at once.
-//   Up to 64 sequences (a lane holds one): tiles in the order of their work, the longest first, whatever sequence they are of, so that the short
-//   ones fill up the end; where there are few tiles, or some far longer than a unit's share, they are cut into pieces of equal length that are
-//   joined afterwards (`pieces_of`).
-//   More sequences: tile t of sequence b has slot (first row of b) / TILE + b + t, which differ whatever the lengths.
+// A sequence's rows (for dK and dV its keys) are cut into tiles of a block each.  The host does not know the lengths: it launches as many blocks as any
+// lengths can need, and those without a tile end at once.  Which tile a block has comes from the starts alone,
+//   by slots: tile t of sequence b has slot (first row of b) / TILE + b + t, which differ whatever the lengths; or
+//   by a plan that k_prompt_plan makes of the starts: the longest tiles first, whatever sequence they are of, so that the short ones fill up the end, and
+//   tiles that are longer than a unit's share cut into pieces of equal length, which are joined afterwards.  It costs a launch, about 5 us.
 #pragma once
 
 #include "attention.h"
@@ -15,153 +14,103 @@
 namespace mmee {
 
 struct PromptArgs {
-    AttnArgs a;                 // batch 1, q_len: all tokens, rows: of all tokens, kv_len: all keys, splits: pieces of a tile at most
+    AttnArgs a;                 // batch 1, q_len: all tokens, rows: of all tokens, kv_len: all keys
     const int32_t *q_starts, *kv_starts;
-    uint32_t seqs, slots;
-    uint32_t room_shift, least; // blocks that run at once (a power of two), steps of a piece at least
+    uint32_t seqs, slots;       // slots: of tiles, or of a plan's entries, of every head
+    const uint32_t *plan;       // the number of entries, and from ENTRIES on the entries; or null
     bool causal;
     bool dies;                  // heads are dealt out to the dies, whose L2 then holds their keys
 };
 
-// A block's tile: rows (or, with KEYS, keys) index * TILE .. of a sequence of m tokens from q0 on over n keys from k0 on, and the steps step0 .. of
-// STEP keys (or rows) that are the block's piece of it.
-template <uint32_t TILE, uint32_t STEP, bool KEYS>
-struct Tile {
-    uint32_t index = 0, q0 = 0, m = 0, k0 = 0, n = 0, kvh, piece, pieces = 1, step0 = 0, count = 0;
-    bool there = false;
+constexpr uint32_t ENTRIES = 8, ENTRY = 8;              // words: q0, m, k0, n, index, step0, count, piece | pieces << 16
 
-    // at: place among heads, tiles and pieces.
-    __device__ __forceinline__ Tile(const PromptArgs &p, uint32_t at)
-    {
-        piece = at % p.a.splits;
-        at /= p.a.splits;
-        const uint32_t order = at % p.slots;
-        kvh = at / p.slots;
-        uint32_t longest = p.least;                     // of a piece, in steps
-        if (p.seqs <= 64) there = by_work(p, order, longest);
-        else there = by_slot(p, p.slots - 1 - order);
-        if (!there) return;
-        const uint32_t steps = steps_of(p, m, n, index);
-        if (p.a.splits > 1) {
-            pieces = (steps + longest - 1) / longest;
-            pieces = pieces < 1 ? 1 : pieces < p.a.splits ? pieces : p.a.splits;
-        }
-        const uint32_t per = pieces > 1 ? (steps + pieces - 1) / pieces : steps;
-        step0 = piece * per < steps ? piece * per : steps;
-        count = step0 + per < steps ? per : steps - step0;
-        there = piece < pieces;
-    }
+// Keys 0 .. of its sequence that a token sees.
+__device__ __forceinline__ uint32_t limit_of(const PromptArgs &p, uint32_t m, uint32_t n, uint32_t token)
+{
+    return p.causal ? (uint32_t)within((int64_t)token + 1 + n - m, 0, n) : n;
+}
 
-    // Of a tile that is there: the same in all lanes, so that loops on its numbers are scalar, and so are the buffers that it is loaded from.  (Said once it is
-    // known to be there; in the constructor, where lanes held numbers of their own, the compiler still made loops over the lanes of every load.)
-    __device__ __forceinline__ void settle()
-    {
-        for (uint32_t *x : {&index, &q0, &m, &k0, &n, &kvh, &piece, &pieces, &step0, &count}) *x = __builtin_amdgcn_readfirstlane(*x);
-    }
+// The first row that sees a key, which may lie before the sequence's first or behind its last one.
+__device__ __forceinline__ int first_row(const PromptArgs &p, uint32_t m, uint32_t n, uint32_t key)
+{
+    return p.causal ? (int)within(((int64_t)key + m - n) * p.a.group, -(1 << 29), (int64_t)m * p.a.group) : 0;
+}
 
-    static __device__ __forceinline__ uint32_t tiles_of(const PromptArgs &p, uint32_t m, uint32_t n) { return ((KEYS ? n : m * p.a.group) + TILE - 1) / TILE; }
-
-    // Keys 0 .. that a token sees.
-    static __device__ __forceinline__ uint32_t limit(const PromptArgs &p, uint32_t m, uint32_t n, uint32_t token)
-    {
-        return p.causal ? (uint32_t)within((int64_t)token + 1 + n - m, 0, n) : n;
-    }
-
-    // The first row that sees a key, which may lie before the first or behind the last one.
-    static __device__ __forceinline__ int first_row(const PromptArgs &p, uint32_t m, uint32_t n, uint32_t key)
-    {
-        return p.causal ? (int)within(((int64_t)key + m - n) * p.a.group, -(1 << 29), (int64_t)m * p.a.group) : 0;
-    }
-
-    static __device__ __forceinline__ uint32_t steps_of(const PromptArgs &p, uint32_t m, uint32_t n, uint32_t index)
-    {
-        const uint32_t rows = m * p.a.group;
-        if (KEYS) {
-            const int begin = first_row(p, m, n, index * TILE);
-            return (rows - (begin < 0 ? 0 : begin) + STEP - 1) / STEP;
-        }
-        const uint32_t behind = (index + 1) * TILE < rows ? (index + 1) * TILE : rows;
-        return (limit(p, m, n, token_of(p.a, behind - 1)) + STEP - 1) / STEP;
-    }
-
-    __device__ __forceinline__ void take(const PromptArgs &p, uint32_t seq)
+// Sequence `seq`: m tokens from q0 on over n keys from k0 on.
+struct Sequence {
+    uint32_t q0, m, k0, n;
+    __device__ __forceinline__ Sequence(const PromptArgs &p, uint32_t seq)
     {
         q0 = (uint32_t)within(p.q_starts[seq], 0, p.a.q_len);
         m = (uint32_t)within(p.q_starts[seq + 1], q0, p.a.q_len) - q0;
         k0 = (uint32_t)within(p.kv_starts[seq], 0, p.a.kv_len);
         n = (uint32_t)within(p.kv_starts[seq + 1], k0, p.a.kv_len) - k0;
     }
-
-    __device__ __forceinline__ bool by_slot(const PromptArgs &p, uint32_t slot)
+    // Rows, or keys, that are cut into tiles; steps of a tile of them: of `step` keys, or rows.
+    __device__ __forceinline__ uint32_t lines(const PromptArgs &p, bool keys) const { return keys ? n : m * p.a.group; }
+    __device__ __forceinline__ uint32_t steps(const PromptArgs &p, bool keys, uint32_t tile, uint32_t step, uint32_t index) const
     {
+        const uint32_t rows = m * p.a.group;
+        if (keys) {
+            const int begin = first_row(p, m, n, index * tile);
+            return (rows - (begin < 0 ? 0 : begin) + step - 1) / step;
+        }
+        const uint32_t behind = (index + 1) * tile < rows ? (index + 1) * tile : rows;
+        return (limit_of(p, m, n, token_of(p.a, behind - 1)) + step - 1) / step;
+    }
+};
+
+// A block's tile: rows (or, with KEYS, keys) index * TILE .. of a sequence, and the steps step0 .. of STEP keys (or rows) that are the block's piece of it.
+template <uint32_t TILE, uint32_t STEP, bool KEYS>
+struct Tile {
+    uint32_t index, q0, m, k0, n, kvh, piece = 0, pieces = 1, step0 = 0, count = 0, slot;
+    bool there;
+
+    // at: place among heads and slots.
+    __device__ __forceinline__ Tile(const PromptArgs &p, uint32_t at)
+    {
+        kvh = p.dies ? at / p.slots : at % p.a.kv_heads;
+        slot = p.dies ? at % p.slots : at / p.a.kv_heads;
+        if (p.plan) {
+            there = slot < p.plan[0];
+            if (!there) return;
+            const uint32_t *e = p.plan + ENTRIES + ENTRY * slot;
+            q0 = e[0];
+            m = e[1];
+            k0 = e[2];
+            n = e[3];
+            index = e[4];
+            step0 = e[5];
+            count = e[6];
+            piece = e[7] & 0xffff;
+            pieces = e[7] >> 16;
+            return;
+        }
         const int32_t *starts = KEYS ? p.kv_starts : p.q_starts;
         const uint32_t tokens = KEYS ? p.a.kv_len : p.a.q_len, each = KEYS ? 1 : p.a.group;
         const auto slot_of = [&](uint32_t i) { return (int64_t)((uint32_t)within(starts[i], 0, tokens) * each / TILE + i); };
         const int seq = __builtin_amdgcn_readfirstlane(last_at_most(p.seqs, slot, slot_of));
-        if (seq < 0) return false;
-        take(p, seq);
+        there = false;
+        if (seq < 0) return;
+        const Sequence s(p, seq);
+        q0 = s.q0;
+        m = s.m;
+        k0 = s.k0;
+        n = s.n;
         index = slot - (uint32_t)slot_of(seq);
-        return index < tiles_of(p, m, n);
+        there = index < (s.lines(p, KEYS) + TILE - 1) / TILE;
+        if (there) count = s.steps(p, KEYS, TILE, STEP, index);
     }
 
-    // Tiles have levels, about their length in tiles: with a causal mask those of a sequence are neighbours, else they are the same.
-    __device__ __forceinline__ bool by_work(const PromptArgs &p, uint32_t order, uint32_t &longest)
+    // Of a tile that is there: the same in all lanes, so that loops on its numbers are scalar, and so are the buffers that it is loaded from.  (Said once it is
+    // known to be there: in the constructor the compiler still made loops over the lanes of every load, 8 % of the forward pass's time.)
+    __device__ __forceinline__ void settle()
     {
-        const uint32_t lane = threadIdx.x & 63;
-        uint32_t tiles = 0, base = 0;
-        if (lane < p.seqs) {
-            take(p, lane);
-            tiles = tiles_of(p, m, n);
-            if (KEYS) base = p.causal ? 0 : m * p.a.group / STEP;
-            else base = p.causal ? (n > m ? (n - m) * p.a.group / TILE : 0) : n / STEP;
-        }
-        if (order >= sum_of_lanes(tiles)) return false;
-        // tiles of a sequence at this level or above
-        const auto above = [&](uint32_t level) {
-            if (!p.causal) return base >= level ? tiles : 0;
-            return level <= base ? tiles : level < base + tiles ? base + tiles - level : 0;
-        };
-        uint32_t low = 0, high = p.seqs == 1 && p.causal ? base + tiles : most_of_lanes(p.causal ? base + tiles : base + 1);
-        high = __builtin_amdgcn_readfirstlane(high);
-        while (high - low > 1) {
-            const uint32_t mid = (low + high) / 2;
-            if (sum_of_lanes(above(mid)) > order) low = mid;
-            else high = mid;
-        }
-        const uint32_t here = above(low) - above(low + 1), rank = order - sum_of_lanes(above(low + 1)), below = sums_below(here) - here;
-        const uint64_t owner = __ballot(rank >= below && rank < below + here);
-        const uint32_t seq = (uint32_t)__builtin_ctzll(owner);
-        index = p.causal ? (KEYS ? tiles - 1 - (low - base) : low - base) : rank - below;
-        if (p.a.splits > 1) longest = pieces_of(p, tiles);
-        index = __builtin_amdgcn_readlane(index, seq);
-        q0 = __builtin_amdgcn_readlane(q0, seq);
-        m = __builtin_amdgcn_readlane(m, seq);
-        k0 = __builtin_amdgcn_readlane(k0, seq);
-        n = __builtin_amdgcn_readlane(n, seq);
-        return true;
+        for (uint32_t *x : {&index, &q0, &m, &k0, &n, &kvh, &piece, &pieces, &step0, &count, &slot}) *x = __builtin_amdgcn_readfirstlane(*x);
     }
 
-    // The length that pieces may have: what each of the blocks that run at once gets of all steps.  Where there are fewer tiles than such blocks, the least
-    // up to three times that with which all pieces run at once.  (The kernels that join the pieces come to the same ones: whole numbers, and products of
-    // floats that nothing is added to.)
-    __device__ __forceinline__ uint32_t pieces_of(const PromptArgs &p, uint32_t tiles) const
-    {
-        const uint32_t a = tiles ? steps_of(p, m, n, 0) : 0, b = tiles ? steps_of(p, m, n, tiles - 1) : 0;
-        const uint32_t most = a > b ? a : b, least = a > b ? b : a;
-        const uint32_t own = (uint32_t)((uint64_t)tiles * (a + b) >> 4);                // in 8 steps, on average over the tiles: below 2^31 in all
-        const uint64_t share = (uint64_t)sum_of_lanes(own) * p.a.kv_heads * 8 >> p.room_shift, blocks = (uint64_t)sum_of_lanes(tiles) * p.a.kv_heads;
-        const uint32_t low = share > p.least ? (uint32_t)share : p.least;
-        if (blocks >> p.room_shift) return low;
-        uint32_t no = low - 1, yes = 3 * low;
-        while (yes - no > 1 + low / 16) {
-            const uint32_t mid = (no + yes) / 2;
-            const float inverse = 1.0f / (float)mid;
-            const uint32_t wanted = most - least < mid ? tiles * ((most + mid - 1) / mid) : (uint32_t)((float)own * (8.0f * inverse)) + tiles / 2 + 1;
-            if (((uint64_t)sum_of_lanes(tiles ? wanted : 0) * p.a.kv_heads - 1) >> p.room_shift == 0) yes = mid;
-            else no = mid;
-        }
-        return yes;
-    }
+    // The tile's place among pieces of all heads.
+    __device__ __forceinline__ int64_t part(const PromptArgs &p) const { return ((int64_t)kvh * p.slots + slot) * TILE; }
 
     // Keys of the sequence as the tiles' loads want them.
     __device__ __forceinline__ Keys<MODE_PLAIN> keys(const PromptArgs &p) const
@@ -171,6 +120,148 @@ struct Tile {
         return k;
     }
 };
+
+// A plan to be made: tiles of `tile` rows or keys, steps of `step` keys or rows.
+struct PlanOf {
+    uint32_t *plan;
+    uint32_t tile, step, slots;
+    uint32_t room, least;       // blocks of all heads that run at once, steps of a piece at least (0: no pieces)
+    bool keys;
+};
+
+struct PlanArgs {
+    PromptArgs p;
+    PlanOf of[2];
+};
+
+constexpr uint32_t PLAN_SEQS = 2048, PLAN_TILES = 8192; // at most
+
+// Plans of[blockIdx.x].  Tiles are sorted by the length of their pieces in 1024 classes; which of a class come first does not matter to any result.
+// One block; for prompts of 17 to 2500 rows 5 us, of which most is the latency of the starts and of a dozen barriers.
+__global__ __launch_bounds__(1024) void k_prompt_plan(const PlanArgs x)
+{
+    constexpr uint32_t MINE = PLAN_TILES / 1024, CLASSES = 1024;
+    const PromptArgs &p = x.p;
+    const PlanOf &of = x.of[blockIdx.x];
+    __shared__ uint32_t first_tile[PLAN_SEQS + 1];
+    __shared__ uint32_t classes[CLASSES], sums[16], more[16];
+    const uint32_t thread = threadIdx.x, lane = thread & 63, wave = thread >> 6;
+
+    // the sum of all threads' x, and the largest y; sums_before: of the threads before this one
+    uint32_t sum_before = 0, sum_all = 0, most_all = 0;
+    const auto reduce = [&](uint32_t a, uint32_t b) {
+        const uint32_t upto = sums_below(a), most = most_of_lanes(b);
+        if (lane == 63) sums[wave] = upto;
+        if (lane == 0) more[wave] = most;
+        __syncthreads();
+        const uint32_t other = lane < 16 ? sums[lane] : 0, below = sums_below(other), top = most_of_lanes(lane < 16 ? more[lane] : 0);
+        sum_all = __builtin_amdgcn_readlane(below, 15);
+        sum_before = upto - a + (wave ? __shfl(below, wave - 1) : 0);
+        most_all = top;
+        __syncthreads();
+    };
+
+    uint32_t tiles = 0;
+    for (uint32_t from = 0; from < p.seqs; from += 1024) {
+        const uint32_t seq = from + thread;
+        const uint32_t here = seq < p.seqs ? (Sequence(p, seq).lines(p, of.keys) + of.tile - 1) / of.tile : 0;
+        reduce(here, 0);
+        if (seq < p.seqs) first_tile[seq] = tiles + sum_before;
+        tiles += sum_all;
+    }
+    classes[thread] = 0;
+    if (thread == 0) first_tile[p.seqs] = tiles;
+    __syncthreads();
+    if (tiles > PLAN_TILES) tiles = PLAN_TILES;         // (starts that do not ascend)
+
+    // This thread's tiles: which sequence, how many steps.
+    uint32_t steps[MINE], seqs[MINE], total = 0, longest = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < MINE; ++i) {
+        const uint32_t t = i * 1024 + thread;
+        steps[i] = seqs[i] = 0;
+        if (i * 1024 >= tiles) continue;                // by the whole block
+        if (t < tiles) {
+            uint32_t low = 0, high = p.seqs;            // first_tile[low] <= t < first_tile[high]
+            while (high - low > 1) {
+                const uint32_t mid = (low + high) / 2;
+                if (first_tile[mid] <= t) low = mid;
+                else high = mid;
+            }
+            seqs[i] = low;
+            steps[i] = Sequence(p, low).steps(p, of.keys, of.tile, of.step, t - first_tile[low]);
+            total += (steps[i] + 7) / 8;                // in 8 steps: below 2^32
+            longest = steps[i] > longest ? steps[i] : longest;
+        }
+    }
+    reduce(total, longest);
+
+    // The length that pieces may have.  With tiles enough to go round: half of what a unit gets of all steps, so that the last ones even it out.  With
+    // fewer: the least with which all pieces run at once, up to three times a unit's share; every wave tries one of sixteen, twice.
+    uint32_t size = most_all ? most_all : 1;
+    if (of.least) {
+        const uint64_t share = (uint64_t)sum_all * 8 * p.a.kv_heads / of.room;
+        uint32_t low = (uint32_t)share > of.least ? (uint32_t)share : of.least;
+        if ((uint64_t)tiles * p.a.kv_heads >= of.room || tiles > 1024) {
+            low = (uint32_t)(share / 2) > of.least ? (uint32_t)(share / 2) : of.least;
+        } else {
+            classes[thread] = steps[0];
+            __syncthreads();
+            uint32_t width = 2 * low;
+            for (int round = 0; round < 2; ++round) {
+                const uint32_t candidate = low + width * wave / 16;
+                uint32_t wanted = 0;
+                for (uint32_t t = lane; t < tiles; t += 64) wanted += classes[t] ? (classes[t] + candidate - 1) / candidate : 1;
+                wanted = sum_of_lanes(wanted);
+                if (lane == 0) more[wave] = (uint64_t)wanted * p.a.kv_heads <= of.room;
+                __syncthreads();
+                const uint32_t fits = (uint32_t)__ballot(lane < 16 && more[lane & 15]), first = fits ? __builtin_ctz(fits) : 15;
+                __syncthreads();
+                if (round == 0 && first) low += width * (first - 1) / 16;
+                else low += width * first / 16;
+                width = (width + 15) / 16;
+            }
+        }
+        size = low;
+    }
+    __syncthreads();
+    classes[thread] = 0;
+    __syncthreads();
+
+    // Tiles' pieces, sorted by their length.
+    const uint32_t top = size < most_all ? size : most_all ? most_all : 1;
+    const auto pieces_of = [&](uint32_t of_steps) { return of_steps > size ? (of_steps + size - 1) / size : 1; };
+    const auto class_of = [&](uint32_t length) {
+        const uint32_t c = (uint32_t)((float)length * ((CLASSES - 1) / (float)top));
+        return CLASSES - 1 - (c < CLASSES ? c : CLASSES - 1);
+    };
+#pragma unroll
+    for (uint32_t i = 0; i < MINE; ++i)
+        if (i * 1024 + thread < tiles) {
+            const uint32_t pieces = pieces_of(steps[i]);
+            atomicAdd(&classes[class_of((steps[i] + pieces - 1) / pieces)], pieces);
+        }
+    __syncthreads();
+    const uint32_t own = classes[thread];
+    reduce(own, 0);
+    classes[thread] = sum_before;
+    if (thread == 0) of.plan[0] = sum_all <= of.slots ? sum_all : 0;        // (more only of sequences that overlap)
+    __syncthreads();
+    if (sum_all > of.slots) return;
+#pragma unroll
+    for (uint32_t i = 0; i < MINE; ++i)
+        if (i * 1024 + thread < tiles) {
+            const uint32_t pieces = pieces_of(steps[i]), per = (steps[i] + pieces - 1) / pieces, index = i * 1024 + thread - first_tile[seqs[i]];
+            const uint32_t at = atomicAdd(&classes[class_of(per)], pieces);
+            const Sequence q(p, seqs[i]);
+            for (uint32_t k = 0; k < pieces; ++k) {
+                const uint32_t step0 = k * per < steps[i] ? k * per : steps[i], count = step0 + per < steps[i] ? per : steps[i] - step0;
+                u32x4 *e = reinterpret_cast<u32x4 *>(of.plan + ENTRIES + ENTRY * (at + k));
+                e[0] = u32x4{q.q0, q.m, q.k0, q.n};
+                e[1] = u32x4{index, step0, count, k | pieces << 16};
+            }
+        }
+}
 
 __device__ __forceinline__ uint32_t block_place(const PromptArgs &p) { return p.dies ? by_die(blockIdx.x, gridDim.x) : blockIdx.x; }
 
@@ -196,7 +287,7 @@ __global__ __launch_bounds__(64 * W, 2) void k_prompt_forward(const PromptArgs p
     const int thread = threadIdx.x, lane = thread & 63, n = lane & 31, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
     const uint32_t rows = tile.m * a.group, row0 = tile.index * 32 * W, row = row0 + 32 * wave + n, step0 = tile.step0, count = tile.count;
     const bool live = row < rows;
-    const uint32_t limit = tile.limit(p, tile.m, tile.n, token_of(a, live ? row : rows - 1)), all_see = tile.limit(p, tile.m, tile.n, token_of(a, row0));
+    const uint32_t limit = limit_of(p, tile.m, tile.n, token_of(a, live ? row : rows - 1)), all_see = limit_of(p, tile.m, tile.n, token_of(a, row0));
 
     const Keys<MODE_PLAIN> keys = tile.keys(p);
     const uint16_t *const k_at = a.k + tile.k0 * a.ks.token, *const v_at = a.v + tile.k0 * a.vs.token;
@@ -216,6 +307,15 @@ __global__ __launch_bounds__(64 * W, 2) void k_prompt_forward(const PromptArgs p
 
     auto load_keys = [&](uint32_t s) { sk.load(keys, k_at, a.ks, thread, first_of(s), 0); };
     auto load_values = [&](uint32_t s) { sv.load(keys, v_at, a.vs, thread, first_of(s), 0); };
+    // Operands: of the product i of a tile's scores (keys 32 (i mod 2) .., columns 16 (i / 2) .. of the head), and of the product i with its values
+    // (columns 32 (i mod DT) .., keys 16 (i / DT) ..).
+    constexpr int DT = DP / 32;
+    auto key_operand = [&](uint32_t s, int i) { return k_tile(s)[32 * (i % MT) * CH + chunk_at<CH>(n, 2 * (i / MT) + h)]; };
+    auto value_operand = [&](s16x4 (&to)[2], uint32_t s, int i) {
+        const int l = lane & 15, c = 4 * (i % DT) + 2 * ((lane >> 4) & 1) + ((l >> 1) & 1);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) to[j] = read_transposed(reinterpret_cast<const char *>(v_tile(s) + 16 * (i / DT) * CH + chunk_at<CH>(4 * h + (l >> 2) + 8 * j, c)) + 8 * (l & 1));
+    };
     auto scores = [&](f32x16 (&to)[MT], uint32_t s) {
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) to[mt] = keys_by_rows<T, DP>(k_tile(s), 32 * mt, q);
@@ -254,12 +354,12 @@ __global__ __launch_bounds__(64 * W, 2) void k_prompt_forward(const PromptArgs p
         for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) now[mt][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(now[mt][r], a.scale_log2, -off));
+            to[mt][0][0] = rounded<T>(now[mt], 0);
+            to[mt][1][0] = rounded<T>(now[mt], 1);
             float sum = 0.0f;
 #pragma unroll
             for (int r = 0; r < 16; ++r) sum += now[mt][r];
             total += sum;
-            to[mt][0][0] = rounded<T>(now[mt], 0);
-            to[mt][1][0] = rounded<T>(now[mt], 1);
         }
     };
     auto values = [&](uint32_t s, const typename T::V8 (&of)[MT][2][1]) {
@@ -286,57 +386,68 @@ __global__ __launch_bounds__(64 * W, 2) void k_prompt_forward(const PromptArgs p
         __syncthreads();
         load_keys(2);
 
-        // Tile s from its scores `now`; unless it is the last, the next one's scores into `next`.
-        auto step = [&](uint32_t s, f32x16 (&now)[MT], f32x16 (&next)[MT], auto more, auto masked) {
+        // Tile s from its scores `now`; the next one's scores into `next`.  In slots of one product, the read of an operand that is wanted some products later
+        // and a share of the vector instructions, in this order: left to itself the compiler reads every operand right before its use.
+        auto step = [&](uint32_t s, f32x16 (&now)[MT], f32x16 (&next)[MT], auto masked) {
+            constexpr int KP = MT * DP / 16, VP = KP, AHEAD = W == 8 ? 3 : 2, EACH = 16 * MT / KP;
             typename T::V8 pr[MT][2][1];
-            constexpr int PRODUCTS = MT * DP / 16;
-            if (more) scores(next, s + 1);
-            exponentials(now, pr);
-            if (more) {
-                // in one block of straight-line code: a product after every operand read and a share of the exponentials' work
-                asm volatile("" ::"v"(total));
+            u32x4 ko[AHEAD];
+            s16x4 vo[AHEAD][2];
+            const float off = top == -INFINITY ? 0.0f : top;
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
+            for (int i = 0; i < AHEAD; ++i) ko[i] = key_operand(s + 1, i);
 #pragma unroll
-                    for (int part = 0; part < 2; ++part) asm volatile("" ::"v"(pr[mt][part][0]));
-                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            for (int i = 0; i < KP; ++i) {
+                next[i % MT] = T::mma(as_operand<T>(ko[i % AHEAD]), q[i / MT], i < MT ? f32x16{} : next[i % MT]);
+                if (i + AHEAD < KP) ko[i % AHEAD] = key_operand(s + 1, i + AHEAD);
+                else value_operand(vo[i + AHEAD - KP], s, i + AHEAD - KP);
 #pragma unroll
-                for (int i = 0; i < PRODUCTS; ++i) {
-                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-                    __builtin_amdgcn_sched_group_barrier(0x002, (MT * 56 + PRODUCTS - 1) / PRODUCTS, 0);
+                for (int e = i * EACH; e < (i + 1) * EACH; ++e) {
+                    now[e / 16][e % 16] = __builtin_amdgcn_exp2f(__builtin_fmaf(now[e / 16][e % 16], a.scale_log2, -off));
+                    total += now[e / 16][e % 16];
+                    if (e % 8 == 7) pr[e / 16][e / 8 % 2][0] = rounded<T>(now[e / 16], e / 8 % 2);
                 }
-                if (masked) mask(next, s + 1);
+                __builtin_amdgcn_sched_barrier(0);
             }
-            values(s, pr);
-            if (!more) return;
-            most = maximum(next);
-            __builtin_amdgcn_sched_group_barrier(0x100, 4, 1);
+            if (masked) mask(next, s + 1);
+            float m = next[0][0];
 #pragma unroll
-            for (int i = 0; i < PRODUCTS; ++i) {
-                __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
-                __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
-                __builtin_amdgcn_sched_group_barrier(0x002, 2, 1);
+            for (int i = 0; i < VP; ++i) {
+                o[i % DT] = T::mma(join<T>(vo[i % AHEAD][0], vo[i % AHEAD][1]), pr[i / DT / 2][i / DT % 2][0], o[i % DT]);
+                if (i + AHEAD < VP) value_operand(vo[i % AHEAD], s, i + AHEAD);
+#pragma unroll
+                for (int e = i * EACH; e < (i + 1) * EACH; ++e) m = __builtin_elementwise_maximum(m, next[e / 16][e % 16]);
+                if (i == VP / 4) {                      // tiles that nobody reads any more since the last barrier
+                    sk.store(k_tile(s), thread);
+                    sv.store(v_tile(s + 1), thread);
+                }
+                if (i == VP / 2) {
+                    load_keys(s + 3);
+                    load_values(s + 2);
+                }
+                __builtin_amdgcn_sched_barrier(0);
             }
+            most = m;
             raise();
-            sk.store(k_tile(s), thread);
-            sv.store(v_tile(s + 1), thread);
             __syncthreads();
-            load_keys(s + 3);
-            load_values(s + 2);
+        };
+        auto last = [&](uint32_t s, f32x16 (&now)[MT]) {
+            typename T::V8 pr[MT][2][1];
+            exponentials(now, pr);
+            values(s, pr);
         };
         uint32_t s = 0;
         for (; s + 3 < count && first_of(s + 3) <= all_see; s += 2) {       // tiles s + 1 and s + 2 are seen whole by every row
-            step(s, x, ahead, std::true_type(), std::false_type());
-            step(s + 1, ahead, x, std::true_type(), std::false_type());
+            step(s, x, ahead, std::false_type());
+            step(s + 1, ahead, x, std::false_type());
         }
 #pragma unroll 1
         for (; s + 1 < count; ++s) {
-            step(s, x, ahead, std::true_type(), std::true_type());
+            step(s, x, ahead, std::true_type());
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) x[mt] = ahead[mt];
         }
-        step(s, x, ahead, std::false_type(), std::false_type());
+        last(s, x);
     }
     total = sum_of_halves(total);
     if (!live) return;
@@ -345,7 +456,7 @@ __global__ __launch_bounds__(64 * W, 2) void k_prompt_forward(const PromptArgs p
         store_row<T, DP>(a.o + tile.q0 * a.os.token + row_at(a, a.os, 0, tile.kvh, row), o, times, a.head_dim);
         if (a.lse && h == 0) a.lse[lse_at(a, 0, tile.kvh, row) + tile.q0] = sum2 * LN2;
     } else {
-        const int64_t line = ((int64_t)tile.piece * a.kv_heads + tile.kvh) * a.rows + tile.q0 * a.group + row;
+        const int64_t line = tile.part(p) + 32 * wave + n;
         store_part<DP>(a.part_o + line * DP, o, times);
         if (h == 0) a.part_lse[line] = sum2;
     }
@@ -357,23 +468,22 @@ __global__ __launch_bounds__(256) void k_prompt_join(const PromptArgs p)
 {
     constexpr int C4 = DP / 4;
     const AttnArgs &a = p.a;
-    Tile<32 * W, 64, false> tile(p, blockIdx.x / W * a.splits);
-    if (!tile.there || tile.pieces == 1) return;
+    Tile<32 * W, 64, false> tile(p, blockIdx.x / W);
+    if (!tile.there || tile.piece || tile.pieces == 1) return;
     tile.settle();
-    const int64_t next = (int64_t)a.kv_heads * a.rows;
     for (uint32_t i = threadIdx.x; i < 32 * C4; i += 256) {
-        const uint32_t row = tile.index * 32 * W + blockIdx.x % W * 32 + i / C4, c = i % C4;
+        const uint32_t within_tile = blockIdx.x % W * 32 + i / C4, row = tile.index * 32 * W + within_tile, c = i % C4;
         if (row >= tile.m * a.group) return;
-        const int64_t line = (int64_t)tile.kvh * a.rows + tile.q0 * a.group + row;
+        const int64_t line = tile.part(p) + within_tile;
         float high = -INFINITY, sum = 0.0f;
-        for (uint32_t s = 0; s < tile.pieces; ++s) high = __builtin_elementwise_maximum(high, a.part_lse[s * next + line]);
+        for (uint32_t s = 0; s < tile.pieces; ++s) high = __builtin_elementwise_maximum(high, a.part_lse[line + s * 32 * W]);
         const float off = high == -INFINITY ? 0.0f : high;
         f32x4 x = {0, 0, 0, 0};
 #pragma unroll 4
         for (uint32_t s = 0; s < tile.pieces; ++s) {
-            const float w = __builtin_amdgcn_exp2f(a.part_lse[s * next + line] - off);
+            const float w = __builtin_amdgcn_exp2f(a.part_lse[line + s * 32 * W] - off);
             sum += w;
-            x += *reinterpret_cast<const f32x4 *>(a.part_o + (s * next + line) * DP + 4 * c) * w;
+            x += *reinterpret_cast<const f32x4 *>(a.part_o + (line + s * 32 * W) * DP + 4 * c) * w;
         }
         x *= sum != 0.0f ? 1.0f / sum : 0.0f;
         if (4 * c < a.head_dim) *reinterpret_cast<typename T::V4 *>(a.o + tile.q0 * a.os.token + row_at(a, a.os, 0, tile.kvh, row) + 4 * c) = __builtin_convertvector(x, typename T::V4);
@@ -394,7 +504,7 @@ __global__ __launch_bounds__(64 * W, 2) void k_prompt_dq(const PromptArgs p)
     const int thread = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(thread >> 6), lane = thread & 63, n = lane & 31, h = lane >> 5;
     const uint32_t rows = tile.m * a.group, row = tile.index * 32 * W + 32 * wave + n, step0 = tile.step0, count = tile.count;
     const bool live = row < rows;
-    const uint32_t limit = tile.limit(p, tile.m, tile.n, token_of(a, live ? row : rows - 1));
+    const uint32_t limit = limit_of(p, tile.m, tile.n, token_of(a, live ? row : rows - 1));
 
     const Keys<MODE_PLAIN> keys = tile.keys(p);
     const uint16_t *const k_at = a.k + tile.k0 * a.ks.token, *const v_at = a.v + tile.k0 * a.vs.token;
@@ -463,7 +573,7 @@ __global__ __launch_bounds__(64 * W, 2) void k_prompt_dq(const PromptArgs p)
     }
     const float times = NARROW<T> ? a.scale * __builtin_amdgcn_exp2f(-(UP + HIGHEST + lowered)) : a.scale;
     if (tile.pieces == 1) store_row<T, DP>(a.dq + tile.q0 * a.dqs.token + row_at(a, a.dqs, 0, tile.kvh, row), dq[0], times, a.head_dim);
-    else store_part<DP>(a.part_o + ((int64_t)tile.piece * a.kv_heads * a.rows + line) * DP, dq[0], times);
+    else store_part<DP>(a.part_o + (tile.part(p) + 32 * wave + n) * DP, dq[0], times);
 }
 
 // dK and dV of 32 W keys, 32 a wave, over the rows that see them, as k_attn_dkv.
@@ -482,8 +592,8 @@ __global__ __launch_bounds__(64 * W, 2) void k_prompt_dkv(const PromptArgs p)
     tile.settle();
     const int thread = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(thread >> 6), lane = thread & 63, n = lane & 31, h = lane >> 5;
     const uint32_t rows = tile.m * a.group, key0 = tile.index * 32 * W, key = key0 + 32 * wave + n;
-    const int own = tile.first_row(p, tile.m, tile.n, key), all_see = tile.first_row(p, tile.m, tile.n, key0 + 32 * W - 1);
-    const int first_seen = tile.first_row(p, tile.m, tile.n, key0);
+    const int own = first_row(p, tile.m, tile.n, key), all_see = first_row(p, tile.m, tile.n, key0 + 32 * W - 1);
+    const int first_seen = first_row(p, tile.m, tile.n, key0);
     const uint32_t begin = first_seen < 0 ? 0 : first_seen, step0 = tile.step0, count = tile.count;
 
     const bool valid = key < tile.n;
@@ -575,7 +685,7 @@ __global__ __launch_bounds__(64 * W, 2) void k_prompt_dkv(const PromptArgs p)
         store_row<T, DP>(a.dk + key_at * a.dks.token + tile.kvh * a.dks.head, dk[0], times, a.head_dim);
         store_row<T, DP>(a.dv + key_at * a.dvs.token + tile.kvh * a.dvs.head, dv[0], times_v, a.head_dim);
     } else {
-        float *part = a.part_o + ((((int64_t)tile.piece * a.kv_heads + tile.kvh) * a.kv_len + key_at) * 2) * DP;
+        float *part = a.part_o + (tile.part(p) + 32 * wave + n) * 2 * DP;
         store_part<DP>(part, dk[0], times);
         store_part<DP>(part + DP, dv[0], times_v);
     }
@@ -587,19 +697,18 @@ __global__ __launch_bounds__(256) void k_prompt_sum(const PromptArgs p)
 {
     constexpr int C4 = DP / 4 * (KEYS ? 2 : 1);
     const AttnArgs &a = p.a;
-    Tile<32 * W, STEP, KEYS> tile(p, blockIdx.x / W * a.splits);
-    if (!tile.there || tile.pieces == 1) return;
+    Tile<32 * W, STEP, KEYS> tile(p, blockIdx.x / W);
+    if (!tile.there || tile.piece || tile.pieces == 1) return;
     tile.settle();
     const uint32_t lines = KEYS ? tile.n : tile.m * a.group;
-    const int64_t next = (int64_t)a.kv_heads * (KEYS ? a.kv_len : a.rows);
     for (uint32_t i = threadIdx.x; i < 32 * C4; i += 256) {
-        const uint32_t own = tile.index * 32 * W + blockIdx.x % W * 32 + i / C4, c = i % C4, d = 4 * c % DP;
+        const uint32_t within_tile = blockIdx.x % W * 32 + i / C4, own = tile.index * 32 * W + within_tile, c = i % C4, d = 4 * c % DP;
         if (own >= lines) return;
         if (d >= a.head_dim) continue;
-        const int64_t line = KEYS ? (int64_t)tile.kvh * a.kv_len + tile.k0 + own : (int64_t)tile.kvh * a.rows + tile.q0 * a.group + own;
+        const int64_t line = tile.part(p) + within_tile;
         f32x4 x = {0, 0, 0, 0};
 #pragma unroll 4
-        for (uint32_t s = 0; s < tile.pieces; ++s) x += *reinterpret_cast<const f32x4 *>(a.part_o + ((s * next + line) * C4 + c) * 4);
+        for (uint32_t s = 0; s < tile.pieces; ++s) x += *reinterpret_cast<const f32x4 *>(a.part_o + ((line + s * 32 * W) * C4 + c) * 4);
         uint16_t *to;
         if (!KEYS) to = a.dq + tile.q0 * a.dqs.token + row_at(a, a.dqs, 0, tile.kvh, own);
         else if (4 * c < DP) to = a.dk + (int64_t)(tile.k0 + own) * a.dks.token + tile.kvh * a.dks.head;

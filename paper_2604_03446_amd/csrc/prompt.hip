@@ -28,31 +28,41 @@ bool take_strides(const int64_t *given, uint64_t tokens, uint64_t heads, bool ou
 
 uint64_t up256(uint64_t x) { return (x + 255) & ~(uint64_t)255; }
 
-// One of the three kernels: waves, slots of tiles, pieces of a tile at most, blocks.
+// One of the three kernels: waves of a block, slots of tiles a head, blocks; whether it has a plan, and one with pieces.
 struct Launch {
     int waves = 4;
-    uint64_t slots = 0, splits = 1, blocks = 0, room = 0, least = 0;
+    uint64_t slots = 0, blocks = 0, room = 0, step = 0, least = 0;
+    bool planned = false, pieces = false;
+    uint64_t plan_bytes() const { return planned ? up256(4 * (ENTRIES + ENTRY * slots)) : 0; }
+    // Results of pieces, so many floats a row or key.
+    uint64_t parts_bytes(uint64_t kv_heads, uint64_t floats) const { return pieces ? up256(4 * slots * kv_heads * 32 * waves * floats) : 0; }
 };
 
 struct Plan {
     PromptArgs p = {};
     int dp = 0, dtype = 0;
     Launch forward, dq, dkv;
-    uint64_t part_bytes = 0, forward_bytes = 0, backward_bytes = 0;
+    uint64_t forward_bytes = 0, backward_bytes = 0;
 };
 
-// Tiles of 32 rows (or keys) a wave, `lines` of them in all; `across`: keys (or rows) in all, `step` of them a step.
-Launch plan_launch(uint64_t lines, uint64_t seqs, uint64_t kv_heads, uint64_t across, uint64_t step, bool eight)
+// Tiles of 32 rows (or keys) a wave, `lines` of them in all; `across`: keys (or rows) in all, `step` of them a step.  The lengths are not known here: a
+// sequence is taken to be as long as the average.
+Launch plan_launch(uint64_t lines, uint64_t seqs, uint64_t kv_heads, uint64_t across, uint64_t step, bool causal, bool eight)
 {
     Launch l;
     l.waves = eight && lines / seqs >= 256 && (lines / 256 + seqs / 2) * kv_heads > 128 ? 8 : 4;
     l.slots = lines / (32 * l.waves) + seqs;
     l.room = 2048 / l.waves;
+    l.step = step;
     l.least = 512 / step;
-    // Pieces: with four times as many tiles as run at once the last ones fill up what the long ones leave.
-    const uint64_t tiles = std::max<uint64_t>(1, lines / (32 * l.waves) + seqs / 2) * kv_heads;
-    l.splits = tiles >= 4 * l.room ? 1 : std::min<uint64_t>({(3 * l.room + tiles - 1) / tiles, std::max<uint64_t>(1, 4 * across / seqs / step / l.least), 128});
-    l.blocks = l.slots * kv_heads * l.splits;
+    const uint64_t tiles = std::max<uint64_t>(1, lines / (32 * l.waves) + seqs / 2), blocks = tiles * kv_heads, steps = across / seqs / step;
+    if (seqs <= PLAN_SEQS && l.slots <= PLAN_TILES) {
+        // Four times as many tiles as run at once even out the end by themselves.
+        l.pieces = blocks < 4 * l.room && steps >= 2 * l.least;
+        l.planned = l.pieces || ((causal || seqs > 1) && blocks > l.room && blocks * steps / l.room > 48);
+    }
+    if (l.pieces) l.slots += 3 * l.room / kv_heads + 1;
+    l.blocks = l.slots * kv_heads;
     return l;
 }
 
@@ -101,15 +111,14 @@ int make_plan(const mmee_prompt_attn *x, bool pointers, Plan &plan)
     p.seqs = x->seqs;
     p.causal = x->causal != 0;
     p.dies = x->kv_heads % 8 == 0;
-    plan.forward = plan_launch(rows, x->seqs, x->kv_heads, x->kv_tokens, 64, plan.dp >= 64);
-    plan.dq = plan_launch(rows, x->seqs, x->kv_heads, x->kv_tokens, 64, plan.dp == 128);
-    plan.dkv = plan_launch(x->kv_tokens, x->seqs, x->kv_heads, rows, plan.dp == 128 ? 32 : 64, plan.dp >= 64);
+    plan.forward = plan_launch(rows, x->seqs, x->kv_heads, x->kv_tokens, 64, p.causal, plan.dp >= 64);
+    plan.dq = plan_launch(rows, x->seqs, x->kv_heads, x->kv_tokens, 64, p.causal, plan.dp == 128);
+    plan.dkv = plan_launch(x->kv_tokens, x->seqs, x->kv_heads, rows, plan.dp == 128 ? 32 : 64, p.causal, plan.dp >= 64);
     for (const Launch *l : {&plan.forward, &plan.dq, &plan.dkv})
-        if (l->blocks > 0x7fffffff || l->slots * x->kv_heads * l->waves > 0x7fffffff) return MMEE_EINVAL;
-    const auto parts = [&](const Launch &l, uint64_t lines) { return l.splits > 1 ? 4 * l.splits * x->kv_heads * lines * plan.dp : 0; };
-    plan.part_bytes = up256(parts(plan.forward, rows));
-    plan.forward_bytes = plan.part_bytes ? plan.part_bytes + 4 * plan.forward.splits * x->kv_heads * rows : 0;
-    plan.backward_bytes = up256(4ull * x->kv_heads * rows) + std::max(parts(plan.dq, rows), parts(plan.dkv, 2ull * x->kv_tokens));
+        if (l->blocks * l->waves > 0x7fffffff) return MMEE_EINVAL;
+    plan.forward_bytes = plan.forward.plan_bytes() + plan.forward.parts_bytes(x->kv_heads, plan.dp + 1);
+    plan.backward_bytes = up256(4ull * x->kv_heads * rows) + plan.dq.plan_bytes() + plan.dkv.plan_bytes() +
+                          std::max(plan.dq.parts_bytes(x->kv_heads, plan.dp), plan.dkv.parts_bytes(x->kv_heads, 2 * plan.dp));
     return MMEE_OK;
 }
 
@@ -126,14 +135,22 @@ void dispatch(const Plan &plan, F f)
     else with_dp(BF16());
 }
 
-PromptArgs with(const PromptArgs &p, const Launch &l)
+// The kernel's arguments: its plan at `at`, if it has one, which moves on behind it; its pieces' results at `parts`.
+PromptArgs with(const PromptArgs &p, const Launch &l, char *&at, float *parts)
 {
     PromptArgs q = p;
     q.slots = (uint32_t)l.slots;
-    q.a.splits = (uint32_t)l.splits;
-    q.room_shift = l.waves == 8 ? 8 : 9;
-    q.least = (uint32_t)l.least;
+    q.plan = l.planned ? (const uint32_t *)at : nullptr;
+    q.a.part_o = parts;
+    at += l.plan_bytes();
     return q;
+}
+
+void make(PlanArgs &x, int &n, const PromptArgs &p, const Launch &l, bool keys)
+{
+    if (!l.planned) return;
+    x.p = p;
+    x.of[n++] = {const_cast<uint32_t *>(p.plan), 32u * l.waves, (uint32_t)l.step, p.slots, (uint32_t)l.room, l.pieces ? (uint32_t)l.least : 0, keys};
 }
 
 // Calls f(8 or 4 waves), 8 where there is such a kernel.
@@ -149,21 +166,21 @@ template <class T, int DP, int W>
 void forward_as(const PromptArgs &p, const Launch &at, Launching &l)
 {
     l.run(k_prompt_forward<T, DP, W>, at.blocks, 64 * W, p);
-    if (at.splits > 1) l.run(k_prompt_join<T, DP, W>, at.slots * p.a.kv_heads * W, 256, p);
+    if (at.pieces) l.run(k_prompt_join<T, DP, W>, at.blocks * W, 256, p);
 }
 
 template <class T, int DP, int W>
 void dq_as(const PromptArgs &p, const Launch &at, Launching &l)
 {
     l.run(k_prompt_dq<T, DP, W>, at.blocks, 64 * W, p);
-    if (at.splits > 1) l.run(k_prompt_sum<T, DP, W, 64, false>, at.slots * p.a.kv_heads * W, 256, p);
+    if (at.pieces) l.run(k_prompt_sum<T, DP, W, 64, false>, at.blocks * W, 256, p);
 }
 
 template <class T, int DP, int W>
 void dkv_as(const PromptArgs &p, const Launch &at, Launching &l)
 {
     l.run(k_prompt_dkv<T, DP, W>, at.blocks, 64 * W, p);
-    if (at.splits > 1) l.run(k_prompt_sum<T, DP, W, DP == 128 ? 32 : 64, true>, at.slots * p.a.kv_heads * W, 256, p);
+    if (at.pieces) l.run(k_prompt_sum<T, DP, W, DP == 128 ? 32 : 64, true>, at.blocks * W, 256, p);
 }
 
 }  // namespace
@@ -190,11 +207,15 @@ int mmee_prompt_attn_forward(const mmee_prompt_attn *x)
     if (rc) return rc;
     if (plan.forward_bytes && (!x->workspace || x->workspace_bytes < plan.forward_bytes)) return MMEE_EWORKSPACE;
     if (!plan.p.a.rows) return MMEE_OK;
-    PromptArgs p = with(plan.p, plan.forward);
-    p.a.part_o = (float *)x->workspace;
-    p.a.part_lse = p.a.part_o + plan.part_bytes / 4;
+    char *at = (char *)x->workspace;
+    PromptArgs p = with(plan.p, plan.forward, at, (float *)(at + plan.forward.plan_bytes()));
+    p.a.part_lse = p.a.part_o + plan.forward.slots * p.a.kv_heads * 32 * plan.forward.waves * plan.dp;
+    PlanArgs plans = {};
+    int n = 0;
+    make(plans, n, p, plan.forward, false);
     Launching l;
     if (l.rc) return l.rc;
+    if (n) l.run(k_prompt_plan, n, 1024, plans);
     dispatch(plan, [&](auto type, auto dp) {
         with_waves<(dp.value >= 64)>(plan.forward.waves, [&](auto w) { forward_as<decltype(type), dp.value, w.value>(p, plan.forward, l); });
     });
@@ -221,10 +242,16 @@ int mmee_prompt_attn_backward(const mmee_prompt_attn *x, const mmee_prompt_attn_
     a.dk = (uint16_t *)g->dk;
     a.dv = (uint16_t *)g->dv;
     a.delta = (float *)x->workspace;
-    a.part_o = a.delta + up256(4ull * a.kv_heads * a.rows) / 4;
-    const PromptArgs dq = with(plan.p, plan.dq), dkv = with(plan.p, plan.dkv);
+    char *at = (char *)x->workspace + up256(4ull * a.kv_heads * a.rows);
+    float *parts = (float *)(at + plan.dq.plan_bytes() + plan.dkv.plan_bytes());
+    const PromptArgs dq = with(plan.p, plan.dq, at, parts), dkv = with(plan.p, plan.dkv, at, parts);
+    PlanArgs plans = {};
+    int n = 0;
+    make(plans, n, dq, plan.dq, false);
+    make(plans, n, dkv, plan.dkv, true);
     Launching l;
     if (l.rc) return l.rc;
+    if (n) l.run(k_prompt_plan, n, 1024, plans);
     dispatch(plan, [&](auto type, auto dp) {
         if (a.rows) with_waves<(dp.value == 128)>(plan.dq.waves, [&](auto w) { dq_as<decltype(type), dp.value, w.value>(dq, plan.dq, l); });
         if (a.kv_len) with_waves<(dp.value >= 64)>(plan.dkv.waves, [&](auto w) { dkv_as<decltype(type), dp.value, w.value>(dkv, plan.dkv, l); });

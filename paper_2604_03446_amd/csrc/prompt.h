@@ -17,12 +17,14 @@ struct PromptArgs {
     AttnArgs a;                 // batch 1, q_len: all tokens, rows: of all tokens, kv_len: all keys
     const int32_t *q_starts, *kv_starts;
     uint32_t seqs, slots;       // slots: of tiles, or of a plan's entries, of every head
+    uint32_t parts;             // pieces of cut tiles, at most, of every head
+    float *lse2;                // backward: [kv_head][row], in powers of two, infinite where a row sees nothing; less what float16 takes off
     const uint32_t *plan;       // the number of entries, and from ENTRIES on the entries; or null
     bool causal;
     bool dies;                  // heads are dealt out to the dies, whose L2 then holds their keys
 };
 
-constexpr uint32_t ENTRIES = 8, ENTRY = 8;              // words: q0, m, k0, n, index, step0, count, piece | pieces << 16
+constexpr uint32_t ENTRIES = 8, ENTRY = 12;             // words: q0, m, k0, n, index, step0, count, piece, pieces, number of the tile's first piece, two unused
 
 // Keys 0 .. of its sequence that a token sees.
 __device__ __forceinline__ uint32_t limit_of(const PromptArgs &p, uint32_t m, uint32_t n, uint32_t token)
@@ -63,14 +65,14 @@ struct Sequence {
 // A block's tile: rows (or, with KEYS, keys) index * TILE .. of a sequence, and the steps step0 .. of STEP keys (or rows) that are the block's piece of it.
 template <uint32_t TILE, uint32_t STEP, bool KEYS>
 struct Tile {
-    uint32_t index, q0, m, k0, n, kvh, piece = 0, pieces = 1, step0 = 0, count = 0, slot;
+    uint32_t index, q0, m, k0, n, kvh, piece = 0, pieces = 1, first_part = 0, step0 = 0, count = 0;
     bool there;
 
     // at: place among heads and slots.
     __device__ __forceinline__ Tile(const PromptArgs &p, uint32_t at)
     {
         kvh = p.dies ? at / p.slots : at % p.a.kv_heads;
-        slot = p.dies ? at % p.slots : at / p.a.kv_heads;
+        const uint32_t slot = p.dies ? at % p.slots : at / p.a.kv_heads;
         if (p.plan) {
             there = slot < p.plan[0];
             if (!there) return;
@@ -82,8 +84,9 @@ struct Tile {
             index = e[4];
             step0 = e[5];
             count = e[6];
-            piece = e[7] & 0xffff;
-            pieces = e[7] >> 16;
+            piece = e[7];
+            pieces = e[8];
+            first_part = e[9];
             return;
         }
         const int32_t *starts = KEYS ? p.kv_starts : p.q_starts;
@@ -106,11 +109,11 @@ struct Tile {
     // known to be there: in the constructor the compiler still made loops over the lanes of every load, 8 % of the forward pass's time.)
     __device__ __forceinline__ void settle()
     {
-        for (uint32_t *x : {&index, &q0, &m, &k0, &n, &kvh, &piece, &pieces, &step0, &count, &slot}) *x = __builtin_amdgcn_readfirstlane(*x);
+        for (uint32_t *x : {&index, &q0, &m, &k0, &n, &kvh, &piece, &pieces, &first_part, &step0, &count}) *x = __builtin_amdgcn_readfirstlane(*x);
     }
 
-    // The tile's place among pieces of all heads.
-    __device__ __forceinline__ int64_t part(const PromptArgs &p) const { return ((int64_t)kvh * p.slots + slot) * TILE; }
+    // Where the results of a piece of this tile lie, in rows or keys.
+    __device__ __forceinline__ int64_t part(const PromptArgs &p, uint32_t of) const { return ((int64_t)kvh * p.parts + first_part + of) * TILE; }
 
     // Keys of the sequence as the tiles' loads want them.
     __device__ __forceinline__ Keys<MODE_PLAIN> keys(const PromptArgs &p) const
@@ -124,7 +127,7 @@ struct Tile {
 // A plan to be made: tiles of `tile` rows or keys, steps of `step` keys or rows.
 struct PlanOf {
     uint32_t *plan;
-    uint32_t tile, step, slots;
+    uint32_t tile, step, slots, parts;
     uint32_t room, least;       // blocks of all heads that run at once, steps of a piece at least (0: no pieces)
     bool keys;
 };
@@ -136,7 +139,7 @@ struct PlanArgs {
 
 constexpr uint32_t PLAN_SEQS = 2048, PLAN_TILES = 8192; // at most
 
-// Plans of[blockIdx.x].  Tiles are sorted by the length of their pieces in 1024 classes; which of a class come first does not matter to any result.
+// Plans of[blockIdx.x].  Tiles and pieces are sorted by their length in 1024 classes; which of a class come first does not matter to any result.
 // One block; for prompts of 17 to 2500 rows 5 us, of which most is the latency of the starts and of a dozen barriers.
 __global__ __launch_bounds__(1024) void k_prompt_plan(const PlanArgs x)
 {
@@ -196,70 +199,55 @@ __global__ __launch_bounds__(1024) void k_prompt_plan(const PlanArgs x)
     }
     reduce(total, longest);
 
-    // The length that pieces may have.  With tiles enough to go round: half of what a unit gets of all steps, so that the last ones even it out.  With
-    // fewer: the least with which all pieces run at once, up to three times a unit's share; every wave tries one of sixteen, twice.
-    uint32_t size = most_all ? most_all : 1;
+    // From tiles longer than a unit's share of all steps, and a thirty-second more, pieces of that length are cut off; the rests are sorted in among the
+    // other tiles.  Longest first, this ends within 12 % of the even share (pieces of equal length: 10 to 50 % behind it).
+    uint32_t size = most_all ? most_all : 1, slack = 0;
     if (of.least) {
         const uint64_t share = (uint64_t)sum_all * 8 * p.a.kv_heads / of.room;
-        uint32_t low = (uint32_t)share > of.least ? (uint32_t)share : of.least;
-        if ((uint64_t)tiles * p.a.kv_heads >= of.room || tiles > 1024) {
-            low = (uint32_t)(share / 2) > of.least ? (uint32_t)(share / 2) : of.least;
-        } else {
-            classes[thread] = steps[0];
-            __syncthreads();
-            uint32_t width = 2 * low;
-            for (int round = 0; round < 2; ++round) {
-                const uint32_t candidate = low + width * wave / 16;
-                uint32_t wanted = 0;
-                for (uint32_t t = lane; t < tiles; t += 64) wanted += classes[t] ? (classes[t] + candidate - 1) / candidate : 1;
-                wanted = sum_of_lanes(wanted);
-                if (lane == 0) more[wave] = (uint64_t)wanted * p.a.kv_heads <= of.room;
-                __syncthreads();
-                const uint32_t fits = (uint32_t)__ballot(lane < 16 && more[lane & 15]), first = fits ? __builtin_ctz(fits) : 15;
-                __syncthreads();
-                if (round == 0 && first) low += width * (first - 1) / 16;
-                else low += width * first / 16;
-                width = (width + 15) / 16;
-            }
-        }
-        size = low;
+        size = (uint32_t)(share + share / 32) + 1;
+        size = size > of.least ? size : of.least;
+        slack = of.least / 2;                           // that is not worth a piece
     }
-    __syncthreads();
-    classes[thread] = 0;
-    __syncthreads();
-
-    // Tiles' pieces, sorted by their length.
-    const uint32_t top = size < most_all ? size : most_all ? most_all : 1;
-    const auto pieces_of = [&](uint32_t of_steps) { return of_steps > size ? (of_steps + size - 1) / size : 1; };
-    const auto class_of = [&](uint32_t length) {
-        const uint32_t c = (uint32_t)((float)length * ((CLASSES - 1) / (float)top));
+    const auto pieces_of = [&](uint32_t n) { return n > size + slack ? (n - slack + size - 1) / size : 1; };
+    const uint32_t top = size + slack < most_all ? size + slack : most_all ? most_all : 1;
+    const float per_class = (CLASSES - 1) / (float)top;
+    const auto class_of = [&](uint32_t n) {
+        const uint32_t c = (uint32_t)((float)n * per_class);
         return CLASSES - 1 - (c < CLASSES ? c : CLASSES - 1);
     };
+    uint32_t cut = 0;                                   // pieces of this thread's cut tiles
 #pragma unroll
     for (uint32_t i = 0; i < MINE; ++i)
         if (i * 1024 + thread < tiles) {
             const uint32_t pieces = pieces_of(steps[i]);
-            atomicAdd(&classes[class_of((steps[i] + pieces - 1) / pieces)], pieces);
+            atomicAdd(&classes[class_of(steps[i] - (pieces - 1) * size)], 1);
+            if (pieces > 1) atomicAdd(&classes[class_of(size)], pieces - 1);
+            cut += pieces > 1 ? pieces : 0;
         }
     __syncthreads();
+    reduce(cut, 0);
+    uint32_t part = sum_before;
+    const bool too_many = sum_all > of.parts;           // (of sequences that overlap)
     const uint32_t own = classes[thread];
     reduce(own, 0);
     classes[thread] = sum_before;
-    if (thread == 0) of.plan[0] = sum_all <= of.slots ? sum_all : 0;        // (more only of sequences that overlap)
+    const bool fits = !too_many && sum_all <= of.slots;
+    if (thread == 0) of.plan[0] = fits ? sum_all : 0;
     __syncthreads();
-    if (sum_all > of.slots) return;
+    if (!fits) return;
 #pragma unroll
     for (uint32_t i = 0; i < MINE; ++i)
         if (i * 1024 + thread < tiles) {
-            const uint32_t pieces = pieces_of(steps[i]), per = (steps[i] + pieces - 1) / pieces, index = i * 1024 + thread - first_tile[seqs[i]];
-            const uint32_t at = atomicAdd(&classes[class_of(per)], pieces);
+            const uint32_t pieces = pieces_of(steps[i]), index = i * 1024 + thread - first_tile[seqs[i]];
             const Sequence q(p, seqs[i]);
             for (uint32_t k = 0; k < pieces; ++k) {
-                const uint32_t step0 = k * per < steps[i] ? k * per : steps[i], count = step0 + per < steps[i] ? per : steps[i] - step0;
-                u32x4 *e = reinterpret_cast<u32x4 *>(of.plan + ENTRIES + ENTRY * (at + k));
+                const uint32_t step0 = k * size, count = k + 1 < pieces ? size : steps[i] - step0, at = atomicAdd(&classes[class_of(count)], 1);
+                u32x4 *e = reinterpret_cast<u32x4 *>(of.plan + ENTRIES + ENTRY * at);
                 e[0] = u32x4{q.q0, q.m, q.k0, q.n};
-                e[1] = u32x4{index, step0, count, k | pieces << 16};
+                e[1] = u32x4{index, step0, count, k};
+                e[2] = u32x4{pieces, part, 0, 0};
             }
+            part += pieces > 1 ? pieces : 0;
         }
 }
 
@@ -456,7 +444,7 @@ __global__ __launch_bounds__(64 * W, 2) void k_prompt_forward(const PromptArgs p
         store_row<T, DP>(a.o + tile.q0 * a.os.token + row_at(a, a.os, 0, tile.kvh, row), o, times, a.head_dim);
         if (a.lse && h == 0) a.lse[lse_at(a, 0, tile.kvh, row) + tile.q0] = sum2 * LN2;
     } else {
-        const int64_t line = tile.part(p) + 32 * wave + n;
+        const int64_t line = tile.part(p, tile.piece) + 32 * wave + n;
         store_part<DP>(a.part_o + line * DP, o, times);
         if (h == 0) a.part_lse[line] = sum2;
     }
@@ -474,7 +462,7 @@ __global__ __launch_bounds__(256) void k_prompt_join(const PromptArgs p)
     for (uint32_t i = threadIdx.x; i < 32 * C4; i += 256) {
         const uint32_t within_tile = blockIdx.x % W * 32 + i / C4, row = tile.index * 32 * W + within_tile, c = i % C4;
         if (row >= tile.m * a.group) return;
-        const int64_t line = tile.part(p) + within_tile;
+        const int64_t line = tile.part(p, 0) + within_tile;
         float high = -INFINITY, sum = 0.0f;
         for (uint32_t s = 0; s < tile.pieces; ++s) high = __builtin_elementwise_maximum(high, a.part_lse[line + s * 32 * W]);
         const float off = high == -INFINITY ? 0.0f : high;
@@ -525,7 +513,10 @@ __global__ __launch_bounds__(64 * W, 2) void k_prompt_dq(const PromptArgs p)
 #pragma unroll
             for (int j = 0; j < 8; ++j) delta += (float)o[t][j] * (float)d_o[t][j];
         delta = sum_of_halves(delta);
-        if (live && h == 0 && tile.piece == 0) a.delta[line] = delta;
+        if (live && h == 0 && tile.piece == 0) {
+            a.delta[line] = delta;
+            p.lse2[line] = NARROW<T> ? lse2 + HIGHEST : lse2;
+        }
     }
 
     f32x16 dq[1][DP / 32] = {};
@@ -573,7 +564,7 @@ __global__ __launch_bounds__(64 * W, 2) void k_prompt_dq(const PromptArgs p)
     }
     const float times = NARROW<T> ? a.scale * __builtin_amdgcn_exp2f(-(UP + HIGHEST + lowered)) : a.scale;
     if (tile.pieces == 1) store_row<T, DP>(a.dq + tile.q0 * a.dqs.token + row_at(a, a.dqs, 0, tile.kvh, row), dq[0], times, a.head_dim);
-    else store_part<DP>(a.part_o + (tile.part(p) + 32 * wave + n) * DP, dq[0], times);
+    else store_part<DP>(a.part_o + (tile.part(p, tile.piece) + 32 * wave + n) * DP, dq[0], times);
 }
 
 // dK and dV of 32 W keys, 32 a wave, over the rows that see them, as k_attn_dkv.
@@ -685,9 +676,225 @@ __global__ __launch_bounds__(64 * W, 2) void k_prompt_dkv(const PromptArgs p)
         store_row<T, DP>(a.dk + key_at * a.dks.token + tile.kvh * a.dks.head, dk[0], times, a.head_dim);
         store_row<T, DP>(a.dv + key_at * a.dvs.token + tile.kvh * a.dvs.head, dv[0], times_v, a.head_dim);
     } else {
-        float *part = a.part_o + (tile.part(p) + 32 * wave + n) * 2 * DP;
+        float *part = a.part_o + (tile.part(p, tile.piece) + 32 * wave + n) * 2 * DP;
         store_part<DP>(part, dk[0], times);
         store_part<DP>(part + DP, dv[0], times_v);
+    }
+}
+
+// Loads straight to shared memory: 16 or 4 bytes a lane, `offset` (a lane's own, in bytes) behind the base, lane after lane to the place `to`.
+// Written out, as the compiler waits for all that are under way at every barrier and at the first read of shared memory after one: who uses them counts them
+// and waits (`arrived`).  (m0 is not said to be written: it is a register that the compiler keeps out of its own hands, and sets before every use.)
+__device__ __forceinline__ void load_16_to_shared(const void *base, uint32_t offset, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory");
+}
+
+__device__ __forceinline__ void load_4_to_shared(const void *base, uint32_t offset, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory");
+}
+
+__device__ __forceinline__ uint32_t place_in_shared(const void *p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)p; }
+
+// All but the last LEFT loads of this wave are there, and, behind the barrier, those of all waves; this wave reads nothing older any more.
+template <int LEFT>
+__device__ __forceinline__ void arrived()
+{
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory");
+}
+
+// dK and dV of 256 keys with 128 values each, 64 a wave and one wave a SIMD, 32 rows a step.
+template <class T>
+__global__ __launch_bounds__(256, 1) void k_prompt_dkv_wide(const PromptArgs p)
+{
+    constexpr int DP = 128, CH = 16, TR = 32, STAGES = 4, NT = DP / 16, DT = DP / 32;
+    __shared__ u32x4 tiles[STAGES][2][TR * CH];         // Q, dO
+    // V's operands, and four of K's, for which registers do not suffice: a lane reads what it has written itself.
+    __shared__ u32x4 away[4][2][NT][64], away_k[4][NT / 2][64];
+    __shared__ f32x4 stats[STAGES][2][TR / 4];          // lse in powers of two (lower lanes), D
+    const AttnArgs &a = p.a;
+    Tile<256, TR, true> tile(p, block_place(p));
+    if (!tile.there) return;
+    tile.settle();
+    const int thread = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(thread >> 6), lane = thread & 63, n = lane & 31, h = lane >> 5;
+    const uint32_t rows = tile.m * a.group, key0 = tile.index * 256 + 64 * wave;
+    const int first_seen = first_row(p, tile.m, tile.n, tile.index * 256), all_see = first_row(p, tile.m, tile.n, key0 + 63);
+    const uint32_t count = tile.count, start = (first_seen < 0 ? 0 : first_seen) + tile.step0 * TR;
+
+    typename T::V8 k[2][NT];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const uint32_t key = key0 + 32 * u + n;
+        const bool valid = key < tile.n;
+        const int64_t at = (int64_t)tile.k0 + (valid ? key : 0);
+        typename T::V8 v[NT];
+        row_operands<T, DP>(k[u], a.k + at * a.ks.token + tile.kvh * a.ks.head, valid, a.head_dim);
+        row_operands<T, DP>(v, a.v + at * a.vs.token + tile.kvh * a.vs.head, valid, a.head_dim);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) away[wave][u][t][lane] = __builtin_bit_cast(u32x4, v[t]);
+    }
+#pragma unroll
+    for (int t = 0; t < NT / 2; ++t) away_k[wave][t][lane] = __builtin_bit_cast(u32x4, k[1][NT / 2 + t]);
+
+    // Loads: a wave has 8 of a step's rows, four at a time.  A step begins with a token (its rows are whole tokens).  Rows past the last one repeat it, and
+    // columns past the head's the first ones: those rows are masked, and K and V are 0 there.  Behind the last step it is loaded again.
+    const float *const stats_at = a.delta + (int64_t)tile.kvh * a.rows + tile.q0 * a.group;
+    const uint32_t stats_offset = h ? 0 : 4 * (uint32_t)(p.lse2 - a.delta);
+    const auto offset_of = [&](const Strides &s, uint32_t most, int i) {       // within a step of so many rows
+        const uint32_t own = 8 * wave + 4 * i + (lane >> 4), row = own < most ? own : most - 1;
+        const int c = (lane & 15) ^ spread<CH>(own), column = 8 * c < (int)a.head_dim ? 8 * c : 0;
+        return 2 * ((uint32_t)row_at(a, s, 0, 0, row) + column);
+    };
+    const uint32_t q_offset[2] = {offset_of(a.qs, TR, 0), offset_of(a.qs, TR, 1)}, do_offset[2] = {offset_of(a.dos, TR, 0), offset_of(a.dos, TR, 1)};
+    const uint16_t *const q_head = a.q + tile.q0 * a.qs.token + tile.kvh * a.group * a.qs.head, *const do_head = a.d_o + tile.q0 * a.dos.token + tile.kvh * a.group * a.dos.head;
+    const auto load = [&](uint32_t s, auto stage) {
+        const uint32_t first = start + (s < count ? s : count - 1) * TR, token = token_of(a, first), left = rows - first;
+        const uint16_t *const q_from = q_head + token * a.qs.token, *const do_from = do_head + token * a.dos.token;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            uint32_t q_own = q_offset[i], do_own = do_offset[i];
+            if (left < TR) {
+                q_own = offset_of(a.qs, left, i);
+                do_own = offset_of(a.dos, left, i);
+            }
+            load_16_to_shared(q_from, q_own, place_in_shared(&tiles[stage][0][(8 * wave + 4 * i) * CH]));
+            load_16_to_shared(do_from, do_own, place_in_shared(&tiles[stage][1][(8 * wave + 4 * i) * CH]));
+        }
+        load_4_to_shared(stats_at + first, 4 * ((uint32_t)n < left ? n : left - 1) + stats_offset, place_in_shared(&stats[stage][0][0]));
+    };
+    constexpr int LOADS = 5, AHEAD = 3, AHEAD_V = 2;
+    const int own_row = first_row(p, tile.m, tile.n, key0 + n), next_keys = p.causal ? 32 * (int)a.group : 0;       // of u = 0; more of u = 1
+
+    f32x16 dk[2][DT] = {}, dv[2][DT] = {};
+    float by[2] = {0x1p60f, 0x1p60f};                   // float16: dS's power of two over P's
+    static_assert(HIGHEST == 60.0f);
+    const auto step = [&](uint32_t s, auto stage) {
+        arrived<LOADS * (STAGES - 2)>();
+        load(s + STAGES - 1, std::integral_constant<int, (stage.value + STAGES - 1) % STAGES>());
+        const u32x4 *const qt = tiles[stage][0], *const ot = tiles[stage][1];
+        const uint32_t first = start + s * TR;
+        const auto along = [&](const u32x4 *of, int t) { return of[chunk_at<CH>(n, 2 * t + h)]; };
+        const auto across = [&](s16x4 (&to)[2], const u32x4 *of, int i) {       // columns 32 (i mod DT) .., rows 16 (i / DT) ..
+            const int l = lane & 15, c = 4 * (i % DT) + 2 * ((lane >> 4) & 1) + ((l >> 1) & 1);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) to[j] = read_transposed(reinterpret_cast<const char *>(of + 16 * (i / DT) * CH + chunk_at<CH>(4 * h + (l >> 2) + 8 * j, c)) + 8 * (l & 1));
+        };
+
+        // S = Q K^T
+        f32x16 x[2], dp[2];
+        u32x4 operand[AHEAD], ko[AHEAD_V], vo[AHEAD_V][2];
+        f32x4 stat[2];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) operand[i] = along(qt, i);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) x[u] = T::mma(as_operand<T>(operand[t % AHEAD]), u && t >= NT / 2 ? as_operand<T>(ko[t % AHEAD_V]) : k[u][t], t ? x[u] : f32x16{});
+            if (t + AHEAD_V >= NT / 2 && t + AHEAD_V < NT) ko[t % AHEAD_V] = away_k[wave][t + AHEAD_V - NT / 2][lane];
+            operand[t % AHEAD] = t + AHEAD < NT ? along(qt, t + AHEAD) : along(ot, t + AHEAD - NT);
+            if (t + AHEAD_V >= NT) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u) vo[t + AHEAD_V - NT][u] = away[wave][u][t + AHEAD_V - NT][lane];
+            }
+            if (t == NT - 1) stat[0] = stats[stage][0][h];
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if ((int)first < all_see || first + TR > rows) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int from = own_row + u * next_keys - (int)first - 4 * h, behind = (int)(rows - first) - 4 * h;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int at = 8 * (r / 4) + r % 4;
+                    x[u][r] = at >= from && at < behind ? x[u][r] : -INFINITY;
+                }
+            }
+        }
+        // dP = dO V^T beside the exponentials, four of one row group at a time; operand[] holds dO's from (NT mod AHEAD) on
+        typename T::V8 pr[2][2], ds[2][2];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const int slot = (t + NT) % AHEAD, g = t / 2, v = t % 2;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) dp[u] = T::mma(as_operand<T>(operand[slot]), as_operand<T>(vo[t % AHEAD_V][u]), t ? dp[u] : f32x16{});
+            if (t + AHEAD < NT) operand[slot] = along(ot, t + AHEAD);
+            if (t + AHEAD_V < NT) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u) vo[t % AHEAD_V][u] = away[wave][u][t + AHEAD_V][lane];
+            }
+            if (v == 0) stat[(g + 1) % 2] = g < 3 ? stats[stage][0][2 * g + 2 + h] : stats[stage][1][h];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[v][4 * g + j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[v][4 * g + j], a.scale_log2, -stat[g % 2][j]));
+            if (g % 2) pr[v][g / 2] = rounded<T>(x[v], g / 2);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        // dV += dO^T P beside dS
+        s16x4 ao[AHEAD][2];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) across(ao[i], ot, i);
+#pragma unroll
+        for (int i = 0; i < 2 * DT; ++i) {
+            const int g = i / 2, v = i % 2;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) dv[u][i % DT] = T::mma(join<T>(ao[i % AHEAD][0], ao[i % AHEAD][1]), pr[u][i / DT], dv[u][i % DT]);
+            if (i + AHEAD < 2 * DT) across(ao[i % AHEAD], ot, i + AHEAD);
+            else across(ao[i % AHEAD], qt, i + AHEAD - 2 * DT);
+            if (v == 0 && g < 3) stat[(g + 1) % 2] = stats[stage][1][2 * g + 2 + h];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float d = dp[v][4 * g + j] - stat[g % 2][j];
+                dp[v][4 * g + j] = x[v][4 * g + j] * (NARROW<T> ? d * by[v] : d);
+            }
+            if (!NARROW<T> && g % 2) ds[v][g / 2] = rounded<T>(dp[v], g / 2);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (NARROW<T>) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                by[u] *= __builtin_amdgcn_exp2f(keep_in_range(dp[u], dk[u]));
+#pragma unroll
+                for (int part = 0; part < 2; ++part) ds[u][part] = rounded<T>(dp[u], part);
+            }
+        }
+        // dK += Q^T dS
+#pragma unroll
+        for (int i = 0; i < 2 * DT; ++i) {
+            const int slot = (i + 2 * DT) % AHEAD;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) dk[u][i % DT] = T::mma(join<T>(ao[slot][0], ao[slot][1]), ds[u][i / DT], dk[u][i % DT]);
+            if (i + AHEAD < 2 * DT) across(ao[slot], qt, i + AHEAD);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    static_assert(STAGES == 4);
+    if (count) {
+        load(0, std::integral_constant<int, 0>());
+        load(1, std::integral_constant<int, 1>());
+        load(2, std::integral_constant<int, 2>());
+    }
+#pragma unroll 1
+    for (uint32_t s = 0; s < count; s += 4) {
+        step(s, std::integral_constant<int, 0>());
+        if (s + 1 < count) step(s + 1, std::integral_constant<int, 1>());
+        if (s + 2 < count) step(s + 2, std::integral_constant<int, 2>());
+        if (s + 3 < count) step(s + 3, std::integral_constant<int, 3>());
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");    // nothing writes to shared memory any more when the block ends
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const uint32_t key = key0 + 32 * u + n;
+        if (key >= tile.n) continue;
+        const int64_t at = (int64_t)tile.k0 + key;
+        const float times = NARROW<T> ? a.scale * 0x1p-15f / by[u] : a.scale, times_v = NARROW<T> ? 0x1p-15f : 1.0f;
+        if (tile.pieces == 1) {
+            store_row<T, DP>(a.dk + at * a.dks.token + tile.kvh * a.dks.head, dk[u], times, a.head_dim);
+            store_row<T, DP>(a.dv + at * a.dvs.token + tile.kvh * a.dvs.head, dv[u], times_v, a.head_dim);
+        } else {
+            float *part = a.part_o + (tile.part(p, tile.piece) + 64 * wave + 32 * u + n) * 2 * DP;
+            store_part<DP>(part, dk[u], times);
+            store_part<DP>(part + DP, dv[u], times_v);
+        }
     }
 }
 
@@ -705,7 +912,7 @@ __global__ __launch_bounds__(256) void k_prompt_sum(const PromptArgs p)
         const uint32_t within_tile = blockIdx.x % W * 32 + i / C4, own = tile.index * 32 * W + within_tile, c = i % C4, d = 4 * c % DP;
         if (own >= lines) return;
         if (d >= a.head_dim) continue;
-        const int64_t line = tile.part(p) + within_tile;
+        const int64_t line = tile.part(p, 0) + within_tile;
         f32x4 x = {0, 0, 0, 0};
 #pragma unroll 4
         for (uint32_t s = 0; s < tile.pieces; ++s) x += *reinterpret_cast<const f32x4 *>(a.part_o + ((line + s * 32 * W) * C4 + c) * 4);

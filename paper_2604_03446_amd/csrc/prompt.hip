@@ -31,11 +31,11 @@ uint64_t up256(uint64_t x) { return (x + 255) & ~(uint64_t)255; }
 // One of the three kernels: waves of a block, slots of tiles a head, blocks; whether it has a plan, and one with pieces.
 struct Launch {
     int waves = 4;
-    uint64_t slots = 0, blocks = 0, room = 0, step = 0, least = 0;
+    uint64_t slots = 0, parts = 0, blocks = 0, room = 0, step = 0, least = 0;
     bool planned = false, pieces = false;
     uint64_t plan_bytes() const { return planned ? up256(4 * (ENTRIES + ENTRY * slots)) : 0; }
     // Results of pieces, so many floats a row or key.
-    uint64_t parts_bytes(uint64_t kv_heads, uint64_t floats) const { return pieces ? up256(4 * slots * kv_heads * 32 * waves * floats) : 0; }
+    uint64_t parts_bytes(uint64_t kv_heads, uint64_t floats) const { return up256(4 * parts * kv_heads * 32 * waves * floats); }
 };
 
 struct Plan {
@@ -50,7 +50,7 @@ struct Plan {
 Launch plan_launch(uint64_t lines, uint64_t seqs, uint64_t kv_heads, uint64_t across, uint64_t step, bool causal, bool eight)
 {
     Launch l;
-    l.waves = eight && lines / seqs >= 256 && (lines / 256 + seqs / 2) * kv_heads > 128 ? 8 : 4;
+    l.waves = eight && lines / seqs >= 256 && ((lines / 256 + seqs / 2) * kv_heads > 128 || across / seqs >= 1024) ? 8 : 4;
     l.slots = lines / (32 * l.waves) + seqs;
     l.room = 2048 / l.waves;
     l.step = step;
@@ -61,7 +61,11 @@ Launch plan_launch(uint64_t lines, uint64_t seqs, uint64_t kv_heads, uint64_t ac
         l.pieces = blocks < 4 * l.room && steps >= 2 * l.least;
         l.planned = l.pieces || ((causal || seqs > 1) && blocks > l.room && blocks * steps / l.room > 48);
     }
-    if (l.pieces) l.slots += 3 * l.room / kv_heads + 1;
+    if (l.pieces) {
+        // all pieces but the last of a tile are a unit's share long at least, and a cut tile has two or more
+        l.slots += l.room / kv_heads + 1;
+        l.parts = 2 * (l.room / kv_heads + 1);
+    }
     l.blocks = l.slots * kv_heads;
     return l;
 }
@@ -117,7 +121,7 @@ int make_plan(const mmee_prompt_attn *x, bool pointers, Plan &plan)
     for (const Launch *l : {&plan.forward, &plan.dq, &plan.dkv})
         if (l->blocks * l->waves > 0x7fffffff) return MMEE_EINVAL;
     plan.forward_bytes = plan.forward.plan_bytes() + plan.forward.parts_bytes(x->kv_heads, plan.dp + 1);
-    plan.backward_bytes = up256(4ull * x->kv_heads * rows) + plan.dq.plan_bytes() + plan.dkv.plan_bytes() +
+    plan.backward_bytes = 2 * up256(4ull * x->kv_heads * rows) + plan.dq.plan_bytes() + plan.dkv.plan_bytes() +
                           std::max(plan.dq.parts_bytes(x->kv_heads, plan.dp), plan.dkv.parts_bytes(x->kv_heads, 2 * plan.dp));
     return MMEE_OK;
 }
@@ -140,6 +144,7 @@ PromptArgs with(const PromptArgs &p, const Launch &l, char *&at, float *parts)
 {
     PromptArgs q = p;
     q.slots = (uint32_t)l.slots;
+    q.parts = (uint32_t)l.parts;
     q.plan = l.planned ? (const uint32_t *)at : nullptr;
     q.a.part_o = parts;
     at += l.plan_bytes();
@@ -150,7 +155,7 @@ void make(PlanArgs &x, int &n, const PromptArgs &p, const Launch &l, bool keys)
 {
     if (!l.planned) return;
     x.p = p;
-    x.of[n++] = {const_cast<uint32_t *>(p.plan), 32u * l.waves, (uint32_t)l.step, p.slots, (uint32_t)l.room, l.pieces ? (uint32_t)l.least : 0, keys};
+    x.of[n++] = {const_cast<uint32_t *>(p.plan), 32u * l.waves, (uint32_t)l.step, p.slots, p.parts, (uint32_t)l.room, l.pieces ? (uint32_t)l.least : 0, keys};
 }
 
 // Calls f(8 or 4 waves), 8 where there is such a kernel.
@@ -176,10 +181,23 @@ void dq_as(const PromptArgs &p, const Launch &at, Launching &l)
     if (at.pieces) l.run(k_prompt_sum<T, DP, W, 64, false>, at.blocks * W, 256, p);
 }
 
+// Whether a step's 32 rows are whole tokens and lie, like the two statistics, within 32 bits of each other.
+bool wide(const AttnArgs &a)
+{
+    const auto spans = [&](const Strides &s) { return (uint64_t)(32 / a.group) * s.token + (uint64_t)a.group * s.head < 1ull << 30; };
+    return 32 % a.group == 0 && spans(a.qs) && spans(a.dos) && (uint64_t)a.kv_heads * a.rows < 1u << 28;
+}
+
 template <class T, int DP, int W>
 void dkv_as(const PromptArgs &p, const Launch &at, Launching &l)
 {
-    l.run(k_prompt_dkv<T, DP, W>, at.blocks, 64 * W, p);
+    bool done = false;
+    if constexpr (DP == 128 && W == 8 && !NARROW<T>)
+        if (wide(p.a)) {
+            l.run(k_prompt_dkv_wide<T>, at.blocks, 256, p);
+            done = true;
+        }
+    if (!done) l.run(k_prompt_dkv<T, DP, W>, at.blocks, 64 * W, p);
     if (at.pieces) l.run(k_prompt_sum<T, DP, W, DP == 128 ? 32 : 64, true>, at.blocks * W, 256, p);
 }
 
@@ -209,7 +227,7 @@ int mmee_prompt_attn_forward(const mmee_prompt_attn *x)
     if (!plan.p.a.rows) return MMEE_OK;
     char *at = (char *)x->workspace;
     PromptArgs p = with(plan.p, plan.forward, at, (float *)(at + plan.forward.plan_bytes()));
-    p.a.part_lse = p.a.part_o + plan.forward.slots * p.a.kv_heads * 32 * plan.forward.waves * plan.dp;
+    p.a.part_lse = p.a.part_o + plan.forward.parts * p.a.kv_heads * 32 * plan.forward.waves * plan.dp;
     PlanArgs plans = {};
     int n = 0;
     make(plans, n, p, plan.forward, false);
@@ -242,7 +260,8 @@ int mmee_prompt_attn_backward(const mmee_prompt_attn *x, const mmee_prompt_attn_
     a.dk = (uint16_t *)g->dk;
     a.dv = (uint16_t *)g->dv;
     a.delta = (float *)x->workspace;
-    char *at = (char *)x->workspace + up256(4ull * a.kv_heads * a.rows);
+    plan.p.lse2 = a.delta + up256(4ull * a.kv_heads * a.rows) / 4;
+    char *at = (char *)x->workspace + 2 * up256(4ull * a.kv_heads * a.rows);
     float *parts = (float *)(at + plan.dq.plan_bytes() + plan.dkv.plan_bytes());
     const PromptArgs dq = with(plan.p, plan.dq, at, parts), dkv = with(plan.p, plan.dkv, at, parts);
     PlanArgs plans = {};

@@ -145,6 +145,21 @@ def test_tiles_of_256(M, dtype):
         compare(t, True, d)
 
 
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
+@pytest.mark.parametrize("group", [1, 3, 8, 32])
+def test_keys_of_64_a_wave(M, group, dtype):
+    """Tiles of 256 keys with 128 (and 104) values: query heads that share a key/value head so that 32 rows are whole tokens, or not."""
+    import torch
+    lens, kv_lens, Hkv = ([600, 257, 3], [900, 257, 40], 6) if group >= 8 else ([200, 257, 3], [520, 257, 40], 40)
+    for causal in (True, False):
+        for d in (128, 104):
+            t = tensors(lens, kv_lens, Hkv * group, Hkv, d, getattr(torch, dtype), group, around=1)
+            for n in ("q", "do"):               # heads first: a token's heads lie apart
+                t[n] = t[n].transpose(0, 1).contiguous().transpose(0, 1)
+            run(M, t, causal=causal)
+            compare(t, causal, (group, causal, d))
+
+
 def test_many_sequences(M):
     """More than a wave looks at in one go, empty ones among them."""
     import torch

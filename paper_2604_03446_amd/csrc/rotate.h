@@ -5,8 +5,8 @@
 //   backward: dz = dy turned back;  dw = sum of dz x r over tokens and heads;  dx = r (w dz - x r * mean(w dz x r))
 //
 // A head is at most 32 chunks of eight values.  G lanes share it, two chunks each: the chunks of a pair's two halves, so that a pair never
-// leaves its lane, and the rest beside each other.  What a wave's lanes need of angles is the same for every head of a token: it is
-// worked out once a token.  Everything between the 16-bit input and the 16-bit output is 32 bits, angles 64.
+// leaves its lane, and the rest beside each other.  Angles are the same for every head of a token: a wave works each out once, a lane a pair, and
+// hands them round through shared memory.  Everything between the 16-bit input and the 16-bit output is 32 bits, angles 64.
 #pragma once
 
 #include "launch.h"
@@ -81,21 +81,27 @@ struct Head {
         }
     }
 
-    __device__ __forceinline__ void angles(const RotateArgs &r, uint32_t token, int64_t place)
+    // shared: this wave's, cosines and sines of the pairs.  (Worked out by every lane that needs them it took a third of the time of 12000 tokens of 24 heads of 64.)
+    __device__ __forceinline__ void angles(const RotateArgs &r, uint32_t token, int64_t place, float (&shared)[2][128])
     {
-        const double first = r.positions ? (double)r.positions[token] : (double)place;
+        wave_sync();                                    // of the token before
+        for (uint32_t pair = threadIdx.x & 63; 2 * pair < r.rot; pair += 64) {
+            double position = (double)place;
+            if (r.positions) {
+                const uint32_t axis = r.axis_of ? r.axis_of[pair] : 0;
+                position = r.positions[(axis < r.axes ? axis : r.axes - 1) * r.axis_stride + token];
+            }
+            turn(position, r.freqs[pair], shared[0][pair], shared[1][pair]);
+        }
+        wave_sync();
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int i = NEIGHBOURS ? j / 4 : 0;
-            cos[j] = sin[j] = 0.0f;
-            if (turned[i]) {
-                const uint32_t pair = NEIGHBOURS ? 4 * at[i] + j % 4 : 8 * at[0] + j;
-                double position = first;
-                if (r.axis_of) {
-                    const uint32_t axis = r.axis_of[pair];
-                    position = r.positions[(axis < r.axes ? axis : r.axes - 1) * r.axis_stride + token];
-                }
-                turn(position, r.freqs[pair], cos[j], sin[j]);
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t first = NEIGHBOURS ? 4 * at[i] : 8 * at[0] + 4 * i;
+            const f32x4 c = *reinterpret_cast<const f32x4 *>(&shared[0][first & 127]), s = *reinterpret_cast<const f32x4 *>(&shared[1][first & 127]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                cos[4 * i + j] = c[j];
+                sin[4 * i + j] = s[j];
             }
         }
     }
@@ -164,6 +170,7 @@ template <class T, int G, bool NEIGHBOURS, bool CACHE>
 __global__ __launch_bounds__(256) void k_rotate(const RotateArgs r)
 {
     constexpr uint32_t PER = 64 / G;
+    __shared__ __align__(16) float shared[4][2][128];
     const uint64_t wave = (uint64_t)blockIdx.x * (blockDim.x / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t token = (uint32_t)(wave / r.shares), share = (uint32_t)(wave % r.shares);
     if (token >= r.tokens) return;
@@ -180,7 +187,7 @@ __global__ __launch_bounds__(256) void k_rotate(const RotateArgs r)
         if ((uint32_t)page >= r.n_pages) page = -1;
     }
     Head<T, G, NEIGHBOURS> h(r);
-    h.angles(r, token, place);
+    h.angles(r, token, place, shared[__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)]);
     float w[2][16];
     const bool norm = r.q_weight || r.k_weight;
     if (norm) {
@@ -225,26 +232,25 @@ __global__ __launch_bounds__(256) void k_rotate(const RotateArgs r)
 // Backward.  A wave takes heads as in the forward pass, and further tokens; the weights' gradients of its lanes' columns stay in registers and
 // leave the block as one line of 32-bit sums.
 template <class T, int G, bool NEIGHBOURS>
-__global__ __launch_bounds__(256) void k_rotate_back(const RotateArgs r)
+__global__ __launch_bounds__(256, 3) void k_rotate_back(const RotateArgs r)
 {
     constexpr uint32_t PER = 64 / G;
     __shared__ float sums[4][2][16 * G];
+    __shared__ __align__(16) float shared[4][2][128];
     const uint32_t w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const bool norm = r.q_weight != nullptr;
     Head<T, G, NEIGHBOURS> h(r);
-    float weight[2][16], dw[2][16] = {};
+    u32x4 weights[2][2];
+    float dw[2][16] = {};
     if (norm) {
-        u32x4 raw[2];
-        h.load(r.q_weight, raw);
-        h.widen(raw, weight[0]);
-        h.load(r.k_weight, raw);
-        h.widen(raw, weight[1]);
+        h.load(r.q_weight, weights[0]);
+        h.load(r.k_weight, weights[1]);
     }
     const uint64_t step = (uint64_t)gridDim.x * 4, all_items = (uint64_t)r.tokens * r.shares;
     const uint32_t all = r.heads + r.kv_heads;
     for (uint64_t item = (uint64_t)blockIdx.x * 4 + w; item < all_items; item += step) {
         const uint32_t token = (uint32_t)(item / r.shares), share = (uint32_t)(item % r.shares);
-        h.angles(r, token, 0);
+        h.angles(r, token, 0, shared[w]);
         for (uint32_t at = share * PER + lane / G; at - lane / G < all; at += r.shares * PER) {
             if (at >= all) continue;
             const bool is_q = at < r.heads;
@@ -259,14 +265,16 @@ __global__ __launch_bounds__(256) void k_rotate_back(const RotateArgs r)
                 float x[16];
                 h.widen(raw, x);
                 const float inverse = __builtin_amdgcn_rsqf(h.squares(x) / (float)r.head_dim + r.eps);
-                float along = 0.0f;
+                const u32x4 own[2] = {is_q ? weights[0][0] : weights[1][0], is_q ? weights[0][1] : weights[1][1]};
+                float along = 0.0f, weight[16];
+                h.widen(own, weight);
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
                     x[j] *= inverse;
                     const float part = d[j] * x[j];
                     dw[0][j] += is_q ? part : 0.0f;
                     dw[1][j] += is_q ? 0.0f : part;
-                    d[j] *= is_q ? weight[0][j] : weight[1][j];
+                    d[j] *= weight[j];
                     along += d[j] * x[j];
                 }
                 along = h.sum(along) / (float)r.head_dim;
@@ -305,6 +313,7 @@ __global__ __launch_bounds__(1024) void k_rotate_weights(const RotateArgs r)
     const uint32_t column = blockIdx.x * 32 + threadIdx.x % 32, slice = threadIdx.x / 32, width = 2 * r.head_dim;
     float x = 0.0f;
     if (column < width)
+#pragma unroll 16
         for (uint32_t i = slice; i < r.blocks; i += 32) x += r.parts[(uint64_t)i * width + column];
     slices[slice][threadIdx.x % 32] = x;
     __syncthreads();

@@ -94,6 +94,11 @@ struct Head {
             turn(position, r.freqs[pair], shared[0][pair], shared[1][pair]);
         }
         wave_sync();
+    }
+
+    // This lane's.
+    __device__ __forceinline__ void take(const float (&shared)[2][128])
+    {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const uint32_t first = NEIGHBOURS ? 4 * at[i] : 8 * at[0] + 4 * i;
@@ -187,7 +192,9 @@ __global__ __launch_bounds__(256) void k_rotate(const RotateArgs r)
         if ((uint32_t)page >= r.n_pages) page = -1;
     }
     Head<T, G, NEIGHBOURS> h(r);
-    h.angles(r, token, place, shared[__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)]);
+    const uint32_t own_wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    h.angles(r, token, place, shared[own_wave]);
+    h.take(shared[own_wave]);
     float w[2][16];
     const bool norm = r.q_weight || r.k_weight;
     if (norm) {
@@ -229,10 +236,10 @@ __global__ __launch_bounds__(256) void k_rotate(const RotateArgs r)
     }
 }
 
-// Backward.  A wave takes heads as in the forward pass, and further tokens; the weights' gradients of its lanes' columns stay in registers and
-// leave the block as one line of 32-bit sums.
+// Backward.  A wave takes heads as in the forward pass, and further tokens: first all queries' heads, then all keys', so that it holds one weight and the
+// gradients of one, which stay in registers and leave the block as one line of 32-bit sums.
 template <class T, int G, bool NEIGHBOURS>
-__global__ __launch_bounds__(256, 3) void k_rotate_back(const RotateArgs r)
+__global__ __launch_bounds__(256, 4) void k_rotate_back(const RotateArgs r)
 {
     constexpr uint32_t PER = 64 / G;
     __shared__ float sums[4][2][16 * G];
@@ -240,60 +247,57 @@ __global__ __launch_bounds__(256, 3) void k_rotate_back(const RotateArgs r)
     const uint32_t w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const bool norm = r.q_weight != nullptr;
     Head<T, G, NEIGHBOURS> h(r);
-    u32x4 weights[2][2];
-    float dw[2][16] = {};
-    if (norm) {
-        h.load(r.q_weight, weights[0]);
-        h.load(r.k_weight, weights[1]);
-    }
-    const uint64_t step = (uint64_t)gridDim.x * 4, all_items = (uint64_t)r.tokens * r.shares;
-    const uint32_t all = r.heads + r.kv_heads;
-    for (uint64_t item = (uint64_t)blockIdx.x * 4 + w; item < all_items; item += step) {
-        const uint32_t token = (uint32_t)(item / r.shares), share = (uint32_t)(item % r.shares);
-        h.angles(r, token, 0, shared[w]);
-        for (uint32_t at = share * PER + lane / G; at - lane / G < all; at += r.shares * PER) {
-            if (at >= all) continue;
-            const bool is_q = at < r.heads;
-            const uint32_t head = is_q ? at : at - r.heads;
-            u32x4 raw[2], raw_d[2];
-            h.load(is_q ? r.dq_out + token * r.dqos.token + head * r.dqos.head : r.dk_out + token * r.dkos.token + head * r.dkos.head, raw_d);
-            float d[16];
-            h.widen(raw_d, d);
-            h.rotate(d, -1.0f);
-            if (norm) {
-                h.load(is_q ? r.q + token * r.qs.token + head * r.qs.head : r.k + token * r.ks.token + head * r.ks.head, raw);
-                float x[16];
-                h.widen(raw, x);
-                const float inverse = __builtin_amdgcn_rsqf(h.squares(x) / (float)r.head_dim + r.eps);
-                const u32x4 own[2] = {is_q ? weights[0][0] : weights[1][0], is_q ? weights[0][1] : weights[1][1]};
-                float along = 0.0f, weight[16];
-                h.widen(own, weight);
+    const auto pass = [&](uint32_t heads, uint32_t which, const uint16_t *x_at, const Rows &xs, const uint16_t *dy_at, const Rows &dys, uint16_t *dx_at, const Rows &dxs, const uint16_t *weight_at) {
+        u32x4 weights[2];
+        float dw[16] = {};
+        if (norm) h.load(weight_at, weights);
+        const uint32_t waves = (heads + PER - 1) / PER, shares = r.shares < waves ? r.shares : waves;
+        const uint64_t step = (uint64_t)gridDim.x * 4, items = (uint64_t)r.tokens * shares;
+        for (uint64_t item = (uint64_t)blockIdx.x * 4 + w; item < items; item += step) {
+            const uint32_t token = (uint32_t)(item / shares), share = (uint32_t)(item % shares);
+            h.angles(r, token, 0, shared[w]);
+            for (uint32_t head = share * PER + lane / G; head - lane / G < heads; head += shares * PER) {
+                if (head >= heads) continue;
+                u32x4 raw[2], raw_d[2];
+                h.load(dy_at + token * dys.token + head * dys.head, raw_d);
+                if (norm) h.load(x_at + token * xs.token + head * xs.head, raw);
+                asm volatile("" ::: "memory");          // the angles are read again for every head: kept, they spill other registers
+                h.take(shared[w]);
+                float d[16];
+                h.widen(raw_d, d);
+                h.rotate(d, -1.0f);
+                if (norm) {
+                    float x[16], weight[16];
+                    h.widen(raw, x);
+                    h.widen(weights, weight);
+                    const float inverse = __builtin_amdgcn_rsqf(h.squares(x) / (float)r.head_dim + r.eps);
+                    float along = 0.0f;
 #pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    x[j] *= inverse;
-                    const float part = d[j] * x[j];
-                    dw[0][j] += is_q ? part : 0.0f;
-                    dw[1][j] += is_q ? 0.0f : part;
-                    d[j] *= weight[j];
-                    along += d[j] * x[j];
+                    for (int j = 0; j < 16; ++j) {
+                        x[j] *= inverse;
+                        dw[j] += d[j] * x[j];
+                        d[j] *= weight[j];
+                        along += d[j] * x[j];
+                    }
+                    along = h.sum(along) / (float)r.head_dim;
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) d[j] = inverse * (d[j] - x[j] * along);
                 }
-                along = h.sum(along) / (float)r.head_dim;
-#pragma unroll
-                for (int j = 0; j < 16; ++j) d[j] = inverse * (d[j] - x[j] * along);
+                h.store(dx_at + token * dxs.token + head * dxs.head, d);
             }
-            h.store(is_q ? r.dq + token * r.dqs.token + head * r.dqs.head : r.dk + token * r.dks.token + head * r.dks.head, d);
         }
-    }
-    if (!norm) return;
-#pragma unroll
-    for (int n = 0; n < 2; ++n)
+        if (!norm) return;
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-            float x = dw[n][j];
+            float x = dw[j];
 #pragma unroll
             for (int d = G; d < 64; d <<= 1) x += __shfl_xor(x, d);
-            if (lane < G) sums[w][n][16 * lane + j] = x;
+            if (lane < G) sums[w][which][16 * lane + j] = x;
         }
+    };
+    pass(r.heads, 0, r.q, r.qs, r.dq_out, r.dqos, r.dq, r.dqs, r.q_weight);
+    pass(r.kv_heads, 1, r.k, r.ks, r.dk_out, r.dkos, r.dk, r.dks, r.k_weight);
+    if (!norm) return;
     __syncthreads();
     for (uint32_t i = threadIdx.x; i < 2 * 16 * G; i += 256) {
         const uint32_t n = i / (16 * G), c = i % (16 * G), chunk = c / 8 % 2, p = c / 16;

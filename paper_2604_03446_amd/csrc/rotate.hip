@@ -92,8 +92,8 @@ int plan_rotate(const mmee_qk_rotate *x, bool pointers, RotateArgs &r)
     if (pointers && (moved(x->q, r.qs, x->q_out, r.qos) || moved(x->k, r.ks, x->k_out, r.kos))) return MMEE_EINVAL;
     if (pointers && r.tokens && (!x->q || !x->k || !x->q_out || !x->k_out || (r.rot && !x->positions) || misaligned({x->k_out, x->workspace}, 16))) return MMEE_EINVAL;
     r.shares = shares(r.tokens, r.heads + r.kv_heads, lanes_of(r.head_dim));
-    // Backward: blocks whose lines of the weights' gradients stay few, three to a unit, as many as run at once.
-    r.blocks = (uint32_t)std::min<uint64_t>(((uint64_t)r.tokens * r.shares + 3) / 4, 768);
+    // Backward: blocks whose lines of the weights' gradients stay few, four to a unit, as many as run at once.
+    r.blocks = (uint32_t)std::min<uint64_t>(((uint64_t)r.tokens * r.shares + 3) / 4, 1024);
     return MMEE_OK;
 }
 

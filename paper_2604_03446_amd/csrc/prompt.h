@@ -261,10 +261,38 @@ __device__ __forceinline__ void mask_behind(f32x16 &x, int left)
     for (int r = 0; r < 16; ++r) x[r] = 8 * (r / 4) + r % 4 < own ? x[r] : -INFINITY;
 }
 
+// Stores a lane's column of a transposed result as store_row does, 16 bytes at a time: the two lanes that hold a row exchange what makes eight neighbours.
+template <class T, int DP>
+__device__ __forceinline__ void store_row_16(uint16_t *row, bool live, const f32x16 (&acc)[DP / 32], float times, uint32_t head_dim)
+{
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    const int h = (threadIdx.x >> 5) & 1;
+#pragma unroll
+    for (int dt = 0; dt < DP / 32; ++dt)
+#pragma unroll
+        for (int u = 0; u < 4; u += 2) {
+            u32x2 four[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const f32x4 x = {acc[dt][4 * (u + k)] * times, acc[dt][4 * (u + k) + 1] * times, acc[dt][4 * (u + k) + 2] * times, acc[dt][4 * (u + k) + 3] * times};
+                four[k] = __builtin_bit_cast(u32x2, __builtin_convertvector(x, typename T::V4));
+            }
+            u32x4 eight;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const auto r = __builtin_amdgcn_permlane32_swap(four[0][k], four[1][k], false, false);
+                eight[k] = r[0];
+                eight[2 + k] = r[1];
+            }
+            const int d = 32 * dt + 8 * (u + h);
+            if (live && d < (int)head_dim) *reinterpret_cast<u32x4 *>(row + d) = eight;
+        }
+}
+
 // Forward: as k_attn_forward with W waves of 32 rows each on a tile of 64 keys, which ends where the block's last row does; only tiles that some row
 // does not see whole are masked.
-template <class T, int DP, int W>
-__global__ __launch_bounds__(64 * W, 2) void k_prompt_forward(const PromptArgs p)
+template <class T, int DP, int W, bool LEAN>
+__global__ __launch_bounds__(64 * W, LEAN ? 4 : 2) void k_prompt_forward(const PromptArgs p)
 {
     constexpr int TN = 64, MT = 2, CH = DP / 8, GT = 64 * W;
     __shared__ u32x4 memory[4 * TN * CH];
@@ -357,22 +385,65 @@ __global__ __launch_bounds__(64 * W, 2) void k_prompt_forward(const PromptArgs p
             for (int part = 0; part < 2; ++part) columns_times<T, DP, 1>(sums, v_tile(s), 32 * mt + 16 * part, of[mt][part]);
     };
 
-    if (count) {
+    if constexpr (LEAN) {
+        // Short sequences: what counts is how many blocks run at once, so that the trips to memory of one overlap those of others.  32 keys at a time, so that
+        // 128 registers suffice.
+        if (count) {
+            load_keys(0);
+            load_values(0);
+        }
+#pragma unroll 1
+        for (uint32_t s = 0; s < count; ++s) {
+            sk.store(k_tile(s), thread);
+            sv.store(v_tile(s), thread);
+            __syncthreads();
+            if (s + 1 < count) {
+                load_keys(s + 1);
+                load_values(s + 1);
+            }
+            const int left = (int)limit - (int)first_of(s);
+            const bool whole = __all(left >= TN);
+#pragma unroll 1
+            for (int mt = 0; mt < MT; ++mt) {
+                f32x16 y = keys_by_rows<T, DP>(k_tile(s), 32 * mt, q);
+                if (!whole) mask_behind(y, left - 32 * mt);
+                most = y[0];
+#pragma unroll
+                for (int r = 1; r < 16; ++r) most = __builtin_elementwise_maximum(most, y[r]);
+                raise();
+                const float off = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    y[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(y[r], a.scale_log2, -off));
+                    total += y[r];
+                }
+#pragma unroll
+                for (int part = 0; part < 2; ++part) {
+                    const typename T::V8 pr[1] = {rounded<T>(y, part)};
+                    columns_times<T, DP, 1>(sums, v_tile(s) + 32 * mt * CH, 16 * part, pr);
+                }
+            }
+        }
+    } else if (count) {
         // Tile s + 1's scores beside tile s's exponentials, its maximum beside tile s's product with V: K runs a tile ahead of V.
-        load_keys(0);
-        load_values(0);
-        sk.store(k_tile(0), thread);
-        sv.store(v_tile(0), thread);
+        // The first tiles' loads all at once: one trip to memory instead of three.
+        {
+            Stage<DP, TN, GT, MODE_PLAIN> k0, v0, k1;
+            k0.load(keys, k_at, a.ks, thread, first_of(0), 0);
+            v0.load(keys, v_at, a.vs, thread, first_of(0), 0);
+            k1.load(keys, k_at, a.ks, thread, first_of(1), 0);
+            load_values(1);
+            load_keys(2);
+            k0.store(k_tile(0), thread);
+            v0.store(v_tile(0), thread);
+            k1.store(k_tile(1), thread);
+        }
         __syncthreads();
-        load_keys(1);
-        load_values(1);
         scores(x, 0);
         mask(x, 0);
         most = maximum(x);
         raise();
-        sk.store(k_tile(1), thread);
         __syncthreads();
-        load_keys(2);
 
         // Tile s from its scores `now`; the next one's scores into `next`.  In slots of one product, the read of an operand that is wanted some products later
         // and a share of the vector instructions, in this order: left to itself the compiler reads every operand right before its use.
@@ -438,12 +509,11 @@ __global__ __launch_bounds__(64 * W, 2) void k_prompt_forward(const PromptArgs p
         last(s, x);
     }
     total = sum_of_halves(total);
-    if (!live) return;
     const float times = total != 0.0f ? 1.0f / total : 0.0f, sum2 = total != 0.0f ? top + __log2f(total) : -INFINITY;
     if (tile.pieces == 1) {
-        store_row<T, DP>(a.o + tile.q0 * a.os.token + row_at(a, a.os, 0, tile.kvh, row), o, times, a.head_dim);
-        if (a.lse && h == 0) a.lse[lse_at(a, 0, tile.kvh, row) + tile.q0] = sum2 * LN2;
-    } else {
+        store_row_16<T, DP>(a.o + tile.q0 * a.os.token + row_at(a, a.os, 0, tile.kvh, live ? row : 0), live, o, times, a.head_dim);
+        if (a.lse && live && h == 0) a.lse[lse_at(a, 0, tile.kvh, row) + tile.q0] = sum2 * LN2;
+    } else if (live) {
         const int64_t line = tile.part(p, tile.piece) + 32 * wave + n;
         store_part<DP>(a.part_o + line * DP, o, times);
         if (h == 0) a.part_lse[line] = sum2;
@@ -557,14 +627,13 @@ __global__ __launch_bounds__(64 * W, 2) void k_prompt_dq(const PromptArgs p)
             }
         }
     }
-    if (!live) return;
     if (lse2 == INFINITY) {                             // (a row that sees nothing, whatever its query and gradient hold)
 #pragma unroll
         for (int dt = 0; dt < DP / 32; ++dt) dq[0][dt] = f32x16{};
     }
     const float times = NARROW<T> ? a.scale * __builtin_amdgcn_exp2f(-(UP + HIGHEST + lowered)) : a.scale;
-    if (tile.pieces == 1) store_row<T, DP>(a.dq + tile.q0 * a.dqs.token + row_at(a, a.dqs, 0, tile.kvh, row), dq[0], times, a.head_dim);
-    else store_part<DP>(a.part_o + (tile.part(p, tile.piece) + 32 * wave + n) * DP, dq[0], times);
+    if (tile.pieces == 1) store_row_16<T, DP>(a.dq + tile.q0 * a.dqs.token + row_at(a, a.dqs, 0, tile.kvh, live ? row : 0), live, dq[0], times, a.head_dim);
+    else if (live) store_part<DP>(a.part_o + (tile.part(p, tile.piece) + 32 * wave + n) * DP, dq[0], times);
 }
 
 // dK and dV of 32 W keys, 32 a wave, over the rows that see them, as k_attn_dkv.
@@ -670,12 +739,11 @@ __global__ __launch_bounds__(64 * W, 2) void k_prompt_dkv(const PromptArgs p)
             }
         }
     }
-    if (!valid) return;
     const float times = NARROW<T> ? a.scale * 0x1p-15f / by : a.scale, times_v = NARROW<T> ? 0x1p-15f : 1.0f;
     if (tile.pieces == 1) {
-        store_row<T, DP>(a.dk + key_at * a.dks.token + tile.kvh * a.dks.head, dk[0], times, a.head_dim);
-        store_row<T, DP>(a.dv + key_at * a.dvs.token + tile.kvh * a.dvs.head, dv[0], times_v, a.head_dim);
-    } else {
+        store_row_16<T, DP>(a.dk + key_at * a.dks.token + tile.kvh * a.dks.head, valid, dk[0], times, a.head_dim);
+        store_row_16<T, DP>(a.dv + key_at * a.dvs.token + tile.kvh * a.dvs.head, valid, dv[0], times_v, a.head_dim);
+    } else if (valid) {
         float *part = a.part_o + (tile.part(p, tile.piece) + 32 * wave + n) * 2 * DP;
         store_part<DP>(part, dk[0], times);
         store_part<DP>(part + DP, dv[0], times_v);
@@ -884,13 +952,13 @@ __global__ __launch_bounds__(256, 1) void k_prompt_dkv_wide(const PromptArgs p)
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
         const uint32_t key = key0 + 32 * u + n;
-        if (key >= tile.n) continue;
-        const int64_t at = (int64_t)tile.k0 + key;
+        const bool valid = key < tile.n;
+        const int64_t at = (int64_t)tile.k0 + (valid ? key : 0);
         const float times = NARROW<T> ? a.scale * 0x1p-15f / by[u] : a.scale, times_v = NARROW<T> ? 0x1p-15f : 1.0f;
         if (tile.pieces == 1) {
-            store_row<T, DP>(a.dk + at * a.dks.token + tile.kvh * a.dks.head, dk[u], times, a.head_dim);
-            store_row<T, DP>(a.dv + at * a.dvs.token + tile.kvh * a.dvs.head, dv[u], times_v, a.head_dim);
-        } else {
+            store_row_16<T, DP>(a.dk + at * a.dks.token + tile.kvh * a.dks.head, valid, dk[u], times, a.head_dim);
+            store_row_16<T, DP>(a.dv + at * a.dvs.token + tile.kvh * a.dvs.head, valid, dv[u], times_v, a.head_dim);
+        } else if (valid) {
             float *part = a.part_o + (tile.part(p, tile.piece) + 64 * wave + 32 * u + n) * 2 * DP;
             store_part<DP>(part, dk[u], times);
             store_part<DP>(part + DP, dv[u], times_v);

@@ -32,7 +32,7 @@ uint64_t up256(uint64_t x) { return (x + 255) & ~(uint64_t)255; }
 struct Launch {
     int waves = 4;
     uint64_t slots = 0, parts = 0, blocks = 0, room = 0, step = 0, least = 0;
-    bool planned = false, pieces = false;
+    bool planned = false, pieces = false, lean = false;
     uint64_t plan_bytes() const { return planned ? up256(4 * (ENTRIES + ENTRY * slots)) : 0; }
     // Results of pieces, so many floats a row or key.
     uint64_t parts_bytes(uint64_t kv_heads, uint64_t floats) const { return up256(4 * parts * kv_heads * 32 * waves * floats); }
@@ -55,6 +55,7 @@ Launch plan_launch(uint64_t lines, uint64_t seqs, uint64_t kv_heads, uint64_t ac
     l.room = 2048 / l.waves;
     l.step = step;
     l.least = 512 / step;
+    l.lean = across / seqs <= 256;
     const uint64_t tiles = std::max<uint64_t>(1, lines / (32 * l.waves) + seqs / 2), blocks = tiles * kv_heads, steps = across / seqs / step;
     if (seqs <= PLAN_SEQS && l.slots <= PLAN_TILES) {
         // Four times as many tiles as run at once even out the end by themselves.
@@ -170,7 +171,13 @@ void with_waves(int waves, F f)
 template <class T, int DP, int W>
 void forward_as(const PromptArgs &p, const Launch &at, Launching &l)
 {
-    l.run(k_prompt_forward<T, DP, W>, at.blocks, 64 * W, p);
+    bool done = false;
+    if constexpr (DP <= 64 && W == 4)
+        if (at.lean) {
+            l.run(k_prompt_forward<T, DP, W, true>, at.blocks, 64 * W, p);
+            done = true;
+        }
+    if (!done) l.run(k_prompt_forward<T, DP, W, false>, at.blocks, 64 * W, p);
     if (at.pieces) l.run(k_prompt_join<T, DP, W>, at.blocks * W, 256, p);
 }
 

@@ -19,11 +19,13 @@ struct PromptArgs {
     uint32_t seqs, slots;       // slots: of tiles, or of a plan's entries, of every head
     uint32_t parts;             // pieces of cut tiles, at most, of every head
     float *lse2;                // backward: [kv_head][row], in powers of two, infinite where a row sees nothing; less what float16 takes off
-    const uint32_t *plan;       // the number of entries, and from ENTRIES on the entries; or null
+    const uint32_t *plan;       // or null
     bool causal;
     bool dies;                  // heads are dealt out to the dies, whose L2 then holds their keys
 };
 
+// A plan: words 0 and 1 the numbers of entries and of tiles that were cut, the entries, the numbers of the cut tiles' first entries (parts / 2 at most).  An
+// entry:
 constexpr uint32_t ENTRIES = 8, ENTRY = 12;             // words: q0, m, k0, n, index, step0, count, piece, pieces, number of the tile's first piece, two unused
 
 // Keys 0 .. of its sequence that a token sees.
@@ -68,25 +70,23 @@ struct Tile {
     uint32_t index, q0, m, k0, n, kvh, piece = 0, pieces = 1, first_part = 0, step0 = 0, count = 0;
     bool there;
 
-    // at: place among heads and slots.
-    __device__ __forceinline__ Tile(const PromptArgs &p, uint32_t at)
+    // at: place among heads and slots; with CUT: among heads and the tiles that were cut.
+    template <bool CUT = false>
+    __device__ __forceinline__ Tile(const PromptArgs &p, uint32_t at, std::integral_constant<bool, CUT> = {})
     {
+        if (CUT) {
+            const uint32_t most = p.parts / 2;
+            kvh = at / most;
+            there = at % most < p.plan[1];
+            if (there) take(p.plan + ENTRIES + ENTRY * p.plan[ENTRIES + ENTRY * p.slots + at % most]);
+            return;
+        }
         kvh = p.dies ? at / p.slots : at % p.a.kv_heads;
         const uint32_t slot = p.dies ? at % p.slots : at / p.a.kv_heads;
         if (p.plan) {
             there = slot < p.plan[0];
             if (!there) return;
-            const uint32_t *e = p.plan + ENTRIES + ENTRY * slot;
-            q0 = e[0];
-            m = e[1];
-            k0 = e[2];
-            n = e[3];
-            index = e[4];
-            step0 = e[5];
-            count = e[6];
-            piece = e[7];
-            pieces = e[8];
-            first_part = e[9];
+            take(p.plan + ENTRIES + ENTRY * slot);
             return;
         }
         const int32_t *starts = KEYS ? p.kv_starts : p.q_starts;
@@ -103,6 +103,20 @@ struct Tile {
         index = slot - (uint32_t)slot_of(seq);
         there = index < (s.lines(p, KEYS) + TILE - 1) / TILE;
         if (there) count = s.steps(p, KEYS, TILE, STEP, index);
+    }
+
+    __device__ __forceinline__ void take(const uint32_t *entry)
+    {
+        q0 = entry[0];
+        m = entry[1];
+        k0 = entry[2];
+        n = entry[3];
+        index = entry[4];
+        step0 = entry[5];
+        count = entry[6];
+        piece = entry[7];
+        pieces = entry[8];
+        first_part = entry[9];
     }
 
     // Of a tile that is there: the same in all lanes, so that loops on its numbers are scalar, and so are the buffers that it is loaded from.  (Said once it is
@@ -137,17 +151,17 @@ struct PlanArgs {
     PlanOf of[2];
 };
 
-constexpr uint32_t PLAN_SEQS = 2048, PLAN_TILES = 8192; // at most
+constexpr uint32_t PLAN_SEQS = 2048, PLAN_TILES = 2048, PLAN_THREADS = 256;     // sequences and tiles at most
 
-// Plans of[blockIdx.x].  Tiles and pieces are sorted by their length in 1024 classes; which of a class come first does not matter to any result.
-// One block; for prompts of 17 to 2500 rows 5 us, of which most is the latency of the starts and of a dozen barriers.
-__global__ __launch_bounds__(1024) void k_prompt_plan(const PlanArgs x)
+// Plans of[blockIdx.x].  Tiles and pieces are sorted by their length in 256 classes; which of a class come first does not matter to any result.
+// One block; for 24 prompts of 17 to 2500 rows 4 us, of which most is the latency of the starts and of a dozen barriers (with 1024 threads 5).
+__global__ __launch_bounds__(PLAN_THREADS) void k_prompt_plan(const PlanArgs x)
 {
-    constexpr uint32_t MINE = PLAN_TILES / 1024, CLASSES = 1024;
+    constexpr uint32_t MINE = PLAN_TILES / PLAN_THREADS, CLASSES = PLAN_THREADS, WAVES = PLAN_THREADS / 64;
     const PromptArgs &p = x.p;
     const PlanOf &of = x.of[blockIdx.x];
     __shared__ uint32_t first_tile[PLAN_SEQS + 1];
-    __shared__ uint32_t classes[CLASSES], sums[16], more[16];
+    __shared__ uint32_t classes[CLASSES], sums[WAVES], more[WAVES], cuts;
     const uint32_t thread = threadIdx.x, lane = thread & 63, wave = thread >> 6;
 
     // the sum of all threads' x, and the largest y; sums_before: of the threads before this one
@@ -157,15 +171,15 @@ __global__ __launch_bounds__(1024) void k_prompt_plan(const PlanArgs x)
         if (lane == 63) sums[wave] = upto;
         if (lane == 0) more[wave] = most;
         __syncthreads();
-        const uint32_t other = lane < 16 ? sums[lane] : 0, below = sums_below(other), top = most_of_lanes(lane < 16 ? more[lane] : 0);
-        sum_all = __builtin_amdgcn_readlane(below, 15);
+        const uint32_t other = lane < WAVES ? sums[lane] : 0, below = sums_below(other), top = most_of_lanes(lane < WAVES ? more[lane] : 0);
+        sum_all = __builtin_amdgcn_readlane(below, WAVES - 1);
         sum_before = upto - a + (wave ? __shfl(below, wave - 1) : 0);
         most_all = top;
         __syncthreads();
     };
 
     uint32_t tiles = 0;
-    for (uint32_t from = 0; from < p.seqs; from += 1024) {
+    for (uint32_t from = 0; from < p.seqs; from += PLAN_THREADS) {
         const uint32_t seq = from + thread;
         const uint32_t here = seq < p.seqs ? (Sequence(p, seq).lines(p, of.keys) + of.tile - 1) / of.tile : 0;
         reduce(here, 0);
@@ -173,7 +187,10 @@ __global__ __launch_bounds__(1024) void k_prompt_plan(const PlanArgs x)
         tiles += sum_all;
     }
     classes[thread] = 0;
-    if (thread == 0) first_tile[p.seqs] = tiles;
+    if (thread == 0) {
+        first_tile[p.seqs] = tiles;
+        cuts = 0;
+    }
     __syncthreads();
     if (tiles > PLAN_TILES) tiles = PLAN_TILES;         // (starts that do not ascend)
 
@@ -181,9 +198,9 @@ __global__ __launch_bounds__(1024) void k_prompt_plan(const PlanArgs x)
     uint32_t steps[MINE], seqs[MINE], total = 0, longest = 0;
 #pragma unroll
     for (uint32_t i = 0; i < MINE; ++i) {
-        const uint32_t t = i * 1024 + thread;
+        const uint32_t t = i * PLAN_THREADS + thread;
         steps[i] = seqs[i] = 0;
-        if (i * 1024 >= tiles) continue;                // by the whole block
+        if (i * PLAN_THREADS >= tiles) continue;                // by the whole block
         if (t < tiles) {
             uint32_t low = 0, high = p.seqs;            // first_tile[low] <= t < first_tile[high]
             while (high - low > 1) {
@@ -218,7 +235,7 @@ __global__ __launch_bounds__(1024) void k_prompt_plan(const PlanArgs x)
     uint32_t cut = 0;                                   // pieces of this thread's cut tiles
 #pragma unroll
     for (uint32_t i = 0; i < MINE; ++i)
-        if (i * 1024 + thread < tiles) {
+        if (i * PLAN_THREADS + thread < tiles) {
             const uint32_t pieces = pieces_of(steps[i]);
             atomicAdd(&classes[class_of(steps[i] - (pieces - 1) * size)], 1);
             if (pieces > 1) atomicAdd(&classes[class_of(size)], pieces - 1);
@@ -232,13 +249,16 @@ __global__ __launch_bounds__(1024) void k_prompt_plan(const PlanArgs x)
     reduce(own, 0);
     classes[thread] = sum_before;
     const bool fits = !too_many && sum_all <= of.slots;
-    if (thread == 0) of.plan[0] = fits ? sum_all : 0;
+    if (thread == 0) {
+        of.plan[0] = fits ? sum_all : 0;
+        of.plan[1] = 0;
+    }
     __syncthreads();
     if (!fits) return;
 #pragma unroll
     for (uint32_t i = 0; i < MINE; ++i)
-        if (i * 1024 + thread < tiles) {
-            const uint32_t pieces = pieces_of(steps[i]), index = i * 1024 + thread - first_tile[seqs[i]];
+        if (i * PLAN_THREADS + thread < tiles) {
+            const uint32_t pieces = pieces_of(steps[i]), index = i * PLAN_THREADS + thread - first_tile[seqs[i]];
             const Sequence q(p, seqs[i]);
             for (uint32_t k = 0; k < pieces; ++k) {
                 const uint32_t step0 = k * size, count = k + 1 < pieces ? size : steps[i] - step0, at = atomicAdd(&classes[class_of(count)], 1);
@@ -246,9 +266,12 @@ __global__ __launch_bounds__(1024) void k_prompt_plan(const PlanArgs x)
                 e[0] = u32x4{q.q0, q.m, q.k0, q.n};
                 e[1] = u32x4{index, step0, count, k};
                 e[2] = u32x4{pieces, part, 0, 0};
+                if (pieces > 1 && k == 0) of.plan[ENTRIES + ENTRY * of.slots + atomicAdd(&cuts, 1)] = at;
             }
             part += pieces > 1 ? pieces : 0;
         }
+    __syncthreads();
+    if (thread == 0) of.plan[1] = cuts;
 }
 
 __device__ __forceinline__ uint32_t block_place(const PromptArgs &p) { return p.dies ? by_die(blockIdx.x, gridDim.x) : blockIdx.x; }
@@ -522,14 +545,15 @@ __global__ __launch_bounds__(64 * W, LEAN ? 4 : 2) void k_prompt_forward(const P
 
 // Joins the pieces of the tiles of 32 W rows that were cut, in ascending order, as k_attn_join does: 32 rows a block.
 template <class T, int DP, int W>
-__global__ __launch_bounds__(256) void k_prompt_join(const PromptArgs p)
+__global__ __launch_bounds__(8 * DP) void k_prompt_join(const PromptArgs p)
 {
     constexpr int C4 = DP / 4;
     const AttnArgs &a = p.a;
-    Tile<32 * W, 64, false> tile(p, blockIdx.x / W);
-    if (!tile.there || tile.piece || tile.pieces == 1) return;
+    Tile<32 * W, 64, false> tile(p, blockIdx.x / W, std::true_type());
+    if (!tile.there) return;
     tile.settle();
-    for (uint32_t i = threadIdx.x; i < 32 * C4; i += 256) {
+    {
+        const uint32_t i = threadIdx.x;
         const uint32_t within_tile = blockIdx.x % W * 32 + i / C4, row = tile.index * 32 * W + within_tile, c = i % C4;
         if (row >= tile.m * a.group) return;
         const int64_t line = tile.part(p, 0) + within_tile;
@@ -968,15 +992,16 @@ __global__ __launch_bounds__(256, 1) void k_prompt_dkv_wide(const PromptArgs p)
 
 // Sums of the pieces of tiles that were cut, in ascending order, rounded once, as k_attn_sum: dQ of 32 rows a block, or, with KEYS, dK and dV of 32 keys.
 template <class T, int DP, int W, int STEP, bool KEYS>
-__global__ __launch_bounds__(256) void k_prompt_sum(const PromptArgs p)
+__global__ __launch_bounds__(8 * DP) void k_prompt_sum(const PromptArgs p)
 {
     constexpr int C4 = DP / 4 * (KEYS ? 2 : 1);
     const AttnArgs &a = p.a;
-    Tile<32 * W, STEP, KEYS> tile(p, blockIdx.x / W);
-    if (!tile.there || tile.piece || tile.pieces == 1) return;
+    Tile<32 * W, STEP, KEYS> tile(p, blockIdx.x / W, std::true_type());
+    if (!tile.there) return;
     tile.settle();
     const uint32_t lines = KEYS ? tile.n : tile.m * a.group;
-    for (uint32_t i = threadIdx.x; i < 32 * C4; i += 256) {
+#pragma unroll
+    for (uint32_t i = threadIdx.x; i < 32 * C4; i += 8 * DP) {
         const uint32_t within_tile = blockIdx.x % W * 32 + i / C4, own = tile.index * 32 * W + within_tile, c = i % C4, d = 4 * c % DP;
         if (own >= lines) return;
         if (d >= a.head_dim) continue;

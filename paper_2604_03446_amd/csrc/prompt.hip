@@ -33,7 +33,9 @@ struct Launch {
     int waves = 4;
     uint64_t slots = 0, parts = 0, blocks = 0, room = 0, step = 0, least = 0;
     bool planned = false, pieces = false, lean = false;
-    uint64_t plan_bytes() const { return planned ? up256(4 * (ENTRIES + ENTRY * slots)) : 0; }
+    // Of the kernels that join pieces: 32 rows or keys each of every tile that may have been cut.
+    uint64_t cut_blocks(const PromptArgs &p) const { return parts / 2 * p.a.kv_heads * waves; }
+    uint64_t plan_bytes() const { return planned ? up256(4 * (ENTRIES + ENTRY * slots + parts / 2)) : 0; }
     // Results of pieces, so many floats a row or key.
     uint64_t parts_bytes(uint64_t kv_heads, uint64_t floats) const { return up256(4 * parts * kv_heads * 32 * waves * floats); }
 };
@@ -180,14 +182,14 @@ void forward_as(const PromptArgs &p, const Launch &at, Launching &l)
             done = true;
         }
     if (!done) l.run(k_prompt_forward<T, DP, W, false>, at.blocks, 64 * W, p);
-    if (at.pieces) l.run(k_prompt_join<T, DP, W>, at.blocks * W, 256, p);
+    if (at.pieces) l.run(k_prompt_join<T, DP, W>, at.cut_blocks(p), 8 * DP, p);
 }
 
 template <class T, int DP, int W>
 void dq_as(const PromptArgs &p, const Launch &at, Launching &l)
 {
     l.run(k_prompt_dq<T, DP, W>, at.blocks, 64 * W, p);
-    if (at.pieces) l.run(k_prompt_sum<T, DP, W, 64, false>, at.blocks * W, 256, p);
+    if (at.pieces) l.run(k_prompt_sum<T, DP, W, 64, false>, at.cut_blocks(p), 8 * DP, p);
 }
 
 // Whether a step's 32 rows are whole tokens and lie, like the two statistics, within 32 bits of each other.
@@ -207,7 +209,7 @@ void dkv_as(const PromptArgs &p, const Launch &at, Launching &l)
             done = true;
         }
     if (!done) l.run(k_prompt_dkv<T, DP, W>, at.blocks, 64 * W, p);
-    if (at.pieces) l.run(k_prompt_sum<T, DP, W, DP == 128 ? 32 : 64, true>, at.blocks * W, 256, p);
+    if (at.pieces) l.run(k_prompt_sum<T, DP, W, DP == 128 ? 32 : 64, true>, at.cut_blocks(p), 8 * DP, p);
 }
 
 }  // namespace
@@ -242,7 +244,7 @@ int mmee_prompt_attn_forward(const mmee_prompt_attn *x)
     make(plans, n, p, plan.forward, false);
     Launching l;
     if (l.rc) return l.rc;
-    if (n) l.run(k_prompt_plan, n, 1024, plans);
+    if (n) l.run(k_prompt_plan, n, PLAN_THREADS, plans);
     dispatch(plan, [&](auto type, auto dp) {
         with_waves<(dp.value >= 64)>(plan.forward.waves, [&](auto w) { forward_as<decltype(type), dp.value, w.value>(p, plan.forward, l); });
     });
@@ -279,7 +281,7 @@ int mmee_prompt_attn_backward(const mmee_prompt_attn *x, const mmee_prompt_attn_
     make(plans, n, dkv, plan.dkv, true);
     Launching l;
     if (l.rc) return l.rc;
-    if (n) l.run(k_prompt_plan, n, 1024, plans);
+    if (n) l.run(k_prompt_plan, n, PLAN_THREADS, plans);
     dispatch(plan, [&](auto type, auto dp) {
         if (a.rows) with_waves<(dp.value == 128)>(plan.dq.waves, [&](auto w) { dq_as<decltype(type), dp.value, w.value>(dq, plan.dq, l); });
         if (a.kv_len) with_waves<(dp.value >= 64)>(plan.dkv.waves, [&](auto w) { dkv_as<decltype(type), dp.value, w.value>(dkv, plan.dkv, l); });

@@ -312,13 +312,76 @@ __device__ __forceinline__ void store_row_16(uint16_t *row, bool live, const f32
         }
 }
 
+// Loads straight to shared memory: 16 or 4 bytes a lane, `offset` (a lane's own, in bytes) behind the base, lane after lane to the place `to`.
+// Written out, as the compiler waits for all that are under way at every barrier and at the first read of shared memory after one: who uses them counts them
+// and waits (`arrived`).  (m0 is not said to be written: it is a register that the compiler keeps out of its own hands, and sets before every use.)
+__device__ __forceinline__ void load_16_to_shared(const void *base, uint32_t offset, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory");
+}
+
+__device__ __forceinline__ void load_4_to_shared(const void *base, uint32_t offset, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory");
+}
+
+__device__ __forceinline__ uint32_t place_in_shared(const void *p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)p; }
+
+// All but the last LEFT loads of this wave are there, and, behind the barrier, those of all waves; this wave reads nothing older any more.
+template <int LEFT>
+__device__ __forceinline__ void arrived()
+{
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory");
+}
+
+// Tiles of 64 keys on their way to shared memory, without registers between: a wave's share, what a lane loads of it.
+template <int DP, int W>
+struct Incoming {
+    static constexpr int CH = DP / 8, MINE = CH / W;    // loads of a wave a tile, 64 chunks each
+    static_assert(MINE * W == CH, "a tile is dealt out evenly");
+    const uint16_t *from;                               // the head's first key of the sequence
+    int64_t stride;
+    uint32_t head_dim;
+    int wave, lane;
+    uint32_t offset[MINE];                              // in a whole tile, bytes
+
+    __device__ __forceinline__ Incoming(const uint16_t *from_, int64_t stride_, uint32_t head_dim_, int wave_, int lane_)
+        : from(from_), stride(stride_), head_dim(head_dim_), wave(wave_), lane(lane_)
+    {
+#pragma unroll
+        for (int i = 0; i < MINE; ++i) offset[i] = offset_of(i, 64);
+    }
+
+    // Keys past the last one repeat it, columns past the head's the first ones: those keys are masked, and the rows' operands are 0 there.
+    __device__ __forceinline__ uint32_t offset_of(int i, uint32_t left) const
+    {
+        const uint32_t at = (wave * MINE + i) * 64 + lane, own = at / CH, row = own < left ? own : left - 1;
+        const int c = (at % CH) ^ spread<CH>(own);
+        return 2 * (row * (uint32_t)stride + (8 * c < (int)head_dim ? 8 * c : 0));
+    }
+
+    // Keys first .. of n; there is one at least.
+    __device__ __forceinline__ void load(u32x4 *tile, uint32_t first, uint32_t n) const
+    {
+        const uint16_t *base = from + first * stride;
+        const uint32_t left = n - first;
+#pragma unroll
+        for (int i = 0; i < MINE; ++i) {
+            uint32_t own = offset[i];
+            if (left < 64) own = offset_of(i, left);
+            load_16_to_shared(base, own, place_in_shared(tile + (wave * MINE + i) * 64));
+        }
+    }
+};
+
 // Forward: as k_attn_forward with W waves of 32 rows each on a tile of 64 keys, which ends where the block's last row does; only tiles that some row
 // does not see whole are masked.
 template <class T, int DP, int W, bool LEAN>
 __global__ __launch_bounds__(64 * W, LEAN ? 4 : 2) void k_prompt_forward(const PromptArgs p)
 {
-    constexpr int TN = 64, MT = 2, CH = DP / 8, GT = 64 * W;
-    __shared__ u32x4 memory[4 * TN * CH];
+    // Tiles under way: K of tile s + 1 + DEEP and V of tile s + DEEP while tile s is worked on.
+    constexpr int TN = 64, MT = 2, CH = DP / 8, GT = 64 * W, DEEP = !LEAN && DP <= 64 ? 3 : 1, RING = DEEP + 1;
+    __shared__ u32x4 memory[2 * RING * TN * CH];
     const AttnArgs &a = p.a;
     Tile<32 * W, TN, false> tile(p, block_place(p));
     if (!tile.there) return;
@@ -328,7 +391,6 @@ __global__ __launch_bounds__(64 * W, LEAN ? 4 : 2) void k_prompt_forward(const P
     const bool live = row < rows;
     const uint32_t limit = limit_of(p, tile.m, tile.n, token_of(a, live ? row : rows - 1)), all_see = limit_of(p, tile.m, tile.n, token_of(a, row0));
 
-    const Keys<MODE_PLAIN> keys = tile.keys(p);
     const uint16_t *const k_at = a.k + tile.k0 * a.ks.token, *const v_at = a.v + tile.k0 * a.vs.token;
     typename T::V8 q[DP / 16];
     row_operands<T, DP>(q, a.q + tile.q0 * a.qs.token + row_at(a, a.qs, 0, tile.kvh, live ? row : 0), live, a.head_dim);
@@ -336,16 +398,13 @@ __global__ __launch_bounds__(64 * W, LEAN ? 4 : 2) void k_prompt_forward(const P
     f32x16 sums[1][DP / 32] = {};
     f32x16(&o)[DP / 32] = sums[0];
     float top = -INFINITY, total = 0.0f;                // mark near the maximum (scaled, in powers of two); this lane's share of the sum
-    Stage<DP, TN, GT, MODE_PLAIN> sk, sv;
-    auto k_tile = [&](uint32_t s) { return memory + (s & 1) * TN * CH; };
-    auto v_tile = [&](uint32_t s) { return memory + (2 + (s & 1)) * TN * CH; };
+    auto k_tile = [&](uint32_t s) { return memory + s % RING * TN * CH; };     // s: of the tile, or its remainder
+    auto v_tile = [&](uint32_t s) { return memory + (RING + s % RING) * TN * CH; };
     auto first_of = [&](uint32_t s) { return (step0 + s) * TN; };
     constexpr float HIGHER = NARROW<T> ? 7.0f : 0.0f;   // powers of two, of probabilities: see k_attn_forward
     f32x16 x[MT], ahead[MT];
     float most = -INFINITY;                             // maximum of the scores that are next, scaled
 
-    auto load_keys = [&](uint32_t s) { sk.load(keys, k_at, a.ks, thread, first_of(s), 0); };
-    auto load_values = [&](uint32_t s) { sv.load(keys, v_at, a.vs, thread, first_of(s), 0); };
     // Operands: of the product i of a tile's scores (keys 32 (i mod 2) .., columns 16 (i / 2) .. of the head), and of the product i with its values
     // (columns 32 (i mod DT) .., keys 16 (i / DT) ..).
     constexpr int DT = DP / 32;
@@ -411,19 +470,19 @@ __global__ __launch_bounds__(64 * W, LEAN ? 4 : 2) void k_prompt_forward(const P
     if constexpr (LEAN) {
         // Short sequences: what counts is how many blocks run at once, so that the trips to memory of one overlap those of others.  32 keys at a time, so that
         // 128 registers suffice.
-        if (count) {
-            load_keys(0);
-            load_values(0);
-        }
+        Stage<DP, TN, GT, MODE_PLAIN> sk, sv;
+        const Keys<MODE_PLAIN> keys = tile.keys(p);
+        auto load = [&](uint32_t s) {
+            sk.load(keys, k_at, a.ks, thread, first_of(s), 0);
+            sv.load(keys, v_at, a.vs, thread, first_of(s), 0);
+        };
+        if (count) load(0);
 #pragma unroll 1
         for (uint32_t s = 0; s < count; ++s) {
             sk.store(k_tile(s), thread);
             sv.store(v_tile(s), thread);
             __syncthreads();
-            if (s + 1 < count) {
-                load_keys(s + 1);
-                load_values(s + 1);
-            }
+            if (s + 1 < count) load(s + 1);
             const int left = (int)limit - (int)first_of(s);
             const bool whole = __all(left >= TN);
 #pragma unroll 1
@@ -449,19 +508,17 @@ __global__ __launch_bounds__(64 * W, LEAN ? 4 : 2) void k_prompt_forward(const P
         }
     } else if (count) {
         // Tile s + 1's scores beside tile s's exponentials, its maximum beside tile s's product with V: K runs a tile ahead of V.
-        // The first tiles' loads all at once: one trip to memory instead of three.
-        {
-            Stage<DP, TN, GT, MODE_PLAIN> k0, v0, k1;
-            k0.load(keys, k_at, a.ks, thread, first_of(0), 0);
-            v0.load(keys, v_at, a.vs, thread, first_of(0), 0);
-            k1.load(keys, k_at, a.ks, thread, first_of(1), 0);
-            load_values(1);
-            load_keys(2);
-            k0.store(k_tile(0), thread);
-            v0.store(v_tile(0), thread);
-            k1.store(k_tile(1), thread);
+        const Incoming<DP, W> k_in(k_at + tile.kvh * a.ks.head, a.ks.token, a.head_dim, wave, lane), v_in(v_at + tile.kvh * a.vs.head, a.vs.token, a.head_dim, wave, lane);
+        constexpr int LOADS = 2 * Incoming<DP, W>::MINE;
+        const auto load_keys = [&](uint32_t s, uint32_t to) { k_in.load(k_tile(to), first_of(s < count ? s : count - 1), tile.n); };    // (behind the last one it is loaded again)
+        const auto load_values = [&](uint32_t s, uint32_t to) { v_in.load(v_tile(to), first_of(s < count ? s : count - 1), tile.n); };
+        load_keys(0, 0);
+#pragma unroll
+        for (uint32_t s = 0; s < DEEP; ++s) {
+            load_values(s, s);
+            load_keys(s + 1, s + 1);
         }
-        __syncthreads();
+        arrived<LOADS * (DEEP - 1)>();
         scores(x, 0);
         mask(x, 0);
         most = maximum(x);
@@ -470,19 +527,22 @@ __global__ __launch_bounds__(64 * W, LEAN ? 4 : 2) void k_prompt_forward(const P
 
         // Tile s from its scores `now`; the next one's scores into `next`.  In slots of one product, the read of an operand that is wanted some products later
         // and a share of the vector instructions, in this order: left to itself the compiler reads every operand right before its use.
-        auto step = [&](uint32_t s, f32x16 (&now)[MT], f32x16 (&next)[MT], auto masked) {
+        // at: s, or what it leaves divided by RING, known when this is compiled.
+        auto step = [&](uint32_t s, auto at, f32x16 (&now)[MT], f32x16 (&next)[MT], auto masked) {
             constexpr int KP = MT * DP / 16, VP = KP, AHEAD = W == 8 ? 3 : 2, EACH = 16 * MT / KP;
             typename T::V8 pr[MT][2][1];
             u32x4 ko[AHEAD];
             s16x4 vo[AHEAD][2];
             const float off = top == -INFINITY ? 0.0f : top;
+            load_keys(s + 1 + DEEP, at + 1 + DEEP);     // to where nobody reads any more since the last barrier
+            load_values(s + DEEP, at + DEEP);
 #pragma unroll
-            for (int i = 0; i < AHEAD; ++i) ko[i] = key_operand(s + 1, i);
+            for (int i = 0; i < AHEAD; ++i) ko[i] = key_operand(at + 1, i);
 #pragma unroll
             for (int i = 0; i < KP; ++i) {
                 next[i % MT] = T::mma(as_operand<T>(ko[i % AHEAD]), q[i / MT], i < MT ? f32x16{} : next[i % MT]);
-                if (i + AHEAD < KP) ko[i % AHEAD] = key_operand(s + 1, i + AHEAD);
-                else value_operand(vo[i + AHEAD - KP], s, i + AHEAD - KP);
+                if (i + AHEAD < KP) ko[i % AHEAD] = key_operand(at + 1, i + AHEAD);
+                else value_operand(vo[i + AHEAD - KP], at, i + AHEAD - KP);
 #pragma unroll
                 for (int e = i * EACH; e < (i + 1) * EACH; ++e) {
                     now[e / 16][e % 16] = __builtin_amdgcn_exp2f(__builtin_fmaf(now[e / 16][e % 16], a.scale_log2, -off));
@@ -496,22 +556,14 @@ __global__ __launch_bounds__(64 * W, LEAN ? 4 : 2) void k_prompt_forward(const P
 #pragma unroll
             for (int i = 0; i < VP; ++i) {
                 o[i % DT] = T::mma(join<T>(vo[i % AHEAD][0], vo[i % AHEAD][1]), pr[i / DT / 2][i / DT % 2][0], o[i % DT]);
-                if (i + AHEAD < VP) value_operand(vo[i % AHEAD], s, i + AHEAD);
+                if (i + AHEAD < VP) value_operand(vo[i % AHEAD], at, i + AHEAD);
 #pragma unroll
                 for (int e = i * EACH; e < (i + 1) * EACH; ++e) m = __builtin_elementwise_maximum(m, next[e / 16][e % 16]);
-                if (i == VP / 4) {                      // tiles that nobody reads any more since the last barrier
-                    sk.store(k_tile(s), thread);
-                    sv.store(v_tile(s + 1), thread);
-                }
-                if (i == VP / 2) {
-                    load_keys(s + 3);
-                    load_values(s + 2);
-                }
                 __builtin_amdgcn_sched_barrier(0);
             }
             most = m;
             raise();
-            __syncthreads();
+            arrived<LOADS * (DEEP - 1)>();              // K of tile s + 2, V of tile s + 1
         };
         auto last = [&](uint32_t s, f32x16 (&now)[MT]) {
             typename T::V8 pr[MT][2][1];
@@ -519,17 +571,22 @@ __global__ __launch_bounds__(64 * W, LEAN ? 4 : 2) void k_prompt_forward(const P
             values(s, pr);
         };
         uint32_t s = 0;
-        for (; s + 3 < count && first_of(s + 3) <= all_see; s += 2) {       // tiles s + 1 and s + 2 are seen whole by every row
-            step(s, x, ahead, std::false_type());
-            step(s + 1, ahead, x, std::false_type());
+        for (; s + RING + 1 < count && first_of(s + RING + 1) <= all_see; s += RING) {      // tiles s + 1 .. s + RING are seen whole by every row
+            step(s, std::integral_constant<uint32_t, 0>(), x, ahead, std::false_type());
+            step(s + 1, std::integral_constant<uint32_t, 1>(), ahead, x, std::false_type());
+            if constexpr (RING == 4) {
+                step(s + 2, std::integral_constant<uint32_t, 2>(), x, ahead, std::false_type());
+                step(s + 3, std::integral_constant<uint32_t, 3>(), ahead, x, std::false_type());
+            }
         }
 #pragma unroll 1
         for (; s + 1 < count; ++s) {
-            step(s, x, ahead, std::true_type());
+            step(s, s, x, ahead, std::true_type());
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) x[mt] = ahead[mt];
         }
         last(s, x);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");        // nothing writes to shared memory any more when the block ends
     }
     total = sum_of_halves(total);
     const float times = total != 0.0f ? 1.0f / total : 0.0f, sum2 = total != 0.0f ? top + __log2f(total) : -INFINITY;
@@ -575,7 +632,7 @@ __global__ __launch_bounds__(8 * DP) void k_prompt_join(const PromptArgs p)
 
 // dQ, and D on the way, as k_attn_dq.
 template <class T, int DP, int W>
-__global__ __launch_bounds__(64 * W, 2) void k_prompt_dq(const PromptArgs p)
+__global__ __launch_bounds__(64 * W, DP <= 64 ? 3 : 2) void k_prompt_dq(const PromptArgs p)
 {
     constexpr int TN = 64, CH = DP / 8;
     __shared__ u32x4 tiles[2][2][TN * CH];
@@ -588,8 +645,13 @@ __global__ __launch_bounds__(64 * W, 2) void k_prompt_dq(const PromptArgs p)
     const bool live = row < rows;
     const uint32_t limit = limit_of(p, tile.m, tile.n, token_of(a, live ? row : rows - 1));
 
-    const Keys<MODE_PLAIN> keys = tile.keys(p);
-    const uint16_t *const k_at = a.k + tile.k0 * a.ks.token, *const v_at = a.v + tile.k0 * a.vs.token;
+    const Incoming<DP, W> k_in(a.k + tile.k0 * a.ks.token + tile.kvh * a.ks.head, a.ks.token, a.head_dim, wave, lane);
+    const Incoming<DP, W> v_in(a.v + tile.k0 * a.vs.token + tile.kvh * a.vs.head, a.vs.token, a.head_dim, wave, lane);
+    const auto load = [&](uint32_t s) {
+        k_in.load(tiles[s & 1][0], (step0 + s) * TN, tile.n);
+        v_in.load(tiles[s & 1][1], (step0 + s) * TN, tile.n);
+    };
+    if (count) load(0);
     const int64_t line = (int64_t)tile.kvh * a.rows + tile.q0 * a.group + row;
     typename T::V8 q[DP / 16], d_o[DP / 16];
     row_operands<T, DP>(q, a.q + tile.q0 * a.qs.token + row_at(a, a.qs, 0, tile.kvh, live ? row : 0), live, a.head_dim);
@@ -615,42 +677,77 @@ __global__ __launch_bounds__(64 * W, 2) void k_prompt_dq(const PromptArgs p)
 
     f32x16 dq[1][DP / 32] = {};
     float lowered = 0.0f;                               // of dS's power of two, which lse2 holds
-    Stage<DP, TN, 64 * W, MODE_PLAIN> sk, sv;
-    auto first_of = [&](uint32_t s) { return (step0 + s) * TN; };
-    if (count) {
-        sk.load(keys, k_at, a.ks, thread, first_of(0), 0);
-        sv.load(keys, v_at, a.vs, thread, first_of(0), 0);
-    }
+    constexpr int NT = DP / 16, DT = DP / 32, AHEAD = 2, EACH = 16 / NT;
     for (uint32_t s = 0; s < count; ++s) {
-        u32x4 *kt = tiles[s & 1][0], *vt = tiles[s & 1][1];
-        sk.store(kt, thread);
-        sv.store(vt, thread);
-        __syncthreads();
-        if (s + 1 < count) {
-            sk.load(keys, k_at, a.ks, thread, first_of(s + 1), 0);
-            sv.load(keys, v_at, a.vs, thread, first_of(s + 1), 0);
-        }
-        const int left = (int)limit - (int)first_of(s);
+        const u32x4 *const kt = tiles[s & 1][0], *const vt = tiles[s & 1][1];
+        arrived<0>();
+        if (s + 1 < count) load(s + 1);
+        const int left = (int)limit - (int)((step0 + s) * TN);
         const bool whole = __all(left >= TN);
+        const auto along = [&](const u32x4 *of, int mt, int t) { return of[32 * mt * CH + chunk_at<CH>(n, 2 * t + h)]; };
+        const auto across = [&](s16x4 (&to)[2], int i) {        // of K: columns 32 (i mod DT) .., keys 16 (i / DT) ..
+            const int l = lane & 15, c = 4 * (i % DT) + 2 * ((lane >> 4) & 1) + ((l >> 1) & 1);
 #pragma unroll
-        for (int mt = 0; mt < 2; ++mt) {
-            f32x16 x = keys_by_rows<T, DP>(kt, 32 * mt, q);
-            const f32x16 dp = keys_by_rows<T, DP>(vt, 32 * mt, d_o);
-            if (!whole) mask_behind(x, left - 32 * mt);
+            for (int j = 0; j < 2; ++j) to[j] = read_transposed(reinterpret_cast<const char *>(kt + 16 * (i / DT) * CH + chunk_at<CH>(4 * h + (l >> 2) + 8 * j, c)) + 8 * (l & 1));
+        };
+        // Products of 32 keys in turn, beside them what the products before left to do: S, S | exponentials, dP | exponentials, dP | dS, dQ | dS, dQ; operands are
+        // read two products ahead.  In float16, where dS is kept in range between, one half of the keys after the other.
+        constexpr int GROUP = NARROW<T> ? 1 : 2, ALL = 2 * GROUP * NT;
+        f32x16 x[2], dp[2];
+        typename T::V8 ds[2][2];
 #pragma unroll
-            for (int r = 0; r < 16; ++r) x[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], a.scale_log2, -lse2)) * (dp[r] - delta);
+        for (int half = 0; half < 2; half += GROUP) {
+            u32x4 operand[AHEAD];
+            s16x4 ko[AHEAD][2];
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) operand[i] = along(kt, half, i);
+#pragma unroll
+            for (int i = 0; i < ALL; ++i) {             // S, then dP
+                const int t = i % NT, mt = half + i / NT % GROUP, later = i + AHEAD;
+                if (i < ALL / 2) x[mt] = T::mma(as_operand<T>(operand[i % AHEAD]), q[t], t ? x[mt] : f32x16{});
+                else dp[mt] = T::mma(as_operand<T>(operand[i % AHEAD]), d_o[t], t ? dp[mt] : f32x16{});
+                if (later < ALL) operand[i % AHEAD] = along(later < ALL / 2 ? kt : vt, half + later / NT % GROUP, later % NT);
+                else across(ko[later - ALL], 2 * DT * half + later - ALL);
+                if (i >= NT && i < ALL / 2 + NT) {
+                    const int of = half + i / NT - 1;
+#pragma unroll
+                    for (int e = EACH * t; e < EACH * (t + 1); ++e) x[of][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[of][e], a.scale_log2, -lse2));
+                }
+                if (GROUP == 2 && i >= 3 * NT) {
+#pragma unroll
+                    for (int e = EACH * t; e < EACH * (t + 1); ++e) {
+                        x[0][e] *= dp[0][e] - delta;
+                        if (e % 8 == 7) ds[0][e / 8] = rounded<T>(x[0], e / 8);
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                if (t == NT - 1 && i < ALL / 2 && !whole) mask_behind(x[mt], left - 32 * mt);
+            }
             if (NARROW<T>) {
-                const float by = keep_in_range(x, dq[0]);
+                x[half] *= dp[half] - delta;
+                const float by = keep_in_range(x[half], dq[0]);
                 lowered += by;
                 lse2 -= by;
+#pragma unroll
+                for (int part = 0; part < 2; ++part) ds[half][part] = rounded<T>(x[half], part);
             }
 #pragma unroll
-            for (int part = 0; part < 2; ++part) {
-                const typename T::V8 ds[1] = {rounded<T>(x, part)};
-                columns_times<T, DP, 1>(dq, kt, 32 * mt + 16 * part, ds);
+            for (int i = 0; i < 2 * DT * GROUP; ++i) {
+                const int at = 2 * DT * half + i, mt = at / (2 * DT);
+                dq[0][i % DT] = T::mma(join<T>(ko[i % AHEAD][0], ko[i % AHEAD][1]), ds[mt][at / DT % 2], dq[0][i % DT]);
+                if (i + AHEAD < 2 * DT * GROUP) across(ko[i % AHEAD], at + AHEAD);
+                if (GROUP == 2 && i < 2 * DT) {
+#pragma unroll
+                    for (int e = EACH * i; e < EACH * (i + 1); ++e) {
+                        x[1][e] *= dp[1][e] - delta;
+                        if (e % 8 == 7) ds[1][e / 8] = rounded<T>(x[1], e / 8);
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");    // nothing writes to shared memory any more when the block ends
     if (lse2 == INFINITY) {                             // (a row that sees nothing, whatever its query and gradient hold)
 #pragma unroll
         for (int dt = 0; dt < DP / 32; ++dt) dq[0][dt] = f32x16{};
@@ -772,28 +869,6 @@ __global__ __launch_bounds__(64 * W, 2) void k_prompt_dkv(const PromptArgs p)
         store_part<DP>(part, dk[0], times);
         store_part<DP>(part + DP, dv[0], times_v);
     }
-}
-
-// Loads straight to shared memory: 16 or 4 bytes a lane, `offset` (a lane's own, in bytes) behind the base, lane after lane to the place `to`.
-// Written out, as the compiler waits for all that are under way at every barrier and at the first read of shared memory after one: who uses them counts them
-// and waits (`arrived`).  (m0 is not said to be written: it is a register that the compiler keeps out of its own hands, and sets before every use.)
-__device__ __forceinline__ void load_16_to_shared(const void *base, uint32_t offset, uint32_t to)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory");
-}
-
-__device__ __forceinline__ void load_4_to_shared(const void *base, uint32_t offset, uint32_t to)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory");
-}
-
-__device__ __forceinline__ uint32_t place_in_shared(const void *p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)p; }
-
-// All but the last LEFT loads of this wave are there, and, behind the barrier, those of all waves; this wave reads nothing older any more.
-template <int LEFT>
-__device__ __forceinline__ void arrived()
-{
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory");
 }
 
 // dK and dV of 256 keys with 128 values each, 64 a wave and one wave a SIMD, 32 rows a step.

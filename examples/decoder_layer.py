@@ -1,8 +1,8 @@
-"""One decoder layer checks a tree of drafted tokens: what the planner says of its chains, and the chains run.
+"""One decoder layer takes in a batch of prompts, then checks a tree of drafted tokens: what the planner says of its chains, and the chains run.
 
-The layer is three chains of two matrix products: attention of the drafted tokens over the cache (I = tokens, L = cache),
-cross attention to an encoder's states (I = tokens, L = encoder's length), and a gated feed-forward block.  For each of them
-the program asks for the mapping with the least energy on an accelerator, then runs the chain on this GPU, on a stream of its own:
+The layer is three chains of two matrix products: attention of a prompt over itself (I = L = tokens) or of the drafted tokens over the
+cache (I = tokens, L = cache), cross attention to an encoder's states (I = tokens, L = encoder's length), and a gated feed-forward block.  For each of
+them the program asks for the mapping with the least energy on an accelerator, then runs the chain on this GPU, on a stream of its own:
 
     python3 examples/decoder_layer.py
 """
@@ -19,7 +19,8 @@ from inputs import CONFIGS  # noqa: E402
 class Layer:
     """Weights of a layer of `heads` query heads over `kv_heads` shared ones, and the buffers of a step of `batch` trees of `nodes` tokens."""
 
-    def __init__(self, batch, nodes, heads, kv_heads, head_dim, hidden, dtype=torch.bfloat16, seed=0):
+    def __init__(self, batch, nodes, heads, kv_heads, head_dim, hidden, dtype=torch.bfloat16, seed=0, base=None):
+        """base: of the frequencies by which queries and keys are rotated, after a norm of each head; None: neither."""
         gen = torch.Generator(device="cuda")
         gen.manual_seed(seed)
         width = heads * head_dim
@@ -29,24 +30,63 @@ class Layer:
         self.w_qkv = weight((heads + 2 * kv_heads) * head_dim, width)
         self.w_self_out, self.w_cross_q, self.w_cross_out = (weight(width, width) for _ in range(3))
         self.w_gate, self.w_up, self.w_down = weight(hidden, width), weight(hidden, width), weight(width, hidden)
+        self.freqs = self.q_weight = self.k_weight = None
+        if base is not None:
+            self.freqs = (base ** (-torch.arange(0, head_dim, 2, dtype=torch.float64) / head_dim)).cuda()
+            self.q_weight, self.k_weight = ((1 + 0.1 * torch.randn(head_dim, generator=gen, device="cuda")).to(dtype) for _ in range(2))
         self.tree_out, self.cross_out = empty(batch, nodes, heads, head_dim), empty(batch, nodes, heads, head_dim)
-        self.ffn_hidden, self.ffn_out = empty(batch * nodes, hidden), empty(batch * nodes, width)
 
     def _run(self, args, size, call):
         args.use_workspace(torch.empty(size, dtype=torch.uint8, device="cuda"))
         call(args)
 
-    def step(self, x, k_pages, v_pages, page_table, cache_lens, ancestors, enc_k, enc_v, enc_lens):
-        """x [batch, nodes, width] -> the layer's output; the drafted tokens' keys and values go into the cache behind what it holds.
+    def _norm(self, t):
+        return torch.nn.functional.layer_norm(t.float(), (self.width,)).to(self.dtype)
+
+    def prompt(self, x, starts, k_pages, v_pages, page_table, cache_lens, enc_k, enc_v, enc_starts):
+        """x [tokens, width], packed prompts that begin at starts -> the layer's output; their keys and values go into the cache, whose cache_lens are 0.
+        enc_k, enc_v: the encoder's states of each prompt, packed likewise, from enc_starts on."""
+        T, H, Hkv, d = x.shape[0], self.heads, self.kv_heads, self.head_dim
+        qkv = (self._norm(x) @ self.w_qkv.t()).view(T, H + 2 * Hkv, d)
+        q, k, v = qkv[:, :H], qkv[:, H:H + Hkv], qkv[:, H + Hkv:]
+        if self.freqs is not None:
+            at = torch.arange(T, device="cuda", dtype=torch.int32)
+            positions = at - starts[torch.bucketize(at, starts, right=True) - 1]
+            q_turned, k_turned = torch.empty_like(q), torch.empty_like(k)
+            M.mmee_qk_rotate_forward(M.qk_rotate(q, k, q_turned, k_turned, self.freqs, positions, q_weight=self.q_weight, k_weight=self.k_weight))
+            q, k = q_turned, k_turned
+        M.mmee_cache_append_forward(M.cache_append(k, v, k_pages, v_pages, page_table, cache_lens, starts=starts))
+        out = torch.empty(T, H, d, dtype=self.dtype, device="cuda")
+        own = M.prompt_attn(q, k, v, out, starts)
+        self._run(own, M.mmee_prompt_attn_workspace(own), M.mmee_prompt_attn_forward)
+        x = x + out.view(T, -1) @ self.w_self_out.t()
+
+        q = (self._norm(x) @ self.w_cross_q.t()).view(T, H, d)
+        cross = M.prompt_attn(q, enc_k, enc_v, out, starts, kv_starts=enc_starts, causal=False)
+        self._run(cross, M.mmee_prompt_attn_workspace(cross), M.mmee_prompt_attn_forward)
+        x = x + out.view(T, -1) @ self.w_cross_out.t()
+        return x + self._feed_forward(x)
+
+    def _feed_forward(self, x):
+        hidden, out = (torch.empty(x.shape[0], n, dtype=self.dtype, device="cuda") for n in (self.hidden, self.width))
+        block = M.ffn(self._norm(x), self.w_gate, self.w_up, self.w_down, out, hidden)
+        self._run(block, M.mmee_ffn_workspace(block), M.mmee_ffn_forward)
+        return out
+
+    def step(self, x, k_pages, v_pages, page_table, cache_lens, ancestors, enc_k, enc_v, enc_lens, positions=None):
+        """x [batch, nodes, width] -> the layer's output; the drafted tokens' keys and values go into the cache behind what it holds.  positions int32
+        [batch * nodes]: of the nodes in their sequences, which have branches; wanted where they are rotated.
         The library's stream (mmee_set_stream) has to be torch's current one."""
         B, n, H, Hkv, d = self.batch, self.nodes, self.heads, self.kv_heads, self.head_dim
-        norm = lambda t: torch.nn.functional.layer_norm(t.float(), (self.width,)).to(self.dtype)  # noqa: E731
-        qkv = (norm(x) @ self.w_qkv.t()).view(B, n, H + 2 * Hkv, d)
-        place = cache_lens[:, None].long() + torch.arange(n, device="cuda")
-        page = page_table.gather(1, place // k_pages.shape[1]).long()
-        k_pages[page, place % k_pages.shape[1]] = qkv[:, :, H:H + Hkv]
-        v_pages[page, place % k_pages.shape[1]] = qkv[:, :, H + Hkv:]
-        tree = M.tree_attn(qkv[:, :, :H], k_pages, v_pages, page_table, cache_lens, ancestors, self.tree_out)
+        norm = self._norm
+        qkv = (norm(x) @ self.w_qkv.t()).view(B * n, H + 2 * Hkv, d)
+        q = qkv[:, :H]
+        rotation = {}
+        if self.freqs is not None:
+            rotation = dict(q=q, q_out=torch.empty_like(q), freqs=self.freqs, positions=positions, q_weight=self.q_weight, k_weight=self.k_weight)
+            q = rotation["q_out"]
+        M.mmee_cache_append_forward(M.cache_append(qkv[:, H:H + Hkv], qkv[:, H + Hkv:], k_pages, v_pages, page_table, cache_lens, **rotation))
+        tree = M.tree_attn(q.view(B, n, H, d), k_pages, v_pages, page_table, cache_lens, ancestors, self.tree_out)
         self._run(tree, M.mmee_tree_attn_workspace(tree), M.mmee_tree_attn_forward)
         x = x + self.tree_out.view(B, n, -1) @ self.w_self_out.t()
 
@@ -55,15 +95,14 @@ class Layer:
         self._run(cross, M.mmee_attn_workspace(cross), M.mmee_attn_forward)
         x = x + self.cross_out.view(B, n, -1) @ self.w_cross_out.t()
 
-        block = M.ffn(norm(x).view(B * n, -1), self.w_gate, self.w_up, self.w_down, self.ffn_out, self.ffn_hidden)
-        self._run(block, M.mmee_ffn_workspace(block), M.mmee_ffn_forward)
-        return x + self.ffn_out.view(B, n, -1)
+        return x + self._feed_forward(x.view(B * n, -1)).view(B, n, -1)
 
 
 def plan(batch, nodes, heads, head_dim, hidden, cache, encoder, hw):
     """The least-energy mappings of the layer's chains on an accelerator: [(name, Result)]."""
     chain = lambda many, I, K, L, J, softmax: dict(batch=many, I=I, K=K, L=L, J=J, word_bytes=2, tiling_mode=1, c_softmax=softmax)  # noqa: E731
-    chains = {"tree attention": chain(batch * heads, nodes, head_dim, cache, head_dim, 10),
+    chains = {"prompt": chain(batch * heads, cache, head_dim, cache, head_dim, 10),
+              "tree attention": chain(batch * heads, nodes, head_dim, cache, head_dim, 10),
               "cross attention": chain(batch * heads, nodes, head_dim, encoder, head_dim, 10),
               "feed-forward": chain(1, batch * nodes, heads * head_dim, hidden, heads * head_dim, 0)}
     return [(name, M.mmee_chain_search_multi(c, hw, [M.OBJ_ENERGY])[0]) for name, c in chains.items()]
@@ -90,6 +129,19 @@ def inputs(layer, cache, encoder, page=16, seed=1):
                 enc_lens=torch.randint(1, encoder + 1, (B,), generator=gen, device="cuda").to(torch.int32))
 
 
+def prompts(layer, lens, enc_lens, page=16, room=64, seed=2):
+    """Prompts of these lengths, packed, the encoder's states of each, and an empty cache with room for so many tokens more."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+    Hkv, d, B = layer.kv_heads, layer.head_dim, len(lens)
+    r = lambda *shape: torch.randn(*shape, generator=gen, device="cuda").to(layer.dtype)  # noqa: E731
+    starts = lambda of: torch.tensor([0] + of, device="cuda").cumsum(0).to(torch.int32)  # noqa: E731
+    width = -(-(max(lens) + room) // page)
+    return dict(x=r(sum(lens), layer.width), starts=starts(lens), k_pages=r(B * width, page, Hkv, d), v_pages=r(B * width, page, Hkv, d),
+                page_table=torch.randperm(B * width, generator=gen, device="cuda").to(torch.int32).view(B, width),
+                cache_lens=torch.zeros(B, dtype=torch.int32, device="cuda"), enc_k=r(sum(enc_lens), Hkv, d), enc_v=r(sum(enc_lens), Hkv, d), enc_starts=starts(enc_lens))
+
+
 def main():
     batch, nodes, heads, kv_heads, head_dim, hidden, cache, encoder = 8, 24, 12, 4, 64, 3072, 512, 300
     for name, r in plan(batch, nodes, heads, head_dim, hidden, cache, encoder, CONFIGS["bert"]["hw"]):
@@ -98,10 +150,18 @@ def main():
             name, list(m.xG), "".join("iklj"[o] for o in m.order), list(m.level), "fused" if m.fused else "unfused", r.cost.energy_pj, r.cost.da_words))
     layer = Layer(batch, nodes, heads, kv_heads, head_dim, hidden)
     batch_in = inputs(layer, cache, encoder)
+    lens = [cache * (i + 1) // batch for i in range(batch)]
+    rotated = Layer(batch, nodes, heads, kv_heads, head_dim, hidden, base=10000.0)
+    prompt_in = prompts(rotated, lens, [encoder - 7 * i for i in range(batch)])
     stream = torch.cuda.Stream()
     stream.wait_stream(torch.cuda.current_stream())
     M.mmee_set_stream(stream.cuda_stream)               # once for all calls
     with torch.cuda.stream(stream):
+        rotated.prompt(**prompt_in)
+        prompt_begin, prompt_end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        prompt_begin.record()
+        z = rotated.prompt(**prompt_in)
+        prompt_end.record()
         y = layer.step(**batch_in)
         begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
         begin.record()
@@ -110,6 +170,8 @@ def main():
         end.record()
     end.synchronize()
     M.mmee_set_stream(None)
+    print("%d prompts of %d to %d tokens: %.3f ms, output %s, finite: %s" % (
+        batch, lens[0], lens[-1], prompt_begin.elapsed_time(prompt_end), tuple(z.shape), bool(torch.isfinite(z).all())))
     print("a step of %d trees of %d tokens: %.3f ms, output %s, finite: %s" % (batch, nodes, begin.elapsed_time(end) / 20, tuple(y.shape), bool(torch.isfinite(y).all())))
 
 

@@ -1,0 +1,32 @@
+"""What the compiler made of the registers of the operators around a prompt, read from the metadata of the library that is built here: which
+kernels spill how many at most, and that the rest spill none."""
+import os
+import re
+
+import pytest
+
+from test_register_budget import LIB, kernels
+
+pytestmark = pytest.mark.skipif(not os.path.exists(LIB), reason="the library is not built")
+
+ALLOWED = {("forward", 64, "L4b1"): 2, ("dq", 64, "L4"): 11, ("dq", 128, "L4"): 7, ("dkv", 128, "L4"): 2, ("dkv", 128, "L8"): 8}
+
+
+def test_spills():
+    found = 0
+    for name, k in kernels(LIB).items():
+        m = re.search(r"k_(prompt|rotate)_?(\w*?)(?:INS_(?:3F16|4BF16)E|ENS_)", name)
+        if not m:
+            continue
+        found += 1
+        spilled = k[".vgpr_spill_count"]
+        assert k[".group_segment_fixed_size"] <= 160 << 10, name
+        if m.group(1) == "rotate":
+            assert spilled == 0, (name, spilled)
+        elif "dkv_wide" in name:                        # 512 registers; what is spilled is not read in the loop
+            assert spilled <= 16 and k[".vgpr_count"] == 512, (name, spilled)
+        else:
+            of = re.search(r"ELi(\d+)ELi(\d)E(Lb1E)?", name)
+            key = (m.group(2), int(of.group(1)), "L" + of.group(2) + ("b1" if of.group(3) else "")) if of else None
+            assert spilled <= ALLOWED.get(key, 0), (name, spilled)
+    assert found >= 90

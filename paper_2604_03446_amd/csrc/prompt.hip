@@ -49,10 +49,10 @@ struct Plan {
 
 // Tiles of 32 rows (or keys) a wave, `lines` of them in all; `across`: keys (or rows) in all, `step` of them a step.  The lengths are not known here: a
 // sequence is taken to be as long as the average.
-Launch plan_launch(uint64_t lines, uint64_t seqs, uint64_t kv_heads, uint64_t across, uint64_t step, bool causal, bool eight, bool lean)
+Launch plan_launch(uint64_t lines, uint64_t seqs, uint64_t kv_heads, uint64_t across, uint64_t step, bool causal, uint64_t eight_from, bool lean)
 {
     Launch l;
-    l.waves = eight && lines / seqs >= 256 && ((lines / 256 + seqs / 2) * kv_heads > 128 || across / seqs >= 1024) ? 8 : 4;
+    l.waves = eight_from && across / seqs >= eight_from && lines / seqs >= 256 && ((lines / 256 + seqs / 2) * kv_heads > 128 || across / seqs >= 1024) ? 8 : 4;
     l.slots = lines / (32 * l.waves) + seqs;
     // Short sequences: the variant of which four blocks run on a unit.  40 sequences of 23 to 509, 12 heads of 64: 23 us instead of 27.
     l.lean = lean && l.waves == 4 && across / seqs <= 256;
@@ -120,9 +120,15 @@ int make_plan(const mmee_prompt_attn *x, bool pointers, Plan &plan)
     p.seqs = x->seqs;
     p.causal = x->causal != 0;
     p.dies = x->kv_heads % 8 == 0;
-    plan.forward = plan_launch(rows, x->seqs, x->kv_heads, x->kv_tokens, 64, p.causal, plan.dp >= 64, plan.dp <= 64);
-    plan.dq = plan_launch(rows, x->seqs, x->kv_heads, x->kv_tokens, 64, p.causal, plan.dp == 128, false);
-    plan.dkv = plan_launch(x->kv_tokens, x->seqs, x->kv_heads, rows, plan.dp == 128 ? 32 : 64, p.causal, plan.dp >= 64, false);
+    // From how many keys (or rows) on average blocks of eight waves, alone on a unit, are worth it: they read each tile half as often as two blocks of four,
+    // which cover each other's beginning and end.  Sequences of 256, 512, 1024, 2048, 4096 over themselves, 32768 in all, 16 heads, eight waves against four,
+    // microseconds.  Forward, 128 a head: 161, 208, 323, 557, 1027 : 142, 193, 313, 552, 1033; 64 a head: 93, 125, 192, 334, 631 : 74, 110, 183, 328, 628.
+    // With the gradients, dQ, 128 a head: 682, 908, 1398, 2424, 4538 : 666, 882, 1384, 2438, 4623; dK and dV, 128 a head: 682, 908, 1398, 2424, 4538 : 678, 928, 1471,
+    // 2665, 4972; 64 a head: 395, 543, 849, 1501, 2817 : 381, 535, 856, 1535, 2910.
+    const uint64_t forward_from = plan.dp == 128 ? 4096 : 0, dq_from = plan.dp == 128 ? 2048 : 0, dkv_from = plan.dp == 128 ? 512 : plan.dp == 64 ? 1024 : 0;
+    plan.forward = plan_launch(rows, x->seqs, x->kv_heads, x->kv_tokens, 64, p.causal, forward_from, plan.dp <= 64);
+    plan.dq = plan_launch(rows, x->seqs, x->kv_heads, x->kv_tokens, 64, p.causal, dq_from, false);
+    plan.dkv = plan_launch(x->kv_tokens, x->seqs, x->kv_heads, rows, plan.dp == 128 ? 32 : 64, p.causal, dkv_from, false);
     for (const Launch *l : {&plan.forward, &plan.dq, &plan.dkv})
         if (l->blocks * l->waves > 0x7fffffff) return MMEE_EINVAL;
     plan.forward_bytes = plan.forward.plan_bytes() + plan.forward.parts_bytes(x->kv_heads, plan.dp + 1);
@@ -246,7 +252,7 @@ int mmee_prompt_attn_forward(const mmee_prompt_attn *x)
     if (l.rc) return l.rc;
     if (n) l.run(k_prompt_plan, n, PLAN_THREADS, plans);
     dispatch(plan, [&](auto type, auto dp) {
-        with_waves<(dp.value >= 64)>(plan.forward.waves, [&](auto w) { forward_as<decltype(type), dp.value, w.value>(p, plan.forward, l); });
+        with_waves<(dp.value == 128)>(plan.forward.waves, [&](auto w) { forward_as<decltype(type), dp.value, w.value>(p, plan.forward, l); });
     });
     return l.result("prompt attention, forward");
 }

@@ -150,7 +150,7 @@ def test_tiles_of_256(M, dtype):
 def test_keys_of_64_a_wave(M, group, dtype):
     """Tiles of 256 keys with 128 (and 104) values: query heads that share a key/value head so that 32 rows are whole tokens, or not."""
     import torch
-    lens, kv_lens, Hkv = ([600, 257, 3], [900, 257, 40], 6) if group >= 8 else ([200, 257, 3], [520, 257, 40], 40)
+    lens, kv_lens, Hkv = {1: ([600, 700, 300], [650, 700, 257], 40), 3: ([300, 257, 3], [520, 257, 40], 40)}.get(group, ([600, 257, 3], [900, 257, 40], 6))
     for causal in (True, False):
         for d in (128, 104):
             t = tensors(lens, kv_lens, Hkv * group, Hkv, d, getattr(torch, dtype), group, around=1)
@@ -158,6 +158,16 @@ def test_keys_of_64_a_wave(M, group, dtype):
                 t[n] = t[n].transpose(0, 1).contiguous().transpose(0, 1)
             run(M, t, causal=causal)
             compare(t, causal, (group, causal, d))
+
+
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
+@pytest.mark.parametrize("q_lens,kv_lens,H,Hkv,d", [([300], [4200], 4, 2, 128), ([257, 1400], [5000, 3300], 2, 1, 112), ([1100], [1100], 36, 36, 64)])
+def test_long_sequences(M, q_lens, kv_lens, H, Hkv, d, dtype):
+    """Blocks of eight waves, which only long sequences take."""
+    import torch
+    t = tensors(q_lens, kv_lens, H, Hkv, d, getattr(torch, dtype), 19, around=1)
+    run(M, t)
+    compare(t, True, (q_lens, kv_lens))
 
 
 def test_many_sequences(M):

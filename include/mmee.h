@@ -401,6 +401,7 @@ int mmee_ffn_backward(const mmee_ffn *f, const mmee_ffn_grads *g);
  * the rest of the head is z.  freqs are radians a position in 64 bits, and so are the angles, whatever the position.  Positions may have several
  * axes (time, height, width): pair i turns by the position along axis axis_of[i] (clamped to axes - 1; null: all along the first).  head_dim: a
  * multiple of 8 up to 256; rot_dim: a multiple of 16 up to head_dim, 0: no rotation (freqs and positions may then be null).  eps at least 1e-30.
+ * Tokens: up to 2^26 - 4.
  * An output may be its input's own buffer with the same strides, not one that overlaps it otherwise. */
 enum { MMEE_PAIRS_HALVES = 0, MMEE_PAIRS_NEIGHBOURS = 1 };
 
@@ -441,8 +442,8 @@ int mmee_qk_rotate_backward(const mmee_qk_rotate *r, const mmee_qk_rotate_grads 
  * `seqs` sequences lie one behind the other: sequence b's are starts[b] .. starts[b + 1] - 1, or, with starts null, tokens / seqs of each (without a
  * remainder).  Its j-th goes to position cache_lens[b] + j, which is also what it is rotated by unless positions are given.  Tokens
  * j >= counts[b] (when given) and tokens of no sequence leave everything as it was.  Positions past the page table and pages outside 0 .. n_pages-1 are
- * not written; the token's query is.  cache_lens stay as they are (clamped to 0 where they are below).  starts ascend and lie within 0 .. tokens.  Two new tokens at one place of the pool
- * (sequences that share the page they write to) leave either's key and value there. */
+ * not written; the token's query is.  cache_lens stay as they are (clamped to 0 where they are below).  starts ascend and lie within 0 .. tokens.
+ * Two new tokens at one place of the pool (sequences that share the page they write to) leave values of either there. */
 typedef struct mmee_cache_append {
     uint32_t dtype, pairs;
     uint32_t tokens, seqs, heads, kv_heads, head_dim, rot_dim;
@@ -470,7 +471,8 @@ int mmee_cache_append_forward(const mmee_cache_append *c);
 
 /* Attention of packed prompts: rows of sequence b are tokens q_starts[b] .. q_starts[b + 1] - 1 of q and o [q_tokens][heads][head_dim], its keys
  * tokens kv_starts[b] .. kv_starts[b + 1] - 1 of k and v [kv_tokens][kv_heads][head_dim] (kv_starts null: q_starts, and kv_tokens = q_tokens).
- * Heads, head_dim, scale as of mmee_attn; strides of the first two dimensions.  causal != 0: row i of a sequence of m rows and n keys sees the
+ * Heads, head_dim, scale as of mmee_attn; strides of the first two dimensions, between tokens 2^24 at most; up to 2^28 keys, and rows that share a
+ * key/value head, in tiles that one launch can hold (kv_heads * (rows / 128 + keys / 128 + seqs) below 2^23 suffices).  causal != 0: row i of a sequence of m rows and n keys sees the
  * keys j <= i + n - m (the last row at the last key: a prompt over itself, or a prompt's next rows over all keys so far); 0: all n.  A row without keys
  * gives zeros, and lse -inf.  Starts ascend and lie within 0 .. tokens (beyond, they are clamped; a sequence whose end lies before its start is empty;
  * sequences that overlap are not looked for: which of them an output belongs to is then undefined).

@@ -130,7 +130,7 @@ int make_plan(const mmee_prompt_attn *x, bool pointers, Plan &plan)
     plan.dq = plan_launch(rows, x->seqs, x->kv_heads, x->kv_tokens, 64, p.causal, dq_from, false);
     plan.dkv = plan_launch(x->kv_tokens, x->seqs, x->kv_heads, rows, plan.dp == 128 ? 32 : 64, p.causal, dkv_from, false);
     for (const Launch *l : {&plan.forward, &plan.dq, &plan.dkv})
-        if (l->blocks * l->waves > 0x7fffffff) return MMEE_EINVAL;
+        if (l->blocks * l->waves * 64 > 0xffffffff) return MMEE_EINVAL;         // a launch's threads
     plan.forward_bytes = plan.forward.plan_bytes() + plan.forward.parts_bytes(x->kv_heads, plan.dp + 1);
     plan.backward_bytes = 2 * up256(4ull * x->kv_heads * rows) + plan.dq.plan_bytes() + plan.dkv.plan_bytes() +
                           std::max(plan.dq.parts_bytes(x->kv_heads, plan.dp), plan.dkv.parts_bytes(x->kv_heads, 2 * plan.dp));

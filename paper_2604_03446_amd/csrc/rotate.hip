@@ -10,7 +10,7 @@
 namespace mmee {
 namespace {
 
-constexpr uint32_t MOST_TOKENS = 1u << 28;
+constexpr uint32_t MOST_TOKENS = (1u << 26) - 4;       // a wave each: a launch has less than 2^32 threads
 
 bool misaligned(std::initializer_list<const void *> list, uintptr_t to)
 {

@@ -63,3 +63,14 @@ def test_backward_refuses():
                  {n: Fake(50, h, 64, dtype=HALF) for n, h in (("do", 4), ("dq", 4), ("dk", 2), ("dv", 2))}):
         refused(lambda: M.mmee_prompt_attn_backward(a, grads(**over)))
     assert M._lib.mmee_prompt_attn_backward(C.byref(a), None) == M.EINVAL
+
+
+def test_more_blocks_than_a_launch_holds():
+    """Every sequence may begin a tile of its own, of every head."""
+    M = A.M
+    a = prompt()
+    a.seqs = 1 << 24
+    refused(lambda: M.mmee_prompt_attn_forward(a))
+    refused(lambda: M.mmee_prompt_attn_workspace(a, True))
+    a.seqs = (1 << 23) - 64
+    M.mmee_prompt_attn_workspace(a, True)

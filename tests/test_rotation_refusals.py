@@ -94,3 +94,16 @@ def test_append_refuses():
         setattr(c, field, value)
         refused(lambda: M.mmee_cache_append_forward(c))
     assert M._lib.mmee_cache_append_forward(None) == M.EINVAL
+
+
+def test_more_tokens_than_a_launch_holds():
+    M = A.M
+    r = rotate()
+    r.tokens = 1 << 26
+    refused(lambda: M.mmee_qk_rotate_forward(r))
+    refused(lambda: M.mmee_qk_rotate_workspace(r))
+    r.tokens = (1 << 26) - 4
+    M.mmee_qk_rotate_workspace(r)
+    c = append()
+    c.tokens = 1 << 26
+    refused(lambda: M.mmee_cache_append_forward(c))

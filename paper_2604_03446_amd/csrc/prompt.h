@@ -5,7 +5,13 @@
 // lengths can need, and those without a tile end at once.  Which tile a block has comes from the starts alone,
 //   by slots: tile t of sequence b has slot (first row of b) / TILE + b + t, which differ whatever the lengths; or
 //   by a plan that k_prompt_plan makes of the starts: the longest tiles first, whatever sequence they are of, so that the short ones fill up the end, and
-//   tiles that are longer than a unit's share cut into pieces of equal length, which are joined afterwards.  It costs a launch, about 5 us.
+//   from tiles that are longer than a unit's share pieces of that length cut off, which are joined afterwards.  It costs a launch, 5 to 8 us.  (Planned by
+//   every block for itself it cost each 1 to 2 us, and blocks without a tile between those with one left some shader engines idle.)
+//
+// Times are of one MI355X, the least of 20 passes; matrix products hold its clock at 1.85 to 2.05 GHz.  `busy` is the share of a unit's busy cycles in which
+// its matrix instructions run.  Registers that are spilled: k_prompt_forward with 64 values a head 2 (four blocks a unit); k_prompt_dq with four
+// waves in float16 2 (128 a head) and 4 (64), in bfloat16 7 and 11; k_prompt_dkv in float16 with 128 a head 2 (four waves) and 8 (eight);
+// k_prompt_dkv_wide 16; all of them outside the loops.
 #pragma once
 
 #include "attention.h"
@@ -154,7 +160,7 @@ struct PlanArgs {
 constexpr uint32_t PLAN_SEQS = 2048, PLAN_TILES = 2048, PLAN_THREADS = 256;     // sequences and tiles at most
 
 // Plans of[blockIdx.x].  Tiles and pieces are sorted by their length in 256 classes; which of a class come first does not matter to any result.
-// One block; for 24 prompts of 17 to 2500 rows 4 us, of which most is the latency of the starts and of a dozen barriers (with 1024 threads 5).
+// One block a plan: 6.1 us for 24 prompts of 17 to 2500 rows, 5.1 for one, most of it the latency of the starts and of a dozen barriers (with 1024 threads 1 us more).
 __global__ __launch_bounds__(PLAN_THREADS) void k_prompt_plan(const PlanArgs x)
 {
     constexpr uint32_t MINE = PLAN_TILES / PLAN_THREADS, CLASSES = PLAN_THREADS, WAVES = PLAN_THREADS / 64;
@@ -374,8 +380,16 @@ struct Incoming {
     }
 };
 
-// Forward: as k_attn_forward with W waves of 32 rows each on a tile of 64 keys, which ends where the block's last row does; only tiles that some row
-// does not see whole are masked.
+// Forward: W waves of 32 rows each share a tile of 64 keys; the block ends with the tile that its last row sees, and only tiles that some row does not
+// see whole are masked.  One pass, with a row's mark (near its maximum) and sum in the two lanes that hold its scores:
+//   x = K q,  p = 2^(scale x - mark),  sum += p,  o = 2^(old mark - mark) o + V^T p,  at the end o / sum and lse.
+// Bound by matrix instructions, two products of 2 head_dim operations a score, and beside them one exponential a score, which issues at a quarter of the
+// rate: a step of 64 keys is 1024 cycles of a wave's matrix instructions at 128 a head, and 512 of exponentials alone; at 64 a head 512 and 512.
+//   One prompt of 8192 rows, 32 heads of 128, bfloat16: 571 us, 0.96 PFLOP/s, busy 58 %, 1.86 GHz (1.19 PFLOP/s where all values are zeros: power).
+//   24 of 17 to 2500, 32 heads over 8 of 128, float16: 184 us, 0.79 PFLOP/s, busy 49 %.  40 of 23 to 509, 12 heads of 64, not causal: 23 us, a round of blocks
+//   whose longest has eight steps.
+// The step in slots of one product took the first from 562 to 546 us a call, tiles straight to shared memory from 559 to 539; operands read 4 to 8 products
+// ahead and three or four tiles under way gained nothing more.
 template <class T, int DP, int W, bool LEAN>
 __global__ __launch_bounds__(64 * W, LEAN ? 4 : 2) void k_prompt_forward(const PromptArgs p)
 {
@@ -600,7 +614,8 @@ __global__ __launch_bounds__(64 * W, LEAN ? 4 : 2) void k_prompt_forward(const P
     }
 }
 
-// Joins the pieces of the tiles of 32 W rows that were cut, in ascending order, as k_attn_join does: 32 rows a block.
+// Joins the pieces of the tiles of 32 W rows that were cut, in ascending order: o = sum of 2^(lse_i - top) o_i over the sum of 2^(lse_i - top).  32 rows a
+// block, a thread four columns.  Reads and writes alone: 33 MB for 703 rows, 32 heads, over 9000 to 16384 keys in 8.3 us.
 template <class T, int DP, int W>
 __global__ __launch_bounds__(8 * DP) void k_prompt_join(const PromptArgs p)
 {
@@ -609,28 +624,29 @@ __global__ __launch_bounds__(8 * DP) void k_prompt_join(const PromptArgs p)
     Tile<32 * W, 64, false> tile(p, blockIdx.x / W, std::true_type());
     if (!tile.there) return;
     tile.settle();
-    {
-        const uint32_t i = threadIdx.x;
-        const uint32_t within_tile = blockIdx.x % W * 32 + i / C4, row = tile.index * 32 * W + within_tile, c = i % C4;
-        if (row >= tile.m * a.group) return;
-        const int64_t line = tile.part(p, 0) + within_tile;
-        float high = -INFINITY, sum = 0.0f;
-        for (uint32_t s = 0; s < tile.pieces; ++s) high = __builtin_elementwise_maximum(high, a.part_lse[line + s * 32 * W]);
-        const float off = high == -INFINITY ? 0.0f : high;
-        f32x4 x = {0, 0, 0, 0};
+    const uint32_t i = threadIdx.x;
+    const uint32_t within_tile = blockIdx.x % W * 32 + i / C4, row = tile.index * 32 * W + within_tile, c = i % C4;
+    if (row >= tile.m * a.group) return;
+    const int64_t line = tile.part(p, 0) + within_tile;
+    float high = -INFINITY, sum = 0.0f;
+    for (uint32_t s = 0; s < tile.pieces; ++s) high = __builtin_elementwise_maximum(high, a.part_lse[line + s * 32 * W]);
+    const float off = high == -INFINITY ? 0.0f : high;
+    f32x4 x = {0, 0, 0, 0};
 #pragma unroll 4
-        for (uint32_t s = 0; s < tile.pieces; ++s) {
-            const float w = __builtin_amdgcn_exp2f(a.part_lse[line + s * 32 * W] - off);
-            sum += w;
-            x += *reinterpret_cast<const f32x4 *>(a.part_o + (line + s * 32 * W) * DP + 4 * c) * w;
-        }
-        x *= sum != 0.0f ? 1.0f / sum : 0.0f;
-        if (4 * c < a.head_dim) *reinterpret_cast<typename T::V4 *>(a.o + tile.q0 * a.os.token + row_at(a, a.os, 0, tile.kvh, row) + 4 * c) = __builtin_convertvector(x, typename T::V4);
-        if (a.lse && c == 0) a.lse[lse_at(a, 0, tile.kvh, row) + tile.q0] = sum != 0.0f ? (high + __log2f(sum)) * LN2 : -INFINITY;
+    for (uint32_t s = 0; s < tile.pieces; ++s) {
+        const float w = __builtin_amdgcn_exp2f(a.part_lse[line + s * 32 * W] - off);
+        sum += w;
+        x += *reinterpret_cast<const f32x4 *>(a.part_o + (line + s * 32 * W) * DP + 4 * c) * w;
     }
+    x *= sum != 0.0f ? 1.0f / sum : 0.0f;
+    if (4 * c < a.head_dim) *reinterpret_cast<typename T::V4 *>(a.o + tile.q0 * a.os.token + row_at(a, a.os, 0, tile.kvh, row) + 4 * c) = __builtin_convertvector(x, typename T::V4);
+    if (a.lse && c == 0) a.lse[lse_at(a, 0, tile.kvh, row) + tile.q0] = sum != 0.0f ? (high + __log2f(sum)) * LN2 : -INFINITY;
 }
 
-// dQ, and D on the way, as k_attn_dq.
+// dQ, and D on the way:  P = 2^(scale S log2 e - lse2),  D = sum of dO O,  dS = P (dO V^T - D),  dQ = scale dS K.  Rows as in the forward pass, Q and dO in
+// registers; three products and an exponential a score.  D and lse2 go to the workspace, where dK and dV read them.
+// Bound as the forward pass: documents of 4096, 1333, 2048 and 715 rows, 32 heads over 8 of 128, bfloat16: 298 us, 0.96 PFLOP/s, busy 55 %, 1.93 GHz 
+// (a call in slots of one product: the step of training 936 us instead of 954).  40 sentences of 23 to 509, 12 heads of 64, float16: 23 us.
 template <class T, int DP, int W>
 __global__ __launch_bounds__(64 * W, DP <= 64 ? 3 : 2) void k_prompt_dq(const PromptArgs p)
 {
@@ -757,7 +773,11 @@ __global__ __launch_bounds__(64 * W, DP <= 64 ? 3 : 2) void k_prompt_dq(const Pr
     else if (live) store_part<DP>(a.part_o + (tile.part(p, tile.piece) + 32 * wave + n) * DP, dq[0], times);
 }
 
-// dK and dV of 32 W keys, 32 a wave, over the rows that see them, as k_attn_dkv.
+// dK and dV of 32 W keys, 32 a wave, over the rows that see them:  dV = P^T dO,  dK = scale dS^T Q.  S and dP are formed again (a row's P is its lse away),
+// which costs two products more than one kernel for all three gradients would, and saves atomics on dQ.  Q, dO and the rows' statistics go through
+// registers to shared memory, so that what is no row is zeros.
+// Bound by matrix instructions and the reads of operands from shared memory (each feeds one product).  40 sentences of 23 to 509, 12 heads of 64, float16:
+// 31 us, busy 25 %: few steps a block, whose beginnings and ends show.
 template <class T, int DP, int W>
 __global__ __launch_bounds__(64 * W, 2) void k_prompt_dkv(const PromptArgs p)
 {
@@ -871,7 +891,11 @@ __global__ __launch_bounds__(64 * W, 2) void k_prompt_dkv(const PromptArgs p)
     }
 }
 
-// dK and dV of 256 keys with 128 values each, 64 a wave and one wave a SIMD, 32 rows a step.
+// dK and dV of 256 keys with 128 values each, 64 a wave and one wave a SIMD, 32 rows a step: every operand read feeds two products, and the step goes in slots
+// of two, S | dP beside the exponentials | dV beside dS | dK.  Rows come straight to shared memory, three steps ahead.
+// Documents of 4096, 1333, 2048 and 715 rows, 32 heads over 8 of 128, bfloat16: 456 us, 0.84 PFLOP/s, busy 51 %, 2.04 GHz (k_prompt_dkv: 502).
+// Bound by the wave's own order: 64 matrix instructions a step are 2048 cycles, the slots with exponentials take 1.4 times theirs, and shared memory
+// hands out operands in 1700 of them for the four waves.  In float16, whose dS is kept in range between, registers do not suffice.
 template <class T>
 __global__ __launch_bounds__(256, 1) void k_prompt_dkv_wide(const PromptArgs p)
 {
@@ -1065,7 +1089,8 @@ __global__ __launch_bounds__(256, 1) void k_prompt_dkv_wide(const PromptArgs p)
     }
 }
 
-// Sums of the pieces of tiles that were cut, in ascending order, rounded once, as k_attn_sum: dQ of 32 rows a block, or, with KEYS, dK and dV of 32 keys.
+// Sums of the pieces of tiles that were cut, in ascending order, rounded once: dQ of 32 rows a block, or, with KEYS, dK and dV of 32 keys.  Reads and writes
+// alone: 57 MB of 8192 documents' keys in 13 us.
 template <class T, int DP, int W, int STEP, bool KEYS>
 __global__ __launch_bounds__(8 * DP) void k_prompt_sum(const PromptArgs p)
 {

@@ -10,8 +10,8 @@
 //
 // Times are of one MI355X, the least of 20 passes; matrix products hold its clock at 1.85 to 2.05 GHz.  `busy` is the share of a unit's busy cycles in which
 // its matrix instructions run.  Registers that are spilled: k_prompt_forward with 64 values a head 2 (four blocks a unit); k_prompt_dq with four
-// waves in float16 2 (128 a head) and 4 (64), in bfloat16 7 and 11; k_prompt_dkv in float16 with 128 a head 2 (four waves) and 8 (eight);
-// k_prompt_dkv_wide 16; all of them outside the loops.
+// waves 2 (float16, 128 a head), 4 (float16, 64) and 7 (bfloat16, 128, one of which is read in the loop); k_prompt_dkv in float16 with 128 a head 2 (four
+// waves) and 8 (eight), once a step; k_prompt_dkv_wide 16, outside its loop.
 #pragma once
 
 #include "attention.h"
@@ -647,8 +647,10 @@ __global__ __launch_bounds__(8 * DP) void k_prompt_join(const PromptArgs p)
 // registers; three products and an exponential a score.  D and lse2 go to the workspace, where dK and dV read them.
 // Bound as the forward pass: documents of 4096, 1333, 2048 and 715 rows, 32 heads over 8 of 128, bfloat16: 298 us, 0.96 PFLOP/s, busy 55 %, 1.93 GHz 
 // (a call in slots of one product: the step of training 936 us instead of 954).  40 sentences of 23 to 509, 12 heads of 64, float16: 23 us.
+// Three waves a SIMD where 168 registers suffice: 64 a head, float16, 79.5 us with three (a training step over the 40 sentences), 81.5 with two; bfloat16 78.5, and 75.7
+// with two.
 template <class T, int DP, int W>
-__global__ __launch_bounds__(64 * W, DP <= 64 ? 3 : 2) void k_prompt_dq(const PromptArgs p)
+__global__ __launch_bounds__(64 * W, DP <= 32 || (DP <= 64 && NARROW<T>) ? 3 : 2) void k_prompt_dq(const PromptArgs p)
 {
     constexpr int TN = 64, CH = DP / 8;
     __shared__ u32x4 tiles[2][2][TN * CH];

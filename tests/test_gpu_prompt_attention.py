@@ -124,6 +124,34 @@ def test_what_rows_without_keys_hold(M):
     compare(clean, True, "rows without keys")
 
 
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("d,lens", [(24, [1, 2, 127, 5, 128]), (64, [1, 2, 3, 5, 33, 64]), (128, [1, 64, 2, 6, 9])])
+def test_gradients_of_few_keys(M, d, lens, causal, dtype):
+    """Where a row sees few keys D does not add the rounding of the output: dQ and dK are off by the rounding of dS and their own alone.
+
+    To u |dS_ij| of each dS (u half a step), summed with what multiplies it, and u of the result come the errors in 32 bits, P of 2^-19 (scores of less than 16
+    powers of two, the exponential's argument, lse and the exponential each below 2^-21) and dP of d 2^-24 of its terms, in dP and in D; 2^-16 of P (|dP| + D's terms)
+    covers them.  Float16 has steps of 2^-24 below its normal numbers."""
+    import torch
+    t = tensors(lens, lens, 4, 2, d, getattr(torch, dtype), 31 + d)
+    run(M, t, kv=False, causal=causal)
+    u, scale = torch.finfo(t["q"].dtype).eps / 2, d ** -0.5
+    for b, n in enumerate(lens):
+        at = slice(sum(lens[:b]), sum(lens[:b]) + n)
+        q, do = (t[x][at].double().cpu().view(n, 2, 2, d).permute(1, 2, 0, 3) for x in ("q", "do"))          # [kv head][its heads][row][d]
+        k, v = (t[x][at].double().cpu().permute(1, 0, 2)[:, None] for x in ("k", "v"))
+        S = q @ k.transpose(2, 3) * scale
+        P = S.masked_fill(~keep_of(n, n, causal), -math.inf).softmax(3)
+        dP, across = do @ v.transpose(2, 3), do.abs() @ v.abs().transpose(2, 3)
+        dS = P * (dP - (P * dP).sum(3, keepdim=True))
+        off = u * dS.abs() + 2.0 ** -16 * P * (across + (P * across).sum(3, keepdim=True))
+        for name, want, bound in (("dq", dS @ k, off @ k.abs()), ("dk", (dS.transpose(2, 3) @ q).sum(1, keepdim=True), (off.transpose(2, 3) @ q.abs()).sum(1, keepdim=True))):
+            got = t[name][at].double().cpu().view(n, 2, -1, d).permute(1, 2, 0, 3)
+            far = (got - want * scale).abs() - (1.01 * bound + u * want.abs()) * scale - 2.0 ** -25
+            assert (far <= 0).all(), (b, n, name, far.max().item())
+
+
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("q_lens,kv_lens,H,Hkv,d,train", [
     ([40], [3000], 4, 1, 128, True), ([1, 1], [5000, 700], 8, 2, 64, True), ([900], [70], 8, 1, 32, True), ([200, 30], [2500, 2600], 2, 1, 72, True),

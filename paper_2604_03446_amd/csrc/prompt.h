@@ -917,12 +917,12 @@ __global__ __launch_bounds__(64 * W, 2) void k_prompt_dkv(const PromptArgs p)
 
 // dK and dV of 256 keys with 128 values each, 64 a wave and one wave a SIMD, 32 rows a step: every operand read feeds two products, and the step goes in slots
 // of two, S | dP beside the exponentials | dV beside dS | dK.  Rows come straight to shared memory, three steps ahead.
-// Documents of 4096, 1333, 2048 and 715 rows, 32 heads over 8 of 128, bfloat16: 456 us, 0.84 PFLOP/s, busy 51 %, 2.04 GHz (k_prompt_dkv: 502).
+// Documents of 4096, 1333, 2048 and 715 rows, 32 heads over 8 of 128, bfloat16: 446 us, 0.85 PFLOP/s, busy 51 %, 2.0 GHz (k_prompt_dkv: 502).
 // Bound by the wave's own order: 64 matrix instructions a step are 2048 cycles, the slots with exponentials take 1.4 times theirs, and shared memory
 // hands out operands in 1700 of them for the four waves.  In float16, whose dS is kept in range between, registers do not suffice.
-template <class T>
 __global__ __launch_bounds__(256, 1) void k_prompt_dkv_wide(const PromptArgs p)
 {
+    using T = BF16;
     constexpr int DP = 128, CH = 16, TR = 32, STAGES = 4, NT = DP / 16, DT = DP / 32;
     __shared__ u32x4 tiles[STAGES][2][TR * CH];         // Q, dO
     // V's operands, and four of K's, for which registers do not suffice: a lane reads what it has written itself.
@@ -937,13 +937,13 @@ __global__ __launch_bounds__(256, 1) void k_prompt_dkv_wide(const PromptArgs p)
     const int first_seen = first_row(p, tile.m, tile.n, tile.index * 256), all_see = first_row(p, tile.m, tile.n, key0 + 63);
     const uint32_t count = tile.count, start = (first_seen < 0 ? 0 : first_seen) + tile.step0 * TR;
 
-    typename T::V8 k[2][NT];
+    T::V8 k[2][NT];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
         const uint32_t key = key0 + 32 * u + n;
         const bool valid = key < tile.n;
         const int64_t at = (int64_t)tile.k0 + (valid ? key : 0);
-        typename T::V8 v[NT];
+        T::V8 v[NT];
         row_operands<T, DP>(k[u], a.k + at * a.ks.token + tile.kvh * a.ks.head, valid, a.head_dim);
         row_operands<T, DP>(v, a.v + at * a.vs.token + tile.kvh * a.vs.head, valid, a.head_dim);
 #pragma unroll
@@ -982,8 +982,6 @@ __global__ __launch_bounds__(256, 1) void k_prompt_dkv_wide(const PromptArgs p)
     const int own_row = first_row(p, tile.m, tile.n, key0 + n), next_keys = p.causal ? 32 * (int)a.group : 0;       // of u = 0; more of u = 1
 
     f32x16 dk[2][DT] = {}, dv[2][DT] = {};
-    float by[2] = {0x1p60f, 0x1p60f};                   // float16: dS's power of two over P's
-    static_assert(HIGHEST == 60.0f);
     const auto step = [&](uint32_t s, auto stage) {
         arrived<LOADS * (STAGES - 2)>();
         load(s + STAGES - 1, std::integral_constant<int, (stage.value + STAGES - 1) % STAGES>());
@@ -999,7 +997,9 @@ __global__ __launch_bounds__(256, 1) void k_prompt_dkv_wide(const PromptArgs p)
         // S = Q K^T
         f32x16 x[2], dp[2];
         u32x4 operand[AHEAD], ko[AHEAD_V], vo[AHEAD_V][2];
-        f32x4 stat[2];
+        f32x4 lse[2], delta[2];                         // of row group g, its four rows, in [g % 2]
+        const auto lse_of = [&](int g) { lse[g % 2] = stats[stage][0][2 * g + h]; };
+        const auto delta_of = [&](int g) { delta[g % 2] = stats[stage][1][2 * g + h]; };
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) operand[i] = along(qt, i);
 #pragma unroll
@@ -1012,7 +1012,7 @@ __global__ __launch_bounds__(256, 1) void k_prompt_dkv_wide(const PromptArgs p)
 #pragma unroll
                 for (int u = 0; u < 2; ++u) vo[t + AHEAD_V - NT][u] = away[wave][u][t + AHEAD_V - NT][lane];
             }
-            if (t == NT - 1) stat[0] = stats[stage][0][h];
+            if (t == NT - 1) lse_of(0);
             __builtin_amdgcn_sched_barrier(0);
         }
         if ((int)first < all_see || first + TR > rows) {
@@ -1026,53 +1026,49 @@ __global__ __launch_bounds__(256, 1) void k_prompt_dkv_wide(const PromptArgs p)
                 }
             }
         }
-        // dP = dO V^T beside the exponentials, four of one row group at a time; operand[] holds dO's from (NT mod AHEAD) on
-        typename T::V8 pr[2][2], ds[2][2];
+        // The 32 exponentials and 32 dS of a lane, four rows of one u after the other, and the operands of 8 rows once they are whole.
+        T::V8 pr[2][2], ds[2][2];
+        const auto exponential = [&](int i) {
+            const int g = i / 8, u = i / 4 % 2, j = i % 4;
+            x[u][4 * g + j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[u][4 * g + j], a.scale_log2, -lse[g % 2][j]));
+            if (g % 2 && j == 3) pr[u][g / 2] = rounded<T>(x[u], g / 2);
+        };
+        const auto gradient = [&](int i) {
+            const int g = i / 8, u = i / 4 % 2, j = i % 4;
+            dp[u][4 * g + j] = x[u][4 * g + j] * (dp[u][4 * g + j] - delta[g % 2][j]);
+            if (g % 2 && j == 3) ds[u][g / 2] = rounded<T>(dp[u], g / 2);
+        };
+        // dP = dO V^T beside three quarters of the exponentials; operand[] holds dO's from (NT mod AHEAD) on
+        s16x4 ao[AHEAD][2];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            const int slot = (t + NT) % AHEAD, g = t / 2, v = t % 2;
+            const int slot = (t + NT) % AHEAD;
 #pragma unroll
             for (int u = 0; u < 2; ++u) dp[u] = T::mma(as_operand<T>(operand[slot]), as_operand<T>(vo[t % AHEAD_V][u]), t ? dp[u] : f32x16{});
             if (t + AHEAD < NT) operand[slot] = along(ot, t + AHEAD);
+            else across(ao[t + AHEAD - NT], ot, t + AHEAD - NT);
             if (t + AHEAD_V < NT) {
 #pragma unroll
                 for (int u = 0; u < 2; ++u) vo[t % AHEAD_V][u] = away[wave][u][t + AHEAD_V][lane];
             }
-            if (v == 0) stat[(g + 1) % 2] = g < 3 ? stats[stage][0][2 * g + 2 + h] : stats[stage][1][h];
+            if (t % 2 == 0) t < 6 ? lse_of(t / 2 + 1) : delta_of(0);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) x[v][4 * g + j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[v][4 * g + j], a.scale_log2, -stat[g % 2][j]));
-            if (g % 2) pr[v][g / 2] = rounded<T>(x[v], g / 2);
+            for (int e = 4 * t; e < 4 * t + 4; ++e) exponential(e);
             __builtin_amdgcn_sched_barrier(0);
         }
-        // dV += dO^T P beside dS
-        s16x4 ao[AHEAD][2];
-#pragma unroll
-        for (int i = 0; i < AHEAD; ++i) across(ao[i], ot, i);
+        // dV += dO^T P beside the others and the first half of dS
 #pragma unroll
         for (int i = 0; i < 2 * DT; ++i) {
-            const int g = i / 2, v = i % 2;
 #pragma unroll
             for (int u = 0; u < 2; ++u) dv[u][i % DT] = T::mma(join<T>(ao[i % AHEAD][0], ao[i % AHEAD][1]), pr[u][i / DT], dv[u][i % DT]);
             if (i + AHEAD < 2 * DT) across(ao[i % AHEAD], ot, i + AHEAD);
             else across(ao[i % AHEAD], qt, i + AHEAD - 2 * DT);
-            if (v == 0 && g < 3) stat[(g + 1) % 2] = stats[stage][1][2 * g + 2 + h];
+            if (i % 2 == 0 && i < 6) delta_of(i / 2 + 1);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float d = dp[v][4 * g + j] - stat[g % 2][j];
-                dp[v][4 * g + j] = x[v][4 * g + j] * (NARROW<T> ? d * by[v] : d);
-            }
-            if (!NARROW<T> && g % 2) ds[v][g / 2] = rounded<T>(dp[v], g / 2);
+            for (int e = 4 * i; e < 4 * i + 4; ++e) gradient(e);
             __builtin_amdgcn_sched_barrier(0);
         }
-        if (NARROW<T>) {
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                by[u] *= __builtin_amdgcn_exp2f(keep_in_range(dp[u], dk[u]));
-#pragma unroll
-                for (int part = 0; part < 2; ++part) ds[u][part] = rounded<T>(dp[u], part);
-            }
-        }
-        // dK += Q^T dS
+        // dK += Q^T dS beside the second half
 #pragma unroll
         for (int i = 0; i < 2 * DT; ++i) {
             const int slot = (i + 2 * DT) % AHEAD;
@@ -1101,14 +1097,13 @@ __global__ __launch_bounds__(256, 1) void k_prompt_dkv_wide(const PromptArgs p)
         const uint32_t key = key0 + 32 * u + n;
         const bool valid = key < tile.n;
         const int64_t at = (int64_t)tile.k0 + (valid ? key : 0);
-        const float times = NARROW<T> ? a.scale * 0x1p-15f / by[u] : a.scale, times_v = NARROW<T> ? 0x1p-15f : 1.0f;
         if (tile.pieces == 1) {
-            store_row_16<T, DP>(a.dk + at * a.dks.token + tile.kvh * a.dks.head, valid, dk[u], times, a.head_dim);
-            store_row_16<T, DP>(a.dv + at * a.dvs.token + tile.kvh * a.dvs.head, valid, dv[u], times_v, a.head_dim);
+            store_row_16<T, DP>(a.dk + at * a.dks.token + tile.kvh * a.dks.head, valid, dk[u], a.scale, a.head_dim);
+            store_row_16<T, DP>(a.dv + at * a.dvs.token + tile.kvh * a.dvs.head, valid, dv[u], 1.0f, a.head_dim);
         } else if (valid) {
             float *part = a.part_o + (tile.part(p, tile.piece) + 64 * wave + 32 * u + n) * 2 * DP;
-            store_part<DP>(part, dk[u], times);
-            store_part<DP>(part + DP, dv[u], times_v);
+            store_part<DP>(part, dk[u], a.scale);
+            store_part<DP>(part + DP, dv[u], 1.0f);
         }
     }
 }

@@ -209,9 +209,9 @@ template <class T, int DP, int W>
 void dkv_as(const PromptArgs &p, const Launch &at, Launching &l)
 {
     bool done = false;
-    if constexpr (DP == 128 && W == 8 && !NARROW<T>)
+    if constexpr (DP == 128 && W == 8 && std::is_same_v<T, BF16>)
         if (wide(p.a)) {
-            l.run(k_prompt_dkv_wide<T>, at.blocks, 256, p);
+            l.run(k_prompt_dkv_wide, at.blocks, 256, p);
             done = true;
         }
     if (!done) l.run(k_prompt_dkv<T, DP, W>, at.blocks, 64 * W, p);

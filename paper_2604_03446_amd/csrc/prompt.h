@@ -538,20 +538,20 @@ __global__ __launch_bounds__(64 * W, LEAN ? 4 : 2) void k_prompt_forward(const P
         most = maximum(x);
         raise();
         __syncthreads();
+        constexpr int KP = MT * DP / 16, VP = KP, AHEAD = W == 8 ? 3 : 2, EACH = 16 * MT / KP;
+        u32x4 ko[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) ko[i] = key_operand(1, i);
 
         // Tile s from its scores `now`; the next one's scores into `next`.  In slots of one product, the read of an operand that is wanted some products later
         // and a share of the vector instructions, in this order: left to itself the compiler reads every operand right before its use.
         // at: s, or what it leaves divided by RING, known when this is compiled.
         auto step = [&](uint32_t s, auto at, f32x16 (&now)[MT], f32x16 (&next)[MT], auto masked) {
-            constexpr int KP = MT * DP / 16, VP = KP, AHEAD = W == 8 ? 3 : 2, EACH = 16 * MT / KP;
             typename T::V8 pr[MT][2][1];
-            u32x4 ko[AHEAD];
             s16x4 vo[AHEAD][2];
             const float off = top == -INFINITY ? 0.0f : top;
             load_keys(s + 1 + DEEP, at + 1 + DEEP);     // to where nobody reads any more since the last barrier
             load_values(s + DEEP, at + DEEP);
-#pragma unroll
-            for (int i = 0; i < AHEAD; ++i) ko[i] = key_operand(at + 1, i);
 #pragma unroll
             for (int i = 0; i < KP; ++i) {
                 next[i % MT] = T::mma(as_operand<T>(ko[i % AHEAD]), q[i / MT], i < MT ? f32x16{} : next[i % MT]);
@@ -571,13 +571,14 @@ __global__ __launch_bounds__(64 * W, LEAN ? 4 : 2) void k_prompt_forward(const P
             for (int i = 0; i < VP; ++i) {
                 o[i % DT] = T::mma(join<T>(vo[i % AHEAD][0], vo[i % AHEAD][1]), pr[i / DT / 2][i / DT % 2][0], o[i % DT]);
                 if (i + AHEAD < VP) value_operand(vo[i % AHEAD], at, i + AHEAD);
+                if (i == VP - AHEAD) arrived<LOADS * (DEEP - 1)>();         // K of tile s + 2, V of tile s + 1; this tile's operands are read
+                if (i >= VP - AHEAD) ko[i - (VP - AHEAD)] = key_operand(at + 2, i - (VP - AHEAD));
 #pragma unroll
                 for (int e = i * EACH; e < (i + 1) * EACH; ++e) m = __builtin_elementwise_maximum(m, next[e / 16][e % 16]);
                 __builtin_amdgcn_sched_barrier(0);
             }
             most = m;
             raise();
-            arrived<LOADS * (DEEP - 1)>();              // K of tile s + 2, V of tile s + 1
         };
         auto last = [&](uint32_t s, f32x16 (&now)[MT]) {
             typename T::V8 pr[MT][2][1];

@@ -983,12 +983,11 @@ __global__ __launch_bounds__(256, 1) void k_prompt_dkv_wide(const PromptArgs p)
     const int own_row = first_row(p, tile.m, tile.n, key0 + n), next_keys = p.causal ? 32 * (int)a.group : 0;       // of u = 0; more of u = 1
 
     f32x16 dk[2][DT] = {}, dv[2][DT] = {};
+    const auto along = [&](const u32x4 *of, int t) { return of[chunk_at<CH>(n, 2 * t + h)]; };
+    u32x4 operand[AHEAD];
     const auto step = [&](uint32_t s, auto stage) {
-        arrived<LOADS * (STAGES - 2)>();
-        load(s + STAGES - 1, std::integral_constant<int, (stage.value + STAGES - 1) % STAGES>());
         const u32x4 *const qt = tiles[stage][0], *const ot = tiles[stage][1];
         const uint32_t first = start + s * TR;
-        const auto along = [&](const u32x4 *of, int t) { return of[chunk_at<CH>(n, 2 * t + h)]; };
         const auto across = [&](s16x4 (&to)[2], const u32x4 *of, int i) {       // columns 32 (i mod DT) .., rows 16 (i / DT) ..
             const int l = lane & 15, c = 4 * (i % DT) + 2 * ((lane >> 4) & 1) + ((l >> 1) & 1);
 #pragma unroll
@@ -997,12 +996,10 @@ __global__ __launch_bounds__(256, 1) void k_prompt_dkv_wide(const PromptArgs p)
 
         // S = Q K^T
         f32x16 x[2], dp[2];
-        u32x4 operand[AHEAD], ko[AHEAD_V], vo[AHEAD_V][2];
+        u32x4 ko[AHEAD_V], vo[AHEAD_V][2];
         f32x4 lse[2], delta[2];                         // of row group g, its four rows, in [g % 2]
         const auto lse_of = [&](int g) { lse[g % 2] = stats[stage][0][2 * g + h]; };
         const auto delta_of = [&](int g) { delta[g % 2] = stats[stage][1][2 * g + h]; };
-#pragma unroll
-        for (int i = 0; i < AHEAD; ++i) operand[i] = along(qt, i);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
 #pragma unroll
@@ -1075,7 +1072,16 @@ __global__ __launch_bounds__(256, 1) void k_prompt_dkv_wide(const PromptArgs p)
             const int slot = (i + 2 * DT) % AHEAD;
 #pragma unroll
             for (int u = 0; u < 2; ++u) dk[u][i % DT] = T::mma(join<T>(ao[slot][0], ao[slot][1]), ds[u][i / DT], dk[u][i % DT]);
-            if (i + AHEAD < 2 * DT) across(ao[slot], qt, i + AHEAD);
+            if (i + AHEAD < 2 * DT) {
+                across(ao[slot], qt, i + AHEAD);
+            } else {                                    // this step's last reads are under way: the next one's first, and loads to where this one's rows were
+                const int next = i + AHEAD - 2 * DT;
+                if (next == 0) {
+                    arrived<LOADS * (STAGES - 2)>();
+                    load(s + STAGES, stage);
+                }
+                operand[next] = along(tiles[(stage.value + 1) % STAGES][0], next);
+            }
             __builtin_amdgcn_sched_barrier(0);
         }
     };
@@ -1084,6 +1090,10 @@ __global__ __launch_bounds__(256, 1) void k_prompt_dkv_wide(const PromptArgs p)
         load(0, std::integral_constant<int, 0>());
         load(1, std::integral_constant<int, 1>());
         load(2, std::integral_constant<int, 2>());
+        arrived<LOADS * (STAGES - 2)>();
+        load(3, std::integral_constant<int, 3>());
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) operand[i] = along(tiles[0][0], i);
     }
 #pragma unroll 1
     for (uint32_t s = 0; s < count; s += 4) {

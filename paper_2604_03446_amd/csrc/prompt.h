@@ -919,8 +919,9 @@ __global__ __launch_bounds__(64 * W, 2) void k_prompt_dkv(const PromptArgs p)
 // dK and dV of 256 keys with 128 values each, 64 a wave and one wave a SIMD, 32 rows a step: every operand read feeds two products, and the step goes in slots
 // of two, S | dP beside the exponentials | dV beside dS | dK.  Rows come straight to shared memory, three steps ahead.
 // Documents of 4096, 1333, 2048 and 715 rows, 32 heads over 8 of 128, bfloat16: 446 us, 0.85 PFLOP/s, busy 51 %, 2.0 GHz (k_prompt_dkv: 502).
-// Bound by the wave's own order: 64 matrix instructions a step are 2048 cycles, the slots with exponentials take 1.4 times theirs, and shared memory
-// hands out operands in 1700 of them for the four waves.  In float16, whose dS is kept in range between, registers do not suffice.
+// Bound by the wave's own instructions: 64 of a step's 750 are matrix instructions (2048 of about 3800 cycles), 192 move sums between the two halves of the
+// register file (the compiler lets all matrix instructions write to one half, which dK and dV fill).  Of 439 us 28 go without the exponentials, 24 without V's
+// reads, 30 without the loads, 80 without all these and the transposing reads.  In float16, whose dS is kept in range between, registers do not suffice.
 __global__ __launch_bounds__(256, 1) void k_prompt_dkv_wide(const PromptArgs p)
 {
     using T = BF16;

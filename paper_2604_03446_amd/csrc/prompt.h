@@ -698,7 +698,7 @@ __global__ __launch_bounds__(64 * W, DP <= 32 || (DP <= 64 && NARROW<T>) ? 3 : 2
             for (uint32_t s = 0; s < FEW && s < count; ++s) {
                 arrived<0>();
                 if (s + 1 < FEW && s + 1 < count) load(s + 1);
-#pragma unroll 1
+#pragma unroll
                 for (int mt = 0; mt < 2; ++mt) {
                     f32x16 x = keys_by_rows<T, DP>(tiles[s & 1][0], 32 * mt, q);
                     const f32x16 dp = keys_by_rows<T, DP>(tiles[s & 1][1], 32 * mt, d_o);

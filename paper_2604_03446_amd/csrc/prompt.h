@@ -90,9 +90,9 @@ struct Tile {
         kvh = p.dies ? at / p.slots : at % p.a.kv_heads;
         const uint32_t slot = p.dies ? at % p.slots : at / p.a.kv_heads;
         if (p.plan) {
-            there = slot < p.plan[0];
-            if (!there) return;
-            take(p.plan + ENTRIES + ENTRY * slot);
+            const uint32_t entries = p.plan[0];
+            take(p.plan + ENTRIES + ENTRY * slot);      // (whatever it holds: one trip to memory for both)
+            there = slot < entries;
             return;
         }
         const int32_t *starts = KEYS ? p.kv_starts : p.q_starts;

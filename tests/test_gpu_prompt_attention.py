@@ -326,6 +326,56 @@ def test_streams_and_graphs(M):
         M.mmee_set_stream(None)
 
 
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
+@pytest.mark.parametrize("lens,H,Hkv,d", [([70, 40, 90], 2, 1, 64), ([70, 40, 300], 4, 2, 128), ([300, 500, 260], 33, 33, 104), ([600, 57, 700], 8, 8, 64)])
+def test_a_sequence_that_is_not_finite(M, lens, H, Hkv, d, dtype):
+    """Reaches none of the others."""
+    import torch
+    t = tensors(lens, lens, H, Hkv, d, getattr(torch, dtype), 41)
+    middle = slice(lens[0], lens[0] + lens[1])
+    for n in ("q", "k", "v", "do"):
+        t[n][middle] = math.nan
+        t[n][middle][::3] = math.inf
+    run(M, t, kv=False)
+    for at in (slice(0, middle.start), slice(middle.stop, sum(lens))):
+        one = {n: t[n][at] for n in ("q", "k", "v", "o", "do", "dq", "dk", "dv")} | {"lse": t["lse"][:, at]}
+        one["q_starts"] = one["kv_starts"] = starts_of([at.stop - at.start])
+        compare(one, True, (lens, at))
+
+
+def test_graphs_that_share_a_workspace(M):
+    """A forward and a backward call, planned and in pieces, captured one by one with one workspace; replayed in turn over other lengths and inputs."""
+    import torch
+    T = 2400
+    make = lambda lens, seed: tensors(lens, lens, 4, 2, 128, torch.bfloat16, seed)  # noqa: E731
+    t = make([1200, 1200], 50)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    M.mmee_set_stream(stream.cuda_stream)
+    try:
+        a, g = calls(M, t)
+        M.mmee_prompt_attn_forward(a)
+        M.mmee_prompt_attn_backward(a, g)
+        stream.synchronize()
+        graphs = []
+        for call in (lambda: M.mmee_prompt_attn_forward(a), lambda: M.mmee_prompt_attn_backward(a, g)):
+            graphs.append(torch.cuda.CUDAGraph())
+            with torch.cuda.graph(graphs[-1], stream=stream):
+                call()
+        for seed, cut in enumerate((2300, 1, 1200, T)):
+            other = make([cut, T - cut], 51 + seed)
+            torch.cuda.synchronize()
+            with torch.cuda.stream(stream):
+                for n in ("q", "k", "v", "do", "q_starts", "kv_starts"):
+                    t[n].copy_(other[n])
+                for graph in graphs:
+                    graph.replay()
+            stream.synchronize()
+            compare(t, True, ("replay", cut))
+    finally:
+        M.mmee_set_stream(None)
+
+
 def test_gradients_against_differences(M):
     """The change of sum(o do) along one direction of each input, in 64 bits, against the gradients."""
     import torch

@@ -10,8 +10,8 @@
 //
 // Times are of one MI355X, the least of 20 passes; matrix products hold its clock at 1.85 to 2.05 GHz.  `busy` is the share of a unit's busy cycles in which
 // its matrix instructions run.  Registers that are spilled: k_prompt_forward with 64 values a head 2 (four blocks a unit); k_prompt_dq with four
-// waves 2 (float16, 128 a head), 4 (float16, 64) and 7 (bfloat16, 128, one of which is read in the loop); k_prompt_dkv in float16 with 128 a head 2 (four
-// waves) and 8 (eight), once a step; k_prompt_dkv_wide 16, outside its loop.
+// waves 4 (float16, 128 a head), 1 (float16, 64) and 8 (bfloat16, 128); k_prompt_dkv with 128 a head and four waves 4 (float16) and 2 (bfloat16), with
+// eight 8 (float16); k_prompt_dkv_wide 16, outside its loop.
 #pragma once
 
 #include "attention.h"
@@ -644,6 +644,20 @@ __global__ __launch_bounds__(8 * DP) void k_prompt_join(const PromptArgs p)
     if (a.lse && c == 0) a.lse[lse_at(a, 0, tile.kvh, row) + tile.q0] = sum != 0.0f ? (high + __log2f(sum)) * LN2 : -INFINITY;
 }
 
+// What rounding the first half of x to `of` left, rounded.
+template <class T>
+__device__ __forceinline__ typename T::V8 left_over(const f32x16 &x, const typename T::V8 &of)
+{
+    f32x8 y;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) y[j] = x[j] - (float)of[j];
+    return __builtin_convertvector(y, typename T::V8);
+}
+
+// Sequences of up to so many keys (one step of a product) take dS into dQ and dK as two operands, the rounded value and what that left: where a call has a handful of
+// dS in all their rounding does not average, and was up to 1.6 times that of the results.  (Blocks of four waves: where there are eight, sequences are long on average.)
+constexpr uint32_t FEW_KEYS = 16;
+
 // dQ, and D on the way:  P = 2^(scale S log2 e - lse2),  D = sum of dO O,  dS = P (dO V^T - D),  dQ = scale dS K.  Rows as in the forward pass, Q and dO in
 // registers; three products and an exponential a score.  D and lse2 go to the workspace, where dK and dV read them.
 // Bound as the forward pass: documents of 4096, 1333, 2048 and 715 rows, 32 heads over 8 of 128, bfloat16: 289 us, 0.99 PFLOP/s, busy 56 %, 1.91 GHz 
@@ -788,6 +802,15 @@ __global__ __launch_bounds__(64 * W, DP <= 32 || (DP <= 64 && NARROW<T>) ? 3 : 2
             }
         }
     }
+    if (W == 4 && tile.n <= FEW_KEYS && count) {        // its one tile is still there; dS is formed again, so that the loop has no registers to keep for this
+        f32x16 x = keys_by_rows<T, DP>(tiles[0][0], 0, q);
+        const f32x16 dp = keys_by_rows<T, DP>(tiles[0][1], 0, d_o);
+        mask_behind(x, (int)limit);
+#pragma unroll
+        for (int r = 0; r < 8; ++r) x[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], a.scale_log2, -lse2)) * (dp[r] - delta);
+        const typename T::V8 rest[1] = {left_over<T>(x, rounded<T>(x, 0))};
+        columns_times<T, DP, 1>(dq, tiles[0][0], 0, rest);
+    }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");    // nothing writes to shared memory any more when the block ends
     if (lse2 == INFINITY) {                             // (a row that sees nothing, whatever its query and gradient hold)
 #pragma unroll
@@ -902,6 +925,15 @@ __global__ __launch_bounds__(64 * W, 2) void k_prompt_dkv(const PromptArgs p)
                 const typename T::V8 pr[1] = {rounded<T>(x, part)}, ds[1] = {rounded<T>(dp, part)};
                 columns_times<T, DP, 1>(dv, ot, 32 * sub + 16 * part, pr);
                 columns_times<T, DP, 1>(dk, qt, 32 * sub + 16 * part, ds);
+            }
+            if (W == 4 && tile.n <= FEW_KEYS) {
+#pragma unroll 1
+                for (int part = 0; part < 2; ++part) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) dp[j] = part ? dp[8 + j] : dp[j];
+                    const typename T::V8 rest[1] = {left_over<T>(dp, rounded<T>(dp, 0))};
+                    columns_times<T, DP, 1>(dk, qt, 32 * sub + 16 * part, rest);
+                }
             }
         }
     }

@@ -126,9 +126,11 @@ def test_what_rows_without_keys_hold(M):
 
 @pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
 @pytest.mark.parametrize("causal", [True, False])
-@pytest.mark.parametrize("d,lens", [(24, [1, 2, 127, 5, 128]), (64, [1, 2, 3, 5, 33, 64]), (128, [1, 64, 2, 6, 9])])
+@pytest.mark.parametrize("d,lens", [(24, [1, 2, 127, 5, 128]), (64, [1, 2, 3, 5, 33, 64]), (128, [1, 64, 2, 6, 9]), (48, [17, 16, 15, 8]), (120, [16, 17])])
 def test_gradients_of_few_keys(M, d, lens, causal, dtype):
     """Where a row sees few keys D does not add the rounding of the output: dQ and dK are off by the rounding of dS and their own alone.
+
+    With up to 16 keys of a sequence those of dS are u^2 alone, as what the first rounding leaves is taken along.
 
     To u |dS_ij| of each dS (u half a step), summed with what multiplies it, and u of the result come the errors in 32 bits, P of 2^-19 (scores of less than 16
     powers of two, the exponential's argument, lse and the exponential each below 2^-21) and dP of d 2^-24 of its terms, in dP and in D; 2^-16 of P (|dP| + D's terms)
@@ -145,7 +147,7 @@ def test_gradients_of_few_keys(M, d, lens, causal, dtype):
         P = S.masked_fill(~keep_of(n, n, causal), -math.inf).softmax(3)
         dP, across = do @ v.transpose(2, 3), do.abs() @ v.abs().transpose(2, 3)
         dS = P * (dP - (P * dP).sum(3, keepdim=True))
-        off = u * dS.abs() + 2.0 ** -16 * P * (across + (P * across).sum(3, keepdim=True))
+        off = (u if n > 16 else u * u) * dS.abs() + 2.0 ** -16 * P * (across + (P * across).sum(3, keepdim=True))
         for name, want, bound in (("dq", dS @ k, off @ k.abs()), ("dk", (dS.transpose(2, 3) @ q).sum(1, keepdim=True), (off.transpose(2, 3) @ q.abs()).sum(1, keepdim=True))):
             got = t[name][at].double().cpu().view(n, 2, -1, d).permute(1, 2, 0, 3)
             far = (got - want * scale).abs() - (1.01 * bound + u * want.abs()) * scale - 2.0 ** -25

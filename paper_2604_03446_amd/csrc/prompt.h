@@ -24,7 +24,7 @@ struct PromptArgs {
     const int32_t *q_starts, *kv_starts;
     uint32_t seqs, slots;       // slots: of tiles, or of a plan's entries, of every head
     uint32_t parts;             // pieces of cut tiles, at most, of every head
-    float *lse2;                // backward: [kv_head][row], in powers of two, infinite where a row sees nothing; less what float16 takes off
+    float *lse2;                // backward, bfloat16: [kv_head][row], in powers of two, infinite where a row sees nothing
     const uint32_t *plan;       // or null
     bool causal;
     bool dies;                  // heads are dealt out to the dies, whose L2 then holds their keys
@@ -655,7 +655,8 @@ __device__ __forceinline__ typename T::V8 left_over(const f32x16 &x, const typen
 }
 
 // Sequences of up to so many keys (one step of a product) take dS into dQ and dK as two operands, the rounded value and what that left: where a call has a handful of
-// dS in all their rounding does not average, and was up to 1.6 times that of the results.  (Blocks of four waves: where there are eight, sequences are long on average.)
+// dS in all their rounding does not average, and was up to 1.6 times that of the results.  In blocks of four waves alone: where there are eight, sequences are long on
+// average, and such a sequence is one of few.
 constexpr uint32_t FEW_KEYS = 16;
 
 // dQ, and D on the way:  P = 2^(scale S log2 e - lse2),  D = sum of dO O,  dS = P (dO V^T - D),  dQ = scale dS K.  Rows as in the forward pass, Q and dO in
@@ -677,6 +678,7 @@ __global__ __launch_bounds__(64 * W, DP <= 32 || (DP <= 64 && NARROW<T>) ? 3 : 2
     const uint32_t rows = tile.m * a.group, row = tile.index * 32 * W + 32 * wave + n, step0 = tile.step0, count = tile.count;
     const bool live = row < rows;
     const uint32_t limit = limit_of(p, tile.m, tile.n, token_of(a, live ? row : rows - 1));
+    const bool few = W == 4 && tile.n <= FEW_KEYS;      // one step, behind the loop
 
     const Incoming<DP, W> k_in(a.k + tile.k0 * a.ks.token + tile.kvh * a.ks.head, a.ks.token, a.head_dim, wave, lane);
     const Incoming<DP, W> v_in(a.v + tile.k0 * a.vs.token + tile.kvh * a.vs.head, a.vs.token, a.head_dim, wave, lane);
@@ -692,7 +694,7 @@ __global__ __launch_bounds__(64 * W, DP <= 32 || (DP <= 64 && NARROW<T>) ? 3 : 2
     float lse2 = INFINITY, delta = 0.0f;                // rows that see nothing: probabilities 0
     if (live) {
         const float l = a.lse_in[lse_at(a, 0, tile.kvh, row) + tile.q0];
-        lse2 = l == -INFINITY ? INFINITY : l * LOG2E - (NARROW<T> ? UP + HIGHEST : 0.0f);
+        lse2 = l == -INFINITY ? INFINITY : l * LOG2E - (NARROW<T> && !few ? UP + HIGHEST : 0.0f);
     }
     {
         typename T::V8 o[DP / 16];
@@ -718,7 +720,7 @@ __global__ __launch_bounds__(64 * W, DP <= 32 || (DP <= 64 && NARROW<T>) ? 3 : 2
                     const f32x16 dp = keys_by_rows<T, DP>(tiles[s & 1][1], 32 * mt, d_o);
                     mask_behind(x, (int)limit - (int)(s * TN) - 32 * mt);
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) exact += __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], a.scale_log2, -(lse2 + (NARROW<T> ? UP + HIGHEST : 0.0f)))) * dp[r];
+                    for (int r = 0; r < 16; ++r) exact += __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], a.scale_log2, -(lse2 + (NARROW<T> && !few ? UP + HIGHEST : 0.0f)))) * dp[r];
                 }
             }
             exact = sum_of_halves(exact);
@@ -726,14 +728,14 @@ __global__ __launch_bounds__(64 * W, DP <= 32 || (DP <= 64 && NARROW<T>) ? 3 : 2
         }
         if (live && h == 0 && tile.piece == 0) {
             a.delta[line] = delta;
-            p.lse2[line] = NARROW<T> ? lse2 + HIGHEST : lse2;
+            if (!NARROW<T>) p.lse2[line] = lse2;
         }
     }
 
     f32x16 dq[1][DP / 32] = {};
     float lowered = 0.0f;                               // of dS's power of two, which lse2 holds
     constexpr int NT = DP / 16, DT = DP / 32, AHEAD = 2, EACH = 16 / NT;
-    for (uint32_t s = 0; s < count; ++s) {
+    for (uint32_t s = 0; s < (few ? 0 : count); ++s) {
         const u32x4 *const kt = tiles[s & 1][0], *const vt = tiles[s & 1][1];
         arrived<0>();
         if (s + 1 < count) load(s + 1);
@@ -802,13 +804,26 @@ __global__ __launch_bounds__(64 * W, DP <= 32 || (DP <= 64 && NARROW<T>) ? 3 : 2
             }
         }
     }
-    if (W == 4 && tile.n <= FEW_KEYS && count) {        // its one tile is still there; dS is formed again, so that the loop has no registers to keep for this
+    if (few && count) {
+        arrived<0>();
         f32x16 x = keys_by_rows<T, DP>(tiles[0][0], 0, q);
         const f32x16 dp = keys_by_rows<T, DP>(tiles[0][1], 0, d_o);
         mask_behind(x, (int)limit);
+        float most = 0.0f;
 #pragma unroll
-        for (int r = 0; r < 8; ++r) x[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], a.scale_log2, -lse2)) * (dp[r] - delta);
-        const typename T::V8 rest[1] = {left_over<T>(x, rounded<T>(x, 0))};
+        for (int r = 0; r < 8; ++r) {
+            x[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], a.scale_log2, -lse2)) * (dp[r] - delta);
+            most = __builtin_fmaxf(most, __builtin_fabsf(x[r]));
+        }
+        if (NARROW<T>) {                                // to 2^10 .. 2^11
+            const int by = 11 - __builtin_amdgcn_frexp_expf(max_of_halves(most));
+#pragma unroll
+            for (int r = 0; r < 8; ++r) x[r] = __builtin_ldexpf(x[r], by);
+            lowered = (float)by - (UP + HIGHEST);
+        }
+        // the rounded value, and what that left
+        const typename T::V8 first[1] = {rounded<T>(x, 0)}, rest[1] = {left_over<T>(x, first[0])};
+        columns_times<T, DP, 1>(dq, tiles[0][0], 0, first);
         columns_times<T, DP, 1>(dq, tiles[0][0], 0, rest);
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");    // nothing writes to shared memory any more when the block ends

@@ -1,0 +1,40 @@
+"""Attention of packed prompts where its ranges end: dS of a handful of keys."""
+import pytest
+
+from test_gpu_prompt_attention import run, tensors
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
+def test_dS_of_up_to_16_keys_one_by_one(M, dtype):
+    """Keys are unit vectors, so that a value of dQ is one dS times the scale, and of V and dO one value is not zero, so that dP is exact: dS goes into dQ as two
+    operands and is off by u^2 and by what errors in 32 bits add, and its result is rounded once, to u.
+
+    P is off by 2^-19 (scores below 8 and their products with log2 e below 2^-21 of a power of two, lse as above 2^-20), D by that and 16 additions, 2^-20.  Float16 has steps
+    of 2^-24 below its normal numbers."""
+    import torch
+    d, dt = 64, getattr(torch, dtype)
+    u, scale = torch.finfo(dt).eps / 2, d ** -0.5
+    lens = [16, 9, 13, 2, 15, 7] * 8
+    t = tensors(lens, lens, 4, 2, d, dt, 101)
+    at = 0
+    for n in lens:
+        t["k"][at:at + n] = torch.eye(n, d, device="cuda")[:, None].to(dt)
+        at += n
+    t["q"] *= 3
+    t["v"][..., 1:], t["do"][..., 1:] = 0, 0
+    run(M, t, kv=False, causal=False)
+    at = 0
+    for b, n in enumerate(lens):
+        one = slice(at, at + n)
+        at += n
+        q, do, v = (t[x][one].double().cpu().transpose(0, 1) for x in ("q", "do", "v"))
+        P = (q[..., :n] * scale).softmax(2)
+        dP = do[..., :1] * v[..., 0].repeat_interleave(2, 0)[:, None]
+        D = (P * dP).sum(2, keepdim=True)
+        dS = P * (dP - D)
+        off = (u + 1.01 * u * u) * dS.abs() + 1.01 * P * (2.0 ** -19 * (dP - D).abs() + (2.0 ** -19 + 2.0 ** -20) * (P * dP.abs()).sum(2, keepdim=True))
+        far = (t["dq"][one].double().cpu().transpose(0, 1)[..., :n] - dS * scale).abs() - off * scale - 2.0 ** -25
+        assert (far <= 0).all(), (b, n, int((far > 0).sum()), far.max().item())

@@ -7,12 +7,19 @@ pytestmark = pytest.mark.gpu
 
 
 @pytest.fixture(scope="module")
+def M():
+    import torch
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    import paper_2604_03446_amd as mod
+    return mod
+
+
 @pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
 def test_dS_of_up_to_16_keys_one_by_one(M, dtype):
     """Keys are unit vectors, so that a value of dQ is one dS times the scale, and of V and dO one value is not zero, so that dP is exact: dS goes into dQ as two
     operands and is off by u^2 and by what errors in 32 bits add, and its result is rounded once, to u.
 
-    P is off by 2^-19 (scores below 8 and their products with log2 e below 2^-21 of a power of two, lse as above 2^-20), D by that and 16 additions, 2^-20.  Float16 has steps
+    P is off by 2^-19 (scores below 8 and their products with log2 e below 2^-21 of a power of two, lse, the logarithm of a sum of up to 2^11, 2^-20), D by that and 16 additions, 2^-20.  Float16 has steps
     of 2^-24 below its normal numbers."""
     import torch
     d, dt = 64, getattr(torch, dtype)

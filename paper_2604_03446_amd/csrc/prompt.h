@@ -709,6 +709,9 @@ __global__ __launch_bounds__(64 * W, DP <= 32 || (DP <= 64 && NARROW<T>) ? 3 : 2
         // dP.  With 65 keys O's rounding adds 4 % to the error, with 32 values a head 5 %, in which that of dS is 5 % larger.
         constexpr uint32_t FEW = DP <= 32 ? 2 : 1;
         if (tile.pieces == 1 && count && limit_of(p, tile.m, tile.n, token_of(a, tile.index * 32 * W)) <= FEW * TN) {
+            // float16: with lse as it is, read again.  (Less what the loop takes off, and that added back, it is rounded near 75 and puts P off by 2^-18; dS can be what little
+            // D and dP leave of each other.)
+            const float as_is = NARROW<T> && lse2 != INFINITY ? a.lse_in[lse_at(a, 0, tile.kvh, row) + tile.q0] * LOG2E : lse2;
             float exact = 0.0f;
 #pragma unroll 1
             for (uint32_t s = 0; s < FEW && s < count; ++s) {
@@ -720,7 +723,7 @@ __global__ __launch_bounds__(64 * W, DP <= 32 || (DP <= 64 && NARROW<T>) ? 3 : 2
                     const f32x16 dp = keys_by_rows<T, DP>(tiles[s & 1][1], 32 * mt, d_o);
                     mask_behind(x, (int)limit - (int)(s * TN) - 32 * mt);
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) exact += __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], a.scale_log2, -(lse2 + (NARROW<T> && !few ? UP + HIGHEST : 0.0f)))) * dp[r];
+                    for (int r = 0; r < 16; ++r) exact += __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], a.scale_log2, -as_is)) * dp[r];
                 }
             }
             exact = sum_of_halves(exact);

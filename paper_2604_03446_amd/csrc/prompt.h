@@ -321,14 +321,19 @@ __device__ __forceinline__ void store_row_16(uint16_t *row, bool live, const f32
 // Loads straight to shared memory: 16 or 4 bytes a lane, `offset` (a lane's own, in bytes) behind the base, lane after lane to the place `to`.
 // Written out, as the compiler waits for all that are under way at every barrier and at the first read of shared memory after one: who uses them counts them
 // and waits (`arrived`).  (m0 is not said to be written: it is a register that the compiler keeps out of its own hands, and sets before every use.)
+// Nor does it keep the distance that such a load wants from what comes before: five wait states behind a vector instruction that has written the base, as a lane read
+// first is or a spilled value read back, and one behind the write of m0.  Scalar instructions wait for such a write by themselves: the base is moved by one, which
+// stands behind m0's.  (8192 rows 510 us instead of 507, a training step 894 instead of 892; with five states before every load 510 and 898.)
 __device__ __forceinline__ void load_16_to_shared(const void *base, uint32_t offset, uint32_t to)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory");
+    uint64_t own;
+    asm volatile("s_mov_b32 m0, %1\n\ts_mov_b64 %0, %3\n\tglobal_load_lds_dwordx4 %2, %0" : "=&s"(own) : "s"(to), "v"(offset), "s"(base) : "memory");
 }
 
 __device__ __forceinline__ void load_4_to_shared(const void *base, uint32_t offset, uint32_t to)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory");
+    uint64_t own;
+    asm volatile("s_mov_b32 m0, %1\n\ts_mov_b64 %0, %3\n\tglobal_load_lds_dword %2, %0" : "=&s"(own) : "s"(to), "v"(offset), "s"(base) : "memory");
 }
 
 __device__ __forceinline__ uint32_t place_in_shared(const void *p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)p; }

@@ -151,7 +151,7 @@ enum {
     MMEE_EDEVICE = -4,      /* HIP error or no device                                         */
     MMEE_EOVERFLOW = -5,    /* mmee_pareto: more front points than `capacity`                 */
     MMEE_ETOOBIG = -6,      /* mmee_search_noalloc: the problem exceeds its fixed scratch     */
-    MMEE_EWORKSPACE = -7    /* mmee_attn_*, mmee_tree_attn_*, mmee_ffn_*: no workspace, or one smaller than asked for */
+    MMEE_EWORKSPACE = -7    /* a call with a mmee_*_workspace of its own: no workspace, or one smaller than asked for */
 };
 
 /* Number of candidates of (workload, hw): #tilings (integer factorisations, Sec. VI-A)

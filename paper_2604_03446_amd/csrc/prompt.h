@@ -1092,7 +1092,7 @@ __global__ __launch_bounds__(256, 1) void k_prompt_dkv_wide(const PromptArgs p)
             dp[u][4 * g + j] = x[u][4 * g + j] * (dp[u][4 * g + j] - delta[g % 2][j]);
             if (g % 2 && j == 3) ds[u][g / 2] = rounded<T>(dp[u], g / 2);
         };
-        // dP = dO V^T beside three quarters of the exponentials; operand[] holds dO's from (NT mod AHEAD) on
+        // dP = dO V^T beside the exponentials; operand[] holds dO's from (NT mod AHEAD) on
         s16x4 ao[AHEAD][2];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
@@ -1110,7 +1110,7 @@ __global__ __launch_bounds__(256, 1) void k_prompt_dkv_wide(const PromptArgs p)
             for (int e = 4 * t; e < 4 * t + 4; ++e) exponential(e);
             __builtin_amdgcn_sched_barrier(0);
         }
-        // dV += dO^T P beside the others and the first half of dS
+        // dV += dO^T P beside dS
 #pragma unroll
         for (int i = 0; i < 2 * DT; ++i) {
 #pragma unroll
@@ -1122,7 +1122,7 @@ __global__ __launch_bounds__(256, 1) void k_prompt_dkv_wide(const PromptArgs p)
             for (int e = 4 * i; e < 4 * i + 4; ++e) gradient(e);
             __builtin_amdgcn_sched_barrier(0);
         }
-        // dK += Q^T dS beside the second half
+        // dK += Q^T dS beside the next step's first reads
 #pragma unroll
         for (int i = 0; i < 2 * DT; ++i) {
             const int slot = (i + 2 * DT) % AHEAD;

@@ -28,7 +28,7 @@ __device__ __forceinline__ int last_at_most(uint32_t n, int64_t x, F value)
 
 __device__ __forceinline__ int64_t within(int64_t x, int64_t lo, int64_t hi) { return x < lo ? lo : x > hi ? hi : x; }
 
-// Sum over the lanes up to a lane's own, and over all of them; the largest of all.
+// Join of the lanes up to a lane's own: their sum, or the largest of all.
 template <class F>
 __device__ __forceinline__ uint32_t scan_lanes(uint32_t x, F join)
 {
@@ -44,8 +44,6 @@ __device__ __forceinline__ uint32_t sums_below(uint32_t x)
 {
     return scan_lanes(x, [](uint32_t a, uint32_t b) { return a + b; });
 }
-
-__device__ __forceinline__ uint32_t sum_of_lanes(uint32_t x) { return __builtin_amdgcn_readlane(sums_below(x), 63); }
 
 __device__ __forceinline__ uint32_t most_of_lanes(uint32_t x)
 {

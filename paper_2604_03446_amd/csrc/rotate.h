@@ -9,6 +9,9 @@
 // hands them round through shared memory.  Everything between the 16-bit input and the 16-bit output is 32 bits, angles 64.
 #pragma once
 
+#include <cmath>
+#include <type_traits>
+
 #include "launch.h"
 #include "mfma.h"
 #include "sequences.h"
@@ -154,10 +157,14 @@ struct Head {
         }
     }
 
+    // Of the head's G lanes, 1, 2, 4 and 8 apart.
     static __device__ __forceinline__ float sum(float x)
     {
-#pragma unroll
-        for (int d = 1; d < G; d <<= 1) x += __shfl_xor(x, d);
+        const auto add = [&x](auto apart) { x += __builtin_bit_cast(float, __builtin_amdgcn_ds_swizzle(__builtin_bit_cast(int, x), apart.value << 10 | 0x1f)); };
+        add(std::integral_constant<int, 1>());
+        if constexpr (G > 2) add(std::integral_constant<int, 2>());
+        if constexpr (G > 4) add(std::integral_constant<int, 4>());
+        if constexpr (G > 8) add(std::integral_constant<int, 8>());
         return x;
     }
 
@@ -167,6 +174,24 @@ struct Head {
 #pragma unroll
         for (int j = 0; j < 16; ++j) s += x[j] * x[j];
         return sum(s);
+    }
+
+    // (mean of the head's x^2 + eps)^-1/2.  Where the squares pass 32 bits, in bfloat16 from 2^60 on, those of 2^-96 times the head are summed, next to which eps is nothing.
+    static __device__ __forceinline__ float inverse_root(const float (&x)[16], const RotateArgs &r)
+    {
+        const float s = squares(x);
+        float inverse = __builtin_amdgcn_rsqf(s / (float)r.head_dim + r.eps);
+        if (std::is_same<T, BF16>::value && __any(s == INFINITY)) {
+            float t = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const float y = 0x1p-96f * x[j];
+                t += y * y;
+            }
+            t = sum(t);
+            if (s == INFINITY) inverse = 0x1p-96f * __builtin_amdgcn_rsqf(t / (float)r.head_dim);
+        }
+        return inverse;
     }
 };
 
@@ -230,7 +255,7 @@ __global__ __launch_bounds__(256) void k_rotate(const RotateArgs r)
         float x[16];
         h.widen(raw, x);
         if (norm) {
-            const float inverse = __builtin_amdgcn_rsqf(h.squares(x) / (float)r.head_dim + r.eps);
+            const float inverse = h.inverse_root(x, r);
 #pragma unroll
             for (int j = 0; j < 16; ++j) x[j] *= inverse * (is_q ? w[0][j] : w[1][j]);
         }
@@ -275,7 +300,7 @@ __global__ __launch_bounds__(256, 4) void k_rotate_back(const RotateArgs r)
                     float x[16], weight[16];
                     h.widen(raw, x);
                     h.widen(weights, weight);
-                    const float inverse = __builtin_amdgcn_rsqf(h.squares(x) / (float)r.head_dim + r.eps);
+                    const float inverse = h.inverse_root(x, r);
                     float along = 0.0f;
 #pragma unroll
                     for (int j = 0; j < 16; ++j) {

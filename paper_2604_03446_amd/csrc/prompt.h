@@ -390,8 +390,8 @@ struct Incoming {
 //   x = K q,  p = 2^(scale x - mark),  sum += p,  o = 2^(old mark - mark) o + V^T p,  at the end o / sum and lse.
 // Bound by matrix instructions, two products of 2 head_dim operations a score, and beside them one exponential a score, which issues at a quarter of the
 // rate: a step of 64 keys is 1024 cycles of a wave's matrix instructions at 128 a head, and 512 of exponentials alone; at 64 a head 512 and 512.
-//   One prompt of 8192 rows, 32 heads of 128, bfloat16: 538 us, 1.02 PFLOP/s, busy 61 %, 1.90 GHz (before its last step 1.19 PFLOP/s where all values are zeros: power).
-//   24 of 17 to 2500, 32 heads over 8 of 128, float16: 179 us, 0.81 PFLOP/s, busy 49 %.  40 of 23 to 509, 12 heads of 64, not causal: 23 us, a round of blocks
+//   One prompt of 8192 rows, 32 heads of 128, bfloat16: 535 us, 1.03 PFLOP/s, busy 60 %, 1.91 GHz (before its last step 1.19 PFLOP/s where all values are zeros: power).
+//   24 of 17 to 2500, 32 heads over 8 of 128, float16: 176 us, 0.83 PFLOP/s, busy 49 %.  40 of 23 to 509, 12 heads of 64, not causal: 23 us, a round of blocks
 //   whose longest has eight steps.
 // The step in slots of one product took the first from 562 to 546 us a call, tiles straight to shared memory from 559 to 539, the next step's first
 // operands before this one's last products from 524 to 515 (another card); operands read 4 to 8 products ahead and three or four tiles under way gained nothing.
@@ -666,7 +666,7 @@ constexpr uint32_t FEW_KEYS = 16;
 
 // dQ, and D on the way:  P = 2^(scale S log2 e - lse2),  D = sum of dO O,  dS = P (dO V^T - D),  dQ = scale dS K.  Rows as in the forward pass, Q and dO in
 // registers; three products and an exponential a score.  D and lse2 go to the workspace, where dK and dV read them.
-// Bound as the forward pass: documents of 4096, 1333, 2048 and 715 rows, 32 heads over 8 of 128, bfloat16: 289 us, 0.99 PFLOP/s, busy 56 %, 1.91 GHz 
+// Bound as the forward pass: documents of 4096, 1333, 2048 and 715 rows, 32 heads over 8 of 128, bfloat16: 288 us, 0.99 PFLOP/s, busy 55 %, 1.94 GHz
 // (a call in slots of one product: the step of training 936 us instead of 954).  40 sentences of 23 to 509, 12 heads of 64, float16: 26 us.
 // Three waves a SIMD where 168 registers suffice: 64 a head, float16, 79.5 us with three (a training step over the 40 sentences), 81.5 with two; bfloat16 78.5, and 75.7
 // with two.
@@ -848,7 +848,7 @@ __global__ __launch_bounds__(64 * W, DP <= 32 || (DP <= 64 && NARROW<T>) ? 3 : 2
 // which costs two products more than one kernel for all three gradients would, and saves atomics on dQ.  Q, dO and the rows' statistics go through
 // registers to shared memory, so that what is no row is zeros.
 // Bound by matrix instructions and the reads of operands from shared memory (each feeds one product).  40 sentences of 23 to 509, 12 heads of 64, float16:
-// 31 us, busy 25 %: few steps a block, whose beginnings and ends show.
+// 31 us, busy 26 %: few steps a block, whose beginnings and ends show.
 template <class T, int DP, int W>
 __global__ __launch_bounds__(64 * W, 2) void k_prompt_dkv(const PromptArgs p)
 {
@@ -973,7 +973,7 @@ __global__ __launch_bounds__(64 * W, 2) void k_prompt_dkv(const PromptArgs p)
 
 // dK and dV of 256 keys with 128 values each, 64 a wave and one wave a SIMD, 32 rows a step: every operand read feeds two products, and the step goes in slots
 // of two, S | dP beside the exponentials | dV beside dS | dK.  Rows come straight to shared memory, three steps ahead.
-// Documents of 4096, 1333, 2048 and 715 rows, 32 heads over 8 of 128, bfloat16: 430 us, 0.89 PFLOP/s, busy 53 %, 2.0 GHz (k_prompt_dkv: 502).
+// Documents of 4096, 1333, 2048 and 715 rows, 32 heads over 8 of 128, bfloat16: 425 us, 0.90 PFLOP/s, busy 53 %, 2.0 GHz (k_prompt_dkv: 502).
 // Bound by the wave's own instructions: 64 of a step's 750 are matrix instructions (2048 of about 3800 cycles), 192 move sums between the two halves of the
 // register file (the compiler lets all matrix instructions write to one half, which dK and dV fill).  Of 439 us 28 go without the exponentials, 24 without V's
 // reads, 30 without the loads, 80 without all these and the transposing reads.  In float16, whose dS is kept in range between, registers do not suffice.

@@ -196,8 +196,8 @@ struct Head {
 };
 
 // Forward: a wave takes 64 / G heads of a token at a time.  CACHE: keys and values go to the pages, values as they are.
-// Bound by HBM where there are many tokens, each value read and written once: 16384 tokens of 32 and 8 heads of 128, 336 MB, 62 us, 5.4 TB/s; 17989 tokens on
-// their way to pages of 64, 442 MB, 90 us, 4.9 TB/s; heads of 80, neighbours paired, 84 MB, 18 us, 4.7 TB/s.  One token: 2.8 us, 64 sequences' next
+// Bound by HBM where there are many tokens, each value read and written once: 16384 tokens of 32 and 8 heads of 128, 336 MB, 63 us, 5.3 TB/s; 17989 tokens on
+// their way to pages of 64, 442 MB, 90 us, 4.9 TB/s; heads of 80, neighbours paired, 84 MB, 17 us, 4.8 TB/s.  One token: 2.8 us, 64 sequences' next
 // ones 4.0: a launch, and the trips for the page or the position, its angle and the head, one after the other.
 template <class T, int G, bool NEIGHBOURS, bool CACHE>
 __global__ __launch_bounds__(256) void k_rotate(const RotateArgs r)
@@ -266,7 +266,7 @@ __global__ __launch_bounds__(256) void k_rotate(const RotateArgs r)
 
 // Backward.  A wave takes heads as in the forward pass, and further tokens: first all queries' heads, then all keys', so that it holds one weight and the
 // gradients of one, which stay in registers and leave the block as one line of 32-bit sums.
-// Bound by HBM, each of three tensors once: 8191 tokens of 2 x 16 heads of 80, 126 MB, 29.6 us, 4.2 TB/s; 12000 of 2 x 12 of 64, three axes, 111 MB, 26.2 us,
+// Bound by HBM, each of three tensors once: 8191 tokens of 2 x 16 heads of 80, 126 MB, 29.0 us, 4.3 TB/s; 12000 of 2 x 12 of 64, three axes, 111 MB, 26.5 us,
 // 4.2 TB/s.  Four waves a SIMD, as many blocks as run at once; the next head's loads ahead of this one's work gained nothing.
 template <class T, int G, bool NEIGHBOURS>
 __global__ __launch_bounds__(256, 4) void k_rotate_back(const RotateArgs r)
